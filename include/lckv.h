@@ -166,8 +166,8 @@ int lckv_cache_lengths(const lckv_cache_t* cache, int32_t* host_out, int32_t bat
 
 /*
  * Reads the device status word (0, or LCKV_ETIMEOUT if some kernel's bounded
- * wait on a copy gave up; the outputs of that launch are then undefined);
- * SYNCHRONISES `stream`.  lckv_cache_reset clears it.
+ * wait on a copy gave up; the outputs of that launch are then undefined; or
+ * LCKV_ECAPACITY, see lckv_rope_append_kv); SYNCHRONISES `stream`.  lckv_cache_reset clears it.
  */
 int lckv_cache_status(const lckv_cache_t* cache, int32_t* host_status, void* stream);
 
@@ -416,6 +416,147 @@ int lckv_decode_attention_static(const void* k, const void* v, const int32_t* le
  */
 int lckv_read_stream_probe(const void* src, size_t bytes, int32_t kind, int32_t repeats, float l2_keep,
                            uint32_t* dev_sum, int32_t* dev_status, void* stream);
+
+/*
+ * Rotary positions (the paper's models are Llama models, whose attention takes rotated queries and keys;
+ * the paper does not restate the rotation).  A layer that owns a cache rotates its query and its key, a
+ * condensed layer only its query.  For pair j < rot_dim / 2 of a head at position p, with
+ * c = cos[p, j] and s = sin[p, j]:
+ *     y0 = x0 c - x1 s,   y1 = x1 c + x0 s       (fp32, one rounding to the output type)
+ * where (x0, x1) is (x[j], x[j + rot_dim/2]) in the half layout (the one lckv_project_append_kv applies)
+ * and (x[2j], x[2j+1]) in the interleaved one.  Dimensions rot_dim .. d_h-1 are copied bit by bit.
+ */
+typedef struct {
+    uint32_t struct_size;  /* sizeof(lckv_rope_t)                                              */
+    int32_t rot_dim;       /* rotated dimensions of a head: even, 2 <= rot_dim <= d_h          */
+    int32_t interleaved;   /* 0 = half layout, 1 = neighbouring pairs                          */
+    int32_t positions;     /* rows of the tables                                               */
+    const float* cos;      /* [positions, rot_dim / 2] fp32, device                            */
+    const float* sin;
+} lckv_rope_t;
+
+/* Frequencies of the tables, before and after scaling for contexts longer than the trained ones. */
+typedef struct {
+    uint32_t struct_size;  /* sizeof(lckv_rope_scaling_t)                                      */
+    int32_t kind;          /* 0 none:   theta_j = base^(-2j / rot_dim)
+                              1 linear: theta_j / factor (position interpolation)
+                              2 base:   the same with base * factor^(rot_dim / (rot_dim - 2))
+                              3 by parts: theta_j (g + (1 - g) / factor), g = (t - low) / (high - low)
+                                clamped to [0, 1], t = original theta_j / (2 pi) = the turns that pair j
+                                makes over the trained context: fast pairs stay, slow ones stretch      */
+    double base;           /* > 1                                                              */
+    double factor;         /* kinds 1 .. 3: > 0                                                */
+    double original;       /* kind 3: the trained context length                               */
+    double low, high;      /* kind 3: 0 <= low < high, in turns                                */
+    double amplitude;      /* multiplies cos and sin; 0 => 1                                   */
+} lckv_rope_scaling_t;
+
+/*
+ * Fills cos and sin, [positions, rot_dim / 2] fp32 on the device, with amplitude * cos(p theta_j) and
+ * amplitude * sin(p theta_j), p = 0 .. positions-1.  Angles are reduced in fp64, so far positions are as
+ * exact as near ones.  rot_dim even, 2 .. 128.  Errors: EINVAL, ECUDA.
+ */
+int lckv_rope_tables(float* cos, float* sin, int32_t positions, int32_t rot_dim,
+                     const lckv_rope_scaling_t* scaling, void* stream);
+
+/*
+ * y[t, h, :] = rotation of x[t, h, :] by position positions[t], for t < n_tokens, h < n_heads.
+ *   positions  [n_tokens] int32, device; a position outside the tables is clamped into them (the host
+ *              cannot see it)
+ *   x, y       bf16 (dtype 0) or fp32 (dtype 1), element strides between tokens and between heads, the
+ *              head_dim (64 or 128) elements of a head contiguous.  x may have strides of 0.  y == x with
+ *              equal strides works in place; y may also be other heads of the tokens that x is in; any
+ *              other overlap is refused.  Fastest with 16-byte aligned pointers and strides, 16-byte
+ *              aligned tables and rot_dim a multiple of 16; any other is correct.
+ *   transpose  1: the transposed rotation (s -> -s): the gradient with respect to x given the gradient with
+ *              respect to y, and the inverse when the tables' amplitude is 1.
+ * Errors: EINVAL, ECUDA.
+ */
+int lckv_rope_apply(const lckv_rope_t* rope, const int32_t* positions, const void* x,
+                    int64_t x_token_stride, int64_t x_head_stride, void* y, int64_t y_token_stride,
+                    int64_t y_head_stride, int32_t n_tokens, int32_t n_heads, int32_t head_dim,
+                    int32_t dtype, int32_t transpose, void* stream);
+
+/*
+ * Rotate-and-append: lckv_append_kv for keys that are not rotated yet, for one or several new tokens per
+ * sequence, with the rotation of the tokens' queries in the same launch.  Token i < n_new of sequence b is at
+ * position p = len[b] + i; its key is rotated by p and stored as row p of slot `slot` (ring position in a
+ * sink + recent-window cache), its value is copied there, its query is rotated by p into q_out.
+ *   q          [batch, n_new, H_q, d_h] bf16, q_stride elements between tokens (0 => H_q * d_h); or NULL
+ *   q_out      [batch, n_new, H_q, d_h] bf16, contiguous; NULL exactly if q is.  May be q itself when q is
+ *              contiguous; any other overlap with q, k_new or v_new is refused
+ *   k_new, v_new  [batch, n_new, H_kv, d_h] bf16, kv_stride elements between tokens (0 => H_kv * d_h); both
+ *              NULL for a condensed layer, which has only a query (then `slot` is not written)
+ *   advance_len   != 0: every len[b], b < batch, grows by n_new afterwards (all slots; needs k_new)
+ * The three inputs may be views of one fused projection.  rope->rot_dim <= d_h.
+ * Errors: EINVAL (null, shape, overlap, rope->positions < some len[b] + n_new, n_new > max_seq - stream_sink in
+ * a sink + recent-window cache), ECAPACITY (some len[b] + n_new > T_cap, or no page left; nothing written),
+ * ECUDA.  While `stream` is capturing, the call is refused with EINVAL if advance_len != 0 (the library's
+ * lengths could not follow the replays) or if new pages are needed (make room with an eager call first).  A replay
+ * uses the lengths it finds on the device; a row that has no place there is not written and lckv_cache_status
+ * then reports LCKV_ECAPACITY.
+ */
+int lckv_rope_append_kv(lckv_cache_t* cache, int32_t slot, const lckv_rope_t* rope, const void* q,
+                        int64_t q_stride, void* q_out, const void* k_new, const void* v_new,
+                        int64_t kv_stride, int32_t n_new, int32_t batch, int32_t advance_len,
+                        void* stream);
+
+/*
+ * The same for prompts, beside lckv_prefill_write_kv: lengths already hold the prompt lengths and do not
+ * change; tokens i < len[b] (of n_max per sequence) are at position i and go to row i.  Rows of q_out and of
+ * the slot behind a prompt are left as they were.  Errors: EINVAL (as above, and as lckv_prefill_write_kv),
+ * ECUDA.
+ */
+int lckv_rope_prefill_write_kv(lckv_cache_t* cache, int32_t slot, const lckv_rope_t* rope, const void* q,
+                               int64_t q_stride, void* q_out, const void* k, const void* v,
+                               int64_t kv_stride, int32_t n_max, int32_t batch, void* stream);
+
+/*
+ * Residual addition and root-mean-square norm (what stands before every projection of the paper's models,
+ * Section 3.1 lists the fused form among its settings).  For each of `rows` rows:
+ *     h = x + residual        (fp32; h = x without a residual)
+ *     y = h / sqrt(mean(h^2) + eps) * weight
+ * h is rounded once into residual_out, y once into its type; the norm is taken of the unrounded h.
+ *   x          [rows, width], x_stride elements between rows (0 => width), x_dtype 0 = bf16, 1 = fp32
+ *   residual, residual_out  [rows, width] in residual_dtype (0 / 1), or NULL; residual_out may be residual
+ *   weight     [width] in weight_dtype (0 / 1)
+ *   y          [rows, width]: y_kind 0 = bf16, 1 = fp32, 2 = e4m3 with scales
+ *   y_scale    y_kind 2 only: fp32 [rows] (scale_group 0) or [rows, ceil(width / 128)] (scale_group 128);
+ *              scale = max|y| / 448 over the row or block and the stored value is e4m3(y / scale), so that
+ *              value * scale stands for y; a block of zeros has scale 0.  lckv_quant_linear takes both.
+ * An output may take the place of a dense input of the same type; other overlaps are refused.
+ * width 1 .. 32768.  Errors: EINVAL, ECUDA.
+ */
+int lckv_rms_norm(const void* x, int64_t x_stride, int32_t x_dtype, const void* residual,
+                  void* residual_out, int32_t residual_dtype, const void* weight, int32_t weight_dtype,
+                  void* y, int32_t y_kind, float* y_scale, int32_t scale_group, int32_t rows,
+                  int32_t width, float eps, void* stream);
+
+/*
+ * Products with 4-bit weights (the projections of a decode step: queries, keys and values of the layers that
+ * own a cache, attention output, MLP):
+ *     y[m, f] = sum_c x[m, c] * scales[f, c / group] * (codes[f, c] - zeros[f, c / group])
+ * lckv_quant_pack lays a weight out once, lckv_quant_linear multiplies by it.
+ *   codes      [n, k / 2] bytes, low nibble = even column
+ *   scales     [n, k / group] bf16;  zeros [n, k / group] bytes 0 .. 15, or NULL (8 everywhere)
+ *   group      32, 64 or 128, dividing k
+ *   packed     lckv_quant_bytes(n, k, group, zeros != NULL) bytes, 256-byte aligned (0: bad shape)
+ *   x          [rows, k], x_stride elements between rows (0 => k), 16-byte aligned rows: bf16 (x_kind 0) or
+ *              e4m3 (x_kind 1) with x_scale fp32, [rows] (x_scale_group 0) or [rows, ceil(k / 128)]
+ *              (x_scale_group 128), as lckv_rms_norm writes them
+ *   y          [rows, n], y_stride elements between rows (0 => n), bf16 (y_dtype 0) or fp32 (1)
+ * codes - zeros are exact on the tensor cores; a group's sum is accumulated in fp32 and scaled in fp32, and
+ * there is one rounding to y's type.  Results do not depend on the order of execution.  rows 1 .. 524288.
+ * Errors: EINVAL (null, shape, alignment, y overlapping x or packed), ENOMEM (packed too small or misaligned,
+ * lckv_quant_pack only), ECUDA.
+ */
+size_t lckv_quant_bytes(int32_t n, int32_t k, int32_t group, int32_t has_zeros);
+int lckv_quant_pack(const void* codes, const void* scales, const void* zeros, int32_t n, int32_t k,
+                    int32_t group, void* packed, size_t packed_bytes, void* stream);
+int lckv_quant_linear(const void* packed, int32_t n, int32_t k, int32_t group, int32_t has_zeros,
+                      const void* x, int64_t x_stride, int32_t x_kind, const float* x_scale,
+                      int32_t x_scale_group, void* y, int64_t y_stride, int32_t y_dtype, int32_t rows,
+                      void* stream);
 
 /* Short English name of a status code. */
 const char* lckv_status_string(int status);

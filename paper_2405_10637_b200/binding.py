@@ -31,8 +31,19 @@ class Info(C.Structure):
                 ("workspace_bytes", C.c_uint64)]
 
 
+class Rope(C.Structure):
+    _fields_ = [("struct_size", C.c_uint32), ("rot_dim", C.c_int32), ("interleaved", C.c_int32),
+                ("positions", C.c_int32), ("cos", C.c_void_p), ("sin", C.c_void_p)]
+
+
+class RopeScaling(C.Structure):
+    _fields_ = [("struct_size", C.c_uint32), ("kind", C.c_int32), ("base", C.c_double),
+                ("factor", C.c_double), ("original", C.c_double), ("low", C.c_double),
+                ("high", C.c_double), ("amplitude", C.c_double)]
+
+
 # name -> (restype, argtypes); also the list of symbols the header declares
-_vp, _i32, _i32p = C.c_void_p, C.c_int32, C.POINTER(C.c_int32)
+_vp, _i32, _i32p, _i64 = C.c_void_p, C.c_int32, C.POINTER(C.c_int32), C.c_int64
 _vpp = C.POINTER(C.c_void_p)
 SIGNATURES = {
     "lckv_plan": (C.c_int, [_i32, _i32, _i32, _i32p, _i32p, _i32p, _i32p, _i32p, _i32p]),
@@ -58,6 +69,16 @@ SIGNATURES = {
     "lckv_decode_attention_static": (C.c_int, [_vp, _vp, _vp, _vp, _vp, _vp, _vp, _i32, _i32, _i32,
                                               _i32, C.c_int64, _i32, C.c_float, _i32, _vp]),
     "lckv_read_stream_probe": (C.c_int, [_vp, C.c_size_t, _i32, _i32, C.c_float, _vp, _vp, _vp]),
+    "lckv_rope_tables": (C.c_int, [_vp, _vp, _i32, _i32, _vp, _vp]),
+    "lckv_rope_apply": (C.c_int, [_vp, _vp, _vp, _i64, _i64, _vp, _i64, _i64, _i32, _i32, _i32, _i32, _i32, _vp]),
+    "lckv_rope_append_kv": (C.c_int, [_vp, _i32, _vp, _vp, _i64, _vp, _vp, _vp, _i64, _i32, _i32, _i32, _vp]),
+    "lckv_rope_prefill_write_kv": (C.c_int, [_vp, _i32, _vp, _vp, _i64, _vp, _vp, _vp, _i64, _i32, _i32, _vp]),
+    "lckv_rms_norm": (C.c_int, [_vp, _i64, _i32, _vp, _vp, _i32, _vp, _i32, _vp, _i32, _vp, _i32, _i32, _i32,
+                                C.c_float, _vp]),
+    "lckv_quant_bytes": (C.c_size_t, [_i32, _i32, _i32, _i32]),
+    "lckv_quant_pack": (C.c_int, [_vp, _vp, _vp, _i32, _i32, _i32, _vp, C.c_size_t, _vp]),
+    "lckv_quant_linear": (C.c_int, [_vp, _i32, _i32, _i32, _i32, _vp, _i64, _i32, _vp, _i32, _vp, _i64, _i32, _i32,
+                                    _vp]),
     "lckv_status_string": (C.c_char_p, [C.c_int]),
     "lckv_last_cuda_error": (C.c_int, []),
 }
@@ -153,6 +174,186 @@ def lckv_read_stream_probe(src, nbytes, kind, dev_sum, dev_status, repeats=1, l2
     dev_sum (uint32/int32 [1]) and dev_status (int32 [1]) are CUDA tensors."""
     _chk(lib().lckv_read_stream_probe(_ptr(src), nbytes, kind, repeats, l2_keep, _ptr(dev_sum),
                                       _ptr(dev_status), _stream(stream)), "lckv_read_stream_probe")
+
+
+# -- operators around the attention ------------------------------------------------------------
+# A decode step makes these calls once or several times per layer, so they marshal plain integers and
+# look the stream up directly; the arguments' types, shapes and devices are checked here, since a
+# tensor of another type would be read past its end on the device.
+_raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None)
+_FLOATS = {torch.bfloat16: 0, torch.float32: 1}
+
+
+def _require(ok, what):
+    if not ok:
+        raise LckvError(EINVAL, what)
+
+
+def _stream_on(device, stream):
+    """cudaStream_t of `stream`, or of the current stream of `device`."""
+    if stream is not None:
+        _require(stream.device == device, "the stream belongs to another device than the tensors")
+        return stream.cuda_stream
+    if _raw_stream is not None:
+        return _raw_stream(device.index)
+    return torch.cuda.current_stream(device).cuda_stream
+
+
+def _call(device, stream, name, *args):
+    """One library call with `device` current; the stream is the last argument."""
+    fn = getattr(_LIB or lib(), name)
+    if torch.cuda.current_device() == device.index:
+        rc = fn(*args, _stream_on(device, stream))
+    else:
+        with torch.cuda.device(device):
+            rc = fn(*args, _stream_on(device, stream))
+    if rc != OK:
+        raise LckvError(rc, name)
+
+
+def _same_device(device, *tensors):
+    for t in tensors:
+        if t is not None and t.device != device:
+            return False
+    return device.type == "cuda"
+
+
+def make_rope_scaling(kind=0, base=10000.0, factor=1.0, original=0.0, low=1.0, high=4.0, amplitude=0.0):
+    """Frequencies of rotary tables: kind 0 none, 1 linear, 2 base, 3 by parts (include/lckv.h)."""
+    return RopeScaling(C.sizeof(RopeScaling), kind, base, factor, original, low, high, amplitude)
+
+
+def lckv_rope_tables(cos, sin, scaling, stream=None):
+    """Fills the CUDA tensors cos, sin [positions, rot_dim / 2] fp32; returns them."""
+    _require(cos.dtype == torch.float32 and sin.dtype == torch.float32 and cos.dim() == 2 and cos.shape == sin.shape
+             and cos.is_contiguous() and sin.is_contiguous() and _same_device(cos.device, cos, sin),
+             "lckv_rope_tables: cos and sin are contiguous fp32 CUDA tensors of one shape")
+    _call(cos.device, stream, "lckv_rope_tables", cos.data_ptr(), sin.data_ptr(), cos.shape[0], 2 * cos.shape[1],
+          C.addressof(scaling))
+    return cos, sin
+
+
+def make_rope(cos, sin, interleaved=False):
+    """A rotation described by its tables, cos and sin [positions, rot_dim / 2] fp32 on the device.  The result keeps
+    the tables alive."""
+    _require(cos.dtype == torch.float32 and sin.dtype == torch.float32 and cos.dim() == 2 and cos.shape == sin.shape
+             and cos.is_contiguous() and sin.is_contiguous() and _same_device(cos.device, cos, sin),
+             "make_rope: cos and sin are contiguous fp32 CUDA tensors of one shape")
+    r = Rope(C.sizeof(Rope), 2 * cos.shape[1], 1 if interleaved else 0, cos.shape[0], cos.data_ptr(), sin.data_ptr())
+    r.tables, r.device, r.address = (cos, sin), cos.device, C.addressof(r)
+    return r
+
+
+def lckv_rope_apply(rope, positions, x, out=None, transpose=False, stream=None):
+    """x [tokens, heads, d_h] bf16 or fp32 (any strides, the last 1) rotated by positions [tokens] int32, into `out`
+    (made if None; may be x)."""
+    if out is None:
+        out = torch.empty(x.shape, dtype=x.dtype, device=x.device)
+    _require(x.dim() == 3 and x.shape == out.shape and x.dtype in _FLOATS and out.dtype == x.dtype
+             and x.stride(2) == 1 and out.stride(2) == 1, "lckv_rope_apply: x and out are [tokens, heads, d_h], bf16 or fp32")
+    _require(positions.dtype == torch.int32 and positions.dim() == 1 and positions.shape[0] == x.shape[0]
+             and positions.is_contiguous() and _same_device(x.device, out, positions, rope.tables[0]),
+             "lckv_rope_apply: positions are [tokens] int32 on x's device")
+    tokens, heads, d = x.shape
+    if tokens == 0:
+        return out
+    _call(x.device, stream, "lckv_rope_apply", rope.address, positions.data_ptr(), x.data_ptr(), x.stride(0), x.stride(1),
+          out.data_ptr(), out.stride(0), out.stride(1), tokens, heads, d, _FLOATS[x.dtype], 1 if transpose else 0)
+    return out
+
+
+def lckv_rms_norm(x, weight, out, residual=None, residual_out=None, out_scale=None, scale_group=0, eps=1e-6,
+                  stream=None):
+    """out = norm(x + residual) * weight over the last dimension of x [rows, width]; the sum goes to residual_out.
+    out is bf16, fp32, or float8_e4m3fn with out_scale fp32 ([rows, 1] or [rows], or [rows, ceil(width / 128)] with
+    scale_group=128)."""
+    rows, width = x.shape
+    kind = 2 if out.dtype == torch.float8_e4m3fn else _FLOATS.get(out.dtype, -1)
+    _require(x.dtype in _FLOATS and kind >= 0 and weight.dtype in _FLOATS and weight.shape == (width,)
+             and out.shape == x.shape and out.is_contiguous() and weight.is_contiguous()
+             and (x.stride(1) == 1 or width == 1) and (rows < 2 or x.stride(0) >= width) and _same_device(x.device, weight, out, residual, residual_out, out_scale),
+             "lckv_rms_norm: x [rows, width], weight [width], out like x, all on one device")
+    r_dtype = 0
+    if residual is not None:
+        _require(residual.dtype in _FLOATS and residual.shape == x.shape and residual.is_contiguous(),
+                 "lckv_rms_norm: residual is contiguous and has x's shape")
+        r_dtype = _FLOATS[residual.dtype]
+    if residual_out is not None:
+        _require(residual is not None and residual_out.dtype == residual.dtype and residual_out.shape == x.shape
+                 and residual_out.is_contiguous(), "lckv_rms_norm: residual_out is like residual")
+    if out_scale is not None:
+        _require(out_scale.dtype == torch.float32 and out_scale.is_contiguous()
+                 and out_scale.numel() == rows * (-(-width // 128) if scale_group else 1),
+                 "lckv_rms_norm: out_scale is contiguous fp32, one per row or per 128 columns")
+    if rows == 0:
+        return out
+    _call(x.device, stream, "lckv_rms_norm", x.data_ptr(), x.stride(0) if rows > 1 else 0, _FLOATS[x.dtype],
+          None if residual is None else residual.data_ptr(), None if residual_out is None else residual_out.data_ptr(),
+          r_dtype, weight.data_ptr(), _FLOATS[weight.dtype], out.data_ptr(), kind,
+          None if out_scale is None else out_scale.data_ptr(), scale_group, rows, width, eps)
+    return out
+
+
+class QuantWeight:
+    """A 4-bit weight [n, k] laid out by lckv_quant_pack, and the buffer behind it."""
+
+    def __init__(self, n, k, group, has_zeros, buf):
+        self.n, self.k, self.group, self.has_zeros, self.buf = n, k, group, has_zeros, buf
+        self.ptr = buf.data_ptr()
+
+
+def lckv_quant_pack(codes, scales, zeros=None, stream=None):
+    """codes [n, k / 2] uint8 (low nibble = even column), scales [n, k / group] bf16, zeros [n, k / group] uint8 or None
+    -> QuantWeight."""
+    n, k = codes.shape[0], 2 * codes.shape[1]
+    _require(codes.dtype == torch.uint8 and codes.is_contiguous() and scales.dtype == torch.bfloat16
+             and scales.is_contiguous() and scales.dim() == 2 and scales.shape[0] == n and scales.shape[1] > 0
+             and k % scales.shape[1] == 0 and _same_device(codes.device, codes, scales, zeros),
+             "lckv_quant_pack: codes [n, k / 2] uint8, scales [n, k / group] bf16, on one device")
+    _require(zeros is None or (zeros.dtype == torch.uint8 and zeros.is_contiguous() and zeros.shape == scales.shape),
+             "lckv_quant_pack: zeros are uint8 of the scales' shape")
+    group = k // scales.shape[1]
+    nbytes = lib().lckv_quant_bytes(n, k, group, 0 if zeros is None else 1)
+    _require(nbytes > 0, "lckv_quant_pack: group is 32, 64 or 128")
+    buf = torch.empty(nbytes, dtype=torch.uint8, device=codes.device)
+    _call(codes.device, stream, "lckv_quant_pack", codes.data_ptr(), scales.data_ptr(),
+          None if zeros is None else zeros.data_ptr(), n, k, group, buf.data_ptr(), nbytes)
+    return QuantWeight(n, k, group, 0 if zeros is None else 1, buf)
+
+
+def lckv_quant_linear(w, x, out=None, x_scale=None, stream=None):
+    """out [rows, n] (bf16 or fp32) = x [rows, k] (bf16, or float8_e4m3fn with x_scale) times the 4-bit weight w."""
+    rows, k = x.shape
+    if out is None:
+        out = torch.empty((rows, w.n), dtype=torch.bfloat16, device=x.device)
+    kind = 1 if x.dtype == torch.float8_e4m3fn else 0
+    _require((kind == 1 or x.dtype == torch.bfloat16) and k == w.k and x.stride(1) == 1 and out.dtype in _FLOATS
+             and out.shape == (rows, w.n) and (out.stride(1) == 1 or w.n == 1)
+             and (rows < 2 or (x.stride(0) >= k and out.stride(0) >= w.n))
+             and _same_device(x.device, w.buf, out, x_scale),
+             "lckv_quant_linear: x [rows, k] bf16 or float8_e4m3fn, out [rows, n], on the weight's device")
+    group = 0
+    if x_scale is not None:
+        _require(kind == 1 and x_scale.dtype == torch.float32 and x_scale.is_contiguous()
+                 and x_scale.numel() in (rows, rows * -(-k // 128)),
+                 "lckv_quant_linear: x_scale is contiguous fp32, one per row or per 128 columns of an 8-bit x")
+        group = 0 if x_scale.numel() == rows else 128
+    if rows == 0:
+        return out
+    _call(x.device, stream, "lckv_quant_linear", w.ptr, w.n, k, w.group, w.has_zeros, x.data_ptr(),
+          x.stride(0) if rows > 1 else 0, kind, None if x_scale is None else x_scale.data_ptr(), group, out.data_ptr(),
+          out.stride(0) if rows > 1 else 0, _FLOATS[out.dtype], rows)
+    return out
+
+
+def _token_stride(t, what):
+    """Elements between consecutive tokens of t [batch, n, heads, d_h], whose heads are dense."""
+    b, n, h, d = t.shape
+    st = t.stride()
+    _require(t.dtype == torch.bfloat16 and (st[3] == 1 or d == 1) and (st[2] == d or h == 1), what)
+    step = st[1] if n > 1 else st[0]
+    _require((n == 1 or b == 1 or st[0] == n * st[1]) and (b * n == 1 or step >= h * d), what)
+    return step if b * n > 1 else 0
 
 
 class Cache:
@@ -256,6 +457,41 @@ class Cache:
         _chk(lib().lckv_project_append_kv(self.h, slot, _ptr(x), x.shape[1], _ptr(w_k), _ptr(w_v),
                                           _ptr(rope_cos), _ptr(rope_sin), n_pos, batch, advance_len,
                                           _stream(stream)), "lckv_project_append_kv")
+
+    def _rope_call(self, name, slot, rope, q, k, v, q_out, extra, stream):
+        c, ref = self.cfg, q if q is not None else k
+        _require(ref is not None and ref.dim() in (3, 4), f"{name}: q, k, v are [batch, tokens, heads, d_h]")
+        if q is not None and q_out is None:
+            q_out = torch.empty(q.shape, dtype=q.dtype, device=q.device)
+        if ref.dim() == 3:       # one token per sequence
+            q, k, v = (None if t is None else t.unsqueeze(1) for t in (q, k, v))
+            ref = ref.unsqueeze(1)
+        batch, n = ref.shape[:2]
+        what = f"{name}: bf16 on the cache's device, heads dense, one token stride"
+        if q is not None:
+            _require(q.shape == (batch, n, c.n_q_heads, c.head_dim) and q_out.numel() == q.numel()
+                     and q_out.dtype == torch.bfloat16 and q_out.is_contiguous(), what)
+        if k is not None:
+            _require(v is not None and k.shape == (batch, n, c.n_kv_heads, c.head_dim) and v.shape == k.shape, what)
+        _require(_same_device(self.buf.device, q, k, v, q_out, rope.tables[0]), what)
+        q_step = 0 if q is None else _token_stride(q, what)
+        kv_step = 0 if k is None else _token_stride(k, what)
+        _require(k is None or _token_stride(v, what) == kv_step, what)
+        _call(self.buf.device, stream, name, self.h, slot, rope.address, None if q is None else q.data_ptr(), q_step,
+              None if q is None else q_out.data_ptr(), None if k is None else k.data_ptr(),
+              None if k is None else v.data_ptr(), kv_step, n, batch, *extra)
+        return q_out
+
+    def lckv_rope_append_kv(self, slot, rope, q, k_new, v_new, q_out=None, advance_len=0, stream=None):
+        """Rotated append of one ([batch, heads, d_h]) or several ([batch, n, heads, d_h]) new tokens per sequence;
+        q, or k_new and v_new, may be None.  Views of a fused projection are taken as they are.  Returns q_out."""
+        return self._rope_call("lckv_rope_append_kv", slot, rope, q, k_new, v_new, q_out, (1 if advance_len else 0,), stream)
+
+    def lckv_rope_prefill_write_kv(self, slot, rope, q, k, v, q_out=None, stream=None):
+        """The same for prompts [batch, n_max, heads, d_h] whose lengths the cache holds already."""
+        if q is not None and q_out is None:
+            q_out = torch.zeros(q.shape, dtype=q.dtype, device=q.device)
+        return self._rope_call("lckv_rope_prefill_write_kv", slot, rope, q, k, v, q_out, (), stream)
 
     def lckv_decode_attention(self, slot, mode, q, out=None, lse=None, batch=None, stream=None):
         batch = q.shape[0] if batch is None else batch

@@ -19,6 +19,9 @@
 #include "lckv_prefill_tc5.cuh"
 #include "lckv_probe.cuh"
 #include "lckv_small_kernels.cuh"
+#include "lckv_rope.cuh"
+#include "lckv_norm.cuh"
+#include "lckv_quant.cuh"
 
 namespace {
 
@@ -456,15 +459,15 @@ int launch_append(lckv_cache* c, int slot, const void* k_new, const void* v_new,
     return cuda_ok(cudaGetLastError()) ? LCKV_OK : LCKV_ECUDA;
 }
 
-int launch_advance(lckv_cache* c, int batch, cudaStream_t st)
+int launch_advance(lckv_cache* c, int batch, cudaStream_t st, int by = 1)
 {
-    lckv::advance_kernel<<<(batch + 255) / 256, 256, 0, st>>>(c->d_lens, batch);
+    lckv::advance_kernel<<<(batch + 255) / 256, 256, 0, st>>>(c->d_lens, batch, by);
     return cuda_ok(cudaGetLastError()) ? LCKV_OK : LCKV_ECUDA;
 }
 
-void mirror_advance(lckv_cache* c, int batch)
+void mirror_advance(lckv_cache* c, int batch, int by = 1)
 {
-    for (int b = 0; b < batch; ++b) c->h_lens[b] += 1;
+    for (int b = 0; b < batch; ++b) c->h_lens[b] += by;
 }
 
 // Fraction of a re-read slot's lines to mark evict-last, judged from the host mirror of the
@@ -1468,3 +1471,5 @@ extern "C" int lckv_decode_attention_static(const void* k, const void* v, const 
         lckv::attn_alu_kernel<64><<<sms * lckv::kAluCtas, lckv::kAluWarps * 32, lckv::kAluSmemBytes, st>>>(p);
     return cuda_ok(cudaGetLastError()) ? LCKV_OK : LCKV_ECUDA;
 }
+
+#include "lckv_api_operators.cuh"

@@ -1,0 +1,493 @@
+// C entry points of the operators around the attention: rotary positions, the rotated append, the residual
+// norm, products with 4-bit weights.  Included at the end of lckv_api.cu (they share its cache object and helpers).
+#pragma once
+
+namespace {
+
+// Do [a, a + na) and [b, b + nb) share a byte?
+bool ranges_meet(const void* a, int64_t na, const void* b, int64_t nb)
+{
+    const uintptr_t x = (uintptr_t)a, y = (uintptr_t)b;
+    return x < y + (uintptr_t)nb && y < x + (uintptr_t)na;
+}
+
+bool aligned(const void* p, uintptr_t to) { return ((uintptr_t)p & (to - 1)) == 0; }
+
+template <typename... KArgs, typename... Args>
+cudaError_t launch_pdl_dims(void (*kernel)(KArgs...), dim3 grid, dim3 block, size_t smem, cudaStream_t st, Args... args)
+{
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = grid;
+    cfg.blockDim = block;
+    cfg.dynamicSmemBytes = smem;
+    cfg.stream = st;
+    cudaLaunchAttribute attr[1];
+    attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    attr[0].val.programmaticStreamSerializationAllowed = 1;
+    cfg.attrs = attr;
+    cfg.numAttrs = 1;
+    return cudaLaunchKernelEx(&cfg, kernel, args...);
+}
+
+int rope_args(const lckv_rope_t* r, int head_dim, lckv::RopeArgs* out)
+{
+    if (!r || r->struct_size != sizeof(lckv_rope_t) || !r->cos || !r->sin) return LCKV_EINVAL;
+    if (r->rot_dim < 2 || (r->rot_dim & 1) || r->rot_dim > head_dim) return LCKV_EINVAL;
+    if (r->positions < 1 || (r->interleaved != 0 && r->interleaved != 1)) return LCKV_EINVAL;
+    if (!aligned(r->cos, 4) || !aligned(r->sin, 4)) return LCKV_EINVAL;
+    out->cos = r->cos;
+    out->sin = r->sin;
+    out->positions = r->positions;
+    out->half = r->rot_dim / 2;
+    out->interleaved = r->interleaved;
+    out->sgn = 1.f;
+    return LCKV_OK;
+}
+
+bool rope_tables_vector(const lckv_rope_t* r) { return r->rot_dim % 16 == 0 && aligned(r->cos, 16) && aligned(r->sin, 16); }
+
+// Heads per thread: four when the launch still fills the GPU's threads several times over (one fetch of the
+// unit's cos and sin serves four heads and four pairs of loads are in flight), one when there are few.
+bool rope_many(int64_t units, int sms) { return units >= (int64_t)sms * 2048 * 4; }
+
+dim3 rope_grid(int64_t tokens, int heads, int d, bool vec, int hp)
+{
+    const int64_t per = (int64_t)((heads + hp - 1) / hp) * (vec ? d / 16 : d / 2);
+    if (per >= lckv::kRopeThreads)
+        return dim3((unsigned)tokens, (unsigned)((per + lckv::kRopeThreads - 1) / lckv::kRopeThreads));
+    const int64_t tb = lckv::kRopeThreads / per;
+    return dim3((unsigned)((tokens + tb - 1) / tb));
+}
+
+bool capturing(cudaStream_t st, int* rc)
+{
+    cudaStreamCaptureStatus cs = cudaStreamCaptureStatusNone;
+    *rc = cuda_ok(cudaStreamIsCapturing(st, &cs)) ? LCKV_OK : LCKV_ECUDA;
+    return cs != cudaStreamCaptureStatusNone;
+}
+
+// Does every sequence own pages for its next `extra` rows, on the device too?
+bool pages_ready(const lckv_cache* c, int batch, int extra)
+{
+    if (!c->cfg.page_rows) return true;
+    if (c->pt_dirty) return false;
+    for (int b = 0; b < batch; ++b)
+        if (((int64_t)c->n_pages_of[b] << c->page_shift) < (int64_t)c->h_lens[b] + extra) return false;
+    return true;
+}
+
+int rope_into_cache(lckv_cache* c, int slot, const lckv_rope_t* rope, const void* q, int64_t q_stride, void* q_out,
+                    const void* k, const void* v, int64_t kv_stride, int n, int batch, int advance_len, bool prompt,
+                    cudaStream_t st)
+{
+    if (!c || batch < 1 || batch > c->cfg.max_batch || n < 1) return LCKV_EINVAL;
+    if (slot < 0 || slot >= c->plan.n_slots) return LCKV_EINVAL;
+    if ((q == nullptr) != (q_out == nullptr) || (k == nullptr) != (v == nullptr) || (!q && !k)) return LCKV_EINVAL;
+    if (advance_len && !k) return LCKV_EINVAL;
+    const int d = c->cfg.head_dim, hq = q ? c->cfg.n_q_heads : 0, hkv = k ? c->cfg.n_kv_heads : 0;
+    lckv::RopeAppendParams p;
+    if (int rc = rope_args(rope, d, &p.r)) return rc;
+    const int64_t tokens = (int64_t)batch * n;
+    if (tokens >= (1ll << 31)) return LCKV_EINVAL;
+    if (q_stride == 0) q_stride = (int64_t)hq * d;
+    if (kv_stride == 0) kv_stride = (int64_t)hkv * d;
+    if (q && q_stride < (int64_t)hq * d) return LCKV_EINVAL;
+    if (k && kv_stride < (int64_t)hkv * d) return LCKV_EINVAL;
+    if (!aligned(q, 2) || !aligned(q_out, 2) || !aligned(k, 2) || !aligned(v, 2)) return LCKV_EINVAL;
+    if (q) {
+        // q_out may be q itself (contiguous), else it lies apart from everything that is read
+        const int64_t out_bytes = tokens * hq * d * 2, q_bytes = ((tokens - 1) * q_stride + (int64_t)hq * d) * 2;
+        const int64_t kv_bytes = k ? ((tokens - 1) * kv_stride + (int64_t)hkv * d) * 2 : 0;
+        if (!(q_out == q && q_stride == (int64_t)hq * d) && ranges_meet(q_out, out_bytes, q, q_bytes)) return LCKV_EINVAL;
+        if (k && (ranges_meet(q_out, out_bytes, k, kv_bytes) || ranges_meet(q_out, out_bytes, v, kv_bytes)))
+            return LCKV_EINVAL;
+    }
+    int64_t longest = 0;
+    for (int b = 0; b < batch; ++b) longest = std::max<int64_t>(longest, c->h_lens[b]);
+    if (prompt) {
+        if (int rc = prefill_check(c, n, batch, false)) return rc;
+        if (longest > rope->positions) return LCKV_EINVAL;
+        if (longest == 0) return LCKV_OK;
+    } else {
+        if (longest + n > rope->positions) return LCKV_EINVAL;
+        if (c->cfg.stream_sink > 0) {
+            // no two tokens of one call may share a row of the ring
+            if (k && n > c->cfg.max_seq - c->cfg.stream_sink) return LCKV_EINVAL;
+        } else if (longest + n > c->cfg.max_seq) {
+            return LCKV_ECAPACITY;
+        }
+    }
+    int rc = LCKV_OK;
+    const int extra = prompt || !k ? 0 : n;
+    if (capturing(st, &rc) && (advance_len || (k && !pages_ready(c, batch, extra)))) return LCKV_EINVAL;
+    if (rc) return rc;
+    int sms = c->sm_count;
+    if (k) {
+        if (int rc2 = ensure_pages(c, batch, extra)) return rc2;
+        if (int rc2 = sync_page_table(c, st)) return rc2;
+    }
+    p.q = static_cast<const uint16_t*>(q);
+    p.q_out = static_cast<uint16_t*>(q_out);
+    p.k = static_cast<const uint16_t*>(k);
+    p.v = static_cast<const uint16_t*>(v);
+    p.K = slot_k(c, slot);
+    p.V = slot_v(c, slot);
+    p.lens = c->d_lens;
+    p.page_table = c->d_pt;
+    p.status = c->d_status;
+    p.q_tok = q_stride;
+    p.kv_tok = kv_stride;
+    p.T_cap = c->cfg.max_seq;
+    p.batch = batch;
+    p.n_new = n;
+    p.hq = hq;
+    p.hkv = hkv;
+    p.d = d;
+    p.n_sink = c->cfg.stream_sink;
+    p.pt_stride = c->pt_stride;
+    p.page_shift = c->page_shift;
+    p.prompt = prompt ? 1 : 0;
+    const bool vec = rope_tables_vector(rope) && aligned(q, 16) && aligned(q_out, 16) && aligned(k, 16) && aligned(v, 16) &&
+                     q_stride % 8 == 0 && kv_stride % 8 == 0;
+    const int heads = hq + 2 * hkv;
+    const int hp = vec && rope_many(tokens * heads * (d / 16), sms) ? 4 : 1;
+    const dim3 grid = rope_grid(tokens, heads, d, vec, hp), block(lckv::kRopeThreads);
+    const cudaError_t e = !vec ? launch_pdl_dims(lckv::rope_append_kernel<false, 1>, grid, block, 0, st, p)
+                          : hp == 4 ? launch_pdl_dims(lckv::rope_append_kernel<true, 4>, grid, block, 0, st, p)
+                                    : launch_pdl_dims(lckv::rope_append_kernel<true, 1>, grid, block, 0, st, p);
+    if (!cuda_ok(e)) return LCKV_ECUDA;
+    if (advance_len) {
+        if (int rc2 = launch_advance(c, batch, st, n)) return rc2;
+        mirror_advance(c, batch, n);
+    }
+    return LCKV_OK;
+}
+
+// Tokens and heads at their strides: does no element lie in two places of the tensor?
+bool rope_layout_ok(int64_t tok, int64_t head, int64_t tokens, int64_t heads, int64_t d)
+{
+    if (tok < 0 || head < 0) return false;
+    if (heads > 1 && head < d) return false;
+    if (tokens > 1 && tok < d) return false;
+    if (tokens == 1 || heads == 1) return true;
+    return tok >= (heads - 1) * head + d || head >= (tokens - 1) * tok + d;
+}
+
+}  // namespace
+
+extern "C" {
+
+int lckv_rope_tables(float* cos, float* sin, int32_t positions, int32_t rot_dim, const lckv_rope_scaling_t* s, void* stream)
+{
+    if (!cos || !sin || !s || s->struct_size != sizeof(lckv_rope_scaling_t)) return LCKV_EINVAL;
+    if (positions < 1 || rot_dim < 2 || (rot_dim & 1) || rot_dim > 2 * lckv::kRopeMaxPairs) return LCKV_EINVAL;
+    if (!aligned(cos, 4) || !aligned(sin, 4)) return LCKV_EINVAL;
+    const int half = rot_dim / 2;
+    const int64_t n = (int64_t)positions * half;
+    if (ranges_meet(cos, n * 4, sin, n * 4)) return LCKV_EINVAL;
+    if (s->kind < 0 || s->kind > 3) return LCKV_EINVAL;
+    if (!(s->base > 1.0) || !std::isfinite(s->base)) return LCKV_EINVAL;
+    const double amplitude = s->amplitude == 0.0 ? 1.0 : s->amplitude;
+    if (!std::isfinite(amplitude)) return LCKV_EINVAL;
+    if (s->kind != 0 && (!(s->factor > 0.0) || !std::isfinite(s->factor))) return LCKV_EINVAL;
+    if (s->kind == 3 && (!(s->original > 0.0) || !std::isfinite(s->original) || !(s->low >= 0.0) || !(s->high > s->low) ||
+                         !std::isfinite(s->high)))
+        return LCKV_EINVAL;
+    const double two_pi = 6.283185307179586476925286766559;
+    lckv::RopeTableParams p;
+    const double base = s->kind == 2 && rot_dim > 2 ? s->base * std::pow(s->factor, (double)rot_dim / (rot_dim - 2.0)) : s->base;
+    for (int i = 0; i < half; ++i) {
+        double theta = std::pow(base, -2.0 * i / rot_dim);
+        if (s->kind == 1) theta /= s->factor;
+        if (s->kind == 3) {
+            double keep = (s->original * theta / two_pi - s->low) / (s->high - s->low);
+            keep = keep < 0.0 ? 0.0 : keep > 1.0 ? 1.0 : keep;
+            theta *= keep + (1.0 - keep) / s->factor;
+        }
+        p.turns[i] = theta / two_pi;
+    }
+    p.cos = cos;
+    p.sin = sin;
+    p.n = n;
+    p.half = half;
+    p.amplitude = (float)amplitude;
+    cudaStream_t st = static_cast<cudaStream_t>(stream);
+    const bool vec = half % 4 == 0 && aligned(cos, 16) && aligned(sin, 16);
+    const int64_t threads = vec ? n / 4 : n;
+    const dim3 grid((unsigned)((threads + lckv::kRopeThreads - 1) / lckv::kRopeThreads)), block(lckv::kRopeThreads);
+    const cudaError_t e = vec ? launch_pdl_dims(lckv::rope_table_kernel<4>, grid, block, 0, st, p)
+                              : launch_pdl_dims(lckv::rope_table_kernel<1>, grid, block, 0, st, p);
+    return cuda_ok(e) ? LCKV_OK : LCKV_ECUDA;
+}
+
+int lckv_rope_apply(const lckv_rope_t* rope, const int32_t* positions, const void* x, int64_t x_token_stride,
+                    int64_t x_head_stride, void* y, int64_t y_token_stride, int64_t y_head_stride, int32_t n_tokens,
+                    int32_t n_heads, int32_t head_dim, int32_t dtype, int32_t transpose, void* stream)
+{
+    if (!positions || !x || !y || n_tokens < 1 || n_heads < 1 || n_heads > 65536) return LCKV_EINVAL;
+    if (head_dim != 64 && head_dim != 128) return LCKV_EINVAL;
+    if ((dtype != 0 && dtype != 1) || (transpose != 0 && transpose != 1)) return LCKV_EINVAL;
+    lckv::RopeApplyParams p;
+    if (int rc = rope_args(rope, head_dim, &p.r)) return rc;
+    const int size = dtype ? 4 : 2;
+    if (!aligned(x, size) || !aligned(y, size) || !aligned(positions, 4)) return LCKV_EINVAL;
+    if (x_token_stride < 0 || x_head_stride < 0) return LCKV_EINVAL;      // (0: one token or head, read many times)
+    if (!rope_layout_ok(y_token_stride, y_head_stride, n_tokens, n_heads, head_dim)) return LCKV_EINVAL;
+    const int64_t last = (int64_t)n_tokens - 1, top = (int64_t)n_heads - 1;
+    const int64_t x_span = last * x_token_stride + top * x_head_stride + head_dim;
+    const int64_t y_span = last * y_token_stride + top * y_head_stride + head_dim;
+    if (ranges_meet(x, x_span * size, y, y_span * size)) {
+        // one buffer: in place, or other heads of the same tokens
+        const bool same = (x_token_stride == y_token_stride || last == 0) && (x_head_stride == y_head_stride || top == 0);
+        const int64_t apart = std::abs((int64_t)((intptr_t)y - (intptr_t)x)) / size, row = top * y_head_stride + head_dim;
+        if (!same || !(apart == 0 || (apart >= row && apart + row <= y_token_stride))) return LCKV_EINVAL;
+    }
+    p.r.sgn = transpose ? -1.f : 1.f;
+    p.pos = positions;
+    p.x = x;
+    p.y = y;
+    p.x_tok = x_token_stride;
+    p.x_head = x_head_stride;
+    p.y_tok = y_token_stride;
+    p.y_head = y_head_stride;
+    p.tokens = n_tokens;
+    p.heads = n_heads;
+    p.d = head_dim;
+    int sms = 0;
+    if (int rc = device_sm_count(&sms)) return rc;
+    cudaStream_t st = static_cast<cudaStream_t>(stream);
+    const int64_t grain = 16 / size;
+    const bool vec = rope_tables_vector(rope) && aligned(x, 16) && aligned(y, 16) && x_token_stride % grain == 0 &&
+                     x_head_stride % grain == 0 && y_token_stride % grain == 0 && y_head_stride % grain == 0;
+    const int hp = vec && rope_many((int64_t)n_tokens * n_heads * (head_dim / 16), sms) ? 4 : 1;
+    const dim3 grid = rope_grid(n_tokens, n_heads, head_dim, vec, hp), block(lckv::kRopeThreads);
+    cudaError_t e;
+    if (dtype)
+        e = !vec ? launch_pdl_dims(lckv::rope_apply_kernel<float, false, 1>, grid, block, 0, st, p)
+            : hp == 4 ? launch_pdl_dims(lckv::rope_apply_kernel<float, true, 4>, grid, block, 0, st, p)
+                      : launch_pdl_dims(lckv::rope_apply_kernel<float, true, 1>, grid, block, 0, st, p);
+    else
+        e = !vec ? launch_pdl_dims(lckv::rope_apply_kernel<uint16_t, false, 1>, grid, block, 0, st, p)
+            : hp == 4 ? launch_pdl_dims(lckv::rope_apply_kernel<uint16_t, true, 4>, grid, block, 0, st, p)
+                      : launch_pdl_dims(lckv::rope_apply_kernel<uint16_t, true, 1>, grid, block, 0, st, p);
+    return cuda_ok(e) ? LCKV_OK : LCKV_ECUDA;
+}
+
+int lckv_rope_append_kv(lckv_cache_t* c, int32_t slot, const lckv_rope_t* rope, const void* q, int64_t q_stride, void* q_out,
+                        const void* k_new, const void* v_new, int64_t kv_stride, int32_t n_new, int32_t batch,
+                        int32_t advance_len, void* stream)
+{
+    return rope_into_cache(c, slot, rope, q, q_stride, q_out, k_new, v_new, kv_stride, n_new, batch, advance_len, false,
+                           static_cast<cudaStream_t>(stream));
+}
+
+int lckv_rope_prefill_write_kv(lckv_cache_t* c, int32_t slot, const lckv_rope_t* rope, const void* q, int64_t q_stride,
+                               void* q_out, const void* k, const void* v, int64_t kv_stride, int32_t n_max, int32_t batch,
+                               void* stream)
+{
+    return rope_into_cache(c, slot, rope, q, q_stride, q_out, k, v, kv_stride, n_max, batch, 0, true,
+                           static_cast<cudaStream_t>(stream));
+}
+
+int lckv_rms_norm(const void* x, int64_t x_stride, int32_t x_dtype, const void* residual, void* residual_out,
+                  int32_t residual_dtype, const void* weight, int32_t weight_dtype, void* y, int32_t y_kind, float* y_scale,
+                  int32_t scale_group, int32_t rows, int32_t width, float eps, void* stream)
+{
+    if (!x || !weight || !y || rows < 1 || width < 1 || width > lckv::kNormMaxWidth) return LCKV_EINVAL;
+    if ((x_dtype | residual_dtype | weight_dtype) & ~1) return LCKV_EINVAL;
+    if (y_kind < 0 || y_kind > 2 || (y_kind == 2) != (y_scale != nullptr)) return LCKV_EINVAL;
+    if (scale_group != 0 && !(scale_group == 128 && y_kind == 2)) return LCKV_EINVAL;
+    if (residual_out && !residual) return LCKV_EINVAL;
+    if (!(eps >= 0.f) || !std::isfinite(eps)) return LCKV_EINVAL;
+    if (x_stride == 0) x_stride = width;
+    if (x_stride < width) return LCKV_EINVAL;
+    const int xs = x_dtype ? 4 : 2, rs = residual_dtype ? 4 : 2, ws = weight_dtype ? 4 : 2;
+    const int ys = y_kind == 1 ? 4 : y_kind == 0 ? 2 : 1;
+    if (!aligned(x, xs) || !aligned(residual, rs) || !aligned(residual_out, rs) || !aligned(weight, ws) || !aligned(y, ys) ||
+        !aligned(y_scale, 4))
+        return LCKV_EINVAL;
+    const int n_groups = scale_group ? (width + 127) / 128 : 1;
+    {
+        // an output may take the place of an input of the same type and layout; else it lies apart
+        const int64_t n = (int64_t)rows * width, x_bytes = ((int64_t)(rows - 1) * x_stride + width) * xs;
+        struct Range { const void* p; int64_t bytes; int size; bool dense; };
+        const Range in[3] = {{x, x_bytes, xs, x_stride == width}, {residual, residual ? n * rs : 0, rs, true}, {weight, (int64_t)width * ws, 0, false}};
+        const Range out[3] = {{residual_out, residual_out ? n * rs : 0, rs, true}, {y, n * ys, ys, true},
+                              {y_scale, y_scale ? (int64_t)rows * n_groups * 4 : 0, 0, false}};
+        for (int o = 0; o < 3; ++o) {
+            if (!out[o].bytes) continue;
+            for (int i = 0; i < 3; ++i)
+                if (in[i].bytes && ranges_meet(out[o].p, out[o].bytes, in[i].p, in[i].bytes) &&
+                    !(out[o].p == in[i].p && out[o].size == in[i].size && out[o].dense && in[i].dense))
+                    return LCKV_EINVAL;
+            for (int j = 0; j < o; ++j)
+                if (out[j].bytes && ranges_meet(out[o].p, out[o].bytes, out[j].p, out[j].bytes)) return LCKV_EINVAL;
+        }
+    }
+    lckv::NormParams p;
+    p.x = x;
+    p.r = residual;
+    p.h = residual_out;
+    p.w = weight;
+    p.y = y;
+    p.scale = y_scale;
+    p.x_stride = x_stride;
+    p.rows = rows;
+    p.width = width;
+    p.eps = eps;
+    p.x32 = x_dtype;
+    p.r32 = residual_dtype;
+    p.w32 = weight_dtype;
+    p.out = y_kind;
+    p.group = scale_group;
+    p.n_groups = n_groups;
+    cudaStream_t st = static_cast<cudaStream_t>(stream);
+    const bool vec = width % 8 == 0 && x_stride % 8 == 0 && aligned(x, 16) && aligned(residual, 16) && aligned(residual_out, 16) &&
+                     aligned(weight, 16) && aligned(y, y_kind == 2 ? 8 : 16);
+    cudaError_t e;
+    if (vec) {
+        // threads of a row: one vector each for short launches, up to four where a row has more than 1024
+        const int n_vec = width / 8;
+        const int nv = n_vec > 2048 ? 4 : n_vec > 1024 ? 2 : 1;
+        const int tpr = ((n_vec + nv - 1) / nv + 31) / 32 * 32;
+        const int rpb = tpr == 32 ? 4 : 1;
+        const dim3 grid((unsigned)((rows + rpb - 1) / rpb)), block(tpr, rpb);
+        e = nv == 4 ? launch_pdl_dims(lckv::norm_vec_kernel<4>, grid, block, 0, st, p)
+            : nv == 2 ? launch_pdl_dims(lckv::norm_vec_kernel<2>, grid, block, 0, st, p)
+                      : launch_pdl_dims(lckv::norm_vec_kernel<1>, grid, block, 0, st, p);
+    } else {
+        const size_t smem = (size_t)width * 4;
+        if (smem > 47 * 1024 &&      // (beside the static arrays)
+            !cuda_ok(cudaFuncSetAttribute(lckv::norm_any_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, lckv::kNormMaxWidth * 4)))
+            return LCKV_ECUDA;
+        e = launch_pdl_dims(lckv::norm_any_kernel, dim3((unsigned)rows), dim3(256), smem, st, p);
+    }
+    return cuda_ok(e) ? LCKV_OK : LCKV_ECUDA;
+}
+
+}  // extern "C"
+
+namespace {
+
+bool quant_shape_ok(int32_t n, int32_t k, int32_t group)
+{
+    return n >= 1 && k >= 1 && n <= (1 << 24) && k <= (1 << 24) && (group == 32 || group == 64 || group == 128) && k % group == 0;
+}
+
+template <bool F8, bool ZEROS, int NT>
+cudaError_t launch_quant_mma(const lckv::QuantParams& p, cudaStream_t st)
+{
+    constexpr int smem = lckv::kQuantWarps * 8 * NT * (lckv::kQuantFeat + 4) * 4;
+    if (smem > 48 * 1024) {
+        const cudaError_t e = cudaFuncSetAttribute(lckv::quant_mma_kernel<F8, ZEROS, NT>, cudaFuncAttributeMaxDynamicSharedMemorySize, smem);
+        if (e != cudaSuccess) return e;
+    }
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = dim3(p.n_blocks, (p.m + 8 * NT - 1) / (8 * NT), p.k_split);
+    cfg.blockDim = dim3(lckv::kQuantWarps * 32);
+    cfg.dynamicSmemBytes = smem;
+    cfg.stream = st;
+    cudaLaunchAttribute at[2];
+    at[0].id = cudaLaunchAttributeClusterDimension;
+    at[0].val.clusterDim.x = 1;
+    at[0].val.clusterDim.y = 1;
+    at[0].val.clusterDim.z = p.k_split;
+    at[1].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    at[1].val.programmaticStreamSerializationAllowed = 1;
+    cfg.attrs = at;
+    cfg.numAttrs = 2;
+    return cudaLaunchKernelEx(&cfg, lckv::quant_mma_kernel<F8, ZEROS, NT>, p);
+}
+
+template <bool F8, bool ZEROS>
+cudaError_t launch_quant_rows(const lckv::QuantParams& p, cudaStream_t st)
+{
+    return p.m <= 8 ? launch_quant_mma<F8, ZEROS, 1>(p, st) : launch_quant_mma<F8, ZEROS, 2>(p, st);
+}
+
+}  // namespace
+
+extern "C" {
+
+size_t lckv_quant_bytes(int32_t n, int32_t k, int32_t group, int32_t has_zeros)
+{
+    if (!quant_shape_ok(n, k, group) || (has_zeros != 0 && has_zeros != 1)) return 0;
+    return (size_t)lckv::quant_layout(n, k, group, has_zeros != 0).total;
+}
+
+int lckv_quant_pack(const void* codes, const void* scales, const void* zeros, int32_t n, int32_t k, int32_t group, void* packed,
+                    size_t packed_bytes, void* stream)
+{
+    if (!codes || !scales || !packed || !quant_shape_ok(n, k, group)) return LCKV_EINVAL;
+    if (!aligned(scales, 2)) return LCKV_EINVAL;
+    const lckv::QuantLayout y = lckv::quant_layout(n, k, group, zeros != nullptr);
+    if (!aligned(packed, 256) || packed_bytes < (size_t)y.total) return LCKV_ENOMEM;
+    const int64_t src = (int64_t)n * (k / group);
+    if (ranges_meet(packed, y.total, codes, (int64_t)n * (k / 2)) || ranges_meet(packed, y.total, scales, src * 2) ||
+        (zeros && ranges_meet(packed, y.total, zeros, src)))
+        return LCKV_EINVAL;
+    lckv::QuantPackParams p;
+    p.codes = static_cast<const uint8_t*>(codes);
+    p.scales = static_cast<const uint16_t*>(scales);
+    p.zeros = static_cast<const uint8_t*>(zeros);
+    p.out = static_cast<uint8_t*>(packed);
+    p.n = n;
+    p.k = k;
+    p.group = group;
+    int sms = 0;
+    if (int rc = device_sm_count(&sms)) return rc;
+    lckv::quant_pack_kernel<<<sms * 8, 256, 0, static_cast<cudaStream_t>(stream)>>>(p);
+    return cuda_ok(cudaGetLastError()) ? LCKV_OK : LCKV_ECUDA;
+}
+
+int lckv_quant_linear(const void* packed, int32_t n, int32_t k, int32_t group, int32_t has_zeros, const void* x, int64_t x_stride,
+                      int32_t x_kind, const float* x_scale, int32_t x_scale_group, void* y, int64_t y_stride, int32_t y_dtype,
+                      int32_t rows, void* stream)
+{
+    if (!packed || !x || !y || !quant_shape_ok(n, k, group) || (has_zeros != 0 && has_zeros != 1)) return LCKV_EINVAL;
+    if (rows < 1 || rows > (1 << 19)) return LCKV_EINVAL;
+    if (x_kind < 0 || x_kind > 1 || y_dtype < 0 || y_dtype > 1) return LCKV_EINVAL;
+    if ((x_kind == 1) != (x_scale != nullptr)) return LCKV_EINVAL;
+    if (x_scale_group != 0 && !(x_kind == 1 && x_scale_group == 128)) return LCKV_EINVAL;
+    if (x_stride == 0) x_stride = k;
+    if (y_stride == 0) y_stride = n;
+    if (x_stride < k || y_stride < n) return LCKV_EINVAL;
+    const int xs = x_kind ? 1 : 2, ys = y_dtype ? 4 : 2;
+    if (!aligned(packed, 256) || !aligned(x, 16) || (x_stride * xs) % 16 || !aligned(y, ys) || !aligned(x_scale, 4)) return LCKV_EINVAL;
+    const lckv::QuantLayout lay = lckv::quant_layout(n, k, group, has_zeros != 0);
+    const int64_t y_bytes = ((int64_t)(rows - 1) * y_stride + n) * ys;
+    if (ranges_meet(y, y_bytes, x, ((int64_t)(rows - 1) * x_stride + k) * xs) || ranges_meet(y, y_bytes, packed, lay.total))
+        return LCKV_EINVAL;
+    lckv::QuantParams p;
+    p.codes = static_cast<const uint8_t*>(packed);
+    p.scales = reinterpret_cast<const uint16_t*>(p.codes + lay.scales_off);
+    p.zeros = has_zeros ? p.codes + lay.zeros_off : nullptr;
+    p.x = x;
+    p.x_scale = x_scale;
+    p.y = y;
+    p.x_stride = x_stride;
+    p.y_stride = y_stride;
+    p.m = rows;
+    p.n = n;
+    p.k = k;
+    p.group = group;
+    p.group_shift = group == 32 ? 5 : group == 64 ? 6 : 7;
+    p.n_blocks = lay.n_blocks;
+    p.k_blocks = lay.k_blocks;
+    p.groups = lay.groups;
+    p.x_blocks = x_scale_group ? (k + 127) / 128 : 0;
+    p.y32 = y_dtype;
+    int sms = 0;
+    if (int rc = device_sm_count(&sms)) return rc;
+    // Few features: share the k range over a cluster until the SMs are filled, one block of 128 k per warp at least.
+    const int64_t tiles = (int64_t)p.n_blocks * ((rows + (rows <= 8 ? 7 : 15)) / (rows <= 8 ? 8 : 16));
+    int ks = 1;
+    while (ks < 8 && tiles * ks * 2 <= 4 * sms && p.k_blocks >= ks * 2 * lckv::kQuantWarps) ks *= 2;
+    p.k_split = ks;
+    cudaStream_t st = static_cast<cudaStream_t>(stream);
+    const cudaError_t e = x_kind ? (has_zeros ? launch_quant_rows<true, true>(p, st) : launch_quant_rows<true, false>(p, st))
+                                 : (has_zeros ? launch_quant_rows<false, true>(p, st) : launch_quant_rows<false, false>(p, st));
+    return cuda_ok(e) ? LCKV_OK : LCKV_ECUDA;
+}
+
+}  // extern "C"
