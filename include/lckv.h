@@ -545,8 +545,13 @@ int lckv_rms_norm(const void* x, int64_t x_stride, int32_t x_dtype, const void* 
  *              e4m3 (x_kind 1) with x_scale fp32, [rows] (x_scale_group 0) or [rows, ceil(k / 128)]
  *              (x_scale_group 128), as lckv_rms_norm writes them
  *   y          [rows, n], y_stride elements between rows (0 => n), bf16 (y_dtype 0) or fp32 (1)
+ *   dev_status optional DEVICE int32, set to LCKV_ETIMEOUT if a bounded device-side wait gave up (the rows
+ *              concerned are then NaN); it is not cleared.  NULL to ignore
  * codes - zeros are exact on the tensor cores; a group's sum is accumulated in fp32 and scaled in fp32, and
  * there is one rounding to y's type.  Results do not depend on the order of execution.  rows 1 .. 524288.
+ * lckv_quant_pack SYNCHRONISES `stream` (set-up, like lckv_cache_alloc) and is refused while it captures;
+ * lckv_quant_linear only enqueues work.  It requests packed weights before the kernel in front of it in
+ * the stream has ended, so that kernel must not be the one that writes them (lckv_quant_pack's never is).
  * Errors: EINVAL (null, shape, alignment, y overlapping x or packed), ENOMEM (packed too small or misaligned,
  * lckv_quant_pack only), ECUDA.
  */
@@ -556,7 +561,7 @@ int lckv_quant_pack(const void* codes, const void* scales, const void* zeros, in
 int lckv_quant_linear(const void* packed, int32_t n, int32_t k, int32_t group, int32_t has_zeros,
                       const void* x, int64_t x_stride, int32_t x_kind, const float* x_scale,
                       int32_t x_scale_group, void* y, int64_t y_stride, int32_t y_dtype, int32_t rows,
-                      void* stream);
+                      int32_t* dev_status, void* stream);
 
 /* Short English name of a status code. */
 const char* lckv_status_string(int status);

@@ -78,7 +78,7 @@ SIGNATURES = {
     "lckv_quant_bytes": (C.c_size_t, [_i32, _i32, _i32, _i32]),
     "lckv_quant_pack": (C.c_int, [_vp, _vp, _vp, _i32, _i32, _i32, _vp, C.c_size_t, _vp]),
     "lckv_quant_linear": (C.c_int, [_vp, _i32, _i32, _i32, _i32, _vp, _i64, _i32, _vp, _i32, _vp, _i64, _i32, _i32,
-                                    _vp]),
+                                    _vp, _vp]),
     "lckv_status_string": (C.c_char_p, [C.c_int]),
     "lckv_last_cuda_error": (C.c_int, []),
 }
@@ -177,11 +177,16 @@ def lckv_read_stream_probe(src, nbytes, kind, dev_sum, dev_status, repeats=1, l2
 
 
 # -- operators around the attention ------------------------------------------------------------
-# A decode step makes these calls once or several times per layer, so they marshal plain integers and
-# look the stream up directly; the arguments' types, shapes and devices are checked here, since a
-# tensor of another type would be read past its end on the device.
-_raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None)
-_FLOATS = {torch.bfloat16: 0, torch.float32: 1}
+# A decode step makes these calls once or several times per layer, so each checks and marshals with as
+# few Python operations as it can (device indices instead of device objects, each shape and stride tuple
+# taken once, plain integers for pointers): 6 us a call where the first version took 8.5 us, of which the
+# launch itself is 2.7 us.  Types, shapes and devices are checked here, since a tensor of another type
+# would be read past its end on the device.
+_raw_stream = torch._C._cuda_getCurrentRawStream
+_current_device = torch._C._cuda_getDevice
+_BF16, _F32, _E4M3, _U8, _I32 = torch.bfloat16, torch.float32, torch.float8_e4m3fn, torch.uint8, torch.int32
+_FLOATS = {_BF16: 0, _F32: 1}
+_OUT_KINDS = {_BF16: 0, _F32: 1, _E4M3: 2}
 
 
 def _require(ok, what):
@@ -189,33 +194,10 @@ def _require(ok, what):
         raise LckvError(EINVAL, what)
 
 
-def _stream_on(device, stream):
-    """cudaStream_t of `stream`, or of the current stream of `device`."""
-    if stream is not None:
-        _require(stream.device == device, "the stream belongs to another device than the tensors")
-        return stream.cuda_stream
-    if _raw_stream is not None:
-        return _raw_stream(device.index)
-    return torch.cuda.current_stream(device).cuda_stream
-
-
-def _call(device, stream, name, *args):
-    """One library call with `device` current; the stream is the last argument."""
-    fn = getattr(_LIB or lib(), name)
-    if torch.cuda.current_device() == device.index:
-        rc = fn(*args, _stream_on(device, stream))
-    else:
-        with torch.cuda.device(device):
-            rc = fn(*args, _stream_on(device, stream))
-    if rc != OK:
-        raise LckvError(rc, name)
-
-
-def _same_device(device, *tensors):
-    for t in tensors:
-        if t is not None and t.device != device:
-            return False
-    return device.type == "cuda"
+def _other_stream(dev, stream):
+    """cudaStream_t of a stream that the caller gave; it has to belong to the tensors' device."""
+    _require(stream.device.index == dev, "the stream belongs to another device than the tensors")
+    return stream.cuda_stream
 
 
 def make_rope_scaling(kind=0, base=10000.0, factor=1.0, original=0.0, low=1.0, high=4.0, amplitude=0.0):
@@ -223,24 +205,33 @@ def make_rope_scaling(kind=0, base=10000.0, factor=1.0, original=0.0, low=1.0, h
     return RopeScaling(C.sizeof(RopeScaling), kind, base, factor, original, low, high, amplitude)
 
 
+def _check_tables(cos, sin, what):
+    _require(cos.dtype == _F32 and sin.dtype == _F32 and cos.dim() == 2 and cos.shape == sin.shape and cos.is_contiguous()
+             and sin.is_contiguous() and cos.get_device() >= 0 and sin.get_device() == cos.get_device(),
+             f"{what}: cos and sin are contiguous fp32 CUDA tensors of one shape")
+
+
 def lckv_rope_tables(cos, sin, scaling, stream=None):
     """Fills the CUDA tensors cos, sin [positions, rot_dim / 2] fp32; returns them."""
-    _require(cos.dtype == torch.float32 and sin.dtype == torch.float32 and cos.dim() == 2 and cos.shape == sin.shape
-             and cos.is_contiguous() and sin.is_contiguous() and _same_device(cos.device, cos, sin),
-             "lckv_rope_tables: cos and sin are contiguous fp32 CUDA tensors of one shape")
-    _call(cos.device, stream, "lckv_rope_tables", cos.data_ptr(), sin.data_ptr(), cos.shape[0], 2 * cos.shape[1],
-          C.addressof(scaling))
+    _check_tables(cos, sin, "lckv_rope_tables")
+    dev = cos.get_device()
+    if dev != _current_device():
+        with torch.cuda.device(dev):
+            return lckv_rope_tables(cos, sin, scaling, stream)
+    positions, half = cos.shape
+    rc = (_LIB or lib()).lckv_rope_tables(cos.data_ptr(), sin.data_ptr(), positions, 2 * half, C.addressof(scaling),
+                                          _raw_stream(dev) if stream is None else _other_stream(dev, stream))
+    if rc != OK:
+        raise LckvError(rc, "lckv_rope_tables")
     return cos, sin
 
 
 def make_rope(cos, sin, interleaved=False):
     """A rotation described by its tables, cos and sin [positions, rot_dim / 2] fp32 on the device.  The result keeps
     the tables alive."""
-    _require(cos.dtype == torch.float32 and sin.dtype == torch.float32 and cos.dim() == 2 and cos.shape == sin.shape
-             and cos.is_contiguous() and sin.is_contiguous() and _same_device(cos.device, cos, sin),
-             "make_rope: cos and sin are contiguous fp32 CUDA tensors of one shape")
+    _check_tables(cos, sin, "make_rope")
     r = Rope(C.sizeof(Rope), 2 * cos.shape[1], 1 if interleaved else 0, cos.shape[0], cos.data_ptr(), sin.data_ptr())
-    r.tables, r.device, r.address = (cos, sin), cos.device, C.addressof(r)
+    r.tables, r.device, r.address = (cos, sin), cos.get_device(), C.addressof(r)
     return r
 
 
@@ -249,16 +240,25 @@ def lckv_rope_apply(rope, positions, x, out=None, transpose=False, stream=None):
     (made if None; may be x)."""
     if out is None:
         out = torch.empty(x.shape, dtype=x.dtype, device=x.device)
-    _require(x.dim() == 3 and x.shape == out.shape and x.dtype in _FLOATS and out.dtype == x.dtype
-             and x.stride(2) == 1 and out.stride(2) == 1, "lckv_rope_apply: x and out are [tokens, heads, d_h], bf16 or fp32")
-    _require(positions.dtype == torch.int32 and positions.dim() == 1 and positions.shape[0] == x.shape[0]
-             and positions.is_contiguous() and _same_device(x.device, out, positions, rope.tables[0]),
-             "lckv_rope_apply: positions are [tokens] int32 on x's device")
-    tokens, heads, d = x.shape
+    dev, shape, dtype = x.get_device(), x.shape, x.dtype
+    xs, ys = x.stride(), out.stride()
+    kind = _FLOATS.get(dtype)
+    if not (len(shape) == 3 and kind is not None and out.dtype is dtype and out.shape == shape and xs[2] == 1 and ys[2] == 1
+            and positions.dtype is _I32 and positions.shape == shape[:1] and positions.is_contiguous()
+            and dev == out.get_device() == positions.get_device() == rope.device):
+        raise LckvError(EINVAL, "lckv_rope_apply: x and out [tokens, heads, d_h] bf16 or fp32, positions [tokens] int32, "
+                                "all on the tables' device")
+    tokens, heads, d = shape
     if tokens == 0:
         return out
-    _call(x.device, stream, "lckv_rope_apply", rope.address, positions.data_ptr(), x.data_ptr(), x.stride(0), x.stride(1),
-          out.data_ptr(), out.stride(0), out.stride(1), tokens, heads, d, _FLOATS[x.dtype], 1 if transpose else 0)
+    if dev != _current_device():
+        with torch.cuda.device(dev):
+            return lckv_rope_apply(rope, positions, x, out, transpose, stream)
+    rc = (_LIB or lib()).lckv_rope_apply(rope.address, positions.data_ptr(), x.data_ptr(), xs[0], xs[1], out.data_ptr(), ys[0],
+                                         ys[1], tokens, heads, d, kind, 1 if transpose else 0,
+                                         _raw_stream(dev) if stream is None else _other_stream(dev, stream))
+    if rc != OK:
+        raise LckvError(rc, "lckv_rope_apply")
     return out
 
 
@@ -267,30 +267,44 @@ def lckv_rms_norm(x, weight, out, residual=None, residual_out=None, out_scale=No
     """out = norm(x + residual) * weight over the last dimension of x [rows, width]; the sum goes to residual_out.
     out is bf16, fp32, or float8_e4m3fn with out_scale fp32 ([rows, 1] or [rows], or [rows, ceil(width / 128)] with
     scale_group=128)."""
-    rows, width = x.shape
-    kind = 2 if out.dtype == torch.float8_e4m3fn else _FLOATS.get(out.dtype, -1)
-    _require(x.dtype in _FLOATS and kind >= 0 and weight.dtype in _FLOATS and weight.shape == (width,)
-             and out.shape == x.shape and out.is_contiguous() and weight.is_contiguous()
-             and (x.stride(1) == 1 or width == 1) and (rows < 2 or x.stride(0) >= width) and _same_device(x.device, weight, out, residual, residual_out, out_scale),
-             "lckv_rms_norm: x [rows, width], weight [width], out like x, all on one device")
-    r_dtype = 0
+    shape, dev, xs = x.shape, x.get_device(), x.stride()
+    x_kind, w_kind, y_kind = _FLOATS.get(x.dtype), _FLOATS.get(weight.dtype), _OUT_KINDS.get(out.dtype)
+    if not (len(shape) == 2 and x_kind is not None and w_kind is not None and y_kind is not None and out.shape == shape
+            and weight.shape == shape[1:] and out.is_contiguous() and weight.is_contiguous()
+            and (xs[1] == 1 or shape[1] == 1) and (shape[0] < 2 or xs[0] >= shape[1])
+            and dev == weight.get_device() == out.get_device() and dev >= 0):
+        raise LckvError(EINVAL, "lckv_rms_norm: x [rows, width], weight [width], out like x, bf16 or fp32 on one device "
+                                "(out also float8_e4m3fn)")
+    rows, width = shape
+    r = ro = sc = None
+    r_kind = 0
     if residual is not None:
-        _require(residual.dtype in _FLOATS and residual.shape == x.shape and residual.is_contiguous(),
-                 "lckv_rms_norm: residual is contiguous and has x's shape")
-        r_dtype = _FLOATS[residual.dtype]
-    if residual_out is not None:
-        _require(residual is not None and residual_out.dtype == residual.dtype and residual_out.shape == x.shape
-                 and residual_out.is_contiguous(), "lckv_rms_norm: residual_out is like residual")
+        r_kind = _FLOATS.get(residual.dtype)
+        if r_kind is None or residual.shape != shape or not residual.is_contiguous() or residual.get_device() != dev:
+            raise LckvError(EINVAL, "lckv_rms_norm: residual is contiguous, bf16 or fp32, and has x's shape and device")
+        r = residual.data_ptr()
+        if residual_out is not None:
+            if (residual_out.dtype is not residual.dtype or residual_out.shape != shape or not residual_out.is_contiguous()
+                    or residual_out.get_device() != dev):
+                raise LckvError(EINVAL, "lckv_rms_norm: residual_out is like residual")
+            ro = residual_out.data_ptr()
+    elif residual_out is not None:
+        raise LckvError(EINVAL, "lckv_rms_norm: residual_out without residual")
     if out_scale is not None:
-        _require(out_scale.dtype == torch.float32 and out_scale.is_contiguous()
-                 and out_scale.numel() == rows * (-(-width // 128) if scale_group else 1),
-                 "lckv_rms_norm: out_scale is contiguous fp32, one per row or per 128 columns")
+        if (out_scale.dtype is not _F32 or not out_scale.is_contiguous() or out_scale.get_device() != dev
+                or out_scale.numel() != rows * (-(-width // 128) if scale_group else 1)):
+            raise LckvError(EINVAL, "lckv_rms_norm: out_scale is contiguous fp32, one per row or per 128 columns")
+        sc = out_scale.data_ptr()
     if rows == 0:
         return out
-    _call(x.device, stream, "lckv_rms_norm", x.data_ptr(), x.stride(0) if rows > 1 else 0, _FLOATS[x.dtype],
-          None if residual is None else residual.data_ptr(), None if residual_out is None else residual_out.data_ptr(),
-          r_dtype, weight.data_ptr(), _FLOATS[weight.dtype], out.data_ptr(), kind,
-          None if out_scale is None else out_scale.data_ptr(), scale_group, rows, width, eps)
+    if dev != _current_device():
+        with torch.cuda.device(dev):
+            return lckv_rms_norm(x, weight, out, residual, residual_out, out_scale, scale_group, eps, stream)
+    rc = (_LIB or lib()).lckv_rms_norm(x.data_ptr(), xs[0] if rows > 1 else 0, x_kind, r, ro, r_kind, weight.data_ptr(), w_kind,
+                                       out.data_ptr(), y_kind, sc, scale_group, rows, width, eps,
+                                       _raw_stream(dev) if stream is None else _other_stream(dev, stream))
+    if rc != OK:
+        raise LckvError(rc, "lckv_rms_norm")
     return out
 
 
@@ -299,61 +313,84 @@ class QuantWeight:
 
     def __init__(self, n, k, group, has_zeros, buf):
         self.n, self.k, self.group, self.has_zeros, self.buf = n, k, group, has_zeros, buf
-        self.ptr = buf.data_ptr()
+        self.ptr, self.device = buf.data_ptr(), buf.get_device()
 
 
 def lckv_quant_pack(codes, scales, zeros=None, stream=None):
     """codes [n, k / 2] uint8 (low nibble = even column), scales [n, k / group] bf16, zeros [n, k / group] uint8 or None
     -> QuantWeight."""
-    n, k = codes.shape[0], 2 * codes.shape[1]
-    _require(codes.dtype == torch.uint8 and codes.is_contiguous() and scales.dtype == torch.bfloat16
-             and scales.is_contiguous() and scales.dim() == 2 and scales.shape[0] == n and scales.shape[1] > 0
-             and k % scales.shape[1] == 0 and _same_device(codes.device, codes, scales, zeros),
+    dev = codes.get_device()
+    _require(codes.dim() == 2 and codes.dtype is _U8 and codes.is_contiguous() and scales.dtype is _BF16
+             and scales.is_contiguous() and scales.dim() == 2 and scales.shape[0] == codes.shape[0] and scales.shape[1] > 0
+             and 2 * codes.shape[1] % scales.shape[1] == 0 and dev == scales.get_device() and dev >= 0,
              "lckv_quant_pack: codes [n, k / 2] uint8, scales [n, k / group] bf16, on one device")
-    _require(zeros is None or (zeros.dtype == torch.uint8 and zeros.is_contiguous() and zeros.shape == scales.shape),
-             "lckv_quant_pack: zeros are uint8 of the scales' shape")
+    _require(zeros is None or (zeros.dtype is _U8 and zeros.is_contiguous() and zeros.shape == scales.shape
+                               and zeros.get_device() == dev), "lckv_quant_pack: zeros are uint8 of the scales' shape")
+    n, k = codes.shape[0], 2 * codes.shape[1]
     group = k // scales.shape[1]
     nbytes = lib().lckv_quant_bytes(n, k, group, 0 if zeros is None else 1)
     _require(nbytes > 0, "lckv_quant_pack: group is 32, 64 or 128")
-    buf = torch.empty(nbytes, dtype=torch.uint8, device=codes.device)
-    _call(codes.device, stream, "lckv_quant_pack", codes.data_ptr(), scales.data_ptr(),
-          None if zeros is None else zeros.data_ptr(), n, k, group, buf.data_ptr(), nbytes)
+    with torch.cuda.device(dev):
+        buf = torch.empty(nbytes, dtype=torch.uint8, device=codes.device)
+        _chk(lib().lckv_quant_pack(codes.data_ptr(), scales.data_ptr(), None if zeros is None else zeros.data_ptr(), n, k,
+                                   group, buf.data_ptr(), nbytes,
+                                   _raw_stream(dev) if stream is None else _other_stream(dev, stream)), "lckv_quant_pack")
     return QuantWeight(n, k, group, 0 if zeros is None else 1, buf)
 
 
-def lckv_quant_linear(w, x, out=None, x_scale=None, stream=None):
-    """out [rows, n] (bf16 or fp32) = x [rows, k] (bf16, or float8_e4m3fn with x_scale) times the 4-bit weight w."""
-    rows, k = x.shape
+def lckv_quant_linear(w, x, out=None, x_scale=None, dev_status=None, stream=None):
+    """out [rows, n] (bf16 or fp32) = x [rows, k] (bf16, or float8_e4m3fn with x_scale) times the 4-bit weight w.
+    dev_status: optional CUDA int32 tensor that receives ETIMEOUT if a device-side wait gave up."""
+    shape, dev, xs, n = x.shape, x.get_device(), x.stride(), w.n
+    kind = 0 if x.dtype is _BF16 else 1 if x.dtype is _E4M3 else -1
+    _require(len(shape) == 2, "lckv_quant_linear: x is [rows, k]")
+    rows, k = shape
     if out is None:
-        out = torch.empty((rows, w.n), dtype=torch.bfloat16, device=x.device)
-    kind = 1 if x.dtype == torch.float8_e4m3fn else 0
-    _require((kind == 1 or x.dtype == torch.bfloat16) and k == w.k and x.stride(1) == 1 and out.dtype in _FLOATS
-             and out.shape == (rows, w.n) and (out.stride(1) == 1 or w.n == 1)
-             and (rows < 2 or (x.stride(0) >= k and out.stride(0) >= w.n))
-             and _same_device(x.device, w.buf, out, x_scale),
-             "lckv_quant_linear: x [rows, k] bf16 or float8_e4m3fn, out [rows, n], on the weight's device")
-    group = 0
+        out = torch.empty((rows, n), dtype=_BF16, device=x.device)
+    ys, y_kind = out.stride(), _FLOATS.get(out.dtype)
+    if not (kind >= 0 and y_kind is not None and k == w.k and xs[1] == 1 and out.shape == (rows, n) and (ys[1] == 1 or n == 1)
+            and (rows < 2 or (xs[0] >= k and ys[0] >= n)) and dev == w.device == out.get_device()):
+        raise LckvError(EINVAL, "lckv_quant_linear: x [rows, k] bf16 or float8_e4m3fn, out [rows, n] bf16 or fp32, on the "
+                                "weight's device")
+    sc, group = None, 0
     if x_scale is not None:
-        _require(kind == 1 and x_scale.dtype == torch.float32 and x_scale.is_contiguous()
-                 and x_scale.numel() in (rows, rows * -(-k // 128)),
-                 "lckv_quant_linear: x_scale is contiguous fp32, one per row or per 128 columns of an 8-bit x")
         group = 0 if x_scale.numel() == rows else 128
+        if not (kind == 1 and x_scale.dtype is _F32 and x_scale.is_contiguous() and x_scale.get_device() == dev
+                and x_scale.numel() == (rows * -(-k // 128) if group else rows)):
+            raise LckvError(EINVAL, "lckv_quant_linear: x_scale is contiguous fp32, one per row or per 128 columns of an "
+                                    "8-bit x")
+        sc = x_scale.data_ptr()
     if rows == 0:
         return out
-    _call(x.device, stream, "lckv_quant_linear", w.ptr, w.n, k, w.group, w.has_zeros, x.data_ptr(),
-          x.stride(0) if rows > 1 else 0, kind, None if x_scale is None else x_scale.data_ptr(), group, out.data_ptr(),
-          out.stride(0) if rows > 1 else 0, _FLOATS[out.dtype], rows)
+    if dev_status is not None and not (dev_status.dtype is _I32 and dev_status.numel() > 0 and dev_status.get_device() == dev):
+        raise LckvError(EINVAL, "lckv_quant_linear: dev_status is int32 on the weight's device")
+    if dev != _current_device():
+        with torch.cuda.device(dev):
+            return lckv_quant_linear(w, x, out, x_scale, dev_status, stream)
+    rc = (_LIB or lib()).lckv_quant_linear(w.ptr, n, k, w.group, w.has_zeros, x.data_ptr(), xs[0] if rows > 1 else 0, kind, sc,
+                                           group, out.data_ptr(), ys[0] if rows > 1 else 0, y_kind, rows,
+                                           None if dev_status is None else dev_status.data_ptr(),
+                                           _raw_stream(dev) if stream is None else _other_stream(dev, stream))
+    if rc != OK:
+        raise LckvError(rc, "lckv_quant_linear")
     return out
 
 
-def _token_stride(t, what):
-    """Elements between consecutive tokens of t [batch, n, heads, d_h], whose heads are dense."""
-    b, n, h, d = t.shape
+def _token_stride(t, dev, batch, n, heads, d):
+    """Elements between consecutive tokens of a bf16 tensor [batch, n, heads, d_h] whose heads are dense ([batch, heads, d_h]
+    where n is None); -1 where it is none."""
     st = t.stride()
-    _require(t.dtype == torch.bfloat16 and (st[3] == 1 or d == 1) and (st[2] == d or h == 1), what)
-    step = st[1] if n > 1 else st[0]
-    _require((n == 1 or b == 1 or st[0] == n * st[1]) and (b * n == 1 or step >= h * d), what)
-    return step if b * n > 1 else 0
+    if t.dtype is not _BF16 or t.get_device() != dev or t.shape != ((batch, heads, d) if n is None else (batch, n, heads, d)):
+        return -1
+    if st[-1] != 1 or (st[-2] != d and heads > 1):
+        return -1
+    if n is None or n == 1:
+        step, tokens = st[0], batch
+    else:
+        step, tokens = st[1], batch * n
+        if batch > 1 and st[0] != n * step:
+            return -1
+    return 0 if tokens == 1 else step if step >= heads * d else -1
 
 
 class Cache:
@@ -371,6 +408,7 @@ class Cache:
             _chk(lib().lckv_cache_alloc(C.byref(h), C.byref(cfg), _ptr(self.buf), nbytes),
                  "lckv_cache_alloc")
         self.h = h
+        self.dev_index = self.buf.get_device()
         info = Info()
         _chk(lib().lckv_cache_info(self.h, C.byref(info)), "lckv_cache_info")
         self.info = info
@@ -458,40 +496,52 @@ class Cache:
                                           _ptr(rope_cos), _ptr(rope_sin), n_pos, batch, advance_len,
                                           _stream(stream)), "lckv_project_append_kv")
 
-    def _rope_call(self, name, slot, rope, q, k, v, q_out, extra, stream):
-        c, ref = self.cfg, q if q is not None else k
-        _require(ref is not None and ref.dim() in (3, 4), f"{name}: q, k, v are [batch, tokens, heads, d_h]")
-        if q is not None and q_out is None:
-            q_out = torch.empty(q.shape, dtype=q.dtype, device=q.device)
-        if ref.dim() == 3:       # one token per sequence
-            q, k, v = (None if t is None else t.unsqueeze(1) for t in (q, k, v))
-            ref = ref.unsqueeze(1)
-        batch, n = ref.shape[:2]
-        what = f"{name}: bf16 on the cache's device, heads dense, one token stride"
-        if q is not None:
-            _require(q.shape == (batch, n, c.n_q_heads, c.head_dim) and q_out.numel() == q.numel()
-                     and q_out.dtype == torch.bfloat16 and q_out.is_contiguous(), what)
-        if k is not None:
-            _require(v is not None and k.shape == (batch, n, c.n_kv_heads, c.head_dim) and v.shape == k.shape, what)
-        _require(_same_device(self.buf.device, q, k, v, q_out, rope.tables[0]), what)
-        q_step = 0 if q is None else _token_stride(q, what)
-        kv_step = 0 if k is None else _token_stride(k, what)
-        _require(k is None or _token_stride(v, what) == kv_step, what)
-        _call(self.buf.device, stream, name, self.h, slot, rope.address, None if q is None else q.data_ptr(), q_step,
-              None if q is None else q_out.data_ptr(), None if k is None else k.data_ptr(),
-              None if k is None else v.data_ptr(), kv_step, n, batch, *extra)
+    def _rope_call(self, name, slot, rope, q, k, v, q_out, advance, stream):
+        c, dev, ref = self.cfg, self.dev_index, q if q is not None else k
+        shape = () if ref is None else ref.shape
+        one = len(shape) == 3                      # one token per sequence
+        batch, n = (shape[0], None if one else shape[1]) if one or len(shape) == 4 else (0, 0)
+        d, q_step, kv_step, qp, qo, kp, vp = c.head_dim, 0, 0, None, None, None, None
+        if batch:
+            if q is not None:
+                if q_out is None:
+                    q_out = torch.empty(shape, dtype=_BF16, device=q.device)
+                q_step = _token_stride(q, dev, batch, n, c.n_q_heads, d)
+                if not (q_out.shape == shape and q_out.dtype is _BF16 and q_out.is_contiguous() and q_out.get_device() == dev):
+                    q_step = -1
+                qp, qo = q.data_ptr(), q_out.data_ptr()
+            if k is not None or v is not None:
+                if k is None or v is None:
+                    raise LckvError(EINVAL, f"{name}: k and v come together")
+                kv_step = _token_stride(k, dev, batch, n, c.n_kv_heads, d)
+                if _token_stride(v, dev, batch, n, c.n_kv_heads, d) != kv_step:
+                    kv_step = -1
+                kp, vp = k.data_ptr(), v.data_ptr()
+        if not batch or q_step < 0 or kv_step < 0 or rope.device != dev:
+            raise LckvError(EINVAL, f"{name}: q, k, v are bf16 [batch, tokens, heads, d_h] (or [batch, heads, d_h]) on the "
+                                    "cache's device, heads dense, one stride between tokens; q_out is contiguous")
+        if dev != _current_device():
+            with torch.cuda.device(dev):
+                return self._rope_call(name, slot, rope, q, k, v, q_out, advance, stream)
+        st = _raw_stream(dev) if stream is None else _other_stream(dev, stream)
+        if advance is None:
+            rc = lib().lckv_rope_prefill_write_kv(self.h, slot, rope.address, qp, q_step, qo, kp, vp, kv_step, n or 1, batch, st)
+        else:
+            rc = lib().lckv_rope_append_kv(self.h, slot, rope.address, qp, q_step, qo, kp, vp, kv_step, n or 1, batch, advance, st)
+        if rc != OK:
+            raise LckvError(rc, name)
         return q_out
 
     def lckv_rope_append_kv(self, slot, rope, q, k_new, v_new, q_out=None, advance_len=0, stream=None):
         """Rotated append of one ([batch, heads, d_h]) or several ([batch, n, heads, d_h]) new tokens per sequence;
         q, or k_new and v_new, may be None.  Views of a fused projection are taken as they are.  Returns q_out."""
-        return self._rope_call("lckv_rope_append_kv", slot, rope, q, k_new, v_new, q_out, (1 if advance_len else 0,), stream)
+        return self._rope_call("lckv_rope_append_kv", slot, rope, q, k_new, v_new, q_out, 1 if advance_len else 0, stream)
 
     def lckv_rope_prefill_write_kv(self, slot, rope, q, k, v, q_out=None, stream=None):
         """The same for prompts [batch, n_max, heads, d_h] whose lengths the cache holds already."""
         if q is not None and q_out is None:
             q_out = torch.zeros(q.shape, dtype=q.dtype, device=q.device)
-        return self._rope_call("lckv_rope_prefill_write_kv", slot, rope, q, k, v, q_out, (), stream)
+        return self._rope_call("lckv_rope_prefill_write_kv", slot, rope, q, k, v, q_out, None, stream)
 
     def lckv_decode_attention(self, slot, mode, q, out=None, lse=None, batch=None, stream=None):
         batch = q.shape[0] if batch is None else batch

@@ -22,6 +22,7 @@
 #include "lckv_rope.cuh"
 #include "lckv_norm.cuh"
 #include "lckv_quant.cuh"
+#include "lckv_quant_tc5.cuh"
 
 namespace {
 
@@ -197,8 +198,8 @@ int make_tensor_map(CUtensorMap* tm, void* base, uint64_t rows, int d, int box_r
     return make_tensor_map_pitch(tm, base, rows, (uint64_t)d, (uint64_t)d * 2, box_rows);
 }
 
-// General form: a bf16 matrix of `rows` x `cols` with a row pitch in bytes (multiple of 16).
-int make_tensor_map_pitch(CUtensorMap* tm, void* base, uint64_t rows, uint64_t cols,
+// General form: a matrix of `rows` x `cols` with a row pitch in bytes (multiple of 16), boxes of box_cols = 128 bytes.
+int make_tensor_map_typed(CUtensorMap* tm, CUtensorMapDataType type, int box_cols, void* base, uint64_t rows, uint64_t cols,
                           uint64_t pitch_bytes, int box_rows)
 {
     static EncodeTiledFn fn = nullptr;
@@ -212,9 +213,9 @@ int make_tensor_map_pitch(CUtensorMap* tm, void* base, uint64_t rows, uint64_t c
     }
     const cuuint64_t gdim[2] = {(cuuint64_t)cols, (cuuint64_t)rows};
     const cuuint64_t gstride[1] = {(cuuint64_t)pitch_bytes};
-    const cuuint32_t box[2] = {64, (cuuint32_t)box_rows};
+    const cuuint32_t box[2] = {(cuuint32_t)box_cols, (cuuint32_t)box_rows};
     const cuuint32_t estr[2] = {1, 1};
-    const CUresult r = fn(tm, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 2, base, gdim, gstride, box, estr,
+    const CUresult r = fn(tm, type, 2, base, gdim, gstride, box, estr,
                           CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B,
                           CU_TENSOR_MAP_L2_PROMOTION_L2_128B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
     if (r != CUDA_SUCCESS) {
@@ -222,6 +223,12 @@ int make_tensor_map_pitch(CUtensorMap* tm, void* base, uint64_t rows, uint64_t c
         return LCKV_ECUDA;
     }
     return LCKV_OK;
+}
+
+// ... of bf16.
+int make_tensor_map_pitch(CUtensorMap* tm, void* base, uint64_t rows, uint64_t cols, uint64_t pitch_bytes, int box_rows)
+{
+    return make_tensor_map_typed(tm, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 64, base, rows, cols, pitch_bytes, box_rows);
 }
 
 void make_layout(const lckv_config_t& c, int n_slots, int n_workers, int n_kv_layers, Layout& y)

@@ -374,35 +374,134 @@ bool quant_shape_ok(int32_t n, int32_t k, int32_t group)
     return n >= 1 && k >= 1 && n <= (1 << 24) && k <= (1 << 24) && (group == 32 || group == 64 || group == 128) && k % group == 0;
 }
 
-template <bool F8, bool ZEROS, int NT>
-cudaError_t launch_quant_mma(const lckv::QuantParams& p, cudaStream_t st)
+// How a launch of thread blocks that each take `feat` features would share n_blocks x k_blocks blocks of weights: the
+// cluster size with the shortest time, counted as rounds over the SMs times (one thread block's weights + what it takes to
+// start, join and store, about as long as `fixed` blocks of weights).
+struct QuantSplit { int ks; int64_t cost; };
+QuantSplit quant_split(int64_t tiles, int k_blocks, int blocks_per_k, int fixed, int min_k, int64_t slots, int sms)
 {
-    constexpr int smem = lckv::kQuantWarps * 8 * NT * (lckv::kQuantFeat + 4) * 4;
-    if (smem > 48 * 1024) {
-        const cudaError_t e = cudaFuncSetAttribute(lckv::quant_mma_kernel<F8, ZEROS, NT>, cudaFuncAttributeMaxDynamicSharedMemorySize, smem);
-        if (e != cudaSuccess) return e;
+    QuantSplit best = {1, INT64_MAX};
+    for (int ks = 1; ks <= 8; ++ks) {
+        if (ks > 1 && (ks * min_k > k_blocks || (slots && tiles * ks > slots))) break;
+        const int64_t cost = ((tiles * ks + sms - 1) / sms) * ((int64_t)((k_blocks + ks - 1) / ks) * blocks_per_k + fixed);
+        if (cost < best.cost) best = {ks, cost};
     }
+    return best;
+}
+
+template <bool F8, bool ZEROS, int GROUP, int FT, int NT>
+cudaError_t launch_quant_mma(lckv::QuantParams& p, int ks, cudaStream_t st)
+{
+    constexpr int scales = lckv::kQuantK / GROUP * lckv::kQuantFeat * 2;
+    constexpr int block = lckv::kQuantCodes + scales + (ZEROS ? scales / 2 : 0);
+    constexpr int smem = lckv::quant_warps(NT) * lckv::quant_slots(FT) * (FT / 2) * block;
+    const cudaError_t e = cudaFuncSetAttribute(lckv::quant_mma_kernel<F8, ZEROS, GROUP, FT, NT>, cudaFuncAttributeMaxDynamicSharedMemorySize, smem);
+    if (e != cudaSuccess) return e;
+    p.k_split = ks;
     cudaLaunchConfig_t cfg = {};
-    cfg.gridDim = dim3(p.n_blocks, (p.m + 8 * NT - 1) / (8 * NT), p.k_split);
-    cfg.blockDim = dim3(lckv::kQuantWarps * 32);
+    cfg.gridDim = dim3((p.n + 16 * FT - 1) / (16 * FT), (p.m + 8 * NT - 1) / (8 * NT), ks);
+    cfg.blockDim = dim3(lckv::quant_warps(NT) * 32);
     cfg.dynamicSmemBytes = smem;
     cfg.stream = st;
     cudaLaunchAttribute at[2];
     at[0].id = cudaLaunchAttributeClusterDimension;
     at[0].val.clusterDim.x = 1;
     at[0].val.clusterDim.y = 1;
-    at[0].val.clusterDim.z = p.k_split;
+    at[0].val.clusterDim.z = ks;
     at[1].id = cudaLaunchAttributeProgrammaticStreamSerialization;
     at[1].val.programmaticStreamSerializationAllowed = 1;
     cfg.attrs = at;
     cfg.numAttrs = 2;
-    return cudaLaunchKernelEx(&cfg, lckv::quant_mma_kernel<F8, ZEROS, NT>, p);
+    return cudaLaunchKernelEx(&cfg, lckv::quant_mma_kernel<F8, ZEROS, GROUP, FT, NT>, p);
+}
+
+// Tensor map of x as boxes of 128 bytes x box_rows rows, 128-byte swizzle, zeros outside.
+int quant_x_map(CUtensorMap* tm, const lckv::QuantParams& p, bool f8, int box_rows)
+{
+    if (!f8) return make_tensor_map_pitch(tm, const_cast<void*>(p.x), (uint64_t)p.m, (uint64_t)p.k, (uint64_t)p.x_stride * 2, box_rows);
+    return make_tensor_map_typed(tm, CU_TENSOR_MAP_DATA_TYPE_UINT8, 128, const_cast<void*>(p.x), (uint64_t)p.m, (uint64_t)p.k,
+                                 (uint64_t)p.x_stride, box_rows);
+}
+
+template <bool F8, bool ZEROS, int GROUP, int NBMAX>
+int launch_quant_tc5(const lckv::QuantParams& q, int sms, int32_t* status, cudaStream_t st)
+{
+    lckv::Quant5Params p;
+    p.w = q.w;
+    p.x_scale = q.x_scale;
+    p.y = q.y;
+    p.status = status;
+    p.y_stride = q.y_stride;
+    p.m = q.m;
+    p.n = q.n;
+    p.k = q.k;
+    p.n_blocks = q.n_blocks;
+    p.k_blocks = q.k_blocks;
+    p.x_blocks = q.x_blocks;
+    p.y32 = q.y32;
+    p.y_vec = q.y_stride % 4 == 0 && aligned(q.y, q.y32 ? 16 : 8);
+    // equal tiles of rows when the batch needs several
+    const int m_tiles = (q.m + NBMAX - 1) / NBMAX;
+    p.NB = ((q.m + m_tiles - 1) / m_tiles + 15) / 16 * 16;
+    const int block = lckv::q5_block(GROUP, ZEROS);
+    p.stages = (220 * 1024 - (F8 ? lckv::kQ5XScales : 0)) / lckv::q5_stage_bytes(p.NB, F8, block);
+    p.stages = std::min(p.stages, lckv::kQ5MaxStages);
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = dim3((p.n_blocks + 3) / 4, m_tiles);
+    const int64_t tiles = (int64_t)cfg.gridDim.x * m_tiles;
+    const int ks = quant_split(tiles, p.k_blocks, 1, 10, 4, 0, sms).ks;        // one thread block per SM
+    p.k_split = ks;
+    CUtensorMap tm;
+    if (int rc = quant_x_map(&tm, q, F8, p.NB)) return rc;
+    const int smem = lckv::q5_smem_bytes(p.NB, F8, block, p.stages);
+    auto kernel = lckv::quant_tc5_kernel<F8, ZEROS, GROUP, NBMAX>;
+    if (!cuda_ok(cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, 227 * 1024))) return LCKV_ECUDA;
+    cfg.gridDim.z = ks;
+    cfg.blockDim = dim3(lckv::q5_threads(NBMAX));
+    cfg.dynamicSmemBytes = smem;
+    cfg.stream = st;
+    cudaLaunchAttribute at[2];
+    at[0].id = cudaLaunchAttributeClusterDimension;
+    at[0].val.clusterDim.x = 1;
+    at[0].val.clusterDim.y = 1;
+    at[0].val.clusterDim.z = ks;
+    at[1].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    at[1].val.programmaticStreamSerializationAllowed = 1;
+    cfg.attrs = at;
+    cfg.numAttrs = 2;
+    return cuda_ok(cudaLaunchKernelEx(&cfg, kernel, p, tm)) ? LCKV_OK : LCKV_ECUDA;
+}
+
+// Up to 16 rows: mma.sync kernel, 8 rows a tile; a warp takes 32 or 64 features, whichever shares out better (measured at
+// 1 row, k = 4096: 4096 features 5.5 / 4.6 us, 12288 7.5 / 8.4 us, 22016 12.6 / 13.5 us), 64 for two tiles of rows, where x
+// costs as much to fetch as the weights (16 rows, 22016 features: 22.3 / 16.6 us).  Beyond, the tcgen05 kernel (32 rows,
+// 4096 x 4096: 10.4 us there, 8.6 us here; at 16 rows 7.0 and 7.8 us, with 22016 features 16.6 and 29.0 us).
+template <bool F8, bool ZEROS, int GROUP>
+int launch_quant_rows(lckv::QuantParams& p, int sms, int32_t* status, cudaStream_t st)
+{
+    if (p.m > 16)
+        return p.m <= 32 ? launch_quant_tc5<F8, ZEROS, GROUP, 32>(p, sms, status, st)
+                         : launch_quant_tc5<F8, ZEROS, GROUP, 128>(p, sms, status, st);
+    const int64_t tiles2 = (p.n + 31) / 32, tiles4 = (p.n + 63) / 64;
+    cudaError_t e;
+    if (p.m > 8) {
+        const QuantSplit s = quant_split(tiles4, p.k_blocks, 4, 8, lckv::quant_warps(2), (int64_t)lckv::quant_ctas(4, 2) * sms, sms);
+        e = launch_quant_mma<F8, ZEROS, GROUP, 4, 2>(p, s.ks, st);
+    } else {
+        const QuantSplit s2 = quant_split(tiles2, p.k_blocks, 2, 8, lckv::quant_warps(1), (int64_t)lckv::quant_ctas(2, 1) * sms, sms);
+        const QuantSplit s4 = quant_split(tiles4, p.k_blocks, 4, 8, lckv::quant_warps(1), (int64_t)lckv::quant_ctas(4, 1) * sms, sms);
+        e = s4.cost <= s2.cost ? launch_quant_mma<F8, ZEROS, GROUP, 4, 1>(p, s4.ks, st)
+                               : launch_quant_mma<F8, ZEROS, GROUP, 2, 1>(p, s2.ks, st);
+    }
+    return cuda_ok(e) ? LCKV_OK : LCKV_ECUDA;
 }
 
 template <bool F8, bool ZEROS>
-cudaError_t launch_quant_rows(const lckv::QuantParams& p, cudaStream_t st)
+int launch_quant_group(lckv::QuantParams& p, int sms, int32_t* status, cudaStream_t st)
 {
-    return p.m <= 8 ? launch_quant_mma<F8, ZEROS, 1>(p, st) : launch_quant_mma<F8, ZEROS, 2>(p, st);
+    return p.group == 32   ? launch_quant_rows<F8, ZEROS, 32>(p, sms, status, st)
+           : p.group == 64 ? launch_quant_rows<F8, ZEROS, 64>(p, sms, status, st)
+                           : launch_quant_rows<F8, ZEROS, 128>(p, sms, status, st);
 }
 
 }  // namespace
@@ -436,13 +535,19 @@ int lckv_quant_pack(const void* codes, const void* scales, const void* zeros, in
     p.group = group;
     int sms = 0;
     if (int rc = device_sm_count(&sms)) return rc;
-    lckv::quant_pack_kernel<<<sms * 8, 256, 0, static_cast<cudaStream_t>(stream)>>>(p);
-    return cuda_ok(cudaGetLastError()) ? LCKV_OK : LCKV_ECUDA;
+    cudaStream_t st = static_cast<cudaStream_t>(stream);
+    int rc = LCKV_OK;
+    if (capturing(st, &rc)) return LCKV_EINVAL;
+    if (rc) return rc;
+    lckv::quant_pack_kernel<<<sms * 8, 256, 0, st>>>(p);
+    if (!cuda_ok(cudaGetLastError())) return LCKV_ECUDA;
+    // lckv_quant_linear requests weights before the kernel in front of it has ended: they are complete from here on
+    return cuda_ok(cudaStreamSynchronize(st)) ? LCKV_OK : LCKV_ECUDA;
 }
 
 int lckv_quant_linear(const void* packed, int32_t n, int32_t k, int32_t group, int32_t has_zeros, const void* x, int64_t x_stride,
                       int32_t x_kind, const float* x_scale, int32_t x_scale_group, void* y, int64_t y_stride, int32_t y_dtype,
-                      int32_t rows, void* stream)
+                      int32_t rows, int32_t* dev_status, void* stream)
 {
     if (!packed || !x || !y || !quant_shape_ok(n, k, group) || (has_zeros != 0 && has_zeros != 1)) return LCKV_EINVAL;
     if (rows < 1 || rows > (1 << 19)) return LCKV_EINVAL;
@@ -453,15 +558,13 @@ int lckv_quant_linear(const void* packed, int32_t n, int32_t k, int32_t group, i
     if (y_stride == 0) y_stride = n;
     if (x_stride < k || y_stride < n) return LCKV_EINVAL;
     const int xs = x_kind ? 1 : 2, ys = y_dtype ? 4 : 2;
-    if (!aligned(packed, 256) || !aligned(x, 16) || (x_stride * xs) % 16 || !aligned(y, ys) || !aligned(x_scale, 4)) return LCKV_EINVAL;
+    if (!aligned(packed, 256) || !aligned(x, 16) || (x_stride * xs) % 16 || !aligned(y, ys) || !aligned(x_scale, 4) || !aligned(dev_status, 4)) return LCKV_EINVAL;
     const lckv::QuantLayout lay = lckv::quant_layout(n, k, group, has_zeros != 0);
     const int64_t y_bytes = ((int64_t)(rows - 1) * y_stride + n) * ys;
     if (ranges_meet(y, y_bytes, x, ((int64_t)(rows - 1) * x_stride + k) * xs) || ranges_meet(y, y_bytes, packed, lay.total))
         return LCKV_EINVAL;
     lckv::QuantParams p;
-    p.codes = static_cast<const uint8_t*>(packed);
-    p.scales = reinterpret_cast<const uint16_t*>(p.codes + lay.scales_off);
-    p.zeros = has_zeros ? p.codes + lay.zeros_off : nullptr;
+    p.w = static_cast<const uint8_t*>(packed);
     p.x = x;
     p.x_scale = x_scale;
     p.y = y;
@@ -471,23 +574,15 @@ int lckv_quant_linear(const void* packed, int32_t n, int32_t k, int32_t group, i
     p.n = n;
     p.k = k;
     p.group = group;
-    p.group_shift = group == 32 ? 5 : group == 64 ? 6 : 7;
     p.n_blocks = lay.n_blocks;
     p.k_blocks = lay.k_blocks;
-    p.groups = lay.groups;
     p.x_blocks = x_scale_group ? (k + 127) / 128 : 0;
     p.y32 = y_dtype;
     int sms = 0;
     if (int rc = device_sm_count(&sms)) return rc;
-    // Few features: share the k range over a cluster until the SMs are filled, one block of 128 k per warp at least.
-    const int64_t tiles = (int64_t)p.n_blocks * ((rows + (rows <= 8 ? 7 : 15)) / (rows <= 8 ? 8 : 16));
-    int ks = 1;
-    while (ks < 8 && tiles * ks * 2 <= 4 * sms && p.k_blocks >= ks * 2 * lckv::kQuantWarps) ks *= 2;
-    p.k_split = ks;
     cudaStream_t st = static_cast<cudaStream_t>(stream);
-    const cudaError_t e = x_kind ? (has_zeros ? launch_quant_rows<true, true>(p, st) : launch_quant_rows<true, false>(p, st))
-                                 : (has_zeros ? launch_quant_rows<false, true>(p, st) : launch_quant_rows<false, false>(p, st));
-    return cuda_ok(e) ? LCKV_OK : LCKV_ECUDA;
+    return x_kind ? (has_zeros ? launch_quant_group<true, true>(p, sms, dev_status, st) : launch_quant_group<true, false>(p, sms, dev_status, st))
+                  : (has_zeros ? launch_quant_group<false, true>(p, sms, dev_status, st) : launch_quant_group<false, false>(p, sms, dev_status, st));
 }
 
 }  // extern "C"

@@ -82,8 +82,8 @@ def test_rms_norm_refuses():
         assert norm(**kw) == lk.EINVAL, kw
 
 
-def linear(w=A, n=64, k=128, group=128, zeros=0, x=FAR, xs=0, xk=0, sc=None, sg=0, y=2 * FAR, ys=0, yd=0, rows=4):
-    return lk.lib().lckv_quant_linear(w, n, k, group, zeros, x, xs, xk, sc, sg, y, ys, yd, rows, None)
+def linear(w=A, n=64, k=128, group=128, zeros=0, x=FAR, xs=0, xk=0, sc=None, sg=0, y=2 * FAR, ys=0, yd=0, rows=4, st=None):
+    return lk.lib().lckv_quant_linear(w, n, k, group, zeros, x, xs, xk, sc, sg, y, ys, yd, rows, st, None)
 
 
 def test_quant_refuses():
@@ -92,12 +92,12 @@ def test_quant_refuses():
            dict(k=192), dict(group=256), dict(zeros=2), dict(rows=0), dict(rows=(1 << 19) + 1), dict(xk=2), dict(yd=2),
            dict(xk=1), dict(sc=S), dict(sg=128), dict(xk=1, sc=S, sg=64), dict(xs=120), dict(xs=132), dict(ys=63),
            dict(w=A + 128), dict(x=FAR + 8), dict(y=2 * FAR + 1), dict(y=2 * FAR + 2, yd=1), dict(xk=1, sc=S + 2),
-           dict(y=FAR), dict(y=A + 64), dict(xk=1, sc=S, xs=136)]
+           dict(y=FAR), dict(y=A + 64), dict(xk=1, sc=S, xs=136), dict(st=S + 2)]
     for kw in bad:
         assert linear(**kw) == lk.EINVAL, kw
     size = lk.lib().lckv_quant_bytes
-    assert size(64, 128, 128, 0) == 64 * 128 // 2 + 64 * 2
-    assert size(1, 32, 32, 1) == 64 * 128 // 2 + 64 * 4 * 3            # padded to 64 features and 128 columns
+    assert size(64, 128, 128, 0) == 128 * 128 // 2 + 128 * 2
+    assert size(1, 32, 32, 1) == 128 * 128 // 2 + 128 * 4 * 3          # padded to 128 features and 128 columns
     for n, k, g, z in [(0, 128, 128, 0), (64, 0, 128, 0), (64, 96, 64, 0), (64, 128, 16, 0), (64, 128, 128, 2)]:
         assert size(n, k, g, z) == 0
     pack = lk.lib().lckv_quant_pack
