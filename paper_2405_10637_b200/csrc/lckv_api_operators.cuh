@@ -50,13 +50,21 @@ bool rope_tables_vector(const lckv_rope_t* r) { return r->rot_dim % 16 == 0 && a
 // unit's cos and sin serves four heads and four pairs of loads are in flight), one when there are few.
 bool rope_many(int64_t units, int sms) { return units >= (int64_t)sms * 2048 * 4; }
 
-dim3 rope_grid(int64_t tokens, int heads, int d, bool vec, int hp)
+dim3 rope_grid(int64_t tokens, int heads, int d, int path, int hp)
 {
-    const int64_t per = (int64_t)((heads + hp - 1) / hp) * (vec ? d / 16 : d / 2);
+    const int64_t per = (int64_t)((heads + hp - 1) / hp) * lckv::rope_units(path, d);
     if (per >= lckv::kRopeThreads)
         return dim3((unsigned)tokens, (unsigned)((per + lckv::kRopeThreads - 1) / lckv::kRopeThreads));
     const int64_t tb = lckv::kRopeThreads / per;
     return dim3((unsigned)((tokens + tb - 1) / tb));
+}
+
+template <typename T>
+void (*rope_apply_variant(int path, int hp))(lckv::RopeApplyParams)
+{
+    if (path == lckv::kRopePairs) return lckv::rope_apply_kernel<T, lckv::kRopePairs, 1>;
+    if (path == lckv::kRopeUnits) return hp == 4 ? lckv::rope_apply_kernel<T, lckv::kRopeUnits, 4> : lckv::rope_apply_kernel<T, lckv::kRopeUnits, 1>;
+    return hp == 4 ? lckv::rope_apply_kernel<T, lckv::kRopeAnySize, 4> : lckv::rope_apply_kernel<T, lckv::kRopeAnySize, 1>;
 }
 
 bool capturing(cudaStream_t st, int* rc)
@@ -147,14 +155,15 @@ int rope_into_cache(lckv_cache* c, int slot, const lckv_rope_t* rope, const void
     p.pt_stride = c->pt_stride;
     p.page_shift = c->page_shift;
     p.prompt = prompt ? 1 : 0;
-    const bool vec = rope_tables_vector(rope) && aligned(q, 16) && aligned(q_out, 16) && aligned(k, 16) && aligned(v, 16) &&
-                     q_stride % 8 == 0 && kv_stride % 8 == 0;
+    const bool vec = aligned(q, 16) && aligned(q_out, 16) && aligned(k, 16) && aligned(v, 16) && q_stride % 8 == 0 && kv_stride % 8 == 0;
+    const int path = !vec ? lckv::kRopePairs : rope_tables_vector(rope) ? lckv::kRopeUnits : lckv::kRopeAnySize;
     const int heads = hq + 2 * hkv;
     const int hp = vec && rope_many(tokens * heads * (d / 16), sms) ? 4 : 1;
-    const dim3 grid = rope_grid(tokens, heads, d, vec, hp), block(lckv::kRopeThreads);
-    const cudaError_t e = !vec ? launch_pdl_dims(lckv::rope_append_kernel<false, 1>, grid, block, 0, st, p)
-                          : hp == 4 ? launch_pdl_dims(lckv::rope_append_kernel<true, 4>, grid, block, 0, st, p)
-                                    : launch_pdl_dims(lckv::rope_append_kernel<true, 1>, grid, block, 0, st, p);
+    const dim3 grid = rope_grid(tokens, heads, d, path, hp), block(lckv::kRopeThreads);
+    const auto kernel = path == lckv::kRopePairs   ? lckv::rope_append_kernel<lckv::kRopePairs, 1>
+                        : path == lckv::kRopeUnits ? (hp == 4 ? lckv::rope_append_kernel<lckv::kRopeUnits, 4> : lckv::rope_append_kernel<lckv::kRopeUnits, 1>)
+                                                   : (hp == 4 ? lckv::rope_append_kernel<lckv::kRopeAnySize, 4> : lckv::rope_append_kernel<lckv::kRopeAnySize, 1>);
+    const cudaError_t e = launch_pdl_dims(kernel, grid, block, 0, st, p);
     if (!cuda_ok(e)) return LCKV_ECUDA;
     if (advance_len) {
         if (int rc2 = launch_advance(c, batch, st, n)) return rc2;
@@ -171,6 +180,82 @@ bool rope_layout_ok(int64_t tok, int64_t head, int64_t tokens, int64_t heads, in
     if (tokens > 1 && tok < d) return false;
     if (tokens == 1 || heads == 1) return true;
     return tok >= (heads - 1) * head + d || head >= (tokens - 1) * tok + d;
+}
+
+}  // namespace
+
+namespace {
+
+// Threads of a row of n_vec vectors at nv vectors each: 8, 16 or 32 lanes of a warp, or whole warps.
+int norm_threads(int n_vec, int nv)
+{
+    const int t = (n_vec + nv - 1) / nv;
+    return t <= 8 ? 8 : t <= 16 ? 16 : (t + 31) / 32 * 32;
+}
+
+struct NormShape { int tpr, rpb, smem, sms; };
+
+template <int NV, bool EDGES, int X32, int RES, int OUT>
+cudaError_t norm_ring_launch(const lckv::NormParams& p, const NormShape& g, cudaStream_t st)
+{
+    const auto kernel = lckv::norm_ring_kernel<NV, EDGES, lckv::NormTypes<X32, RES, OUT>>;
+    cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, 224 * 1024);
+    if (e != cudaSuccess) return e;
+    int per_sm = 0;
+    e = cudaOccupancyMaxActiveBlocksPerMultiprocessor(&per_sm, kernel, g.tpr * g.rpb, g.smem);
+    if (e != cudaSuccess) return e;
+    const int64_t blocks = std::min<int64_t>((int64_t)g.sms * std::max(1, per_sm), ((int64_t)p.rows + g.rpb - 1) / g.rpb);
+    return launch_pdl_dims(kernel, dim3((unsigned)blocks), dim3(g.tpr, g.rpb), g.smem, st, p);
+}
+template <int NV, bool EDGES, int X32, int RES>
+cudaError_t norm_ring_out(const lckv::NormParams& p, const NormShape& g, cudaStream_t st)
+{
+    if constexpr (!EDGES)
+        if (p.out == 2 && p.group) return norm_ring_launch<NV, EDGES, X32, RES, 3>(p, g, st);
+    return p.out == 0   ? norm_ring_launch<NV, EDGES, X32, RES, 0>(p, g, st)
+           : p.out == 1 ? norm_ring_launch<NV, EDGES, X32, RES, 1>(p, g, st)
+                        : norm_ring_launch<NV, EDGES, X32, RES, 2>(p, g, st);
+}
+template <int NV, bool EDGES>
+cudaError_t norm_ring(const lckv::NormParams& p, const NormShape& g, cudaStream_t st)
+{
+    if (p.x32)
+        return !p.r ? norm_ring_out<NV, EDGES, 1, 0>(p, g, st) : !p.r32 ? norm_ring_out<NV, EDGES, 1, 1>(p, g, st) : norm_ring_out<NV, EDGES, 1, 2>(p, g, st);
+    return !p.r ? norm_ring_out<NV, EDGES, 0, 0>(p, g, st) : !p.r32 ? norm_ring_out<NV, EDGES, 0, 1>(p, g, st) : norm_ring_out<NV, EDGES, 0, 2>(p, g, st);
+}
+
+// Few rows (up to one per SM): one vector per thread, the shortest chain.  More: the ring, two vectors per thread
+// (a thread block of 256 threads serves a row of 4096), four where a row has more than 1024 vectors.  Not the ring
+// where fp32 tensors make the bytes and not the instructions the bound and rows are short: 2^26 elements, ring / one row
+// per thread block, us, with 512, 2048, 4096, 8192 columns: bf16 49 / 60, 43 / 64, 43 / 70, 44 / 78; bf16 + bf16 94 / 102,
+// 95 / 105, 95 / 109, 95 / 115; bf16 + fp32 148 / 121, 146 / 124, 146 / 128, 148 / 132; fp32 99 / 80, 101 / 84, 101 / 89,
+// 88 / 106; bf16 + fp32 to e4m3 134 / 123, 136 / 128, 114 / 131, 122 / 138.
+cudaError_t norm_launch(const lckv::NormParams& p, int n_vec, bool edges, int sms, cudaStream_t st)
+{
+    const bool fp32 = p.x32 || (p.r && p.r32);
+    const bool many = p.rows > sms;
+    if (many && (!fp32 || edges || n_vec > 512 + 256 || (p.out == 2 && n_vec >= 512))) {
+        const int nv = n_vec > 1024 ? 4 : 2;
+        NormShape g;
+        g.tpr = norm_threads(n_vec, nv);
+        g.rpb = g.tpr <= 32 ? 128 / g.tpr : 1;
+        const int parts = (p.x32 ? 2 : 1) + (p.r ? (p.r32 ? 2 : 1) : 0);
+        const int64_t smem = (int64_t)lckv::kNormRing * nv * parts * g.tpr * g.rpb * 16;
+        g.smem = (int)smem;
+        g.sms = sms;
+        if (g.tpr <= 512 && smem <= 222 * 1024) {
+            if (nv == 2) return edges ? norm_ring<2, true>(p, g, st) : norm_ring<2, false>(p, g, st);
+            if (!edges) return norm_ring<4, false>(p, g, st);
+        }
+    }
+    int nv = many && n_vec >= 64 ? 2 : 1;
+    while ((n_vec + nv - 1) / nv > (nv == 1 ? 1024 : 512)) nv *= 2;
+    const int tpr = norm_threads(n_vec, nv), rpb = tpr <= 32 ? 128 / tpr : 1;
+    const auto kernel = !edges ? (nv == 1   ? lckv::norm_vec_kernel<1, 1024, false>
+                                  : nv == 2 ? lckv::norm_vec_kernel<2, 512, false> : nv == 4 ? lckv::norm_vec_kernel<4, 512, false> : lckv::norm_vec_kernel<8, 512, false>)
+                               : (nv == 1   ? lckv::norm_vec_kernel<1, 1024, true>
+                                  : nv == 2 ? lckv::norm_vec_kernel<2, 512, true> : nv == 4 ? lckv::norm_vec_kernel<4, 512, true> : lckv::norm_vec_kernel<8, 512, true>);
+    return launch_pdl_dims(kernel, dim3((unsigned)((p.rows + rpb - 1) / rpb)), dim3(tpr, rpb), 0, st, p);
 }
 
 }  // namespace
@@ -204,7 +289,9 @@ int lckv_rope_tables(float* cos, float* sin, int32_t positions, int32_t rot_dim,
             keep = keep < 0.0 ? 0.0 : keep > 1.0 ? 1.0 : keep;
             theta *= keep + (1.0 - keep) / s->factor;
         }
-        p.turns[i] = theta / two_pi;
+        double turns = theta / two_pi;
+        turns -= std::floor(turns);
+        p.turns[i] = (uint64_t)std::ldexp(turns, 64);        // (turns < 1: at most 2^64 - 2^11)
     }
     p.cos = cos;
     p.sin = sin;
@@ -213,10 +300,14 @@ int lckv_rope_tables(float* cos, float* sin, int32_t positions, int32_t rot_dim,
     p.amplitude = (float)amplitude;
     cudaStream_t st = static_cast<cudaStream_t>(stream);
     const bool vec = half % 4 == 0 && aligned(cos, 16) && aligned(sin, 16);
-    const int64_t threads = vec ? n / 4 : n;
-    const dim3 grid((unsigned)((threads + lckv::kRopeThreads - 1) / lckv::kRopeThreads)), block(lckv::kRopeThreads);
-    const cudaError_t e = vec ? launch_pdl_dims(lckv::rope_table_kernel<4>, grid, block, 0, st, p)
-                              : launch_pdl_dims(lckv::rope_table_kernel<1>, grid, block, 0, st, p);
+    // four positions per thread where that leaves enough threads (one fetch of the frequencies serves them all)
+    const int v = vec ? 4 : 1, many = positions >= 4096 ? 4 : 1;
+    p.step = (int64_t)((positions + many - 1) / many) * (half / v);
+    const dim3 grid((unsigned)((p.step + lckv::kRopeThreads - 1) / lckv::kRopeThreads)), block(lckv::kRopeThreads);
+    const cudaError_t e = vec ? (many == 4 ? launch_pdl_dims(lckv::rope_table_kernel<4, 4>, grid, block, 0, st, p)
+                                           : launch_pdl_dims(lckv::rope_table_kernel<4, 1>, grid, block, 0, st, p))
+                              : (many == 4 ? launch_pdl_dims(lckv::rope_table_kernel<1, 4>, grid, block, 0, st, p)
+                                           : launch_pdl_dims(lckv::rope_table_kernel<1, 1>, grid, block, 0, st, p));
     return cuda_ok(e) ? LCKV_OK : LCKV_ECUDA;
 }
 
@@ -257,19 +348,12 @@ int lckv_rope_apply(const lckv_rope_t* rope, const int32_t* positions, const voi
     if (int rc = device_sm_count(&sms)) return rc;
     cudaStream_t st = static_cast<cudaStream_t>(stream);
     const int64_t grain = 16 / size;
-    const bool vec = rope_tables_vector(rope) && aligned(x, 16) && aligned(y, 16) && x_token_stride % grain == 0 &&
-                     x_head_stride % grain == 0 && y_token_stride % grain == 0 && y_head_stride % grain == 0;
+    const bool vec = aligned(x, 16) && aligned(y, 16) && x_token_stride % grain == 0 && x_head_stride % grain == 0 &&
+                     y_token_stride % grain == 0 && y_head_stride % grain == 0;
+    const int path = !vec ? lckv::kRopePairs : rope_tables_vector(rope) ? lckv::kRopeUnits : lckv::kRopeAnySize;
     const int hp = vec && rope_many((int64_t)n_tokens * n_heads * (head_dim / 16), sms) ? 4 : 1;
-    const dim3 grid = rope_grid(n_tokens, n_heads, head_dim, vec, hp), block(lckv::kRopeThreads);
-    cudaError_t e;
-    if (dtype)
-        e = !vec ? launch_pdl_dims(lckv::rope_apply_kernel<float, false, 1>, grid, block, 0, st, p)
-            : hp == 4 ? launch_pdl_dims(lckv::rope_apply_kernel<float, true, 4>, grid, block, 0, st, p)
-                      : launch_pdl_dims(lckv::rope_apply_kernel<float, true, 1>, grid, block, 0, st, p);
-    else
-        e = !vec ? launch_pdl_dims(lckv::rope_apply_kernel<uint16_t, false, 1>, grid, block, 0, st, p)
-            : hp == 4 ? launch_pdl_dims(lckv::rope_apply_kernel<uint16_t, true, 4>, grid, block, 0, st, p)
-                      : launch_pdl_dims(lckv::rope_apply_kernel<uint16_t, true, 1>, grid, block, 0, st, p);
+    const dim3 grid = rope_grid(n_tokens, n_heads, head_dim, path, hp), block(lckv::kRopeThreads);
+    const cudaError_t e = launch_pdl_dims(dtype ? rope_apply_variant<float>(path, hp) : rope_apply_variant<uint16_t>(path, hp), grid, block, 0, st, p);
     return cuda_ok(e) ? LCKV_OK : LCKV_ECUDA;
 }
 
@@ -342,19 +426,15 @@ int lckv_rms_norm(const void* x, int64_t x_stride, int32_t x_dtype, const void* 
     p.group = scale_group;
     p.n_groups = n_groups;
     cudaStream_t st = static_cast<cudaStream_t>(stream);
-    const bool vec = width % 8 == 0 && x_stride % 8 == 0 && aligned(x, 16) && aligned(residual, 16) && aligned(residual_out, 16) &&
-                     aligned(weight, 16) && aligned(y, y_kind == 2 ? 8 : 16);
+    const bool grid16 = aligned(x, 16) && aligned(residual, 16) && aligned(residual_out, 16) && aligned(y, y_kind == 2 ? 8 : 16);
+    const bool even = grid16 && width % 8 == 0 && x_stride % 8 == 0 && aligned(weight, 16);
+    const bool edges = grid16 && !even && x_stride == width && !scale_group;
     cudaError_t e;
-    if (vec) {
-        // threads of a row: one vector each for short launches, up to four where a row has more than 1024
-        const int n_vec = width / 8;
-        const int nv = n_vec > 2048 ? 4 : n_vec > 1024 ? 2 : 1;
-        const int tpr = ((n_vec + nv - 1) / nv + 31) / 32 * 32;
-        const int rpb = tpr == 32 ? 4 : 1;
-        const dim3 grid((unsigned)((rows + rpb - 1) / rpb)), block(tpr, rpb);
-        e = nv == 4 ? launch_pdl_dims(lckv::norm_vec_kernel<4>, grid, block, 0, st, p)
-            : nv == 2 ? launch_pdl_dims(lckv::norm_vec_kernel<2>, grid, block, 0, st, p)
-                      : launch_pdl_dims(lckv::norm_vec_kernel<1>, grid, block, 0, st, p);
+    if (even || edges) {
+        int sms = 0;
+        if (int rc = device_sm_count(&sms)) return rc;
+        const int n_vec = (width + (edges ? 14 : 7)) / 8;
+        e = norm_launch(p, n_vec, edges, sms, st);
     } else {
         const size_t smem = (size_t)width * 4;
         if (smem > 47 * 1024 &&      // (beside the static arrays)

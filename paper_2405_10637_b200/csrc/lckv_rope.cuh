@@ -12,14 +12,17 @@
 // and [rot/2 + 8u, ...) in the half layout, [16u, 16u+16) in the interleaved one - for HP heads of one
 // token, so that the 8 cos and 8 sin of the unit are fetched once for HP heads and HP * 32 bytes of
 // loads are in flight per thread.  Neighbouring threads hold neighbouring units, then neighbouring
-// heads.  Rotary sizes that are not a multiple of 16, and tensors off the 16-byte grid, go pair by pair
-// (VEC = false).
+// heads (kRopeUnits).  Where the rotated size is not a multiple of 16, a thread takes 8 consecutive elements: an
+// interleaved pair lies within them, the other half of a pair in the half layout comes through the warp's corner of
+// shared memory (kRopeAnySize: prompts' rotated append with 34 of 128 dimensions 653 us pair by pair, 170 us so).
+// Tensors off the 16-byte grid go pair by pair (kRopePairs).
 #pragma once
 #include "lckv_device.cuh"
 
 namespace lckv {
 
 constexpr int kRopeThreads = 256;
+enum RopePath { kRopeUnits, kRopeAnySize, kRopePairs };
 constexpr int kRopeMaxPairs = 64;      // rot_dim <= 128 = the largest head
 constexpr int kStatusCapacity = 2;     // a row of a replayed append had no place in the cache
 
@@ -67,6 +70,7 @@ __device__ __forceinline__ void rope_st(uint16_t* p, float v) { *p = (uint16_t)f
 template <typename T> struct Vec8;
 template <> struct Vec8<uint16_t> {
     uint4 w;
+    __device__ __forceinline__ void zero() { w = make_uint4(0, 0, 0, 0); }
     __device__ __forceinline__ void load(const uint16_t* p) { w = __ldcs(reinterpret_cast<const uint4*>(p)); }
     __device__ __forceinline__ void store(uint16_t* p) const { *reinterpret_cast<uint4*>(p) = w; }
     __device__ __forceinline__ void get(float (&f)[8]) const
@@ -79,9 +83,17 @@ template <> struct Vec8<uint16_t> {
         w = make_uint4(cvt_bf16x2(f[0], f[1]), cvt_bf16x2(f[2], f[3]), cvt_bf16x2(f[4], f[5]),
                        cvt_bf16x2(f[6], f[7]));
     }
+    __device__ __forceinline__ void set_until(const float (&f)[8], int n)      // elements 0 .. n-1, n even
+    {
+        if (n > 0) w.x = cvt_bf16x2(f[0], f[1]);
+        if (n > 2) w.y = cvt_bf16x2(f[2], f[3]);
+        if (n > 4) w.z = cvt_bf16x2(f[4], f[5]);
+        if (n > 6) w.w = cvt_bf16x2(f[6], f[7]);
+    }
 };
 template <> struct Vec8<float> {
     float4 a, b;
+    __device__ __forceinline__ void zero() { a = b = make_float4(0.f, 0.f, 0.f, 0.f); }
     __device__ __forceinline__ void load(const float* p)
     {
         a = __ldcs(reinterpret_cast<const float4*>(p));
@@ -100,6 +112,13 @@ template <> struct Vec8<float> {
     {
         a = make_float4(f[0], f[1], f[2], f[3]);
         b = make_float4(f[4], f[5], f[6], f[7]);
+    }
+    __device__ __forceinline__ void set_until(const float (&f)[8], int n)
+    {
+        if (n > 0) { a.x = f[0]; a.y = f[1]; }
+        if (n > 2) { a.z = f[2]; a.w = f[3]; }
+        if (n > 4) { b.x = f[4]; b.y = f[5]; }
+        if (n > 6) { b.z = f[6]; b.w = f[7]; }
     }
 };
 
@@ -152,7 +171,52 @@ struct RopeUnit {
     }
 };
 
-// One pair (or two copied elements) of a head, for VEC = false.
+// 8 consecutive elements 8 u .. 8 u + 7 of a head, any even rotated size.  All 32 lanes of the warp call it; the lanes of a
+// head are neighbours.  sh: 256 floats of the warp's own, element i of lane l at [i][l].
+template <typename T>
+__device__ __forceinline__ void rope_any(const RopeArgs& r, int u, int pos, Vec8<T>& v, bool turn, float* sh)
+{
+    const int lane = threadIdx.x & 31, first = lane - u;                // first lane of the head
+    float x[8], y[8];
+    v.get(x);
+    pos = pos < 0 ? 0 : (pos < r.positions ? pos : r.positions - 1);
+    const float* pc = r.cos + (int64_t)pos * r.half;
+    const float* ps = r.sin + (int64_t)pos * r.half;
+    const int rot = 2 * r.half;
+    if (r.interleaved) {
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+            const int pair = u * 4 + j;
+            y[2 * j] = x[2 * j];
+            y[2 * j + 1] = x[2 * j + 1];
+            if (turn && pair < r.half) {
+                const float c = __ldg(pc + pair), s = r.sgn * __ldg(ps + pair);
+                y[2 * j] = fmaf(-x[2 * j + 1], s, x[2 * j] * c);
+                y[2 * j + 1] = fmaf(x[2 * j], s, x[2 * j + 1] * c);
+            }
+        }
+    } else {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) sh[i * 32 + lane] = x[i];
+        __syncwarp();
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            const int e = u * 8 + i;
+            y[i] = x[i];
+            if (turn && e < rot) {
+                const bool low = e < r.half;
+                const int j = low ? e : e - r.half, o = low ? e + r.half : j;
+                const float c = __ldg(pc + j), s = r.sgn * __ldg(ps + j), other = sh[(o & 7) * 32 + first + (o >> 3)];
+                y[i] = fmaf(low ? -other : other, s, x[i] * c);
+            }
+        }
+        __syncwarp();
+    }
+    // dimensions behind the rotated ones keep their bits
+    if (turn && u * 8 < rot) v.set_until(y, rot - u * 8);
+}
+
+// One pair (or two copied elements) of a head, for kRopePairs.
 template <typename T>
 __device__ __forceinline__ void rope_pair(const RopeArgs& r, int u, int pos, const T* src, T* dst, bool turn_head)
 {
@@ -175,11 +239,12 @@ __device__ __forceinline__ void rope_pair(const RopeArgs& r, int u, int pos, con
 // The thread's place: token `t`, unit `u`, first head `h0` (further heads at steps of `hg`).  A block
 // holds 256 / (units * head groups) tokens, or a 256-thread part (grid.y) of one token.
 struct RopePlace { int t, u, h0, hg; bool ok; };
-template <bool VEC, int HP>
+__host__ __device__ constexpr int rope_units(int path, int d) { return path == kRopeUnits ? d / 16 : path == kRopeAnySize ? d / 8 : d / 2; }
+template <int PATH, int HP>
 __device__ __forceinline__ RopePlace rope_place(int tokens, int heads, int d)
 {
     RopePlace w;
-    const int units = VEC ? d >> 4 : d >> 1;
+    const int units = rope_units(PATH, d);
     w.hg = (heads + HP - 1) / HP;
     const uint32_t per = (uint32_t)(w.hg * units);
     uint32_t r, tl = 0;
@@ -200,16 +265,33 @@ __device__ __forceinline__ RopePlace rope_place(int tokens, int heads, int d)
     return w;
 }
 
-template <typename T, bool VEC, int HP>
+template <typename T, int PATH, int HP>
 __global__ void __launch_bounds__(kRopeThreads) rope_apply_kernel(const RopeApplyParams p)
 {
+    __shared__ float sh[PATH == kRopeAnySize ? kRopeThreads * 8 : 1];
     pdl_wait_then_release();
-    const RopePlace w = rope_place<VEC, HP>(p.tokens, p.heads, p.d);
-    if (!w.ok) return;
-    const T* x = static_cast<const T*>(p.x) + (int64_t)w.t * p.x_tok;
-    T* y = static_cast<T*>(p.y) + (int64_t)w.t * p.y_tok;
-    const int pos = __ldg(p.pos + w.t);
-    if constexpr (!VEC) {
+    const RopePlace w = rope_place<PATH, HP>(p.tokens, p.heads, p.d);
+    if (PATH != kRopeAnySize && !w.ok) return;
+    const int t = w.ok ? w.t : 0;
+    const T* x = static_cast<const T*>(p.x) + (int64_t)t * p.x_tok;
+    T* y = static_cast<T*>(p.y) + (int64_t)t * p.y_tok;
+    const int pos = __ldg(p.pos + t);
+    if constexpr (PATH == kRopeAnySize) {
+        Vec8<T> v[HP];
+#pragma unroll
+        for (int j = 0; j < HP; ++j) {
+            const int h = w.h0 + j * w.hg;
+            if (w.ok && h < p.heads) v[j].load(x + (int64_t)h * p.x_head + w.u * 8);
+            else v[j].zero();
+        }
+#pragma unroll
+        for (int j = 0; j < HP; ++j) {
+            const int h = w.h0 + j * w.hg;
+            const bool in = w.ok && h < p.heads;
+            rope_any(p.r, w.u, pos, v[j], in, sh + (threadIdx.x >> 5) * 256);
+            if (in) v[j].store(y + (int64_t)h * p.y_head + w.u * 8);
+        }
+    } else if constexpr (PATH == kRopePairs) {
 #pragma unroll
         for (int j = 0; j < HP; ++j) {
             const int h = w.h0 + j * w.hg;
@@ -240,16 +322,21 @@ __global__ void __launch_bounds__(kRopeThreads) rope_apply_kernel(const RopeAppl
 
 // Heads 0 .. hq-1 of a token are its query heads (rotated, to q_out), the next hkv its keys (rotated, to
 // the row), the last hkv its values (copied to the row).
-template <bool VEC, int HP>
+template <int PATH, int HP>
 __global__ void __launch_bounds__(kRopeThreads) rope_append_kernel(const RopeAppendParams p)
 {
+    __shared__ float sh[PATH == kRopeAnySize ? kRopeThreads * 8 : 1];
     pdl_wait_then_release();
     const int heads = p.hq + 2 * p.hkv;
-    const RopePlace w = rope_place<VEC, HP>(p.batch * p.n_new, heads, p.d);
-    if (!w.ok) return;
+    RopePlace w = rope_place<PATH, HP>(p.batch * p.n_new, heads, p.d);
+    if (PATH != kRopeAnySize && !w.ok) return;
+    if (!w.ok) w.t = 0;
     const int b = w.t / p.n_new, i = w.t - b * p.n_new;
     const int len = __ldg(p.lens + b);
-    if (p.prompt && i >= len) return;
+    if (p.prompt && i >= len) {
+        if (PATH != kRopeAnySize) return;
+        w.ok = false;
+    }
     const int pos = p.prompt ? i : len + i;
     // the row: ring position in a sink + recent-window cache, page look-up in a paged one
     int64_t row = pos;
@@ -265,9 +352,7 @@ __global__ void __launch_bounds__(kRopeThreads) rope_append_kernel(const RopeApp
         row0 = (int64_t)b * p.hkv * p.T_cap + row;
     }
     // the host refuses calls without room; a graph that replays one finds the lengths on the device
-    if (!place && p.hkv > 0 && w.h0 == 0 && w.u == 0) atomicExch(p.status, kStatusCapacity);
-    RopeUnit un;
-    un.init(p.r, w.u);
+    if (!place && w.ok && p.hkv > 0 && w.h0 == 0 && w.u == 0) atomicExch(p.status, kStatusCapacity);
     const uint16_t* src[HP];
     uint16_t* dst[HP];
     bool turn[HP];
@@ -276,6 +361,7 @@ __global__ void __launch_bounds__(kRopeThreads) rope_append_kernel(const RopeApp
         int h = w.h0 + j * w.hg;
         src[j] = nullptr;
         turn[j] = true;
+        if (!w.ok) continue;
         if (h < p.hq) {
             src[j] = p.q + (int64_t)w.t * p.q_tok + (int64_t)h * p.d;
             dst[j] = p.q_out + ((int64_t)w.t * p.hq + h) * p.d;
@@ -287,11 +373,25 @@ __global__ void __launch_bounds__(kRopeThreads) rope_append_kernel(const RopeApp
             dst[j] = (turn[j] ? p.K : p.V) + (row0 + h * head_step) * p.d;
         }
     }
-    if constexpr (!VEC) {
+    if constexpr (PATH == kRopePairs) {
 #pragma unroll
         for (int j = 0; j < HP; ++j)
             if (src[j]) rope_pair(p.r, w.u, pos, src[j], dst[j], turn[j]);
+    } else if constexpr (PATH == kRopeAnySize) {
+        Vec8<uint16_t> v[HP];
+#pragma unroll
+        for (int j = 0; j < HP; ++j) {
+            if (src[j]) v[j].load(src[j] + w.u * 8);
+            else v[j].zero();
+        }
+#pragma unroll
+        for (int j = 0; j < HP; ++j) {
+            rope_any(p.r, w.u, pos, v[j], src[j] && turn[j], sh + (threadIdx.x >> 5) * 256);
+            if (src[j]) v[j].store(dst[j] + w.u * 8);
+        }
     } else {
+        RopeUnit un;
+        un.init(p.r, w.u);
         Vec8<uint16_t> lo[HP], hi[HP];
 #pragma unroll
         for (int j = 0; j < HP; ++j) {
@@ -310,41 +410,75 @@ __global__ void __launch_bounds__(kRopeThreads) rope_append_kernel(const RopeApp
     }
 }
 
-// cos and sin of p * theta_j for p < positions.  `turns` holds theta_j / (2 pi): the angle in turns is
-// reduced to [-1/2, 1/2] in fp64 (far positions lose nothing), the functions are then taken in fp32 of
-// half turns.  V pairs per thread.
+// cos and sin of p * theta_j for p < positions.  `turns` holds theta_j / (2 pi) modulo 1 in units of 2^-64: the angle of
+// position p is p * turns modulo 2^64, exact in integers, so far positions lose nothing.  Its upper 32 bits are split into a
+// quarter turn and a rest of at most an eighth, for which the Taylor series of sin (to x^9) and cos (to x^10) are off by
+// less than 2e-9.  V neighbouring pairs and P positions per thread.
+//
+// 67 MB of tables for 131072 positions of 64 pairs: 10.4 us of stores.  Reducing the angle in fp64 and calling the
+// library's sincospif took 34.6 us (fp64 rounding and conversions run at a sixteenth of the rate).
 struct RopeTableParams {
-    double turns[kRopeMaxPairs];
+    uint64_t turns[kRopeMaxPairs];
     float* cos;
     float* sin;
     int64_t n;                         // positions * half
+    int64_t step;                      // items between a thread's positions: a multiple of half / V
     int32_t half;
     float amplitude;
 };
 
-template <int V>
+__device__ __forceinline__ void rope_sincos(uint32_t turn, float& s, float& c)
+{
+    const uint32_t q = (turn + 0x20000000u) >> 30;
+    const float x = (float)(int32_t)(turn - (q << 30)) * 1.4629180792671596e-9f;        // 2 pi / 2^32
+    const float x2 = x * x;
+    float ps = fmaf(x2, 2.7557319e-6f, -1.9841270e-4f);                                 // 1/9!, -1/7!
+    ps = fmaf(ps, x2, 8.3333333e-3f);
+    ps = fmaf(ps, x2, -1.6666667e-1f);
+    ps = fmaf(ps * x2, x, x);
+    float pc = fmaf(x2, -2.7557319e-7f, 2.4801587e-5f);                                 // -1/10!, 1/8!
+    pc = fmaf(pc, x2, -1.3888889e-3f);
+    pc = fmaf(pc, x2, 4.1666667e-2f);
+    pc = fmaf(pc, x2, -0.5f);
+    pc = fmaf(pc, x2, 1.0f);
+    s = q & 1 ? pc : ps;
+    c = q & 1 ? ps : pc;
+    s = __uint_as_float(__float_as_uint(s) ^ ((q & 2) << 30));
+    c = __uint_as_float(__float_as_uint(c) ^ (((q + 1) & 2) << 30));
+}
+
+template <int V, int P>
 __global__ void __launch_bounds__(kRopeThreads) rope_table_kernel(const __grid_constant__ RopeTableParams p)
 {
     pdl_wait_then_release();
     const uint32_t per = (uint32_t)(p.half / V);
-    const int64_t i = (int64_t)blockIdx.x * kRopeThreads + threadIdx.x;
-    if (i * V >= p.n) return;
-    const uint32_t pos = (uint32_t)(i / per), j0 = (uint32_t)(i - (int64_t)pos * per) * V;
-    float c[V], s[V];
+    int64_t i = (int64_t)blockIdx.x * kRopeThreads + threadIdx.x;
+    if (i >= p.step) return;
+    uint32_t pos = (uint32_t)(i / per);
+    const uint32_t j0 = (uint32_t)(i - (int64_t)pos * per) * V, stride = (uint32_t)(p.step / per);
+    uint32_t hi[V], lo[V];
 #pragma unroll
     for (int j = 0; j < V; ++j) {
-        double t = (double)pos * p.turns[j0 + j];
-        t -= rint(t);
-        sincospif((float)(2.0 * t), &s[j], &c[j]);
-        c[j] *= p.amplitude;
-        s[j] *= p.amplitude;
+        hi[j] = (uint32_t)(p.turns[j0 + j] >> 32);
+        lo[j] = (uint32_t)p.turns[j0 + j];
     }
-    if constexpr (V == 4) {
-        *reinterpret_cast<float4*>(p.cos + i * 4) = make_float4(c[0], c[1], c[2], c[3]);
-        *reinterpret_cast<float4*>(p.sin + i * 4) = make_float4(s[0], s[1], s[2], s[3]);
-    } else {
-        p.cos[i] = c[0];
-        p.sin[i] = s[0];
+#pragma unroll
+    for (int k = 0; k < P; ++k, i += p.step, pos += stride) {
+        if (i * V >= p.n) return;
+        float c[V], s[V];
+#pragma unroll
+        for (int j = 0; j < V; ++j) {
+            rope_sincos(pos * hi[j] + __umulhi(pos, lo[j]), s[j], c[j]);
+            c[j] *= p.amplitude;
+            s[j] *= p.amplitude;
+        }
+        if constexpr (V == 4) {
+            *reinterpret_cast<float4*>(p.cos + i * 4) = make_float4(c[0], c[1], c[2], c[3]);
+            *reinterpret_cast<float4*>(p.sin + i * 4) = make_float4(s[0], s[1], s[2], s[3]);
+        } else {
+            p.cos[i] = c[0];
+            p.sin[i] = s[0];
+        }
     }
 }
 
