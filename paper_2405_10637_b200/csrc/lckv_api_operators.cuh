@@ -46,16 +46,30 @@ int rope_args(const lckv_rope_t* r, int head_dim, lckv::RopeArgs* out)
 
 bool rope_tables_vector(const lckv_rope_t* r) { return r->rot_dim % 16 == 0 && aligned(r->cos, 16) && aligned(r->sin, 16); }
 
-// Heads per thread: four when the launch still fills the GPU's threads several times over (one fetch of the
-// unit's cos and sin serves four heads and four pairs of loads are in flight), one when there are few.
-bool rope_many(int64_t units, int sms) { return units >= (int64_t)sms * 2048 * 4; }
+// Heads per thread: four when there are enough units to fill the GPU's threads one and a half times (one fetch of the
+// unit's cos and sin serves four heads and four pairs of loads are in flight: 32768 tokens of 8 heads of 64 13.2 us, with
+// one 15.1 us), one when there are few (64 x 8 tokens of 96 heads 6.1 us, with four 6.5 us).
+bool rope_many(int64_t units, int sms) { return units * 2 >= (int64_t)sms * 2048 * 3; }
 
-dim3 rope_grid(int64_t tokens, int heads, int d, int path, int hp)
+// Where a thread fetches its factors one by one: as many heads as leave half of the GPU's threads busy, in fours.
+int rope_heads(int path, int hp, int64_t tokens, int heads, int d, int sms)
 {
-    const int64_t per = (int64_t)((heads + hp - 1) / hp) * lckv::rope_units(path, d);
-    if (per >= lckv::kRopeThreads)
-        return dim3((unsigned)tokens, (unsigned)((per + lckv::kRopeThreads - 1) / lckv::kRopeThreads));
-    const int64_t tb = lckv::kRopeThreads / per;
+    if (path != lckv::kRopeAnySize || hp == 1) return hp;
+    const int64_t fit = tokens * heads * (d / 8) / ((int64_t)sms * 1024);
+    return (int)std::max<int64_t>(4, std::min<int64_t>(fit, heads) / 4 * 4);
+}
+
+dim3 rope_grid(int64_t tokens, int heads, int d, int path, int hp, lckv::RopeGrid* g)
+{
+    const int units = lckv::rope_units(path, d);             // a power of two, as d is
+    g->hg = (heads + hp - 1) / hp;
+    g->units_shift = 0;
+    while ((1 << g->units_shift) < units) ++g->units_shift;
+    g->per = (uint32_t)(g->hg * units);
+    g->inv = (65536 + g->per - 1) / g->per;
+    if (g->per >= (uint32_t)lckv::kRopeThreads)
+        return dim3((unsigned)tokens, (g->per + lckv::kRopeThreads - 1) / lckv::kRopeThreads);
+    const int64_t tb = lckv::kRopeThreads / g->per;
     return dim3((unsigned)((tokens + tb - 1) / tb));
 }
 
@@ -159,7 +173,8 @@ int rope_into_cache(lckv_cache* c, int slot, const lckv_rope_t* rope, const void
     const int path = !vec ? lckv::kRopePairs : rope_tables_vector(rope) ? lckv::kRopeUnits : lckv::kRopeAnySize;
     const int heads = hq + 2 * hkv;
     const int hp = vec && rope_many(tokens * heads * (d / 16), sms) ? 4 : 1;
-    const dim3 grid = rope_grid(tokens, heads, d, path, hp), block(lckv::kRopeThreads);
+    p.hp = rope_heads(path, hp, tokens, heads, d, sms);
+    const dim3 grid = rope_grid(tokens, heads, d, path, p.hp, &p.g), block(lckv::kRopeThreads);
     const auto kernel = path == lckv::kRopePairs   ? lckv::rope_append_kernel<lckv::kRopePairs, 1>
                         : path == lckv::kRopeUnits ? (hp == 4 ? lckv::rope_append_kernel<lckv::kRopeUnits, 4> : lckv::rope_append_kernel<lckv::kRopeUnits, 1>)
                                                    : (hp == 4 ? lckv::rope_append_kernel<lckv::kRopeAnySize, 4> : lckv::rope_append_kernel<lckv::kRopeAnySize, 1>);
@@ -352,7 +367,8 @@ int lckv_rope_apply(const lckv_rope_t* rope, const int32_t* positions, const voi
                      y_token_stride % grain == 0 && y_head_stride % grain == 0;
     const int path = !vec ? lckv::kRopePairs : rope_tables_vector(rope) ? lckv::kRopeUnits : lckv::kRopeAnySize;
     const int hp = vec && rope_many((int64_t)n_tokens * n_heads * (head_dim / 16), sms) ? 4 : 1;
-    const dim3 grid = rope_grid(n_tokens, n_heads, head_dim, path, hp), block(lckv::kRopeThreads);
+    p.hp = rope_heads(path, hp, n_tokens, n_heads, head_dim, sms);
+    const dim3 grid = rope_grid(n_tokens, n_heads, head_dim, path, p.hp, &p.g), block(lckv::kRopeThreads);
     const cudaError_t e = launch_pdl_dims(dtype ? rope_apply_variant<float>(path, hp) : rope_apply_variant<uint16_t>(path, hp), grid, block, 0, st, p);
     return cuda_ok(e) ? LCKV_OK : LCKV_ECUDA;
 }

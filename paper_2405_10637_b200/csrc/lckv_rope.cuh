@@ -14,7 +14,7 @@
 // loads are in flight per thread.  Neighbouring threads hold neighbouring units, then neighbouring
 // heads (kRopeUnits).  Where the rotated size is not a multiple of 16, a thread takes 8 consecutive elements: an
 // interleaved pair lies within them, the other half of a pair in the half layout comes through the warp's corner of
-// shared memory (kRopeAnySize: prompts' rotated append with 34 of 128 dimensions 653 us pair by pair, 170 us so).
+// shared memory, and the thread serves more heads, since its factors are 16 separate loads (kRopeAnySize).
 // Tensors off the 16-byte grid go pair by pair (kRopePairs).
 #pragma once
 #include "lckv_device.cuh"
@@ -34,17 +34,25 @@ struct RopeArgs {
     float sgn;                         // +1, or -1 for the transposed rotation
 };
 
+struct RopeGrid {
+    uint32_t per, inv;
+    int32_t hg, units_shift;
+};
+
 struct RopeApplyParams {
     RopeArgs r;
+    RopeGrid g;
     const int32_t* pos;
     const void* x;
     void* y;
     int64_t x_tok, x_head, y_tok, y_head;   // element strides
     int32_t tokens, heads, d;
+    int32_t hp;                        // heads per thread: a multiple of the kernel's HP
 };
 
 struct RopeAppendParams {
     RopeArgs r;
+    RopeGrid g;
     const uint16_t* q;                 // token (b, i) at (b * n_new + i) * q_tok, heads contiguous; null: none
     uint16_t* q_out;                   // contiguous
     const uint16_t* k;                 // null: none
@@ -57,6 +65,7 @@ struct RopeAppendParams {
     int64_t q_tok, kv_tok, T_cap;
     int32_t batch, n_new, hq, hkv, d;  // hq = 0 without q, hkv = 0 without k and v
     int32_t n_sink, pt_stride, page_shift;
+    int32_t hp;                        // heads per thread: a multiple of the kernel's HP
     int32_t prompt;                    // 0: tokens i < n_new at positions len[b] + i; 1: tokens i < len[b] at i
 };
 
@@ -171,50 +180,55 @@ struct RopeUnit {
     }
 };
 
-// 8 consecutive elements 8 u .. 8 u + 7 of a head, any even rotated size.  All 32 lanes of the warp call it; the lanes of a
-// head are neighbours.  sh: 256 floats of the warp's own, element i of lane l at [i][l].
-template <typename T>
-__device__ __forceinline__ void rope_any(const RopeArgs& r, int u, int pos, Vec8<T>& v, bool turn, float* sh)
-{
-    const int lane = threadIdx.x & 31, first = lane - u;                // first lane of the head
-    float x[8], y[8];
-    v.get(x);
-    pos = pos < 0 ? 0 : (pos < r.positions ? pos : r.positions - 1);
-    const float* pc = r.cos + (int64_t)pos * r.half;
-    const float* ps = r.sin + (int64_t)pos * r.half;
-    const int rot = 2 * r.half;
-    if (r.interleaved) {
-#pragma unroll
-        for (int j = 0; j < 4; ++j) {
-            const int pair = u * 4 + j;
-            y[2 * j] = x[2 * j];
-            y[2 * j + 1] = x[2 * j + 1];
-            if (turn && pair < r.half) {
-                const float c = __ldg(pc + pair), s = r.sgn * __ldg(ps + pair);
-                y[2 * j] = fmaf(-x[2 * j + 1], s, x[2 * j] * c);
-                y[2 * j + 1] = fmaf(x[2 * j], s, x[2 * j + 1] * c);
-            }
-        }
-    } else {
-#pragma unroll
-        for (int i = 0; i < 8; ++i) sh[i * 32 + lane] = x[i];
-        __syncwarp();
+// 8 consecutive elements 8 u .. 8 u + 7 of a head, any even rotated size: the factors of each element and of its partner,
+// fetched once for all heads of the thread, and where the partner lies.  All 32 lanes of a warp take part; the lanes of
+// a head are neighbours.  sh: 256 floats of the warp's own, element i of lane l at [i][l].
+struct RopeAny {
+    float c[8], s[8];                   // y = x c + partner s
+    int from[8];                        // the partner's place in sh (half layout)
+    int n;                              // rotated elements among the 8: 0 .. 8, even
+    __device__ __forceinline__ void fetch(const RopeArgs& r, int u, int pos)
+    {
+        const int first = (threadIdx.x & 31) - u, rot = 2 * r.half;
+        pos = pos < 0 ? 0 : (pos < r.positions ? pos : r.positions - 1);
+        const float* pc = r.cos + (int64_t)pos * r.half;
+        const float* ps = r.sin + (int64_t)pos * r.half;
+        n = rot - u * 8;
+        n = n < 0 ? 0 : n > 8 ? 8 : n;
 #pragma unroll
         for (int i = 0; i < 8; ++i) {
             const int e = u * 8 + i;
-            y[i] = x[i];
-            if (turn && e < rot) {
-                const bool low = e < r.half;
-                const int j = low ? e : e - r.half, o = low ? e + r.half : j;
-                const float c = __ldg(pc + j), s = r.sgn * __ldg(ps + j), other = sh[(o & 7) * 32 + first + (o >> 3)];
-                y[i] = fmaf(low ? -other : other, s, x[i] * c);
+            const bool low = r.interleaved ? (i & 1) == 0 : e < r.half;
+            const int j = r.interleaved ? e >> 1 : low ? e : e - r.half, o = low ? e + r.half : j;
+            c[i] = s[i] = 0.f;
+            from[i] = 0;
+            if (i < n) {
+                c[i] = __ldg(pc + j);
+                s[i] = (low ? -r.sgn : r.sgn) * __ldg(ps + j);
+                from[i] = (o & 7) * 32 + first + (o >> 3);
             }
         }
-        __syncwarp();
     }
-    // dimensions behind the rotated ones keep their bits
-    if (turn && u * 8 < rot) v.set_until(y, rot - u * 8);
-}
+    template <typename T>
+    __device__ __forceinline__ void rotate(const RopeArgs& r, Vec8<T>& v, bool turn, float* sh) const
+    {
+        float x[8], y[8];
+        v.get(x);
+        if (r.interleaved) {
+#pragma unroll
+            for (int i = 0; i < 8; ++i) y[i] = fmaf(x[i ^ 1], s[i], x[i] * c[i]);
+        } else {
+            const int lane = threadIdx.x & 31;
+#pragma unroll
+            for (int i = 0; i < 8; ++i) sh[i * 32 + lane] = x[i];
+            __syncwarp();
+#pragma unroll
+            for (int i = 0; i < 8; ++i) y[i] = fmaf(sh[from[i]], s[i], x[i] * c[i]);
+            __syncwarp();
+        }
+        if (turn) v.set_until(y, n);    // dimensions behind the rotated ones keep their bits
+    }
+};
 
 // One pair (or two copied elements) of a head, for kRopePairs.
 template <typename T>
@@ -236,32 +250,30 @@ __device__ __forceinline__ void rope_pair(const RopeArgs& r, int u, int pos, con
     rope_st(dst + e1, fmaf(a, s, b * c));
 }
 
-// The thread's place: token `t`, unit `u`, first head `h0` (further heads at steps of `hg`).  A block
-// holds 256 / (units * head groups) tokens, or a 256-thread part (grid.y) of one token.
-struct RopePlace { int t, u, h0, hg; bool ok; };
 __host__ __device__ constexpr int rope_units(int path, int d) { return path == kRopeUnits ? d / 16 : path == kRopeAnySize ? d / 8 : d / 2; }
-template <int PATH, int HP>
-__device__ __forceinline__ RopePlace rope_place(int tokens, int heads, int d)
+
+// The thread's place: token `t`, unit `u`, first head `h0` (further heads at steps of `hg`).  A block holds 256 / per tokens
+// of per = units * head groups threads, or a 256-thread part (grid.y) of one token.  The host does the divisions
+// (a one-token launch took 0.15 us longer with them here): `inv` = ceil(2^16 / per), with which thread * inv / 2^16 is
+// thread / per for all threads below 256.
+struct RopePlace { int t, u, h0; bool ok; };
+__device__ __forceinline__ RopePlace rope_place(const RopeGrid& g, int tokens)
 {
     RopePlace w;
-    const int units = rope_units(PATH, d);
-    w.hg = (heads + HP - 1) / HP;
-    const uint32_t per = (uint32_t)(w.hg * units);
-    uint32_t r, tl = 0;
-    if (per >= (uint32_t)kRopeThreads) {
+    uint32_t r;
+    if (g.per >= (uint32_t)kRopeThreads) {
         r = blockIdx.y * kRopeThreads + threadIdx.x;
         w.t = blockIdx.x;
-        w.ok = r < per;
+        w.ok = r < g.per;
     } else {
-        const uint32_t tb = kRopeThreads / per;
-        tl = threadIdx.x / per;
-        r = threadIdx.x - tl * per;
+        const uint32_t tb = (kRopeThreads * g.inv) >> 16, tl = (threadIdx.x * g.inv) >> 16;
+        r = threadIdx.x - tl * g.per;
         const int64_t t = (int64_t)blockIdx.x * tb + tl;
         w.ok = tl < tb && t < tokens;
         w.t = (int)t;
     }
-    w.h0 = (int)(r / (uint32_t)units);
-    w.u = (int)(r - (uint32_t)w.h0 * units);
+    w.h0 = (int)(r >> g.units_shift);
+    w.u = (int)(r - ((uint32_t)w.h0 << g.units_shift));
     return w;
 }
 
@@ -270,31 +282,35 @@ __global__ void __launch_bounds__(kRopeThreads) rope_apply_kernel(const RopeAppl
 {
     __shared__ float sh[PATH == kRopeAnySize ? kRopeThreads * 8 : 1];
     pdl_wait_then_release();
-    const RopePlace w = rope_place<PATH, HP>(p.tokens, p.heads, p.d);
+    const RopePlace w = rope_place(p.g, p.tokens);
     if (PATH != kRopeAnySize && !w.ok) return;
     const int t = w.ok ? w.t : 0;
     const T* x = static_cast<const T*>(p.x) + (int64_t)t * p.x_tok;
     T* y = static_cast<T*>(p.y) + (int64_t)t * p.y_tok;
     const int pos = __ldg(p.pos + t);
     if constexpr (PATH == kRopeAnySize) {
-        Vec8<T> v[HP];
+        RopeAny any;
+        any.fetch(p.r, w.u, pos);
+        for (int j0 = 0; j0 < p.hp; j0 += HP) {
+            Vec8<T> v[HP];
 #pragma unroll
-        for (int j = 0; j < HP; ++j) {
-            const int h = w.h0 + j * w.hg;
-            if (w.ok && h < p.heads) v[j].load(x + (int64_t)h * p.x_head + w.u * 8);
-            else v[j].zero();
-        }
+            for (int j = 0; j < HP; ++j) {
+                const int h = w.h0 + (j0 + j) * p.g.hg;
+                if (w.ok && h < p.heads) v[j].load(x + (int64_t)h * p.x_head + w.u * 8);
+                else v[j].zero();
+            }
 #pragma unroll
-        for (int j = 0; j < HP; ++j) {
-            const int h = w.h0 + j * w.hg;
-            const bool in = w.ok && h < p.heads;
-            rope_any(p.r, w.u, pos, v[j], in, sh + (threadIdx.x >> 5) * 256);
-            if (in) v[j].store(y + (int64_t)h * p.y_head + w.u * 8);
+            for (int j = 0; j < HP; ++j) {
+                const int h = w.h0 + (j0 + j) * p.g.hg;
+                const bool in = w.ok && h < p.heads;
+                any.rotate(p.r, v[j], in, sh + (threadIdx.x >> 5) * 256);
+                if (in) v[j].store(y + (int64_t)h * p.y_head + w.u * 8);
+            }
         }
     } else if constexpr (PATH == kRopePairs) {
 #pragma unroll
         for (int j = 0; j < HP; ++j) {
-            const int h = w.h0 + j * w.hg;
+            const int h = w.h0 + j * p.g.hg;
             if (h < p.heads) rope_pair(p.r, w.u, pos, x + (int64_t)h * p.x_head, y + (int64_t)h * p.y_head, true);
         }
     } else {
@@ -303,7 +319,7 @@ __global__ void __launch_bounds__(kRopeThreads) rope_apply_kernel(const RopeAppl
         Vec8<T> lo[HP], hi[HP];
 #pragma unroll
         for (int j = 0; j < HP; ++j) {
-            const int h = w.h0 + j * w.hg;
+            const int h = w.h0 + j * p.g.hg;
             if (h >= p.heads) break;
             lo[j].load(x + (int64_t)h * p.x_head + un.e0);
             hi[j].load(x + (int64_t)h * p.x_head + un.e1);
@@ -311,7 +327,7 @@ __global__ void __launch_bounds__(kRopeThreads) rope_apply_kernel(const RopeAppl
         un.fetch(p.r, w.u, pos);
 #pragma unroll
         for (int j = 0; j < HP; ++j) {
-            const int h = w.h0 + j * w.hg;
+            const int h = w.h0 + j * p.g.hg;
             if (h >= p.heads) break;
             if (un.turn) un.rotate(p.r, lo[j], hi[j]);
             lo[j].store(y + (int64_t)h * p.y_head + un.e0);
@@ -323,15 +339,15 @@ __global__ void __launch_bounds__(kRopeThreads) rope_apply_kernel(const RopeAppl
 // Heads 0 .. hq-1 of a token are its query heads (rotated, to q_out), the next hkv its keys (rotated, to
 // the row), the last hkv its values (copied to the row).
 template <int PATH, int HP>
-__global__ void __launch_bounds__(kRopeThreads) rope_append_kernel(const RopeAppendParams p)
+__global__ void __launch_bounds__(kRopeThreads, PATH == kRopeAnySize ? 3 : 1) rope_append_kernel(const RopeAppendParams p)
 {
     __shared__ float sh[PATH == kRopeAnySize ? kRopeThreads * 8 : 1];
     pdl_wait_then_release();
     const int heads = p.hq + 2 * p.hkv;
-    RopePlace w = rope_place<PATH, HP>(p.batch * p.n_new, heads, p.d);
+    RopePlace w = rope_place(p.g, p.batch * p.n_new);
     if (PATH != kRopeAnySize && !w.ok) return;
     if (!w.ok) w.t = 0;
-    const int b = w.t / p.n_new, i = w.t - b * p.n_new;
+    const int b = p.n_new == 1 ? w.t : w.t / p.n_new, i = w.t - b * p.n_new;
     const int len = __ldg(p.lens + b);
     if (p.prompt && i >= len) {
         if (PATH != kRopeAnySize) return;
@@ -353,46 +369,54 @@ __global__ void __launch_bounds__(kRopeThreads) rope_append_kernel(const RopeApp
     }
     // the host refuses calls without room; a graph that replays one finds the lengths on the device
     if (!place && w.ok && p.hkv > 0 && w.h0 == 0 && w.u == 0) atomicExch(p.status, kStatusCapacity);
+    // where head h of the token is read and written, and whether it is rotated; false: nowhere
+    auto where = [&](int h, const uint16_t*& src, uint16_t*& dst, bool& turn) {
+        turn = true;
+        if (!w.ok || h >= heads) return false;
+        if (h < p.hq) {
+            src = p.q + (int64_t)w.t * p.q_tok + (int64_t)h * p.d;
+            dst = p.q_out + ((int64_t)w.t * p.hq + h) * p.d;
+            return true;
+        }
+        if (!place) return false;
+        h -= p.hq;
+        turn = h < p.hkv;
+        if (!turn) h -= p.hkv;
+        src = (turn ? p.k : p.v) + (int64_t)w.t * p.kv_tok + (int64_t)h * p.d;
+        dst = (turn ? p.K : p.V) + (row0 + h * head_step) * p.d;
+        return true;
+    };
     const uint16_t* src[HP];
     uint16_t* dst[HP];
-    bool turn[HP];
-#pragma unroll
-    for (int j = 0; j < HP; ++j) {
-        int h = w.h0 + j * w.hg;
-        src[j] = nullptr;
-        turn[j] = true;
-        if (!w.ok) continue;
-        if (h < p.hq) {
-            src[j] = p.q + (int64_t)w.t * p.q_tok + (int64_t)h * p.d;
-            dst[j] = p.q_out + ((int64_t)w.t * p.hq + h) * p.d;
-        } else if (h < heads && place) {
-            h -= p.hq;
-            turn[j] = h < p.hkv;
-            if (!turn[j]) h -= p.hkv;
-            src[j] = (turn[j] ? p.k : p.v) + (int64_t)w.t * p.kv_tok + (int64_t)h * p.d;
-            dst[j] = (turn[j] ? p.K : p.V) + (row0 + h * head_step) * p.d;
-        }
-    }
+    bool turn[HP], in[HP];
     if constexpr (PATH == kRopePairs) {
 #pragma unroll
         for (int j = 0; j < HP; ++j)
-            if (src[j]) rope_pair(p.r, w.u, pos, src[j], dst[j], turn[j]);
+            if (where(w.h0 + j * p.g.hg, src[j], dst[j], turn[j])) rope_pair(p.r, w.u, pos, src[j], dst[j], turn[j]);
     } else if constexpr (PATH == kRopeAnySize) {
-        Vec8<uint16_t> v[HP];
+        RopeAny any;
+        any.fetch(p.r, w.u, pos);
+        for (int j0 = 0; j0 < p.hp; j0 += HP) {
+            Vec8<uint16_t> v[HP];
 #pragma unroll
-        for (int j = 0; j < HP; ++j) {
-            if (src[j]) v[j].load(src[j] + w.u * 8);
-            else v[j].zero();
-        }
+            for (int j = 0; j < HP; ++j) {
+                in[j] = where(w.h0 + (j0 + j) * p.g.hg, src[j], dst[j], turn[j]);
+                if (in[j]) v[j].load(src[j] + w.u * 8);
+                else v[j].zero();
+            }
 #pragma unroll
-        for (int j = 0; j < HP; ++j) {
-            rope_any(p.r, w.u, pos, v[j], src[j] && turn[j], sh + (threadIdx.x >> 5) * 256);
-            if (src[j]) v[j].store(dst[j] + w.u * 8);
+            for (int j = 0; j < HP; ++j) {
+                any.rotate(p.r, v[j], in[j] && turn[j], sh + (threadIdx.x >> 5) * 256);
+                if (in[j]) v[j].store(dst[j] + w.u * 8);
+            }
         }
     } else {
         RopeUnit un;
         un.init(p.r, w.u);
         Vec8<uint16_t> lo[HP], hi[HP];
+#pragma unroll
+        for (int j = 0; j < HP; ++j)
+            if (!where(w.h0 + j * p.g.hg, src[j], dst[j], turn[j])) src[j] = nullptr;
 #pragma unroll
         for (int j = 0; j < HP; ++j) {
             if (!src[j]) continue;
