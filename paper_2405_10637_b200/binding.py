@@ -5,6 +5,7 @@ computation runs in the library's own kernels.  There is no fallback: if the lib
 or does not load, the first call raises.
 """
 import ctypes as C
+import importlib.util
 import os
 
 import torch
@@ -177,16 +178,27 @@ def lckv_read_stream_probe(src, nbytes, kind, dev_sum, dev_status, repeats=1, l2
 
 
 # -- operators around the attention ------------------------------------------------------------
-# A decode step makes these calls once or several times per layer, so each checks and marshals with as
-# few Python operations as it can (device indices instead of device objects, each shape and stride tuple
-# taken once, plain integers for pointers): 6 us a call where the first version took 8.5 us, of which the
-# launch itself is 2.7 us.  Types, shapes and devices are checked here, since a tensor of another type
-# would be read past its end on the device.
-_raw_stream = torch._C._cuda_getCurrentRawStream
-_current_device = torch._C._cuda_getDevice
-_BF16, _F32, _E4M3, _U8, _I32 = torch.bfloat16, torch.float32, torch.float8_e4m3fn, torch.uint8, torch.int32
-_FLOATS = {_BF16: 0, _F32: 1}
-_OUT_KINDS = {_BF16: 0, _F32: 1, _E4M3: 2}
+# A decode step makes these calls several times per layer, so their checks and marshalling are native
+# (csrc/lckv_calls.cpp); what a call takes of its tensors is stated there and in include/lckv.h.
+_CALLS = None
+_BAD_TENSOR = -1
+
+
+def calls():
+    """Load (building first if the sources are newer) the native calls.  Raises if impossible."""
+    global _CALLS
+    if _CALLS is None:
+        lib()
+        path = _build.build_calls()
+        spec = importlib.util.spec_from_file_location("_lckv_calls", path)
+        module = importlib.util.module_from_spec(spec)
+        spec.loader.exec_module(module)
+        _CALLS = module
+    return _CALLS
+
+
+def _fail(rc, name, takes):
+    raise LckvError(EINVAL, f"{name}: {takes}") if rc == _BAD_TENSOR else LckvError(rc, name)
 
 
 def _require(ok, what):
@@ -194,42 +206,34 @@ def _require(ok, what):
         raise LckvError(EINVAL, what)
 
 
-def _other_stream(dev, stream):
+def _address(device, stream):
     """cudaStream_t of a stream that the caller gave; it has to belong to the tensors' device."""
-    _require(stream.device.index == dev, "the stream belongs to another device than the tensors")
+    _require(stream.device.index == device, "the stream belongs to another device than the tensors")
     return stream.cuda_stream
 
 
 def make_rope_scaling(kind=0, base=10000.0, factor=1.0, original=0.0, low=1.0, high=4.0, amplitude=0.0):
     """Frequencies of rotary tables: kind 0 none, 1 linear, 2 base, 3 by parts (include/lckv.h)."""
-    return RopeScaling(C.sizeof(RopeScaling), kind, base, factor, original, low, high, amplitude)
-
-
-def _check_tables(cos, sin, what):
-    _require(cos.dtype == _F32 and sin.dtype == _F32 and cos.dim() == 2 and cos.shape == sin.shape and cos.is_contiguous()
-             and sin.is_contiguous() and cos.get_device() >= 0 and sin.get_device() == cos.get_device(),
-             f"{what}: cos and sin are contiguous fp32 CUDA tensors of one shape")
+    r = RopeScaling(C.sizeof(RopeScaling), kind, base, factor, original, low, high, amplitude)
+    r.address = C.addressof(r)
+    return r
 
 
 def lckv_rope_tables(cos, sin, scaling, stream=None):
     """Fills the CUDA tensors cos, sin [positions, rot_dim / 2] fp32; returns them."""
-    _check_tables(cos, sin, "lckv_rope_tables")
-    dev = cos.get_device()
-    if dev != _current_device():
-        with torch.cuda.device(dev):
-            return lckv_rope_tables(cos, sin, scaling, stream)
-    positions, half = cos.shape
-    rc = (_LIB or lib()).lckv_rope_tables(cos.data_ptr(), sin.data_ptr(), positions, 2 * half, C.addressof(scaling),
-                                          _raw_stream(dev) if stream is None else _other_stream(dev, stream))
-    if rc != OK:
-        raise LckvError(rc, "lckv_rope_tables")
+    rc = (_CALLS or calls()).rope_tables(cos, sin, scaling.address,
+                                         None if stream is None else _address(cos.get_device(), stream))
+    if rc:
+        _fail(rc, "lckv_rope_tables", "cos and sin are contiguous fp32 CUDA tensors of one shape")
     return cos, sin
 
 
 def make_rope(cos, sin, interleaved=False):
     """A rotation described by its tables, cos and sin [positions, rot_dim / 2] fp32 on the device.  The result keeps
     the tables alive."""
-    _check_tables(cos, sin, "make_rope")
+    _require(cos.dtype == torch.float32 and sin.dtype == torch.float32 and cos.dim() == 2 and cos.shape == sin.shape
+             and cos.is_contiguous() and sin.is_contiguous() and cos.get_device() >= 0 and sin.get_device() == cos.get_device(),
+             "make_rope: cos and sin are contiguous fp32 CUDA tensors of one shape")
     r = Rope(C.sizeof(Rope), 2 * cos.shape[1], 1 if interleaved else 0, cos.shape[0], cos.data_ptr(), sin.data_ptr())
     r.tables, r.device, r.address = (cos, sin), cos.get_device(), C.addressof(r)
     return r
@@ -240,25 +244,11 @@ def lckv_rope_apply(rope, positions, x, out=None, transpose=False, stream=None):
     (made if None; may be x)."""
     if out is None:
         out = torch.empty(x.shape, dtype=x.dtype, device=x.device)
-    dev, shape, dtype = x.get_device(), x.shape, x.dtype
-    xs, ys = x.stride(), out.stride()
-    kind = _FLOATS.get(dtype)
-    if not (len(shape) == 3 and kind is not None and out.dtype is dtype and out.shape == shape and xs[2] == 1 and ys[2] == 1
-            and positions.dtype is _I32 and positions.shape == shape[:1] and positions.is_contiguous()
-            and dev == out.get_device() == positions.get_device() == rope.device):
-        raise LckvError(EINVAL, "lckv_rope_apply: x and out [tokens, heads, d_h] bf16 or fp32, positions [tokens] int32, "
-                                "all on the tables' device")
-    tokens, heads, d = shape
-    if tokens == 0:
-        return out
-    if dev != _current_device():
-        with torch.cuda.device(dev):
-            return lckv_rope_apply(rope, positions, x, out, transpose, stream)
-    rc = (_LIB or lib()).lckv_rope_apply(rope.address, positions.data_ptr(), x.data_ptr(), xs[0], xs[1], out.data_ptr(), ys[0],
-                                         ys[1], tokens, heads, d, kind, 1 if transpose else 0,
-                                         _raw_stream(dev) if stream is None else _other_stream(dev, stream))
-    if rc != OK:
-        raise LckvError(rc, "lckv_rope_apply")
+    rc = (_CALLS or calls()).rope_apply(rope.address, rope.device, positions, x, out, 1 if transpose else 0,
+                                        None if stream is None else _address(rope.device, stream))
+    if rc:
+        _fail(rc, "lckv_rope_apply", "x and out are [tokens, heads, d_h] bf16 or fp32, positions [tokens] int32, all on the "
+                                     "tables' device")
     return out
 
 
@@ -267,44 +257,12 @@ def lckv_rms_norm(x, weight, out, residual=None, residual_out=None, out_scale=No
     """out = norm(x + residual) * weight over the last dimension of x [rows, width]; the sum goes to residual_out.
     out is bf16, fp32, or float8_e4m3fn with out_scale fp32 ([rows, 1] or [rows], or [rows, ceil(width / 128)] with
     scale_group=128)."""
-    shape, dev, xs = x.shape, x.get_device(), x.stride()
-    x_kind, w_kind, y_kind = _FLOATS.get(x.dtype), _FLOATS.get(weight.dtype), _OUT_KINDS.get(out.dtype)
-    if not (len(shape) == 2 and x_kind is not None and w_kind is not None and y_kind is not None and out.shape == shape
-            and weight.shape == shape[1:] and out.is_contiguous() and weight.is_contiguous()
-            and (xs[1] == 1 or shape[1] == 1) and (shape[0] < 2 or xs[0] >= shape[1])
-            and dev == weight.get_device() == out.get_device() and dev >= 0):
-        raise LckvError(EINVAL, "lckv_rms_norm: x [rows, width], weight [width], out like x, bf16 or fp32 on one device "
-                                "(out also float8_e4m3fn)")
-    rows, width = shape
-    r = ro = sc = None
-    r_kind = 0
-    if residual is not None:
-        r_kind = _FLOATS.get(residual.dtype)
-        if r_kind is None or residual.shape != shape or not residual.is_contiguous() or residual.get_device() != dev:
-            raise LckvError(EINVAL, "lckv_rms_norm: residual is contiguous, bf16 or fp32, and has x's shape and device")
-        r = residual.data_ptr()
-        if residual_out is not None:
-            if (residual_out.dtype is not residual.dtype or residual_out.shape != shape or not residual_out.is_contiguous()
-                    or residual_out.get_device() != dev):
-                raise LckvError(EINVAL, "lckv_rms_norm: residual_out is like residual")
-            ro = residual_out.data_ptr()
-    elif residual_out is not None:
-        raise LckvError(EINVAL, "lckv_rms_norm: residual_out without residual")
-    if out_scale is not None:
-        if (out_scale.dtype is not _F32 or not out_scale.is_contiguous() or out_scale.get_device() != dev
-                or out_scale.numel() != rows * (-(-width // 128) if scale_group else 1)):
-            raise LckvError(EINVAL, "lckv_rms_norm: out_scale is contiguous fp32, one per row or per 128 columns")
-        sc = out_scale.data_ptr()
-    if rows == 0:
-        return out
-    if dev != _current_device():
-        with torch.cuda.device(dev):
-            return lckv_rms_norm(x, weight, out, residual, residual_out, out_scale, scale_group, eps, stream)
-    rc = (_LIB or lib()).lckv_rms_norm(x.data_ptr(), xs[0] if rows > 1 else 0, x_kind, r, ro, r_kind, weight.data_ptr(), w_kind,
-                                       out.data_ptr(), y_kind, sc, scale_group, rows, width, eps,
-                                       _raw_stream(dev) if stream is None else _other_stream(dev, stream))
-    if rc != OK:
-        raise LckvError(rc, "lckv_rms_norm")
+    rc = (_CALLS or calls()).rms_norm(x, weight, out, residual, residual_out, out_scale, scale_group, eps,
+                                      None if stream is None else _address(x.get_device(), stream))
+    if rc:
+        _fail(rc, "lckv_rms_norm", "x is [rows, width], weight [width], residual, residual_out (like residual) and out have x's "
+                                   "shape and are contiguous, bf16 or fp32 (out also float8_e4m3fn, with out_scale fp32, one "
+                                   "per row or per 128 columns), all on one device")
     return out
 
 
@@ -313,18 +271,19 @@ class QuantWeight:
 
     def __init__(self, n, k, group, has_zeros, buf):
         self.n, self.k, self.group, self.has_zeros, self.buf = n, k, group, has_zeros, buf
-        self.ptr, self.device = buf.data_ptr(), buf.get_device()
+        self.device = buf.get_device()
+        self.call = (buf.data_ptr(), self.device, n, k, group, has_zeros)
 
 
 def lckv_quant_pack(codes, scales, zeros=None, stream=None):
     """codes [n, k / 2] uint8 (low nibble = even column), scales [n, k / group] bf16, zeros [n, k / group] uint8 or None
-    -> QuantWeight."""
+    -> QuantWeight.  Synchronises the stream."""
     dev = codes.get_device()
-    _require(codes.dim() == 2 and codes.dtype is _U8 and codes.is_contiguous() and scales.dtype is _BF16
+    _require(codes.dim() == 2 and codes.dtype == torch.uint8 and codes.is_contiguous() and scales.dtype == torch.bfloat16
              and scales.is_contiguous() and scales.dim() == 2 and scales.shape[0] == codes.shape[0] and scales.shape[1] > 0
              and 2 * codes.shape[1] % scales.shape[1] == 0 and dev == scales.get_device() and dev >= 0,
              "lckv_quant_pack: codes [n, k / 2] uint8, scales [n, k / group] bf16, on one device")
-    _require(zeros is None or (zeros.dtype is _U8 and zeros.is_contiguous() and zeros.shape == scales.shape
+    _require(zeros is None or (zeros.dtype == torch.uint8 and zeros.is_contiguous() and zeros.shape == scales.shape
                                and zeros.get_device() == dev), "lckv_quant_pack: zeros are uint8 of the scales' shape")
     n, k = codes.shape[0], 2 * codes.shape[1]
     group = k // scales.shape[1]
@@ -332,65 +291,23 @@ def lckv_quant_pack(codes, scales, zeros=None, stream=None):
     _require(nbytes > 0, "lckv_quant_pack: group is 32, 64 or 128")
     with torch.cuda.device(dev):
         buf = torch.empty(nbytes, dtype=torch.uint8, device=codes.device)
+        st = torch.cuda.current_stream(dev).cuda_stream if stream is None else _address(dev, stream)
         _chk(lib().lckv_quant_pack(codes.data_ptr(), scales.data_ptr(), None if zeros is None else zeros.data_ptr(), n, k,
-                                   group, buf.data_ptr(), nbytes,
-                                   _raw_stream(dev) if stream is None else _other_stream(dev, stream)), "lckv_quant_pack")
+                                   group, buf.data_ptr(), nbytes, st), "lckv_quant_pack")
     return QuantWeight(n, k, group, 0 if zeros is None else 1, buf)
 
 
 def lckv_quant_linear(w, x, out=None, x_scale=None, dev_status=None, stream=None):
     """out [rows, n] (bf16 or fp32) = x [rows, k] (bf16, or float8_e4m3fn with x_scale) times the 4-bit weight w.
     dev_status: optional CUDA int32 tensor that receives ETIMEOUT if a device-side wait gave up."""
-    shape, dev, xs, n = x.shape, x.get_device(), x.stride(), w.n
-    kind = 0 if x.dtype is _BF16 else 1 if x.dtype is _E4M3 else -1
-    _require(len(shape) == 2, "lckv_quant_linear: x is [rows, k]")
-    rows, k = shape
     if out is None:
-        out = torch.empty((rows, n), dtype=_BF16, device=x.device)
-    ys, y_kind = out.stride(), _FLOATS.get(out.dtype)
-    if not (kind >= 0 and y_kind is not None and k == w.k and xs[1] == 1 and out.shape == (rows, n) and (ys[1] == 1 or n == 1)
-            and (rows < 2 or (xs[0] >= k and ys[0] >= n)) and dev == w.device == out.get_device()):
-        raise LckvError(EINVAL, "lckv_quant_linear: x [rows, k] bf16 or float8_e4m3fn, out [rows, n] bf16 or fp32, on the "
-                                "weight's device")
-    sc, group = None, 0
-    if x_scale is not None:
-        group = 0 if x_scale.numel() == rows else 128
-        if not (kind == 1 and x_scale.dtype is _F32 and x_scale.is_contiguous() and x_scale.get_device() == dev
-                and x_scale.numel() == (rows * -(-k // 128) if group else rows)):
-            raise LckvError(EINVAL, "lckv_quant_linear: x_scale is contiguous fp32, one per row or per 128 columns of an "
-                                    "8-bit x")
-        sc = x_scale.data_ptr()
-    if rows == 0:
-        return out
-    if dev_status is not None and not (dev_status.dtype is _I32 and dev_status.numel() > 0 and dev_status.get_device() == dev):
-        raise LckvError(EINVAL, "lckv_quant_linear: dev_status is int32 on the weight's device")
-    if dev != _current_device():
-        with torch.cuda.device(dev):
-            return lckv_quant_linear(w, x, out, x_scale, dev_status, stream)
-    rc = (_LIB or lib()).lckv_quant_linear(w.ptr, n, k, w.group, w.has_zeros, x.data_ptr(), xs[0] if rows > 1 else 0, kind, sc,
-                                           group, out.data_ptr(), ys[0] if rows > 1 else 0, y_kind, rows,
-                                           None if dev_status is None else dev_status.data_ptr(),
-                                           _raw_stream(dev) if stream is None else _other_stream(dev, stream))
-    if rc != OK:
-        raise LckvError(rc, "lckv_quant_linear")
+        out = torch.empty((x.shape[0], w.n), dtype=torch.bfloat16, device=x.device)
+    rc = (_CALLS or calls()).quant_linear(*w.call, x, out, x_scale, dev_status,
+                                          None if stream is None else _address(w.device, stream))
+    if rc:
+        _fail(rc, "lckv_quant_linear", "x is [rows, k] bf16 or float8_e4m3fn (with x_scale fp32, one per row or per 128 columns), "
+                                       "out [rows, n] bf16 or fp32, on the weight's device")
     return out
-
-
-def _token_stride(t, dev, batch, n, heads, d):
-    """Elements between consecutive tokens of a bf16 tensor [batch, n, heads, d_h] whose heads are dense ([batch, heads, d_h]
-    where n is None); -1 where it is none."""
-    st = t.stride()
-    if t.dtype is not _BF16 or t.get_device() != dev or t.shape != ((batch, heads, d) if n is None else (batch, n, heads, d)):
-        return -1
-    if st[-1] != 1 or (st[-2] != d and heads > 1):
-        return -1
-    if n is None or n == 1:
-        step, tokens = st[0], batch
-    else:
-        step, tokens = st[1], batch * n
-        if batch > 1 and st[0] != n * step:
-            return -1
-    return 0 if tokens == 1 else step if step >= heads * d else -1
 
 
 class Cache:
@@ -408,7 +325,8 @@ class Cache:
             _chk(lib().lckv_cache_alloc(C.byref(h), C.byref(cfg), _ptr(self.buf), nbytes),
                  "lckv_cache_alloc")
         self.h = h
-        self.dev_index = self.buf.get_device()
+        self.call = (h.value, self.buf.get_device())       # what the native calls take
+        self.heads = (cfg.n_q_heads, cfg.n_kv_heads, cfg.head_dim)
         info = Info()
         _chk(lib().lckv_cache_info(self.h, C.byref(info)), "lckv_cache_info")
         self.info = info
@@ -418,6 +336,7 @@ class Cache:
         if getattr(self, "h", None):
             lib().lckv_cache_free(self.h)
             self.h = None
+            self.call = (None, -1)
             self.buf = None
 
     def __del__(self):
@@ -497,51 +416,27 @@ class Cache:
                                           _stream(stream)), "lckv_project_append_kv")
 
     def _rope_call(self, name, slot, rope, q, k, v, q_out, advance, stream):
-        c, dev, ref = self.cfg, self.dev_index, q if q is not None else k
-        shape = () if ref is None else ref.shape
-        one = len(shape) == 3                      # one token per sequence
-        batch, n = (shape[0], None if one else shape[1]) if one or len(shape) == 4 else (0, 0)
-        d, q_step, kv_step, qp, qo, kp, vp = c.head_dim, 0, 0, None, None, None, None
-        if batch:
-            if q is not None:
-                if q_out is None:
-                    q_out = torch.empty(shape, dtype=_BF16, device=q.device)
-                q_step = _token_stride(q, dev, batch, n, c.n_q_heads, d)
-                if not (q_out.shape == shape and q_out.dtype is _BF16 and q_out.is_contiguous() and q_out.get_device() == dev):
-                    q_step = -1
-                qp, qo = q.data_ptr(), q_out.data_ptr()
-            if k is not None or v is not None:
-                if k is None or v is None:
-                    raise LckvError(EINVAL, f"{name}: k and v come together")
-                kv_step = _token_stride(k, dev, batch, n, c.n_kv_heads, d)
-                if _token_stride(v, dev, batch, n, c.n_kv_heads, d) != kv_step:
-                    kv_step = -1
-                kp, vp = k.data_ptr(), v.data_ptr()
-        if not batch or q_step < 0 or kv_step < 0 or rope.device != dev:
-            raise LckvError(EINVAL, f"{name}: q, k, v are bf16 [batch, tokens, heads, d_h] (or [batch, heads, d_h]) on the "
-                                    "cache's device, heads dense, one stride between tokens; q_out is contiguous")
-        if dev != _current_device():
-            with torch.cuda.device(dev):
-                return self._rope_call(name, slot, rope, q, k, v, q_out, advance, stream)
-        st = _raw_stream(dev) if stream is None else _other_stream(dev, stream)
-        if advance is None:
-            rc = lib().lckv_rope_prefill_write_kv(self.h, slot, rope.address, qp, q_step, qo, kp, vp, kv_step, n or 1, batch, st)
-        else:
-            rc = lib().lckv_rope_append_kv(self.h, slot, rope.address, qp, q_step, qo, kp, vp, kv_step, n or 1, batch, advance, st)
-        if rc != OK:
-            raise LckvError(rc, name)
+        h, dev = self.call
+        rc = (_CALLS or calls()).rope_cache(h, dev, slot, rope.address, rope.device, *self.heads, q, k, v, q_out, advance,
+                                            None if stream is None else _address(dev, stream))
+        if rc:
+            _fail(rc, name, "q, k, v are bf16 [batch, tokens, heads, d_h] (or [batch, heads, d_h]) on the cache's device, heads "
+                            "dense, one stride between tokens, k and v alike; q_out is like q, contiguous")
         return q_out
 
     def lckv_rope_append_kv(self, slot, rope, q, k_new, v_new, q_out=None, advance_len=0, stream=None):
         """Rotated append of one ([batch, heads, d_h]) or several ([batch, n, heads, d_h]) new tokens per sequence;
         q, or k_new and v_new, may be None.  Views of a fused projection are taken as they are.  Returns q_out."""
+        if q is not None and q_out is None:
+            q_out = torch.empty(q.shape, dtype=q.dtype, device=q.device)
         return self._rope_call("lckv_rope_append_kv", slot, rope, q, k_new, v_new, q_out, 1 if advance_len else 0, stream)
 
     def lckv_rope_prefill_write_kv(self, slot, rope, q, k, v, q_out=None, stream=None):
-        """The same for prompts [batch, n_max, heads, d_h] whose lengths the cache holds already."""
+        """The same for prompts [batch, n_max, heads, d_h] whose lengths the cache holds already.  Rows of q_out behind a
+        prompt are left as they were (zero where q_out is made here)."""
         if q is not None and q_out is None:
             q_out = torch.zeros(q.shape, dtype=q.dtype, device=q.device)
-        return self._rope_call("lckv_rope_prefill_write_kv", slot, rope, q, k, v, q_out, None, stream)
+        return self._rope_call("lckv_rope_prefill_write_kv", slot, rope, q, k, v, q_out, -1, stream)
 
     def lckv_decode_attention(self, slot, mode, q, out=None, lse=None, batch=None, stream=None):
         batch = q.shape[0] if batch is None else batch
