@@ -453,8 +453,9 @@ typedef struct {
 
 /*
  * Fills cos and sin, [positions, rot_dim / 2] fp32 on the device, with amplitude * cos(p theta_j) and
- * amplitude * sin(p theta_j), p = 0 .. positions-1.  Angles are reduced in fp64, so far positions are as
- * exact as near ones.  rot_dim even, 2 .. 128.  Errors: EINVAL, ECUDA.
+ * amplitude * sin(p theta_j), p = 0 .. positions-1.  theta_j is fp64, angles are reduced in 64-bit
+ * integers, so far positions are nearly as exact as near ones.  rot_dim even, 2 .. 128.  Errors: EINVAL (also a base
+ * or a frequency outside fp64's range after scaling), ECUDA.
  */
 int lckv_rope_tables(float* cos, float* sin, int32_t positions, int32_t rot_dim,
                      const lckv_rope_scaling_t* scaling, void* stream);
@@ -466,7 +467,7 @@ int lckv_rope_tables(float* cos, float* sin, int32_t positions, int32_t rot_dim,
  *   x, y       bf16 (dtype 0) or fp32 (dtype 1), element strides between tokens and between heads, the
  *              head_dim (64 or 128) elements of a head contiguous.  x may have strides of 0.  y == x with
  *              equal strides works in place; y may also be other heads of the tokens that x is in; any
- *              other overlap is refused.  Fastest with 16-byte aligned pointers and strides, 16-byte
+ *              other overlap with what is read is refused.  Fastest with 16-byte aligned pointers and strides, 16-byte
  *              aligned tables and rot_dim a multiple of 16; any other is correct.
  *   transpose  1: the transposed rotation (s -> -s): the gradient with respect to x given the gradient with
  *              respect to y, and the inverse when the tables' amplitude is 1.
@@ -484,7 +485,7 @@ int lckv_rope_apply(const lckv_rope_t* rope, const int32_t* positions, const voi
  * sink + recent-window cache), its value is copied there, its query is rotated by p into q_out.
  *   q          [batch, n_new, H_q, d_h] bf16, q_stride elements between tokens (0 => H_q * d_h); or NULL
  *   q_out      [batch, n_new, H_q, d_h] bf16, contiguous; NULL exactly if q is.  May be q itself when q is
- *              contiguous; any other overlap with q, k_new or v_new is refused
+ *              contiguous; any other overlap with q, k_new, v_new or the tables is refused
  *   k_new, v_new  [batch, n_new, H_kv, d_h] bf16, kv_stride elements between tokens (0 => H_kv * d_h); both
  *              NULL for a condensed layer, which has only a query (then `slot` is not written)
  *   advance_len   != 0: every len[b], b < batch, grows by n_new afterwards (all slots; needs k_new)
@@ -549,10 +550,12 @@ int lckv_rms_norm(const void* x, int64_t x_stride, int32_t x_dtype, const void* 
  *              concerned are then NaN); it is not cleared.  NULL to ignore
  * codes - zeros are exact on the tensor cores; a group's sum is accumulated in fp32 and scaled in fp32, and
  * there is one rounding to y's type.  Results do not depend on the order of execution.  rows 1 .. 524288.
+ * A row of x with an infinity or a NaN gives infinities or NaN, and leaves the other rows alone; up to 16 rows of bf16 also
+ * need 31 sum|x| over a group to be finite in fp32.
  * lckv_quant_pack SYNCHRONISES `stream` (set-up, like lckv_cache_alloc) and is refused while it captures;
  * lckv_quant_linear only enqueues work.  It requests packed weights before the kernel in front of it in
  * the stream has ended, so that kernel must not be the one that writes them (lckv_quant_pack's never is).
- * Errors: EINVAL (null, shape, alignment, y overlapping x or packed), ENOMEM (packed too small or misaligned,
+ * Errors: EINVAL (null, shape, alignment, y overlapping what is read), ENOMEM (packed too small or misaligned,
  * lckv_quant_pack only), ECUDA.
  */
 size_t lckv_quant_bytes(int32_t n, int32_t k, int32_t group, int32_t has_zeros);

@@ -212,6 +212,15 @@ def _address(device, stream):
     return stream.cuda_stream
 
 
+def _made(make, stream, shape, **kw):
+    """An output made here: by the stream that will write it, so that neither what its memory held before nor a fill of
+    it is still under way on another one."""
+    if stream is None:
+        return make(shape, **kw)
+    with torch.cuda.stream(stream):
+        return make(shape, **kw)
+
+
 def make_rope_scaling(kind=0, base=10000.0, factor=1.0, original=0.0, low=1.0, high=4.0, amplitude=0.0):
     """Frequencies of rotary tables: kind 0 none, 1 linear, 2 base, 3 by parts (include/lckv.h)."""
     r = RopeScaling(C.sizeof(RopeScaling), kind, base, factor, original, low, high, amplitude)
@@ -243,7 +252,7 @@ def lckv_rope_apply(rope, positions, x, out=None, transpose=False, stream=None):
     """x [tokens, heads, d_h] bf16 or fp32 (any strides, the last 1) rotated by positions [tokens] int32, into `out`
     (made if None; may be x)."""
     if out is None:
-        out = torch.empty(x.shape, dtype=x.dtype, device=x.device)
+        out = _made(torch.empty, stream, x.shape, dtype=x.dtype, device=x.device)
     rc = (_CALLS or calls()).rope_apply(rope.address, rope.device, positions, x, out, 1 if transpose else 0,
                                         None if stream is None else _address(rope.device, stream))
     if rc:
@@ -290,7 +299,7 @@ def lckv_quant_pack(codes, scales, zeros=None, stream=None):
     nbytes = lib().lckv_quant_bytes(n, k, group, 0 if zeros is None else 1)
     _require(nbytes > 0, "lckv_quant_pack: group is 32, 64 or 128")
     with torch.cuda.device(dev):
-        buf = torch.empty(nbytes, dtype=torch.uint8, device=codes.device)
+        buf = _made(torch.empty, stream, nbytes, dtype=torch.uint8, device=codes.device)
         st = torch.cuda.current_stream(dev).cuda_stream if stream is None else _address(dev, stream)
         _chk(lib().lckv_quant_pack(codes.data_ptr(), scales.data_ptr(), None if zeros is None else zeros.data_ptr(), n, k,
                                    group, buf.data_ptr(), nbytes, st), "lckv_quant_pack")
@@ -301,7 +310,7 @@ def lckv_quant_linear(w, x, out=None, x_scale=None, dev_status=None, stream=None
     """out [rows, n] (bf16 or fp32) = x [rows, k] (bf16, or float8_e4m3fn with x_scale) times the 4-bit weight w.
     dev_status: optional CUDA int32 tensor that receives ETIMEOUT if a device-side wait gave up."""
     if out is None:
-        out = torch.empty((x.shape[0], w.n), dtype=torch.bfloat16, device=x.device)
+        out = _made(torch.empty, stream, (x.shape[0], w.n), dtype=torch.bfloat16, device=x.device)
     rc = (_CALLS or calls()).quant_linear(*w.call, x, out, x_scale, dev_status,
                                           None if stream is None else _address(w.device, stream))
     if rc:
@@ -428,14 +437,14 @@ class Cache:
         """Rotated append of one ([batch, heads, d_h]) or several ([batch, n, heads, d_h]) new tokens per sequence;
         q, or k_new and v_new, may be None.  Views of a fused projection are taken as they are.  Returns q_out."""
         if q is not None and q_out is None:
-            q_out = torch.empty(q.shape, dtype=q.dtype, device=q.device)
+            q_out = _made(torch.empty, stream, q.shape, dtype=q.dtype, device=q.device)
         return self._rope_call("lckv_rope_append_kv", slot, rope, q, k_new, v_new, q_out, 1 if advance_len else 0, stream)
 
     def lckv_rope_prefill_write_kv(self, slot, rope, q, k, v, q_out=None, stream=None):
         """The same for prompts [batch, n_max, heads, d_h] whose lengths the cache holds already.  Rows of q_out behind a
         prompt are left as they were (zero where q_out is made here)."""
         if q is not None and q_out is None:
-            q_out = torch.zeros(q.shape, dtype=q.dtype, device=q.device)
+            q_out = _made(torch.zeros, stream, q.shape, dtype=q.dtype, device=q.device)
         return self._rope_call("lckv_rope_prefill_write_kv", slot, rope, q, k, v, q_out, -1, stream)
 
     def lckv_decode_attention(self, slot, mode, q, out=None, lse=None, batch=None, stream=None):

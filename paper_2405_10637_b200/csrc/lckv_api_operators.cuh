@@ -44,6 +44,12 @@ int rope_args(const lckv_rope_t* r, int head_dim, lckv::RopeArgs* out)
     return LCKV_OK;
 }
 
+bool rope_tables_meet(const lckv_rope_t* r, const void* out, int64_t bytes)
+{
+    const int64_t n = (int64_t)r->positions * (r->rot_dim / 2) * 4;
+    return ranges_meet(out, bytes, r->cos, n) || ranges_meet(out, bytes, r->sin, n);
+}
+
 bool rope_tables_vector(const lckv_rope_t* r) { return r->rot_dim % 16 == 0 && aligned(r->cos, 16) && aligned(r->sin, 16); }
 
 // Heads per thread: four when there are enough units to fill the GPU's threads one and a half times (one fetch of the
@@ -121,6 +127,7 @@ int rope_into_cache(lckv_cache* c, int slot, const lckv_rope_t* rope, const void
         const int64_t out_bytes = tokens * hq * d * 2, q_bytes = ((tokens - 1) * q_stride + (int64_t)hq * d) * 2;
         const int64_t kv_bytes = k ? ((tokens - 1) * kv_stride + (int64_t)hkv * d) * 2 : 0;
         if (!(q_out == q && q_stride == (int64_t)hq * d) && ranges_meet(q_out, out_bytes, q, q_bytes)) return LCKV_EINVAL;
+        if (rope_tables_meet(rope, q_out, out_bytes)) return LCKV_EINVAL;
         if (k && (ranges_meet(q_out, out_bytes, k, kv_bytes) || ranges_meet(q_out, out_bytes, v, kv_bytes)))
             return LCKV_EINVAL;
     }
@@ -201,11 +208,12 @@ bool rope_layout_ok(int64_t tok, int64_t head, int64_t tokens, int64_t heads, in
 
 namespace {
 
-// Threads of a row of n_vec vectors at nv vectors each: 8, 16 or 32 lanes of a warp, or whole warps.
-int norm_threads(int n_vec, int nv)
+// Threads of a row of n_vec vectors at nv vectors each: 8, 16 or 32 lanes of a warp, or whole warps.  With a scale per 128
+// columns at least the 16 lanes that hold one such block.
+int norm_threads(int n_vec, int nv, bool blocks)
 {
     const int t = (n_vec + nv - 1) / nv;
-    return t <= 8 ? 8 : t <= 16 ? 16 : (t + 31) / 32 * 32;
+    return t <= 8 && !blocks ? 8 : t <= 16 ? 16 : (t + 31) / 32 * 32;
 }
 
 struct NormShape { int tpr, rpb, smem, sms; };
@@ -252,7 +260,7 @@ cudaError_t norm_launch(const lckv::NormParams& p, int n_vec, bool edges, int sm
     if (many && (!fp32 || edges || n_vec > 512 + 256 || (p.out == 2 && n_vec >= 512))) {
         const int nv = n_vec > 1024 ? 4 : 2;
         NormShape g;
-        g.tpr = norm_threads(n_vec, nv);
+        g.tpr = norm_threads(n_vec, nv, p.group != 0);
         g.rpb = g.tpr <= 32 ? 128 / g.tpr : 1;
         const int parts = (p.x32 ? 2 : 1) + (p.r ? (p.r32 ? 2 : 1) : 0);
         const int64_t smem = (int64_t)lckv::kNormRing * nv * parts * g.tpr * g.rpb * 16;
@@ -265,7 +273,7 @@ cudaError_t norm_launch(const lckv::NormParams& p, int n_vec, bool edges, int sm
     }
     int nv = many && n_vec >= 64 ? 2 : 1;
     while ((n_vec + nv - 1) / nv > (nv == 1 ? 1024 : 512)) nv *= 2;
-    const int tpr = norm_threads(n_vec, nv), rpb = tpr <= 32 ? 128 / tpr : 1;
+    const int tpr = norm_threads(n_vec, nv, p.group != 0), rpb = tpr <= 32 ? 128 / tpr : 1;
     const auto kernel = !edges ? (nv == 1   ? lckv::norm_vec_kernel<1, 1024, false>
                                   : nv == 2 ? lckv::norm_vec_kernel<2, 512, false> : nv == 4 ? lckv::norm_vec_kernel<4, 512, false> : lckv::norm_vec_kernel<8, 512, false>)
                                : (nv == 1   ? lckv::norm_vec_kernel<1, 1024, true>
@@ -288,7 +296,7 @@ int lckv_rope_tables(float* cos, float* sin, int32_t positions, int32_t rot_dim,
     if (s->kind < 0 || s->kind > 3) return LCKV_EINVAL;
     if (!(s->base > 1.0) || !std::isfinite(s->base)) return LCKV_EINVAL;
     const double amplitude = s->amplitude == 0.0 ? 1.0 : s->amplitude;
-    if (!std::isfinite(amplitude)) return LCKV_EINVAL;
+    if (!std::isfinite((float)amplitude)) return LCKV_EINVAL;
     if (s->kind != 0 && (!(s->factor > 0.0) || !std::isfinite(s->factor))) return LCKV_EINVAL;
     if (s->kind == 3 && (!(s->original > 0.0) || !std::isfinite(s->original) || !(s->low >= 0.0) || !(s->high > s->low) ||
                          !std::isfinite(s->high)))
@@ -305,6 +313,7 @@ int lckv_rope_tables(float* cos, float* sin, int32_t positions, int32_t rot_dim,
             theta *= keep + (1.0 - keep) / s->factor;
         }
         double turns = theta / two_pi;
+        if (!std::isfinite(turns)) return LCKV_EINVAL;       // a factor so small that base or frequency leave fp64
         turns -= std::floor(turns);
         p.turns[i] = (uint64_t)std::ldexp(turns, 64);        // (turns < 1: at most 2^64 - 2^11)
     }
@@ -317,7 +326,7 @@ int lckv_rope_tables(float* cos, float* sin, int32_t positions, int32_t rot_dim,
     const bool vec = half % 4 == 0 && aligned(cos, 16) && aligned(sin, 16);
     // four positions per thread where that leaves enough threads (one fetch of the frequencies serves them all)
     const int v = vec ? 4 : 1, many = positions >= 4096 ? 4 : 1;
-    p.step = (int64_t)((positions + many - 1) / many) * (half / v);
+    p.step = ((int64_t)positions + many - 1) / many * (half / v);
     const dim3 grid((unsigned)((p.step + lckv::kRopeThreads - 1) / lckv::kRopeThreads)), block(lckv::kRopeThreads);
     const cudaError_t e = vec ? (many == 4 ? launch_pdl_dims(lckv::rope_table_kernel<4, 4>, grid, block, 0, st, p)
                                            : launch_pdl_dims(lckv::rope_table_kernel<4, 1>, grid, block, 0, st, p))
@@ -348,6 +357,7 @@ int lckv_rope_apply(const lckv_rope_t* rope, const int32_t* positions, const voi
         const int64_t apart = std::abs((int64_t)((intptr_t)y - (intptr_t)x)) / size, row = top * y_head_stride + head_dim;
         if (!same || !(apart == 0 || (apart >= row && apart + row <= y_token_stride))) return LCKV_EINVAL;
     }
+    if (rope_tables_meet(rope, y, y_span * size) || ranges_meet(y, y_span * size, positions, (int64_t)n_tokens * 4)) return LCKV_EINVAL;
     p.r.sgn = transpose ? -1.f : 1.f;
     p.pos = positions;
     p.x = x;
@@ -657,7 +667,9 @@ int lckv_quant_linear(const void* packed, int32_t n, int32_t k, int32_t group, i
     if (!aligned(packed, 256) || !aligned(x, 16) || (x_stride * xs) % 16 || !aligned(y, ys) || !aligned(x_scale, 4) || !aligned(dev_status, 4)) return LCKV_EINVAL;
     const lckv::QuantLayout lay = lckv::quant_layout(n, k, group, has_zeros != 0);
     const int64_t y_bytes = ((int64_t)(rows - 1) * y_stride + n) * ys;
-    if (ranges_meet(y, y_bytes, x, ((int64_t)(rows - 1) * x_stride + k) * xs) || ranges_meet(y, y_bytes, packed, lay.total))
+    const int64_t n_scales = (int64_t)rows * (x_scale_group ? (k + 127) / 128 : 1);
+    if (ranges_meet(y, y_bytes, x, ((int64_t)(rows - 1) * x_stride + k) * xs) || ranges_meet(y, y_bytes, packed, lay.total) ||
+        (x_scale && ranges_meet(y, y_bytes, x_scale, n_scales * 4)) || (dev_status && ranges_meet(y, y_bytes, dev_status, 4)))
         return LCKV_EINVAL;
     lckv::QuantParams p;
     p.w = static_cast<const uint8_t*>(packed);

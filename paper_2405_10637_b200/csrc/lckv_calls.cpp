@@ -39,6 +39,12 @@ struct Args {
         if (v == -1 && PyErr_Occurred()) { PyErr_Clear(); ok = false; }
         return v;
     }
+    int32_t integer32()
+    {
+        const int64_t v = integer();
+        if (v != (int32_t)v) ok = false;
+        return (int32_t)v;
+    }
     void* address() { return reinterpret_cast<void*>(integer()); }
     double real()
     {
@@ -128,7 +134,7 @@ PyObject* rope_apply(Args& a)
 PyObject* rms_norm(Args& a)
 {
     const at::Tensor *x = a.tensor(), *w = a.tensor(), *y = a.tensor(), *r = a.tensor(), *h = a.tensor(), *s = a.tensor();
-    const int64_t group = a.integer();
+    const int32_t group = a.integer32();
     const double eps = a.real();
     if (!a.ok || !x || !w || !y || x->dim() != 2 || !x->is_cuda()) return code(kBadTensor);
     const int64_t dev = x->get_device(), rows = x->size(0), width = x->size(1);
@@ -145,7 +151,7 @@ PyObject* rms_norm(Args& a)
     if (s && (!dense(s, at::kFloat, dev) || s->numel() != rows * (group ? (width + 127) / 128 : 1))) return code(kBadTensor);
     if (rows == 0) return code(LCKV_OK);
     return run(a, dev, [&](void* st) {
-        return lckv_rms_norm(ptr(x), rows > 1 ? x->stride(0) : 0, xk, ptr(r), mut(h), rk, ptr(w), wk, mut(y), yk, static_cast<float*>(mut(s)), (int32_t)group,
+        return lckv_rms_norm(ptr(x), rows > 1 ? x->stride(0) : 0, xk, ptr(r), mut(h), rk, ptr(w), wk, mut(y), yk, static_cast<float*>(mut(s)), group,
                              (int32_t)rows, (int32_t)width, (float)eps, st);
     });
 }
@@ -198,7 +204,8 @@ int64_t token_stride(const at::Tensor* t, int64_t dev, int64_t batch, int64_t n,
 PyObject* rope_cache(Args& a)
 {
     auto* cache = static_cast<lckv_cache_t*>(a.address());
-    const int64_t dev = a.integer(), slot = a.integer();
+    const int64_t dev = a.integer();
+    const int32_t slot = a.integer32();
     const auto* rope = static_cast<const lckv_rope_t*>(a.address());
     const int64_t rope_dev = a.integer(), hq = a.integer(), hkv = a.integer(), d = a.integer();
     const at::Tensor *q = a.tensor(), *k = a.tensor(), *v = a.tensor(), *o = a.tensor();
@@ -220,8 +227,8 @@ PyObject* rope_cache(Args& a)
     }
     return run(a, dev, [&](void* st) {
         if (advance < 0)
-            return lckv_rope_prefill_write_kv(cache, (int32_t)slot, rope, ptr(q), q_step, mut(o), ptr(k), ptr(v), kv_step, (int32_t)n, (int32_t)batch, st);
-        return lckv_rope_append_kv(cache, (int32_t)slot, rope, ptr(q), q_step, mut(o), ptr(k), ptr(v), kv_step, (int32_t)n, (int32_t)batch, (int32_t)advance, st);
+            return lckv_rope_prefill_write_kv(cache, slot, rope, ptr(q), q_step, mut(o), ptr(k), ptr(v), kv_step, (int32_t)n, (int32_t)batch, st);
+        return lckv_rope_append_kv(cache, slot, rope, ptr(q), q_step, mut(o), ptr(k), ptr(v), kv_step, (int32_t)n, (int32_t)batch, (int32_t)advance, st);
     });
 }
 

@@ -300,7 +300,8 @@ __device__ __forceinline__ void norm_finish(const NormParams& p, const Types& t,
         for (int j = 0; j < 8; ++j) m = max_nan(m, fabsf(f[i][j]));
         if (!EDGES && t.group()) {
             // 16 lanes hold 128 columns
-            for (int o = tpr < 16 ? tpr >> 1 : 8; o > 0; o >>= 1) m = max_nan(m, __shfl_xor_sync(0xffffffffu, m, o));
+#pragma unroll
+            for (int o = 8; o > 0; o >>= 1) m = max_nan(m, __shfl_xor_sync(0xffffffffu, m, o));
             const float s = m / kE4m3Max;
             if (v < w.n_vec) {
                 if ((tx & 15) == 0) p.scale[w.row * p.n_groups + (v >> 4)] = s;
@@ -410,9 +411,9 @@ __global__ void __launch_bounds__(512) norm_ring_kernel(const NormParams p)
     const uint32_t slot_bytes = (uint32_t)(NV * PARTS * threads) * 16, smem0 = smem_u32(norm_smem);
     const int64_t step = (int64_t)gridDim.x * blockDim.y, xs = step * p.x_stride, es = step * p.width;
     const int64_t last_e = (int64_t)p.rows * p.width, last_x = (int64_t)(p.rows - 1) * p.x_stride + p.width;
-    const int lane = tx & 31;
     const bool wide = tpr >= 32;                     // a warp's vectors are neighbours in one row
     const uint32_t lin = threadIdx.y * tpr + tx;
+    const int lane = lin & 31;                       // (a warp may hold several rows)
     // vector v = i tpr + tx of the row (of a tensor whose vector 0 is at element `at` and that has `total` elements), into
     // `part` of the slot's i-th vectors
     auto copy = [&](uint32_t dst, const void* base, bool is32, int64_t at, int64_t total, int v, int n_vec) {

@@ -222,15 +222,17 @@ quant_tc5_kernel(const Quant5Params p, const __grid_constant__ CUtensorMap tmX)
     };
 
     bool ok = true;
+    if (warp != 0) pdl_wait();                       // the bounded waits below count no other kernel's time
     if (warp == 0 || warp == 2) {
         // ------------------------------------------------------------------ producers: weights (0), x (2)
+        // (weights never come from the kernel before this one: the first stages are requested before its end)
         const bool is_w = warp == 0;
         const uint32_t leader = elect_one();
         const uint8_t* src = p.w + ((int64_t)blockIdx.x * p.k_blocks + k_lo) * (4 * BLOCK);
-        if (!is_w) pdl_wait();                       // weights never come from the kernel before this one
         RingPos r = {0, 0};
         int issued = 0;
         for (; issued < n_k; ++issued, r.next(NS)) {
+            if (is_w && issued == NS) pdl_wait();    // (from here on it waits for work that waits for x)
             ok = mbar_wait_bounded(bEmpty + 8 * r.s, r.phase ^ 1, kQ5WaitLimit);
             ok = __all_sync(0xffffffffu, ok);
             if (!ok) break;
@@ -336,7 +338,6 @@ quant_tc5_kernel(const Quant5Params p, const __grid_constant__ CUtensorMap tmX)
             const int m = m0 + c0 + lane;
             xn = k < n_k && c0 + lane < NB && m < p.m ? __ldg(p.x_scale + (int64_t)m * p.x_blocks + k_lo + k) : 0.f;
         };
-        if (F8) pdl_wait();
         if (blocks) fetch_scales(0);
         RingPos rd = {0, 0};
         auto step = [&](int k, uint16_t (&scale)[GPS]) {

@@ -121,3 +121,20 @@ def test_binding_refuses_tensors_that_are_not_on_a_gpu():
         lk.lckv_rms_norm(t, torch.ones(64), torch.zeros(4, 64))
     with pytest.raises(lk.LckvError):
         lk.lckv_quant_pack(torch.zeros(4, 64, dtype=torch.uint8), torch.zeros(4, 1, dtype=torch.bfloat16))
+
+
+def test_rope_tables_refuses_frequencies_outside_fp64():
+    assert tables(rot_dim=4, s=scaling(kind=2, factor=1e-300)) == lk.EINVAL         # the base becomes 0, a frequency infinite
+    assert tables(s=scaling(kind=1, factor=1e-310)) == lk.EINVAL
+    assert tables(s=scaling(amplitude=1e300)) == lk.EINVAL                          # infinite in fp32
+
+
+def test_outputs_apart_from_what_is_read():
+    cos, sin, pos, y = 16 * FAR, 20 * FAR, 24 * FAR, 2 * FAR
+    r = rope(cos=cos, sin=sin)
+    size = 64 * 64 * 4
+    for bad in (cos, cos + size - 256, sin - 128, pos):
+        assert apply(r=r, pos=pos, y=bad) == lk.EINVAL
+    S = 4 * FAR
+    assert linear(xk=1, sc=y + 64 * 2, y=y) == lk.EINVAL
+    assert linear(xk=1, sc=S, st=y + 8, y=y) == lk.EINVAL
