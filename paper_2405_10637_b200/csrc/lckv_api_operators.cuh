@@ -563,7 +563,7 @@ int launch_quant_tc5(const lckv::QuantParams& q, int sms, int32_t* status, cudaS
     auto kernel = lckv::quant_tc5_kernel<F8, ZEROS, GROUP, NBMAX>;
     if (!cuda_ok(cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, 227 * 1024))) return LCKV_ECUDA;
     cfg.gridDim.z = ks;
-    cfg.blockDim = dim3(lckv::q5_threads(NBMAX));
+    cfg.blockDim = dim3(lckv::q5_threads(NBMAX, F8));
     cfg.dynamicSmemBytes = smem;
     cfg.stream = st;
     cudaLaunchAttribute at[2];

@@ -34,8 +34,10 @@ constexpr uint32_t kQ5WaitLimit = 1u << 16;
 constexpr int kQ5MaxStages = 12;
 
 __host__ __device__ constexpr int q5_fold_warps(int NBMAX) { return NBMAX / 8; }     // 32 columns each, by 4 quadrants
-__host__ __device__ constexpr int q5_sets(int NBMAX) { return NBMAX > 32 ? 3 : 4; }   // sets of nibble warps, and A buffers
-__host__ __device__ constexpr int q5_threads(int NBMAX) { return (4 + q5_fold_warps(NBMAX) + 4 * q5_sets(NBMAX)) * 32; }
+// Sets of nibble warps, and A buffers.  In e4m3, with half of the nibbles' instructions, two sets suffice, which leaves the
+// fold warps 72 registers a thread and no spills (512 rows, 4096 x 12288: 92.9 / 89.6 us with three / two).
+__host__ __device__ constexpr int q5_sets(int NBMAX, bool f8) { return NBMAX > 32 ? (f8 ? 2 : 3) : 4; }
+__host__ __device__ constexpr int q5_threads(int NBMAX, bool f8) { return (4 + q5_fold_warps(NBMAX) + 4 * q5_sets(NBMAX, f8)) * 32; }
 __host__ __device__ constexpr int q5_block(int group, bool zeros)      // bytes of 32 features x 128 k
 {
     return kQuantCodes + kQuantK / group * kQuantFeat * (zeros ? 3 : 2);
@@ -155,11 +157,11 @@ struct RingPos {
 };
 
 template <bool F8, bool ZEROS, int GROUP, int NBMAX>
-__global__ void __launch_bounds__(q5_threads(NBMAX), 1)
+__global__ void __launch_bounds__(q5_threads(NBMAX, F8), 1)
 quant_tc5_kernel(const Quant5Params p, const __grid_constant__ CUtensorMap tmX)
 {
     constexpr int BLOCK = q5_block(GROUP, ZEROS), SCALES = kQuantK / GROUP * kQuantFeat * 2, GPS = kQuantK / GROUP;
-    constexpr int FOLD = q5_fold_warps(NBMAX), FOLD0 = 4, DEQ0 = FOLD0 + FOLD, SETS = q5_sets(NBMAX), NBC = 32;
+    constexpr int FOLD = q5_fold_warps(NBMAX), FOLD0 = 4, DEQ0 = FOLD0 + FOLD, SETS = q5_sets(NBMAX, F8), NBC = 32;
     constexpr int A_COLS = F8 ? 32 + (ZEROS ? GPS * 8 : 0) : 64, CONST_COLS = F8 && !ZEROS ? 8 : 0;
     constexpr int TM_NEED = SETS * A_COLS + CONST_COLS + 2 * NBMAX;
     constexpr uint32_t TM_COLS = TM_NEED <= 32 ? 32 : TM_NEED <= 64 ? 64 : TM_NEED <= 128 ? 128 : TM_NEED <= 256 ? 256 : 512;
@@ -330,22 +332,28 @@ quant_tc5_kernel(const Quant5Params p, const __grid_constant__ CUtensorMap tmX)
         };
         fetch_groups(0, sc[0]);
         fetch_groups(1, sc[1]);
-        // one scale of x per row and k block: lane c fetches column c of the next block while this one is folded, and the
-        // warp reads them back from its own corner of shared memory
-        const bool blocks = F8 && p.x_blocks;
-        float xn = 0.f;
-        auto fetch_scales = [&](int k) {
+        // one scale of x per row and k block: lane c fetches column c two blocks ahead, and the warp reads them back from its
+        // own corner of shared memory
+        float xn[2];
+        auto fetch_scales = [&](int k, float& to) {
             const int m = m0 + c0 + lane;
-            xn = k < n_k && c0 + lane < NB && m < p.m ? __ldg(p.x_scale + (int64_t)m * p.x_blocks + k_lo + k) : 0.f;
+            to = k < n_k && c0 + lane < NB && m < p.m ? __ldg(p.x_scale + (int64_t)m * p.x_blocks + k_lo + k) : 0.f;
         };
-        if (blocks) fetch_scales(0);
+        if (F8 && p.x_blocks) {
+            fetch_scales(0, xn[0]);
+            fetch_scales(1, xn[1]);
+        }
+        // D is free once its last columns are in registers, before they are added (512 rows of bf16: 62.9 / 60.6 us; up to 32
+        // rows, and in e4m3, where it costs registers, no gain)
+        constexpr bool EARLY = NBMAX > 32 && !F8;
         RingPos rd = {0, 0};
-        auto step = [&](int k, uint16_t (&scale)[GPS]) {
+        // (`blocks` is a constant of each of its two copies: asked in the inner loop it cost 512 rows in e4m3 88.5 us for 72.1)
+        auto step = [&](const bool blocks, int k, uint16_t (&scale)[GPS], float& xk) {
             const uint32_t xs0 = sXS + (uint32_t)(((warp - FOLD0) * 2 + (k & 1)) * NBC) * 4;
             if (blocks) {
-                asm volatile("st.shared.f32 [%0], %1;" ::"r"(xs0 + lane * 4), "f"(xn) : "memory");
+                asm volatile("st.shared.f32 [%0], %1;" ::"r"(xs0 + lane * 4), "f"(xk) : "memory");
                 __syncwarp();
-                fetch_scales(k + 1);
+                fetch_scales(k + 2, xk);
             }
 #pragma unroll
             for (int gl = 0; gl < GPS; ++gl, rd.next(2)) {
@@ -357,12 +365,21 @@ quant_tc5_kernel(const Quant5Params p, const __grid_constant__ CUtensorMap tmX)
                 if (!ok) return;
                 tc5_fence_after();
                 const uint32_t d = dl + rd.s * NBMAX;
+                auto free_d = [&] {
+                    tc5_fence_before();
+                    __syncwarp();
+                    if (lane == 0) mbar_arrive(bDEmpty + 8 * rd.s);
+                };
 #pragma unroll
                 for (int c = 0; c < NBC; c += 16) {
                     float v[16];
-                    if (c0 + c >= NB) break;
+                    if (c0 + c >= NB) {
+                        if (EARLY && c + 16 == NBC) free_d();
+                        continue;
+                    }
                     tmem_ld16_nowait(d + c, v);
                     tmem_ld_wait();
+                    if (EARLY && c + 16 == NBC) free_d();
 #pragma unroll
                     for (int j = 0; j < 16; j += 4) {
                         uint64_t fa = f2, fb = f2;
@@ -375,16 +392,18 @@ quant_tc5_kernel(const Quant5Params p, const __grid_constant__ CUtensorMap tmX)
                         acc[(c + j) / 2 + 1] = ffma2(fb, pack_f32x2(v[j + 2], v[j + 3]), acc[(c + j) / 2 + 1]);
                     }
                 }
-                tc5_fence_before();
-                __syncwarp();
-                if (lane == 0) mbar_arrive(bDEmpty + 8 * rd.s);
+                if (!EARLY) free_d();
             }
             fetch_groups(k + 2, scale);
         };
-        for (int k = 0; k < n_k && ok; k += 2) {
-            step(k, sc[0]);
-            if (k + 1 < n_k && ok) step(k + 1, sc[1]);
-        }
+        auto steps = [&](const bool blocks) {
+            for (int k = 0; k < n_k && ok; k += 2) {
+                step(blocks, k, sc[0], xn[0]);
+                if (k + 1 < n_k && ok) step(blocks, k + 1, sc[1], xn[1]);
+            }
+        };
+        if (F8 && p.x_blocks) steps(true);
+        else steps(false);
         finish(ok);
         // the block's stages become its result, [column][feature] in fp32
         uint32_t bad;
