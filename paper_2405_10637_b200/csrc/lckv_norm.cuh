@@ -171,7 +171,7 @@ __device__ __forceinline__ void norm_st(void* base, int is32, int64_t e, float v
 
 // The types of a call, read from its parameters (one kernel for all, for few rows) or fixed at compile time (one kernel
 // each, for many: with the types looked up per vector a row of 4096 took 400 instructions of a warp's 16 elements per
-// lane, and the kernel was bound by their issue: 16384 rows 59 us, 46 us with them fixed).
+// lane, and the kernel was bound by their issue: 16384 rows 59 us, 43 us with them fixed).
 struct NormAnyTypes {
     const NormParams& p;
     __device__ __forceinline__ int x32() const { return p.x32; }
