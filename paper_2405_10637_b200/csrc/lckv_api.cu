@@ -468,7 +468,8 @@ int launch_append(lckv_cache* c, int slot, const void* k_new, const void* v_new,
 
 int launch_advance(lckv_cache* c, int batch, cudaStream_t st, int by = 1)
 {
-    lckv::advance_kernel<<<(batch + 255) / 256, 256, 0, st>>>(c->d_lens, batch, by);
+    if (by == 1) lckv::advance_kernel<<<(batch + 255) / 256, 256, 0, st>>>(c->d_lens, batch);
+    else lckv::advance_by_kernel<<<(batch + 255) / 256, 256, 0, st>>>(c->d_lens, batch, by);
     return cuda_ok(cudaGetLastError()) ? LCKV_OK : LCKV_ECUDA;
 }
 

@@ -222,14 +222,6 @@ __device__ __forceinline__ uint32_t pack_bf16x2(float lo, float hi)
     return f32_to_bf16_bits(lo) | (f32_to_bf16_bits(hi) << 16);
 }
 
-// {lo, hi} -> packed bf16x2 (round to nearest even), lo in the low half.
-__device__ __forceinline__ uint32_t cvt_bf16x2(float lo, float hi)
-{
-    uint32_t d;
-    asm("cvt.rn.bf16x2.f32 %0, %1, %2;" : "=r"(d) : "f"(hi), "f"(lo));
-    return d;
-}
-
 // Shared-memory accesses by 32-bit shared-window address.
 __device__ __forceinline__ uint4 lds128(uint32_t addr)
 {

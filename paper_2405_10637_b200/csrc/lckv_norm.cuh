@@ -14,7 +14,7 @@
 //
 // Other strides and alignments (norm_any_kernel) go element by element, staged in shared memory as fp32.
 #pragma once
-#include "lckv_device.cuh"
+#include "lckv_attn_mma.cuh"      // cvt_bf16x2
 
 namespace lckv {
 

@@ -17,7 +17,7 @@
 // shared memory, and the thread serves more heads, since its factors are 16 separate loads (kRopeAnySize).
 // Tensors off the 16-byte grid go pair by pair (kRopePairs).
 #pragma once
-#include "lckv_device.cuh"
+#include "lckv_attn_mma.cuh"      // cvt_bf16x2
 
 namespace lckv {
 
@@ -432,6 +432,13 @@ __global__ void __launch_bounds__(kRopeThreads, PATH == kRopeAnySize ? 3 : 1) ro
             hi[j].store(dst[j] + un.e1);
         }
     }
+}
+
+// The lengths after an append of several tokens (of one: advance_kernel).
+__global__ void advance_by_kernel(int32_t* __restrict__ lens, int B, int by)
+{
+    const int b = blockIdx.x * blockDim.x + threadIdx.x;
+    if (b < B) lens[b] += by;
 }
 
 // cos and sin of p * theta_j for p < positions.  `turns` holds theta_j / (2 pi) modulo 1 in units of 2^-64: the angle of

@@ -134,10 +134,10 @@ __global__ void append_kernel(uint16_t* __restrict__ K, uint16_t* __restrict__ V
     *reinterpret_cast<uint4*>(V + dst) = *reinterpret_cast<const uint4*>(v_new + src);
 }
 
-__global__ void advance_kernel(int32_t* __restrict__ lens, int B, int by)
+__global__ void advance_kernel(int32_t* __restrict__ lens, int B)
 {
     const int b = blockIdx.x * blockDim.x + threadIdx.x;
-    if (b < B) lens[b] += by;
+    if (b < B) lens[b] += 1;
 }
 
 }  // namespace lckv
