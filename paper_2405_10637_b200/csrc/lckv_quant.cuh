@@ -4,12 +4,12 @@
 //
 // Bound by the bytes of the codes: 2 m multiply-adds per half byte, and close behind by the integer instructions that
 // turn nibbles into numbers.  The operands are swapped so that 16 output features are the rows of an MMA tile and up to
-// 8 rows of x its columns, and the codes enter the tensor cores in the form that costs fewest instructions:
-//   x in bf16: 16 + c, a nibble or'ed into the upper mantissa bits of 16.0 (7 instructions per 8 codes, m16n8k16);
-//   x in e4m3: c / 512, which is what a byte with c in its low half reads as in e4m3: its smallest numbers and the first
-//              binade above them are one even scale (4 instructions per 8 codes, m16n8k32, x as it lies in memory).
-// Both are exact.  A tile of ones gives the sums of x beside them, so that a group's
-//     sum x (c - z) = sum x (16 + c) - (16 + z) sum x = 512 (sum x (c / 512) - z sum x / 512)
+// 8 rows of x its columns, and the codes enter the tensor cores as 16 + c, a nibble or'ed into the upper mantissa bits of
+// 16.0 (7 or 8 instructions per 8 codes): in bf16 for x in bf16, in fp16 for x in e4m3, which is converted when it is loaded.
+// All three are exact.  (mma.sync on e4m3 itself, with c / 512 as an e4m3 byte, needs fewer instructions of the program, but the
+// counters showed two tensor instructions per MMA and a dozen others beside them: 16 rows, 4096 x 22016 features, groups of 64
+// 22.7 us, this 20.7.)  A tile of ones gives the sums of x, so that a group's
+//     sum x (c - z) = sum x (16 + c) - (16 + z) sum x
 // costs one multiply-add per group where subtracting z from every weight would cost one instruction per two
 // weights.  Products are exact, sums fp32, scales and zero points are applied in fp32; the terms are at most 4 times
 // as large as those of x (c - z) with z = 8, which costs two of fp32's bits and none of the output's.
@@ -112,14 +112,14 @@ struct QuantParams {
     int32_t k_split;         // thread blocks of a cluster that share the k range
 };
 
-// c (+)= a b, m16n8k16 in bf16 or m16n8k32 in e4m3; FIRST starts from zero
+// c (+)= a b, m16n8k16 in bf16 or fp16; FIRST starts from zero
 template <bool F8, bool FIRST>
 __device__ __forceinline__ void quant_mma(float (&c)[4], const uint32_t (&a)[4], uint32_t b0, uint32_t b1)
 {
     if (FIRST) c[0] = c[1] = c[2] = c[3] = 0.f;
     float d0, d1, d2, d3;
     if (F8)
-        asm("mma.sync.aligned.m16n8k32.row.col.f32.e4m3.e4m3.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%10,%11,%12,%13};"
+        asm("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%10,%11,%12,%13};"
             : "=f"(d0), "=f"(d1), "=f"(d2), "=f"(d3)
             : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1), "f"(c[0]), "f"(c[1]), "f"(c[2]), "f"(c[3]));
     else
@@ -172,11 +172,14 @@ template <> struct QuantX<true> {
             if (s < 2 ? in : in2) v[s] = __ldg(reinterpret_cast<const uint32_t*>(p + s * 16));
         }
     }
-    // k32 step S of the half, k in the order of the codes
+    // k16 step S of the half, in fp16
     template <int S> __device__ __forceinline__ void frag(uint32_t& b0, uint32_t& b1) const
     {
-        b0 = __byte_perm(v[2 * S], 0, 0x3120);
-        b1 = __byte_perm(v[2 * S + 1], 0, 0x3120);
+        asm("{\n\t.reg .b16 lo, hi;\n\t"
+            "mov.b32 {lo, hi}, %2;\n\t"
+            "cvt.rn.f16x2.e4m3x2 %0, lo;\n\t"
+            "cvt.rn.f16x2.e4m3x2 %1, hi;\n\t}"
+            : "=r"(b0), "=r"(b1) : "r"(v[S]));
     }
 };
 
@@ -194,48 +197,31 @@ __device__ __forceinline__ uint32_t and_or(uint32_t a, uint32_t mask, uint32_t b
 template <bool F8, int FT, int NT, int SECOND, bool FIRST>
 __device__ __forceinline__ void quant_32k(float (&grp)[FT][NT][4], float (&sum)[NT][4], const uint4 (&c)[FT], const QuantX<F8> (&x)[NT])
 {
-    if constexpr (F8) {
-        const uint32_t ones[4] = {0x01010101u, 0x01010101u, 0x01010101u, 0x01010101u};     // 1 / 512, as a code of 1
+    constexpr uint32_t ONE = F8 ? 0x3c003c00u : 0x3f803f80u, MASK = F8 ? 0x03c003c0u : 0x00780078u, SIXTEEN = F8 ? 0x4c004c00u : 0x41804180u;
+    const uint32_t ones[4] = {ONE, ONE, ONE, ONE};
+#pragma unroll
+    for (int s = 0; s < 2; ++s) {
         uint32_t b[NT][2];
 #pragma unroll
         for (int j = 0; j < NT; ++j) {
-            x[j].template frag<SECOND>(b[j][0], b[j][1]);
-            quant_mma<true, FIRST>(sum[j], ones, b[j][0], b[j][1]);
+            if (s == 0) x[j].template frag<SECOND * 2>(b[j][0], b[j][1]);
+            else x[j].template frag<SECOND * 2 + 1>(b[j][0], b[j][1]);
+            if (s == 0) quant_mma<F8, FIRST>(sum[j], ones, b[j][0], b[j][1]);
+            else quant_mma<F8, false>(sum[j], ones, b[j][0], b[j][1]);
         }
 #pragma unroll
         for (int i = 0; i < FT; ++i) {
             const uint32_t w0 = SECOND ? c[i].z : c[i].x, w1 = SECOND ? c[i].w : c[i].y;     // features g and g + 8
-            const uint32_t a[4] = {__funnelshift_r(w0, w0, 3) & 0x0f0f0f0fu, __funnelshift_r(w1, w1, 3) & 0x0f0f0f0fu,
-                                   __funnelshift_r(w0, w0, 7) & 0x0f0f0f0fu, __funnelshift_r(w1, w1, 7) & 0x0f0f0f0fu};
+            uint32_t a[4];
 #pragma unroll
-            for (int j = 0; j < NT; ++j) quant_mma<true, FIRST>(grp[i][j], a, b[j][0], b[j][1]);
-        }
-    } else {
-        const uint32_t ones[4] = {0x3f803f80u, 0x3f803f80u, 0x3f803f80u, 0x3f803f80u};
-#pragma unroll
-        for (int s = 0; s < 2; ++s) {
-            uint32_t b[NT][2];
-#pragma unroll
-            for (int j = 0; j < NT; ++j) {
-                if (s == 0) x[j].template frag<SECOND * 2>(b[j][0], b[j][1]);
-                else x[j].template frag<SECOND * 2 + 1>(b[j][0], b[j][1]);
-                if (s == 0) quant_mma<false, FIRST>(sum[j], ones, b[j][0], b[j][1]);
-                else quant_mma<false, false>(sum[j], ones, b[j][0], b[j][1]);
+            for (int r = 0; r < 4; ++r) {
+                const uint32_t w = r & 1 ? w1 : w0;
+                a[r] = and_or(__funnelshift_r(w, w, (4 * (s + (r & 2)) + (F8 ? 29 : 0)) & 31), MASK, SIXTEEN);
             }
 #pragma unroll
-            for (int i = 0; i < FT; ++i) {
-                const uint32_t w0 = SECOND ? c[i].z : c[i].x, w1 = SECOND ? c[i].w : c[i].y;
-                uint32_t a[4];
-#pragma unroll
-                for (int r = 0; r < 4; ++r) {
-                    const uint32_t w = r & 1 ? w1 : w0;
-                    a[r] = and_or(__funnelshift_r(w, w, 4 * (s + (r & 2))), 0x00780078u, 0x41804180u);
-                }
-#pragma unroll
-                for (int j = 0; j < NT; ++j) {
-                    if (s == 0) quant_mma<false, FIRST>(grp[i][j], a, b[j][0], b[j][1]);
-                    else quant_mma<false, false>(grp[i][j], a, b[j][0], b[j][1]);
-                }
+            for (int j = 0; j < NT; ++j) {
+                if (s == 0) quant_mma<F8, FIRST>(grp[i][j], a, b[j][0], b[j][1]);
+                else quant_mma<F8, false>(grp[i][j], a, b[j][0], b[j][1]);
             }
         }
     }
@@ -353,12 +339,10 @@ __global__ void __launch_bounds__(quant_warps(NT) * 32, quant_ctas(FT, NT)) quan
                 for (int i = 0; i < 2; ++i)
 #pragma unroll
                     for (int hi = 0; hi < 2; ++hi) {
-                        float f = hi ? bf16hi(sw[i]) : bf16lo(sw[i]);
-                        if (F8) f *= 512.f;
-                        float zp = 24.f;             // 16 + z: bytes 0, 0, the stored one, 0x41
-                        if (ZEROS) zp = __uint_as_float(__byte_perm(z, 0x41000000u, 0x7044u | (uint32_t)((i * 2 + hi) << 8)));
-                        if (F8) zp -= 16.f;
-                        const uint64_t f2 = pack_f32x2(f, f), z2 = pack_f32x2(-zp, -zp);
+                        const float f = hi ? bf16hi(sw[i]) : bf16lo(sw[i]);
+                        float zp = -24.f;            // -(16 + z): bytes 0, 0, the stored one, 0xc1
+                        if (ZEROS) zp = __uint_as_float(__byte_perm(z, 0xc1000000u, 0x7044u | (uint32_t)((i * 2 + hi) << 8)));
+                        const uint64_t f2 = pack_f32x2(f, f), z2 = pack_f32x2(zp, zp);
 #pragma unroll
                         for (int j = 0; j < NT; ++j) {
                             const uint64_t v = ffma2(z2, pack_f32x2(sum[j][0], sum[j][1]),
