@@ -65,18 +65,28 @@ int rope_heads(int path, int hp, int64_t tokens, int heads, int d, int sms)
     return (int)std::max<int64_t>(4, std::min<int64_t>(fit, heads) / 4 * 4);
 }
 
-dim3 rope_grid(int64_t tokens, int heads, int d, int path, int hp, lckv::RopeGrid* g)
+// A token takes `per` threads.  Blocks of 256, or of up to 384 where 256 would leave a fifth of them idle and there are many
+// tokens: 96 heads of 128, four a thread, make 192 (32768 tokens 248 us, with one token in 256 threads 259; 16384 tokens of
+// 32768 places 136, 145: a block whose tokens lie behind their prompts costs a nanosecond).
+dim3 rope_grid(int64_t tokens, int heads, int d, int path, int hp, lckv::RopeGrid* g, dim3* block)
 {
     const int units = lckv::rope_units(path, d);             // a power of two, as d is
     g->hg = (heads + hp - 1) / hp;
     g->units_shift = 0;
     while ((1 << g->units_shift) < units) ++g->units_shift;
     g->per = (uint32_t)(g->hg * units);
-    g->inv = (65536 + g->per - 1) / g->per;
+    g->inv = ((1u << 20) + g->per - 1) / g->per;
+    g->tb = 0;
+    *block = dim3(lckv::kRopeThreads);
     if (g->per >= (uint32_t)lckv::kRopeThreads)
         return dim3((unsigned)tokens, (g->per + lckv::kRopeThreads - 1) / lckv::kRopeThreads);
-    const int64_t tb = lckv::kRopeThreads / g->per;
-    return dim3((unsigned)((tokens + tb - 1) / tb));
+    g->tb = lckv::kRopeThreads / g->per;
+    const uint32_t more = lckv::kRopeMostThreads / g->per;
+    if (path != lckv::kRopeAnySize && tokens >= (1 << 14) && g->tb * g->per * 5 < (uint32_t)lckv::kRopeThreads * 4 && more > g->tb) {
+        g->tb = more;
+        *block = dim3((more * g->per + 31) / 32 * 32);
+    }
+    return dim3((unsigned)((tokens + g->tb - 1) / g->tb));
 }
 
 template <typename T>
@@ -181,7 +191,8 @@ int rope_into_cache(lckv_cache* c, int slot, const lckv_rope_t* rope, const void
     const int heads = hq + 2 * hkv;
     const int hp = vec && rope_many(tokens * heads * (d / 16), sms) ? 4 : 1;
     p.hp = rope_heads(path, hp, tokens, heads, d, sms);
-    const dim3 grid = rope_grid(tokens, heads, d, path, p.hp, &p.g), block(lckv::kRopeThreads);
+    dim3 block;
+    const dim3 grid = rope_grid(tokens, heads, d, path, p.hp, &p.g, &block);
     const auto kernel = path == lckv::kRopePairs   ? lckv::rope_append_kernel<lckv::kRopePairs, 1>
                         : path == lckv::kRopeUnits ? (hp == 4 ? lckv::rope_append_kernel<lckv::kRopeUnits, 4> : lckv::rope_append_kernel<lckv::kRopeUnits, 1>)
                                                    : (hp == 4 ? lckv::rope_append_kernel<lckv::kRopeAnySize, 4> : lckv::rope_append_kernel<lckv::kRopeAnySize, 1>);
@@ -378,7 +389,8 @@ int lckv_rope_apply(const lckv_rope_t* rope, const int32_t* positions, const voi
     const int path = !vec ? lckv::kRopePairs : rope_tables_vector(rope) ? lckv::kRopeUnits : lckv::kRopeAnySize;
     const int hp = vec && rope_many((int64_t)n_tokens * n_heads * (head_dim / 16), sms) ? 4 : 1;
     p.hp = rope_heads(path, hp, n_tokens, n_heads, head_dim, sms);
-    const dim3 grid = rope_grid(n_tokens, n_heads, head_dim, path, p.hp, &p.g), block(lckv::kRopeThreads);
+    dim3 block;
+    const dim3 grid = rope_grid(n_tokens, n_heads, head_dim, path, p.hp, &p.g, &block);
     const cudaError_t e = launch_pdl_dims(dtype ? rope_apply_variant<float>(path, hp) : rope_apply_variant<uint16_t>(path, hp), grid, block, 0, st, p);
     return cuda_ok(e) ? LCKV_OK : LCKV_ECUDA;
 }

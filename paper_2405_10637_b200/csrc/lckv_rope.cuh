@@ -22,6 +22,7 @@
 namespace lckv {
 
 constexpr int kRopeThreads = 256;
+constexpr int kRopeMostThreads = 384;  // of a block that holds several tokens
 enum RopePath { kRopeUnits, kRopeAnySize, kRopePairs };
 constexpr int kRopeMaxPairs = 64;      // rot_dim <= 128 = the largest head
 constexpr int kStatusCapacity = 2;     // a row of a replayed append had no place in the cache
@@ -35,7 +36,7 @@ struct RopeArgs {
 };
 
 struct RopeGrid {
-    uint32_t per, inv;
+    uint32_t per, inv, tb;
     int32_t hg, units_shift;
 };
 
@@ -252,24 +253,24 @@ __device__ __forceinline__ void rope_pair(const RopeArgs& r, int u, int pos, con
 
 __host__ __device__ constexpr int rope_units(int path, int d) { return path == kRopeUnits ? d / 16 : path == kRopeAnySize ? d / 8 : d / 2; }
 
-// The thread's place: token `t`, unit `u`, first head `h0` (further heads at steps of `hg`).  A block holds 256 / per tokens
-// of per = units * head groups threads, or a 256-thread part (grid.y) of one token.  The host does the divisions
-// (a one-token launch took 0.15 us longer with them here): `inv` = ceil(2^16 / per), with which thread * inv / 2^16 is
-// thread / per for all threads below 256.
+// The thread's place: token `t`, unit `u`, first head `h0` (further heads at steps of `hg`).  A block holds `tb` tokens
+// of per = units * head groups threads, or a 256-thread part (grid.y) of one token (tb = 0).  The host does the divisions
+// (a one-token launch took 0.15 us longer with them here): `inv` = ceil(2^20 / per), with which thread * inv / 2^20 is
+// thread / per for all threads below 384.
 struct RopePlace { int t, u, h0; bool ok; };
 __device__ __forceinline__ RopePlace rope_place(const RopeGrid& g, int tokens)
 {
     RopePlace w;
     uint32_t r;
-    if (g.per >= (uint32_t)kRopeThreads) {
+    if (g.tb == 0) {
         r = blockIdx.y * kRopeThreads + threadIdx.x;
         w.t = blockIdx.x;
         w.ok = r < g.per;
     } else {
-        const uint32_t tb = (kRopeThreads * g.inv) >> 16, tl = (threadIdx.x * g.inv) >> 16;
+        const uint32_t tl = (threadIdx.x * g.inv) >> 20;
         r = threadIdx.x - tl * g.per;
-        const int64_t t = (int64_t)blockIdx.x * tb + tl;
-        w.ok = tl < tb && t < tokens;
+        const int64_t t = (int64_t)blockIdx.x * g.tb + tl;
+        w.ok = tl < g.tb && t < tokens;
         w.t = (int)t;
     }
     w.h0 = (int)(r >> g.units_shift);
@@ -278,7 +279,7 @@ __device__ __forceinline__ RopePlace rope_place(const RopeGrid& g, int tokens)
 }
 
 template <typename T, int PATH, int HP>
-__global__ void __launch_bounds__(kRopeThreads) rope_apply_kernel(const RopeApplyParams p)
+__global__ void __launch_bounds__(PATH == kRopeAnySize ? kRopeThreads : kRopeMostThreads) rope_apply_kernel(const RopeApplyParams p)
 {
     __shared__ float sh[PATH == kRopeAnySize ? kRopeThreads * 8 : 1];
     pdl_wait_then_release();
@@ -339,7 +340,7 @@ __global__ void __launch_bounds__(kRopeThreads) rope_apply_kernel(const RopeAppl
 // Heads 0 .. hq-1 of a token are its query heads (rotated, to q_out), the next hkv its keys (rotated, to
 // the row), the last hkv its values (copied to the row).
 template <int PATH, int HP>
-__global__ void __launch_bounds__(kRopeThreads, PATH == kRopeAnySize ? 3 : 1) rope_append_kernel(const RopeAppendParams p)
+__global__ void __launch_bounds__(PATH == kRopeAnySize ? kRopeThreads : kRopeMostThreads, PATH == kRopeAnySize ? 3 : 1) rope_append_kernel(const RopeAppendParams p)
 {
     __shared__ float sh[PATH == kRopeAnySize ? kRopeThreads * 8 : 1];
     pdl_wait_then_release();

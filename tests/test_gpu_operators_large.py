@@ -105,6 +105,48 @@ def test_rotated_append_many_tokens(interleaved, rot, prompt, page_rows):
     c.close()
 
 
+@pytest.mark.parametrize("Hq,Hkv,d", [(64, 16, 64), (32, 32, 128), (7, 7, 64)])
+def test_long_ragged_prompts(Hq, Hkv, d):
+    """Thread blocks that hold several tokens, of different prompts and behind their ends."""
+    lens, n = [3301, 0, 1, 1650, 3300], 3301
+    cfg = lk.make_config(2, 0, Hq, Hkv, d, len(lens), 3328, page_rows=64, n_pages=52 * len(lens))
+    c = lk.Cache(cfg)
+    c.lckv_cache_reset(lens)
+    g = gen(12)
+    cos, sin = (t.float() for t in tables64(d, n))
+    rope = lk.make_rope(cos, sin)
+    q, k, v = fused(g, len(lens), n, Hq, Hkv, d)
+    out = torch.full((len(lens), n, Hq, d), 3.0, dtype=torch.bfloat16, device=DEV)
+    c.lckv_rope_prefill_write_kv(0, rope, q, k, v, out)
+    kt, vt = c.slot_tensors(0)
+    table = c.lckv_cache_page_table().to(DEV)
+    for b, m in enumerate(lens):
+        assert bool((out[b, m:] == 3.0).all())
+        if m == 0:
+            continue
+        want, mag = rotate64(q[b, :m], cos[:m], sin[:m], d, False)
+        within(out[b, :m], want, 3 * E * mag * (1 + 2.0 ** -8) + 2.0 ** -8 * want.abs(), "q")
+        row = torch.arange(m, device=DEV)
+        page, at = table[b, row // 64], row % 64
+        want, mag = rotate64(k[b, :m], cos[:m], sin[:m], d, False)
+        within(kt[page, :, at], want, 3 * E * mag * (1 + 2.0 ** -8) + 2.0 ** -8 * want.abs(), "k")
+        assert torch.equal(vt[page, :, at], v[b, :m])
+    assert c.lckv_cache_status() == 0
+    c.close()
+
+
+@pytest.mark.parametrize("heads,d", [(96, 64), (44, 128), (11, 128)])
+def test_rotation_many_tokens(heads, d):
+    g = gen(13)
+    tokens = 16500
+    cos, sin = (t.float() for t in tables64(d, 999))
+    x = randn(g, tokens, heads, d)
+    pos = torch.randint(0, 999, (tokens,), generator=g, device=DEV, dtype=torch.int32)
+    y = lk.lckv_rope_apply(lk.make_rope(cos, sin), pos, x)
+    want, mag = rotate64(x, cos[pos.long()], sin[pos.long()], d, False)
+    within(y, want, 3 * E * mag * (1 + 2.0 ** -8) + 2.0 ** -8 * want.abs())
+
+
 @pytest.mark.parametrize("kind", ["bf16", "row", "block"])
 @pytest.mark.parametrize("n,k,group,has_zeros", [(9001, 288, 32, True), (20000, 640, 128, False), (2561, 4096, 64, True)])
 def test_quant_linear_many_features(n, k, group, has_zeros, kind):
