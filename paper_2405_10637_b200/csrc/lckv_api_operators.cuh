@@ -258,6 +258,11 @@ cudaError_t norm_ring(const lckv::NormParams& p, const NormShape& g, cudaStream_
     return !p.r ? norm_ring_out<NV, EDGES, 0, 0>(p, g, st) : !p.r32 ? norm_ring_out<NV, EDGES, 0, 1>(p, g, st) : norm_ring_out<NV, EDGES, 0, 2>(p, g, st);
 }
 
+// Vectors that a thread of the largest kernel holds: eight, of a row of up to 512 x 8.  A row of 32762 or more elements that shares its
+// first and last vector with its neighbours can touch 4097.
+constexpr int kNormMostVectors = 8;
+bool norm_row_fits(int n_vec) { return n_vec <= 512 * kNormMostVectors; }
+
 // Few rows (up to one per SM): one vector per thread, the shortest chain.  More: the ring, two vectors per thread
 // (a thread block of 256 threads serves a row of 4096), four where a row has more than 1024 vectors.  Not the ring
 // where fp32 tensors make the bytes and not the instructions the bound and rows are short: 2^26 elements, ring / one row
@@ -284,6 +289,7 @@ cudaError_t norm_launch(const lckv::NormParams& p, int n_vec, bool edges, int sm
     }
     int nv = many && n_vec >= 64 ? 2 : 1;
     while ((n_vec + nv - 1) / nv > (nv == 1 ? 1024 : 512)) nv *= 2;
+    if (nv > kNormMostVectors) return cudaErrorInvalidValue;         // (the caller sends no such row here)
     const int tpr = norm_threads(n_vec, nv, p.group != 0), rpb = tpr <= 32 ? 128 / tpr : 1;
     const auto kernel = !edges ? (nv == 1   ? lckv::norm_vec_kernel<1, 1024, false>
                                   : nv == 2 ? lckv::norm_vec_kernel<2, 512, false> : nv == 4 ? lckv::norm_vec_kernel<4, 512, false> : lckv::norm_vec_kernel<8, 512, false>)
@@ -466,12 +472,12 @@ int lckv_rms_norm(const void* x, int64_t x_stride, int32_t x_dtype, const void* 
     cudaStream_t st = static_cast<cudaStream_t>(stream);
     const bool grid16 = aligned(x, 16) && aligned(residual, 16) && aligned(residual_out, 16) && aligned(y, y_kind == 2 ? 8 : 16);
     const bool even = grid16 && width % 8 == 0 && x_stride % 8 == 0 && aligned(weight, 16);
-    const bool edges = grid16 && !even && x_stride == width && !scale_group;
+    const int n_vec = (width + (even ? 7 : 14)) / 8;
+    const bool edges = grid16 && !even && x_stride == width && !scale_group && norm_row_fits(n_vec);
     cudaError_t e;
     if (even || edges) {
         int sms = 0;
         if (int rc = device_sm_count(&sms)) return rc;
-        const int n_vec = (width + (edges ? 14 : 7)) / 8;
         e = norm_launch(p, n_vec, edges, sms, st);
     } else {
         const size_t smem = (size_t)width * 4;

@@ -12,7 +12,8 @@
 // Rows whose width is not a multiple of 8 (EDGES): the vectors lie on the tensor's own 16-byte grid, and only those at
 // the two ends of a row, which it shares with its neighbours, go element by element; so do the weights.
 //
-// Other strides and alignments (norm_any_kernel) go element by element, staged in shared memory as fp32.
+// Other strides and alignments, and such rows of more than 4096 vectors, go element by element, staged in shared memory as
+// fp32 (norm_any_kernel).
 #pragma once
 #include "lckv_attn_mma.cuh"      // cvt_bf16x2
 
