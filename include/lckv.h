@@ -494,8 +494,9 @@ int lckv_rope_apply(const lckv_rope_t* rope, const int32_t* positions, const voi
  * a sink + recent-window cache), ECAPACITY (some len[b] + n_new > T_cap, or no page left; nothing written),
  * ECUDA.  While `stream` is capturing, the call is refused with EINVAL if advance_len != 0 (the library's
  * lengths could not follow the replays) or if new pages are needed (make room with an eager call first).  A replay
- * uses the lengths it finds on the device; a row that has no place there is not written and lckv_cache_status
- * then reports LCKV_ECAPACITY.
+ * uses the lengths it finds on the device; a row that has no place there is not written, of a token whose position
+ * lies behind the tables nothing is written (neither its row nor its part of q_out), and lckv_cache_status then
+ * reports LCKV_ECAPACITY.
  */
 int lckv_rope_append_kv(lckv_cache_t* cache, int32_t slot, const lckv_rope_t* rope, const void* q,
                         int64_t q_stride, void* q_out, const void* k_new, const void* v_new,
@@ -505,8 +506,8 @@ int lckv_rope_append_kv(lckv_cache_t* cache, int32_t slot, const lckv_rope_t* ro
 /*
  * The same for prompts, beside lckv_prefill_write_kv: lengths already hold the prompt lengths and do not
  * change; tokens i < len[b] (of n_max per sequence) are at position i and go to row i.  Rows of q_out and of
- * the slot behind a prompt are left as they were.  Errors: EINVAL (as above, and as lckv_prefill_write_kv),
- * ECUDA.
+ * the slot behind a prompt are left as they were.  Replays as above.  Errors: EINVAL (as above, and as
+ * lckv_prefill_write_kv), ECUDA.
  */
 int lckv_rope_prefill_write_kv(lckv_cache_t* cache, int32_t slot, const lckv_rope_t* rope, const void* q,
                                int64_t q_stride, void* q_out, const void* k, const void* v,

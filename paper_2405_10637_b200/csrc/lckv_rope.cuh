@@ -25,7 +25,7 @@ constexpr int kRopeThreads = 256;
 constexpr int kRopeMostThreads = 384;  // of a block that holds several tokens
 enum RopePath { kRopeUnits, kRopeAnySize, kRopePairs };
 constexpr int kRopeMaxPairs = 64;      // rot_dim <= 128 = the largest head
-constexpr int kStatusCapacity = 2;     // a row of a replayed append had no place in the cache
+constexpr int kStatusCapacity = 2;     // a token of a replayed append had no place in the cache or no position in the tables
 
 struct RopeArgs {
     const float* cos;                  // [positions, half]
@@ -354,7 +354,15 @@ __global__ void __launch_bounds__(PATH == kRopeAnySize ? kRopeThreads : kRopeMos
         if (PATH != kRopeAnySize) return;
         w.ok = false;
     }
-    const int pos = p.prompt ? i : len + i;
+    // The host refuses calls without a position in the tables or without a row; a graph that replays one finds the lengths on
+    // the device.  A token without a position is left out whole, one without a row loses its key and value.
+    const int64_t at = p.prompt ? i : (int64_t)len + i;
+    if (w.ok && (at < 0 || at >= p.r.positions)) {
+        if (w.h0 == 0 && w.u == 0) atomicExch(p.status, kStatusCapacity);
+        if (PATH != kRopeAnySize) return;
+        w.ok = false;
+    }
+    const int pos = (int)at;
     // the row: ring position in a sink + recent-window cache, page look-up in a paged one
     int64_t row = pos;
     if (p.n_sink > 0 && row >= p.T_cap) row = p.n_sink + (row - p.n_sink) % (p.T_cap - p.n_sink);
@@ -368,7 +376,6 @@ __global__ void __launch_bounds__(PATH == kRopeAnySize ? kRopeThreads : kRopeMos
     } else {
         row0 = (int64_t)b * p.hkv * p.T_cap + row;
     }
-    // the host refuses calls without room; a graph that replays one finds the lengths on the device
     if (!place && w.ok && p.hkv > 0 && w.h0 == 0 && w.u == 0) atomicExch(p.status, kStatusCapacity);
     // where head h of the token is read and written, and whether it is rotated; false: nowhere
     auto where = [&](int h, const uint16_t*& src, uint16_t*& dst, bool& turn) {

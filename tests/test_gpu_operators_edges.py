@@ -5,7 +5,7 @@ import torch
 
 from paper_2405_10637_b200 import binding as lk
 
-from test_gpu_operators import DEV, E, HALF, check_norm, gen, norm64, randn, within
+from test_gpu_operators import DEV, E, HALF, check_norm, gen, norm64, randn, tables64, within
 
 pytestmark = pytest.mark.gpu
 
@@ -33,3 +33,108 @@ def test_norm_widest_rows(width, shift, out):
         check_norm(y, scale, y64, group)
         if res:
             within(h, h64, h64.abs() * (HALF[h.dtype] + E) * (1 + E))
+
+
+# ---- replays of a rotated append -------------------------------------------------------------------------------------------
+
+
+SHORT = 8                              # positions of the tables
+
+
+def replayed(c, g, lens, n, rot, interleaved, with_kv, prompt, aligned):
+    """Captures a call with tables of SHORT positions at lengths that fit, replays it at `lens`, and compares with an eager call
+    that has longer tables: tokens with a position are the same, of the others nothing is written."""
+    B, (Hq, Hkv, d) = len(lens), c.heads
+    cos, sin = (t.float() for t in tables64(rot, 64))
+    rope, short = lk.make_rope(cos, sin, interleaved), lk.make_rope(cos[:SHORT].contiguous(), sin[:SHORT].contiguous(), interleaved)
+    flat = randn(g, B * n * (Hq + 2 * Hkv) * d + 8)[0 if aligned else 1:][:B * n * (Hq + 2 * Hkv) * d]
+    flat = flat.view(B, n, Hq + 2 * Hkv, d)
+    q, k, v = flat[:, :, :Hq], flat[:, :, Hq:Hq + Hkv], flat[:, :, Hq + Hkv:]
+    if not with_kv:
+        k = v = None
+
+    def call(r, out):
+        if prompt:
+            c.lckv_rope_prefill_write_kv(0, r, q, k, v, out)
+        else:
+            c.lckv_rope_append_kv(0, r, q, k, v, out)
+
+    pools = c.slot_tensors(0)
+    c.lckv_cache_reset(lens)
+    for t in pools:
+        t.fill_(5.0)
+    want = torch.full((B, n, Hq, d), 9.0, dtype=torch.bfloat16, device=DEV)
+    call(rope, want)
+    want_pools = [t.clone() for t in pools]
+    assert c.lckv_cache_status() == 0
+
+    c.lckv_cache_reset([0] * B)
+    for t in pools:
+        t.fill_(5.0)
+    out = torch.full_like(want, 9.0)
+    if prompt:
+        c.lckv_cache_reset([1] * B)
+    call(short, out)                                  # pages for the captured call
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        call(short, out)
+    c.lckv_cache_reset(lens)
+    for t in (*pools, out):
+        t.fill_(5.0 if t is not out else 9.0)
+    graph.replay()
+    status = c.lckv_cache_status()
+    lost = False
+    for b in range(B):
+        for i in range(n):
+            if prompt and i >= lens[b]:
+                assert bool((out[b, i] == 9.0).all())
+                continue
+            at = i if prompt else lens[b] + i
+            if at < SHORT:
+                assert torch.equal(out[b, i], want[b, i]), (b, i)
+            else:
+                lost = True
+                assert bool((out[b, i] == 9.0).all()), (b, i)
+                # the rows that the eager call wrote for this token stay as they were
+                if with_kv:
+                    row = at
+                    if c.cfg.stream_sink and row >= c.cfg.max_seq:
+                        row = c.cfg.stream_sink + (row - c.cfg.stream_sink) % (c.cfg.max_seq - c.cfg.stream_sink)
+                    for t, w in zip(pools, want_pools):
+                        place = (b, slice(None), row) if not c.cfg.page_rows else (int(c.lckv_cache_page_table()[b, row // c.cfg.page_rows]), slice(None), row % c.cfg.page_rows)
+                        w[place] = 5.0
+    if not c.cfg.page_rows:
+        for t, w in zip(pools, want_pools):
+            assert torch.equal(t, w)
+    else:
+        # (pages may have changed hands between the two)
+        assert with_kv or bool((pools[0] == 5.0).all())
+        for b in range(B):
+            for i in range(n):
+                at = i if prompt else lens[b] + i
+                if (prompt and i >= lens[b]) or not with_kv:
+                    continue
+                page = int(c.lckv_cache_page_table()[b, at // c.cfg.page_rows])
+                got = pools[1][page, :, at % c.cfg.page_rows]
+                assert torch.equal(got, v[b, i]) if at < SHORT else bool((got == 5.0).all())
+    assert lost and status == lk.ECAPACITY
+    c.lckv_cache_reset([0] * B)
+    assert c.lckv_cache_status() == 0
+
+
+REPLAY_LAYOUTS = {"contiguous": dict(), "paged": dict(page_rows=64, n_pages=6), "ring": dict(stream_sink=4)}
+
+
+@pytest.mark.parametrize("layout", list(REPLAY_LAYOUTS))
+@pytest.mark.parametrize("rot,interleaved,aligned", [(64, False, True), (50, False, True), (22, True, True), (64, True, False)])
+def test_replay_behind_the_tables(rot, interleaved, aligned, layout):
+    g = gen(rot)
+    T = 12 if layout == "ring" else 40
+    c = lk.Cache(lk.make_config(2, 0, 4, 2, 64, 3, T, **REPLAY_LAYOUTS[layout]))
+    for with_kv in (True, False):
+        replayed(c, g, [3, 20, 8], 1, rot, interleaved, with_kv, False, aligned)
+        replayed(c, g, [7, 2, 30], 3, rot, interleaved, with_kv, False, aligned)
+        if layout != "ring":
+            replayed(c, g, [11, 3, 0], 12, rot, interleaved, with_kv, True, aligned)
+    c.close()
