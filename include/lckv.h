@@ -567,6 +567,14 @@ int lckv_quant_linear(const void* packed, int32_t n, int32_t k, int32_t group, i
                       int32_t x_scale_group, void* y, int64_t y_stride, int32_t y_dtype, int32_t rows,
                       int32_t* dev_status, void* stream);
 
+/*
+ * For tests of the bounded waits: products of more than 16 rows launched from now on request only the first `weights`
+ * blocks of 128 columns of the weights and the first `x` of x (each thread block of its own; -1, the default: all).  Where
+ * a thread block has more, its waits for the rest run out within a second, without anything hanging.  One value per
+ * process; a captured call keeps the one that it was captured with.  Errors: EINVAL.
+ */
+int lckv_quant_set_copy_limits(int32_t weights, int32_t x);
+
 /* Short English name of a status code. */
 const char* lckv_status_string(int status);
 

@@ -80,6 +80,7 @@ SIGNATURES = {
     "lckv_quant_pack": (C.c_int, [_vp, _vp, _vp, _i32, _i32, _i32, _vp, C.c_size_t, _vp]),
     "lckv_quant_linear": (C.c_int, [_vp, _i32, _i32, _i32, _i32, _vp, _i64, _i32, _vp, _i32, _vp, _i64, _i32, _i32,
                                     _vp, _vp]),
+    "lckv_quant_set_copy_limits": (C.c_int, [_i32, _i32]),
     "lckv_status_string": (C.c_char_p, [C.c_int]),
     "lckv_last_cuda_error": (C.c_int, []),
 }
@@ -317,6 +318,11 @@ def lckv_quant_linear(w, x, out=None, x_scale=None, dev_status=None, stream=None
         _fail(rc, "lckv_quant_linear", "x is [rows, k] bf16 or float8_e4m3fn (with x_scale fp32, one per row or per 128 columns), "
                                        "out [rows, n] bf16 or fp32, on the weight's device")
     return out
+
+
+def lckv_quant_set_copy_limits(weights=-1, x=-1):
+    """For tests of the bounded waits: blocks of weights and of x that products of more than 16 rows request (include/lckv.h)."""
+    _chk(lib().lckv_quant_set_copy_limits(weights, x), "lckv_quant_set_copy_limits")
 
 
 class Cache:

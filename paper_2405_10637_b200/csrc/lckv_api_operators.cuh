@@ -493,6 +493,8 @@ int lckv_rms_norm(const void* x, int64_t x_stride, int32_t x_dtype, const void* 
 
 namespace {
 
+std::atomic<int32_t> quant_w_limit{INT32_MAX}, quant_x_limit{INT32_MAX};        // lckv_quant_set_copy_limits
+
 bool quant_shape_ok(int32_t n, int32_t k, int32_t group)
 {
     return n >= 1 && k >= 1 && n <= (1 << 24) && k <= (1 << 24) && (group == 32 || group == 64 || group == 128) && k % group == 0;
@@ -575,6 +577,8 @@ int launch_quant_tc5(const lckv::QuantParams& q, int sms, int32_t* status, cudaS
     const int64_t tiles = (int64_t)cfg.gridDim.x * m_tiles;
     const int ks = quant_split(tiles, p.k_blocks, 1, 10, 4, 0, sms).ks;        // one thread block per SM
     p.k_split = ks;
+    p.w_limit = quant_w_limit.load(std::memory_order_relaxed);
+    p.x_limit = quant_x_limit.load(std::memory_order_relaxed);
     CUtensorMap tm;
     if (int rc = quant_x_map(&tm, q, F8, p.NB)) return rc;
     const int smem = lckv::q5_smem_bytes(p.NB, F8, block, p.stages);
@@ -709,6 +713,14 @@ int lckv_quant_linear(const void* packed, int32_t n, int32_t k, int32_t group, i
     cudaStream_t st = static_cast<cudaStream_t>(stream);
     return x_kind ? (has_zeros ? launch_quant_group<true, true>(p, sms, dev_status, st) : launch_quant_group<true, false>(p, sms, dev_status, st))
                   : (has_zeros ? launch_quant_group<false, true>(p, sms, dev_status, st) : launch_quant_group<false, false>(p, sms, dev_status, st));
+}
+
+int lckv_quant_set_copy_limits(int32_t weights, int32_t x)
+{
+    if (weights < -1 || x < -1) return LCKV_EINVAL;
+    quant_w_limit.store(weights < 0 ? INT32_MAX : weights, std::memory_order_relaxed);
+    quant_x_limit.store(x < 0 ? INT32_MAX : x, std::memory_order_relaxed);
+    return LCKV_OK;
 }
 
 }  // extern "C"

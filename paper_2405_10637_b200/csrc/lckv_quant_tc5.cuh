@@ -24,12 +24,14 @@
 // Bound by the integer instructions of the nibbles for few rows (7 or 6 per 8 codes: 224 cycles per SM and 128 x 128 block)
 // and by the MMAs for many (512 cycles at NB = 128).  Few features: d_model is shared by a cluster whose partial results meet
 // in distributed shared memory, as in lckv_project.cuh, in a fixed order.  Every wait is bounded; one that runs out sets
-// the status word, if the caller gave one, and the tile's results become NaN.
+// the status word, if the caller gave one, and the tile's results become NaN.  Any role may give up alone; the roles that
+// started copies and MMAs then wait for their end before the thread block's memory serves the result.
 #pragma once
 #include "lckv_quant.cuh"
 
 namespace lckv {
 
+// Polls of a wait.  A constant: with the limit read from the parameters the roles took 3 to 5 % longer (512 rows of bf16 60.3 / 63.5 us).
 constexpr uint32_t kQ5WaitLimit = 1u << 16;
 constexpr int kQ5MaxStages = 12;
 
@@ -66,6 +68,7 @@ struct Quant5Params {
     int32_t x_blocks;
     int32_t y32, y_vec;      // y_vec: 4 features of y can be stored at once
     int32_t k_split, NB, stages;
+    int32_t w_limit, x_limit;            // blocks of 128 k that a thread block requests; fewer than there are only in tests
 };
 
 // D[tmem] (+)= A[tmem] * B[smem], fp32 accumulate (ACC = 0: from zero); bf16 and e4m3 inputs.
@@ -166,6 +169,7 @@ quant_tc5_kernel(const Quant5Params p, const __grid_constant__ CUtensorMap tmX)
     constexpr int TM_NEED = SETS * A_COLS + CONST_COLS + 2 * NBMAX;
     constexpr uint32_t TM_COLS = TM_NEED <= 32 ? 32 : TM_NEED <= 64 ? 64 : TM_NEED <= 128 ? 128 : TM_NEED <= 256 ? 256 : 512;
     static_assert(TM_NEED <= 512, "tensor memory");
+    static_assert(16 * kQ5MaxStages + 16 * SETS + 56 <= 512, "barriers");
     constexpr uint32_t A_CONST = SETS * A_COLS, D0 = A_CONST + CONST_COLS;
     constexpr int ROW = F8 ? 128 : 256;              // bytes of x per row and k block
     extern __shared__ uint8_t smem_raw[];
@@ -176,7 +180,8 @@ quant_tc5_kernel(const Quant5Params p, const __grid_constant__ CUtensorMap tmX)
     const uint32_t sXS = smem0 + (uint32_t)q5_pipe_bytes(NB, F8, BLOCK, NS);          // x scales
     const uint32_t bars = sXS + (F8 ? kQ5XScales : 0);
     const uint32_t bFull = bars, bEmpty = bars + 8 * kQ5MaxStages, bAFull = bars + 16 * kQ5MaxStages, bAEmpty = bAFull + 8 * SETS,
-                   bDFull = bAFull + 16 * SETS, bDEmpty = bDFull + 16, bDrain = bDFull + 32, sTaddr = bDFull + 40, sBad = sTaddr + 4;
+                   bDFull = bAFull + 16 * SETS, bDEmpty = bDFull + 16, bDrain = bDFull + 32, sTaddr = bDFull + 40, sBad = sTaddr + 4,
+                   sIssued = sTaddr + 8;             // stages that the two producers have requested
     const int tid = threadIdx.x, lane = tid & 31, warp = __shfl_sync(0xffffffffu, tid >> 5, 0);
     const int m0 = blockIdx.y * NB, nb0 = blockIdx.x * 4;
     const int KS = p.k_split;
@@ -213,7 +218,8 @@ quant_tc5_kernel(const Quant5Params p, const __grid_constant__ CUtensorMap tmX)
 
     float* out = reinterpret_cast<float*>(smem_raw + (smem0 - smem_u32(smem_raw)));
     // The end of every role: all MMAs and copies of the block are done, and a wait that ran out is known to all.
-    auto finish = [&](bool ok) {
+    int mma_lane = 0;                                // which lane of warp 1 issues MMAs
+    auto finish = [&](bool ok) -> uint32_t {
         if (!ok) {
             asm volatile("st.shared.u32 [%0], %1;" ::"r"(sBad), "r"(1) : "memory");
             if (p.status) atomicExch(p.status, kStatusTimeout);
@@ -221,6 +227,28 @@ quant_tc5_kernel(const Quant5Params p, const __grid_constant__ CUtensorMap tmX)
         tc5_fence_before();
         __syncthreads();
         tc5_fence_after();
+        uint32_t bad;
+        asm volatile("ld.shared.u32 %0, [%1];" : "=r"(bad) : "r"(sBad) : "memory");
+        if (bad) {
+            // Without a wait that ran out the fold warps have seen every MMA end, and so every copy land.  Here copies and MMAs may
+            // still be under way.  The producers may have stopped at different stages, at most NS apart: the one behind arrives
+            // for what it has not requested, so that the barriers of the last NS stages count the bytes that are under way.
+            if (warp == 0 || warp == 2) {
+                int mine, other;
+                asm volatile("ld.shared.u32 %0, [%1];" : "=r"(mine) : "r"(sIssued + 2u * warp) : "memory");
+                asm volatile("ld.shared.u32 %0, [%1];" : "=r"(other) : "r"(sIssued + 4u - 2u * warp) : "memory");
+                if (lane == 0)
+                    for (int k = mine; k < other; ++k) mbar_arrive(bFull + 8 * (k % NS));
+                const int end = mine > other ? mine : other;
+                for (int k = end > NS ? end - NS : 0; k < end; ++k) (void)mbar_wait_bounded(bFull + 8 * (k % NS), (k / NS) & 1, kQ5WaitLimit);
+            } else if (warp == 1) {
+                if (lane == mma_lane) tc5_commit(bDrain);
+                __syncwarp();
+                (void)mbar_wait_bounded(bDrain, 0, kQ5WaitLimit);
+            }
+            __syncthreads();
+        }
+        return bad;
     };
 
     bool ok = true;
@@ -232,8 +260,9 @@ quant_tc5_kernel(const Quant5Params p, const __grid_constant__ CUtensorMap tmX)
         const uint32_t leader = elect_one();
         const uint8_t* src = p.w + ((int64_t)blockIdx.x * p.k_blocks + k_lo) * (4 * BLOCK);
         RingPos r = {0, 0};
+        const int limit = is_w ? p.w_limit : p.x_limit, n_mine = n_k < limit ? n_k : limit;
         int issued = 0;
-        for (; issued < n_k; ++issued, r.next(NS)) {
+        for (; issued < n_mine; ++issued, r.next(NS)) {
             if (is_w && issued == NS) pdl_wait();    // (from here on it waits for work that waits for x)
             ok = mbar_wait_bounded(bEmpty + 8 * r.s, r.phase ^ 1, kQ5WaitLimit);
             ok = __all_sync(0xffffffffu, ok);
@@ -250,9 +279,7 @@ quant_tc5_kernel(const Quant5Params p, const __grid_constant__ CUtensorMap tmX)
             }
             __syncwarp();
         }
-        if (!ok)                                     // a wait ran out: the copies in flight land before the block ends
-            for (int k = issued > NS ? issued - NS : 0; k < issued; ++k)
-                (void)mbar_wait_bounded(bFull + 8 * (k % NS), (k / NS) & 1, kQ5WaitLimit);
+        if (leader) asm volatile("st.shared.u32 [%0], %1;" ::"r"(sIssued + 2u * warp), "r"(issued) : "memory");
         __syncwarp();
         pdl_release();
         finish(ok);
@@ -307,11 +334,7 @@ quant_tc5_kernel(const Quant5Params p, const __grid_constant__ CUtensorMap tmX)
             }
             if (!ok) break;
         }
-        if (!ok && leader) {                         // a wait ran out: the MMAs in flight end before their memory is given back
-            tc5_commit(bDrain);
-            (void)mbar_wait_bounded(bDrain, 0, kQ5WaitLimit);
-        }
-        __syncwarp();
+        mma_lane = __ffs(__ballot_sync(0xffffffffu, leader)) - 1;
         finish(ok);
     } else if (warp < FOLD0) {
         finish(true);
@@ -404,10 +427,8 @@ quant_tc5_kernel(const Quant5Params p, const __grid_constant__ CUtensorMap tmX)
         };
         if (F8 && p.x_blocks) steps(true);
         else steps(false);
-        finish(ok);
+        const uint32_t bad = finish(ok);
         // the block's stages become its result, [column][feature] in fp32
-        uint32_t bad;
-        asm volatile("ld.shared.u32 %0, [%1];" : "=r"(bad) : "r"(sBad) : "memory");
 #pragma unroll
         for (int c = 0; c < NBC; c += 2) {
             if (c0 + c >= NB) break;

@@ -5,7 +5,7 @@ import torch
 
 from paper_2405_10637_b200 import binding as lk
 
-from test_gpu_operators import DEV, E, HALF, check_norm, gen, norm64, randn, tables64, within
+from test_gpu_operators import DEV, E, HALF, check_linear, check_norm, gen, make_weight, make_x, norm64, randn, tables64, within
 
 pytestmark = pytest.mark.gpu
 
@@ -138,3 +138,38 @@ def test_replay_behind_the_tables(rot, interleaved, aligned, layout):
         if layout != "ring":
             replayed(c, g, [11, 3, 0], 12, rot, interleaved, with_kv, True, aligned)
     c.close()
+
+
+# ---- products whose device-side waits run out --------------------------------------------------------------------------------
+
+
+@pytest.fixture
+def copy_limits():
+    yield lk.lckv_quant_set_copy_limits
+    lk.lckv_quant_set_copy_limits()
+
+
+@pytest.mark.parametrize("weights,x_blocks", [(-1, 0), (1, -1), (-1, 3), (2, 2)])
+@pytest.mark.parametrize("rows,n,k,group,has_zeros,kind", [(17, 130, 512, 128, False, "bf16"), (32, 1000, 4096, 64, True, "block"),
+                                                           (200, 600, 2048, 32, False, "row"), (129, 300, 11008, 128, True, "bf16")])
+def test_quant_waits_that_run_out(rows, n, k, group, has_zeros, kind, weights, x_blocks, copy_limits):
+    """Copies that are not requested: the outputs are NaN and that is reported, nothing else is written, and calls queued
+    behind are right (what the call that gave up still had under way does not reach their memory)."""
+    g = gen(rows)
+    w, w64 = make_weight(g, n, k, group, has_zeros)
+    x, s, x64 = make_x(g, rows, k, kind)
+    clean = lk.lckv_quant_linear(w, x, torch.empty(rows, n, device=DEV), x_scale=s)
+    check_linear(clean, x64, w64, k)
+    status = torch.zeros(1, dtype=torch.int32, device=DEV)
+    buf = torch.full((rows, n + 8), 7.0, device=DEV)
+    after = [torch.full((rows, n), 3.0, device=DEV) for _ in range(2)]
+    copy_limits(weights, x_blocks)
+    lk.lckv_quant_linear(w, x, buf[:, 4:4 + n], x_scale=s, dev_status=status)
+    copy_limits()
+    for y in after:
+        lk.lckv_quant_linear(w, x, y, x_scale=s)
+    torch.cuda.synchronize()
+    assert status.item() == lk.ETIMEOUT
+    assert bool(torch.isnan(buf[:, 4:4 + n]).all())
+    assert bool((buf[:, :4] == 7.0).all()) and bool((buf[:, 4 + n:] == 7.0).all())
+    assert all(torch.equal(y, clean) for y in after)
