@@ -321,6 +321,7 @@ int lckv_rope_tables(float* cos, float* sin, int32_t positions, int32_t rot_dim,
     const double two_pi = 6.283185307179586476925286766559;
     lckv::RopeTableParams p;
     const double base = s->kind == 2 && rot_dim > 2 ? s->base * std::pow(s->factor, (double)rot_dim / (rot_dim - 2.0)) : s->base;
+    if (!std::isfinite(base)) return LCKV_EINVAL;              // (an infinite base would make every frequency but the first 0)
     for (int i = 0; i < half; ++i) {
         double theta = std::pow(base, -2.0 * i / rot_dim);
         if (s->kind == 1) theta /= s->factor;
