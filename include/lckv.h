@@ -551,8 +551,7 @@ int lckv_rms_norm(const void* x, int64_t x_stride, int32_t x_dtype, const void* 
  *              concerned are then NaN); it is not cleared.  NULL to ignore
  * codes - zeros are exact on the tensor cores; a group's sum is accumulated in fp32 and scaled in fp32, and
  * there is one rounding to y's type.  Results do not depend on the order of execution.  rows 1 .. 524288.
- * A row of x with an infinity or a NaN gives infinities or NaN, and leaves the other rows alone; up to 16 rows of bf16 also
- * need 31 sum|x| over a group to be finite in fp32.
+ * A row of x with an infinity or a NaN gives infinities or NaN, and leaves the other rows alone.
  * lckv_quant_pack SYNCHRONISES `stream` (set-up, like lckv_cache_alloc) and is refused while it captures;
  * lckv_quant_linear only enqueues work.  It requests packed weights before the kernel in front of it in
  * the stream has ended, so that kernel must not be the one that writes them (lckv_quant_pack's never is).

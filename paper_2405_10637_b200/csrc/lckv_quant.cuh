@@ -4,15 +4,11 @@
 //
 // Bound by the bytes of the codes: 2 m multiply-adds per half byte, and close behind by the integer instructions that
 // turn nibbles into numbers.  The operands are swapped so that 16 output features are the rows of an MMA tile and up to
-// 8 rows of x its columns, and the codes enter the tensor cores as 16 + c, a nibble or'ed into the upper mantissa bits of
-// 16.0 (7 or 8 instructions per 8 codes): in bf16 for x in bf16, in fp16 for x in e4m3, which is converted when it is loaded.
-// All three are exact.  (mma.sync on e4m3 itself, with c / 512 as an e4m3 byte, needs fewer instructions of the program, but the
-// counters showed two tensor instructions per MMA and a dozen others beside them: 16 rows, 4096 x 22016 features, groups of 64
-// 22.7 us, this 20.7.)  A tile of ones gives the sums of x, so that a group's
-//     sum x (c - z) = sum x (16 + c) - (16 + z) sum x
-// costs one multiply-add per group where subtracting z from every weight would cost one instruction per two
-// weights.  Products are exact, sums fp32, scales and zero points are applied in fp32; the terms are at most 4 times
-// as large as those of x (c - z) with z = 8, which costs two of fp32's bits and none of the output's.
+// 8 rows of x its columns.  A nibble or'ed into the upper mantissa bits of 16.0 is 16 + c (7 or 8 instructions per 8 codes), and
+// 16 + z subtracted from it leaves c - z (4 more): in bf16 for x in bf16, in fp16 for x in e4m3, which is converted when it is
+// loaded.  All of these are exact, sums are fp32, scales are applied in fp32 once per group.  (Taking x (16 + c) and correcting
+// by (16 + z) times a sum of x once per group cancels sums of up to 31 |x|, and needs an MMA with a tile of ones: 4096 x 22016,
+// 1 row 12.7 us, 16 rows of e4m3 in groups of 64 20.6, of 32 22.0; this 12.4, 20.2 and 19.7.)
 //
 // Layout (quant_pack_kernel, once per weight).  The codes are cut into blocks of 32 features x 128 k = 2 KB,
 // k fastest; such a block holds [2 halves of 64 k][2 tiles of 16 features][32 lanes][16 bytes], where lane (g, t) of a
@@ -93,7 +89,7 @@ __global__ void __launch_bounds__(256) quant_pack_kernel(const QuantPackParams p
             const int f = nb * kQuantFeat + ((o >> 1) & 1) * 16 + (o & 1) * 8 + (o >> 2);
             const bool in = f < p.n && grp < src_groups;
             reinterpret_cast<uint16_t*>(out + kQuantCodes)[i] = in ? p.scales[(int64_t)f * src_groups + grp] : (uint16_t)0;
-            // a zero point is kept as the third byte of the fp32 number 16 + z (0x41800000 + z 2^19)
+            // a zero point is kept as the low byte of the bf16 number 16 + z (0x4180 + 8 z)
             if (p.zeros) out[y.zeros_off + i] = 0x80 | (in ? (p.zeros[(int64_t)f * src_groups + grp] & 15) << 3 : 0);
         }
     }
@@ -192,13 +188,25 @@ __device__ __forceinline__ uint32_t and_or(uint32_t a, uint32_t mask, uint32_t b
     return d;
 }
 
-// 32 k of a warp (first or second of a half): FT tiles of 16 features, and the tile of ones, times NT tiles of 8 rows.
-// FIRST: of a group.
-template <bool F8, int FT, int NT, int SECOND, bool FIRST>
-__device__ __forceinline__ void quant_32k(float (&grp)[FT][NT][4], float (&sum)[NT][4], const uint4 (&c)[FT], const QuantX<F8> (&x)[NT])
+__device__ __forceinline__ uint32_t sub_bf16x2(uint32_t a, uint32_t b)
 {
-    constexpr uint32_t ONE = F8 ? 0x3c003c00u : 0x3f803f80u, MASK = F8 ? 0x03c003c0u : 0x00780078u, SIXTEEN = F8 ? 0x4c004c00u : 0x41804180u;
-    const uint32_t ones[4] = {ONE, ONE, ONE, ONE};
+    uint32_t d;
+    asm("sub.rn.bf16x2 %0, %1, %2;" : "=r"(d) : "r"(a), "r"(b));
+    return d;
+}
+__device__ __forceinline__ uint32_t sub_f16x2(uint32_t a, uint32_t b)
+{
+    uint32_t d;
+    asm("sub.rn.f16x2 %0, %1, %2;" : "=r"(d) : "r"(a), "r"(b));
+    return d;
+}
+
+// 32 k of a warp (first or second of a half): FT tiles of 16 features times NT tiles of 8 rows.  zp: 16 + z of features g and
+// g + 8 of each tile, as pairs.  FIRST: of a group.
+template <bool F8, int FT, int NT, int SECOND, bool FIRST>
+__device__ __forceinline__ void quant_32k(float (&grp)[FT][NT][4], const uint32_t (&zp)[FT][2], const uint4 (&c)[FT], const QuantX<F8> (&x)[NT])
+{
+    constexpr uint32_t MASK = F8 ? 0x03c003c0u : 0x00780078u, SIXTEEN = F8 ? 0x4c004c00u : 0x41804180u;
 #pragma unroll
     for (int s = 0; s < 2; ++s) {
         uint32_t b[NT][2];
@@ -206,8 +214,6 @@ __device__ __forceinline__ void quant_32k(float (&grp)[FT][NT][4], float (&sum)[
         for (int j = 0; j < NT; ++j) {
             if (s == 0) x[j].template frag<SECOND * 2>(b[j][0], b[j][1]);
             else x[j].template frag<SECOND * 2 + 1>(b[j][0], b[j][1]);
-            if (s == 0) quant_mma<F8, FIRST>(sum[j], ones, b[j][0], b[j][1]);
-            else quant_mma<F8, false>(sum[j], ones, b[j][0], b[j][1]);
         }
 #pragma unroll
         for (int i = 0; i < FT; ++i) {
@@ -216,7 +222,8 @@ __device__ __forceinline__ void quant_32k(float (&grp)[FT][NT][4], float (&sum)[
 #pragma unroll
             for (int r = 0; r < 4; ++r) {
                 const uint32_t w = r & 1 ? w1 : w0;
-                a[r] = and_or(__funnelshift_r(w, w, (4 * (s + (r & 2)) + (F8 ? 29 : 0)) & 31), MASK, SIXTEEN);
+                const uint32_t u = and_or(__funnelshift_r(w, w, (4 * (s + (r & 2)) + (F8 ? 29 : 0)) & 31), MASK, SIXTEEN);
+                a[r] = F8 ? sub_f16x2(u, zp[i][r & 1]) : sub_bf16x2(u, zp[i][r & 1]);
             }
 #pragma unroll
             for (int j = 0; j < NT; ++j) {
@@ -298,7 +305,7 @@ __global__ void __launch_bounds__(quant_warps(NT) * 32, quant_ctas(FT, NT)) quan
     fetch_x(kb0, 1);
 
     uint64_t acc[FT][NT][2];                         // pairs of columns, features g and g + 8
-    float grp[FT][NT][4], sum[NT][4];
+    float grp[FT][NT][4];
 #pragma unroll
     for (int j = 0; j < NT; ++j)
 #pragma unroll
@@ -326,27 +333,39 @@ __global__ void __launch_bounds__(quant_warps(NT) * 32, quant_ctas(FT, NT)) quan
         __syncwarp();
         const uint32_t blk = ring + slot * (NB * BLOCK);
         slot = slot == SLOTS - 1 ? 0 : slot + 1;
-        // A complete group: its zero points, its scales; two columns per instruction.  With a scale of x per block the
-        // groups of the block are summed first.
+        // The zero points of group gi of the block.
+        uint32_t zp[FT][2];
+        auto zero_points = [&](int gi) {
+#pragma unroll
+            for (int b = 0; b < NB; ++b) {
+                uint32_t z = 0;
+                if (ZEROS) asm volatile("ld.shared.u32 %0, [%1];" : "=r"(z) : "r"(blk + b * BLOCK + kQuantCodes + SCALES + gi * kQuantFeat + g * 4));
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    uint32_t& to = zp[b * 2 + (i >> 1)][i & 1];
+                    if (!ZEROS) to = F8 ? 0x4e004e00u : 0x41c041c0u;                              // 24
+                    else if (F8) to = (__byte_perm(z, 0u, 0x4040u + 0x0101u * i) << 3) + 0x48004800u;    // (the stored byte is 0x80 + 8 z)
+                    else to = __byte_perm(z, 0x41414141u, 0x4040u + 0x0101u * i);
+                }
+            }
+        };
+        // A complete group: its scales; two columns per instruction.  With a scale of x per block the groups of the block are
+        // summed first.
         uint64_t blk_sum[FT][NT][2];
         auto fold = [&](int gi) {
 #pragma unroll
             for (int b = 0; b < NB; ++b) {
-                uint32_t sw[2], z = 0;
+                uint32_t sw[2];
                 asm volatile("ld.shared.v2.u32 {%0,%1}, [%2];" : "=r"(sw[0]), "=r"(sw[1]) : "r"(blk + b * BLOCK + kQuantCodes + gi * (kQuantFeat * 2) + g * 8));
-                if (ZEROS) asm volatile("ld.shared.u32 %0, [%1];" : "=r"(z) : "r"(blk + b * BLOCK + kQuantCodes + SCALES + gi * kQuantFeat + g * 4));
 #pragma unroll
                 for (int i = 0; i < 2; ++i)
 #pragma unroll
                     for (int hi = 0; hi < 2; ++hi) {
                         const float f = hi ? bf16hi(sw[i]) : bf16lo(sw[i]);
-                        float zp = -24.f;            // -(16 + z): bytes 0, 0, the stored one, 0xc1
-                        if (ZEROS) zp = __uint_as_float(__byte_perm(z, 0xc1000000u, 0x7044u | (uint32_t)((i * 2 + hi) << 8)));
-                        const uint64_t f2 = pack_f32x2(f, f), z2 = pack_f32x2(zp, zp);
+                        const uint64_t f2 = pack_f32x2(f, f);
 #pragma unroll
                         for (int j = 0; j < NT; ++j) {
-                            const uint64_t v = ffma2(z2, pack_f32x2(sum[j][0], sum[j][1]),
-                                                     pack_f32x2(grp[b * 2 + i][j][hi * 2], grp[b * 2 + i][j][hi * 2 + 1]));
+                            const uint64_t v = pack_f32x2(grp[b * 2 + i][j][hi * 2], grp[b * 2 + i][j][hi * 2 + 1]);
                             if (F8 && GROUP < kQuantK) {
                                 blk_sum[b * 2 + i][j][hi] = gi == 0 ? fmul2(f2, v) : ffma2(f2, v, blk_sum[b * 2 + i][j][hi]);
                             } else if (F8) {
@@ -365,10 +384,14 @@ __global__ void __launch_bounds__(quant_warps(NT) * 32, quant_ctas(FT, NT)) quan
             uint4 c[FT];
 #pragma unroll
             for (int i = 0; i < FT; ++i) c[i] = lds128(blk + (i >> 1) * BLOCK + ((h * 2 + (i & 1)) * 32 + lane) * 16);
-            if (h == 0 || GROUP <= 64) quant_32k<F8, FT, NT, 0, true>(grp, sum, c, xr[h]);
-            else quant_32k<F8, FT, NT, 0, false>(grp, sum, c, xr[h]);
-            if (GROUP == 32) fold(h * 2);
-            quant_32k<F8, FT, NT, 1, GROUP == 32>(grp, sum, c, xr[h]);
+            if (h == 0 || GROUP <= 64) zero_points(GROUP == 32 ? h * 2 : GROUP == 64 ? h : 0);
+            if (h == 0 || GROUP <= 64) quant_32k<F8, FT, NT, 0, true>(grp, zp, c, xr[h]);
+            else quant_32k<F8, FT, NT, 0, false>(grp, zp, c, xr[h]);
+            if (GROUP == 32) {
+                fold(h * 2);
+                zero_points(h * 2 + 1);
+            }
+            quant_32k<F8, FT, NT, 1, GROUP == 32>(grp, zp, c, xr[h]);
             if (kb + 1 < kb1) fetch_x(kb + 1, h);
             if (h == 1 || GROUP <= 64) fold(GROUP == 32 ? h * 2 + 1 : GROUP == 64 ? h : 0);
         }

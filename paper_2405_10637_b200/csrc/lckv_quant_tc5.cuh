@@ -139,13 +139,6 @@ __device__ __forceinline__ float lds_f32(uint32_t addr)
     asm volatile("ld.shared.f32 %0, [%1];" : "=f"(v) : "r"(addr) : "memory");
     return v;
 }
-__device__ __forceinline__ uint32_t sub_bf16x2(uint32_t a, uint32_t b)
-{
-    uint32_t d;
-    asm("sub.rn.bf16x2 %0, %1, %2;" : "=r"(d) : "r"(a), "r"(b));
-    return d;
-}
-
 // Place in a ring of n slots and the parity of its round.  A role that waits for a slot to be filled waits for `phase`, one
 // that waits for it to be free for phase ^ 1 (true at once in the first round).  Kept by addition: a division by the
 // number of slots per step and role was half of a step's time.

@@ -173,3 +173,50 @@ def test_quant_waits_that_run_out(rows, n, k, group, has_zeros, kind, weights, x
     assert bool(torch.isnan(buf[:, 4:4 + n]).all())
     assert bool((buf[:, :4] == 7.0).all()) and bool((buf[:, 4 + n:] == 7.0).all())
     assert all(torch.equal(y, clean) for y in after)
+
+
+# ---- products: weights at and beside their zero point, one large activation --------------------------------------------------
+
+
+@pytest.mark.parametrize("kind", ["bf16", "row", "block"])
+@pytest.mark.parametrize("rows", [1, 8, 16, 17, 40])
+@pytest.mark.parametrize("k,group,has_zeros", [(128, 128, False), (1024, 64, True), (2080, 32, True), (4096, 128, True)])
+def test_quant_small_weights_large_activation(k, group, has_zeros, rows, kind):
+    """c - z is exact before it meets x: a feature whose codes are its zero points gives 0 whatever x is, and an x of some
+    thousands leaves no trace in a feature that has a zero weight there."""
+    g = gen(k + rows)
+    n = 72
+    zeros = torch.randint(1, 15, (n, k // group), generator=g, device=DEV, dtype=torch.uint8) if has_zeros else None
+    z = zeros.repeat_interleave(group, 1) if has_zeros else torch.full((n, k), 8, dtype=torch.uint8, device=DEV)
+    w = torch.randint(-1, 2, (n, k), generator=g, device=DEV, dtype=torch.int32)
+    w[:16] = 0
+    big = 37
+    w[16:48, big] = 0
+    codes = (z.int() + w).to(torch.uint8)
+    scales = (torch.rand((n, k // group), generator=g, device=DEV) + 0.5).to(torch.bfloat16)
+    packed = lk.lckv_quant_pack(codes[:, 0::2] | (codes[:, 1::2] << 4), scales, zeros)
+    w64 = w.double() * scales.double().repeat_interleave(group, 1)
+    x, s, _ = make_x(g, rows, k, kind)
+    if kind == "bf16":
+        x[:, big] = 3333.0
+        x64 = x.double()
+    else:
+        x = (x.float() / 64).to(torch.float8_e4m3fn)
+        x[:, big] = 448.0
+        x64 = x.float().double() * (s.double() if kind == "row" else s.double().repeat_interleave(128, 1)[:, :k])
+    y = lk.lckv_quant_linear(packed, x, torch.empty(rows, n, device=DEV), x_scale=s)
+    assert bool((y[:, :16] == 0).all())
+    check_linear(y, x64, w64, k)
+
+
+def test_quant_sums_of_large_activations():
+    """x whose products with 16 + c would leave fp32 while those with c - z do not."""
+    g = gen(8)
+    n, k = 64, 256
+    codes = torch.full((n, k // 2), 0x88, dtype=torch.uint8, device=DEV)
+    codes[:, 5] = 0x89                                       # one weight of 1, the others 0
+    w = lk.lckv_quant_pack(codes, torch.ones(n, 2, dtype=torch.bfloat16, device=DEV))
+    for rows in (1, 16, 17):
+        x = torch.full((rows, k), 1e38, device=DEV).to(torch.bfloat16)
+        y = lk.lckv_quant_linear(w, x, torch.empty(rows, n, device=DEV))
+        assert torch.equal(y, x[:, :1].float().expand(rows, n))
