@@ -268,12 +268,12 @@ bool norm_row_fits(int n_vec) { return n_vec <= 512 * kNormMostVectors; }
 // where fp32 tensors make the bytes and not the instructions the bound and rows are short: 2^26 elements, ring / one row
 // per thread block, us, with 512, 2048, 4096, 8192 columns: bf16 49 / 60, 43 / 64, 43 / 70, 44 / 78; bf16 + bf16 94 / 102,
 // 95 / 105, 95 / 109, 95 / 115; bf16 + fp32 148 / 121, 146 / 124, 146 / 128, 148 / 132; fp32 99 / 80, 101 / 84, 101 / 89,
-// 88 / 106; bf16 + fp32 to e4m3 134 / 123, 136 / 128, 114 / 131, 122 / 138.
+// 88 / 106; bf16 + fp32 to e4m3 134 / 123, 136 / 128, 114 / 131, 122 / 138.  Nor with an eps of 0 (norm_factor).
 cudaError_t norm_launch(const lckv::NormParams& p, int n_vec, bool edges, int sms, cudaStream_t st)
 {
     const bool fp32 = p.x32 || (p.r && p.r32);
     const bool many = p.rows > sms;
-    if (many && (!fp32 || edges || n_vec > 512 + 256 || (p.out == 2 && n_vec >= 512))) {
+    if (many && p.eps > 0.f && (!fp32 || edges || n_vec > 512 + 256 || (p.out == 2 && n_vec >= 512))) {
         const int nv = n_vec > 1024 ? 4 : 2;
         NormShape g;
         g.tpr = norm_threads(n_vec, nv, p.group != 0);

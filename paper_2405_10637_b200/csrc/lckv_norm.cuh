@@ -144,18 +144,25 @@ __device__ __forceinline__ float norm_reduce(float v, float* sh)
 }
 
 // 1 / sqrt(mean + eps) of a row whose squares sum to `ss`.  Where fp32 squares overflow, or vanish beside an
-// eps that is as small, `again(k)` sums the squares of k h once more with k a power of two that brings them into
-// range.  `again` holds a reduction, so all rows of a warp go through it together.
-template <typename F>
+// eps that is as small, `again(k, c)` sums the squares of k h once more with k a power of two that brings them into
+// range: the largest h, 2^128, to 2^48, whose squares 32768 times are 2^111; the smallest, 2^-149, to 2^-49.  `again` holds a
+// reduction, so all rows of a warp go through it together.
+//
+// With an eps above 0, at least 2^-149, the factor is at most 2^75 and at least 2^-128, an fp32 number (good to 2^-22 at that end).
+// With an eps of 0 it can be 2^149: such calls go to the kernels with SPLIT, where a part of the factor, c, goes into h.
+// (Not everywhere: the multiplications by c, never carried out, changed the compiler's registers and cost the ring kernel up to
+// a quarter, 512 x 4096 of fp32 6.1 / 7.7 us.)
+template <bool SPLIT, typename F>
 __device__ __forceinline__ float norm_factor(float ss, const NormParams& p, F again)
 {
     const float v = ss / (float)p.width + p.eps;
     const bool fine = (v >= 0x1p-100f && ss <= 3.402823466e+38f) || isnan(ss);
     float rs = isnan(ss) ? ss : rsqrtf(v);
     if (!__all_sync(0xffffffffu, fine)) {
-        const float k = v < 1.f ? 0x1p70f : 0x1p-70f;
-        const float s2 = again(k);
-        if (!fine) rs = rsqrtf(s2 / (float)p.width + p.eps * k * k) * k;
+        const bool small = v < 1.f;
+        const float k = small ? 0x1p100f : 0x1p-80f, c = !SPLIT || fine ? 1.f : small ? 0x1p100f : 0x1p-4f;
+        const float s2 = again(k, c);
+        if (!fine) rs = rsqrtf(s2 / (float)p.width + p.eps * k * k) * (k / c);
     }
     return rs;
 }
@@ -242,7 +249,7 @@ __device__ __forceinline__ void norm_weights(const NormParams& p, const NormRow<
 }
 
 // From h = x + r in f to the outputs of the row; `sh`: 2 x 32 floats; weight(i, g) gives the weights of the thread's i-th vector.
-template <int NV, bool EDGES, typename Types, typename W>
+template <int NV, bool EDGES, bool SPLIT, typename Types, typename W>
 __device__ __forceinline__ void norm_finish(const NormParams& p, const Types& t, const NormRow<EDGES>& w, float (&f)[NV][8], float* sh, W weight)
 {
     const int tx = threadIdx.x, tpr = blockDim.x;
@@ -268,12 +275,15 @@ __device__ __forceinline__ void norm_finish(const NormParams& p, const Types& t,
     float ss, ss_odd;
     unpack_f32x2(s2, ss, ss_odd);
     ss = norm_reduce<false>(ss + ss_odd, sh);
-    const float rs = norm_factor(ss, p, [&](float k) {
+    const float rs = norm_factor<SPLIT>(ss, p, [&](float k, float c) {
         float s3 = 0.f;
 #pragma unroll
         for (int i = 0; i < NV; ++i)
 #pragma unroll
-            for (int j = 0; j < 8; ++j) s3 = fmaf(f[i][j] * k, f[i][j] * k, s3);
+            for (int j = 0; j < 8; ++j) {
+                s3 = fmaf(f[i][j] * k, f[i][j] * k, s3);
+                if constexpr (SPLIT) f[i][j] *= c;
+            }
         if (blockDim.x > 32) __syncthreads();
         return norm_reduce<false>(s3, sh);
     });
@@ -385,7 +395,7 @@ __global__ void __launch_bounds__(MAX_THREADS) norm_vec_kernel(const NormParams 
             for (int j = 0; j < 8; ++j) f[i][j] += g[j];
         }
     }
-    norm_finish<NV, EDGES>(p, NormAnyTypes{p}, w, f, sh, [&](int i, float (&g)[8]) { norm_weights(p, w, i * blockDim.x + threadIdx.x, g); });
+    norm_finish<NV, EDGES, true>(p, NormAnyTypes{p}, w, f, sh, [&](int i, float (&g)[8]) { norm_weights(p, w, i * blockDim.x + threadIdx.x, g); });
 }
 
 // The same for many rows: resident thread blocks walk over the rows, and each warp's vectors of the next row are
@@ -500,7 +510,7 @@ __global__ void __launch_bounds__(512) norm_ring_kernel(const NormParams p)
         }
         slot = slot == kNormRing - 1 ? 0 : slot + 1;
         // (the other half of sh may still be read by a slower warp)
-        norm_finish<NV, EDGES>(p, t, w, f, sh[odd], [&](int i, float (&g)[8]) {
+        norm_finish<NV, EDGES, false>(p, t, w, f, sh[odd], [&](int i, float (&g)[8]) {
             if constexpr (EDGES) norm_weights(p, w, i * tpr + tx, g);
             else {
 #pragma unroll
@@ -530,9 +540,12 @@ __global__ void __launch_bounds__(256) norm_any_kernel(const NormParams p)
         ss = fmaf(v, v, ss);
     }
     ss = norm_reduce<false>(ss, sh_sum);
-    const float rs = norm_factor(ss, p, [&](float k) {
+    const float rs = norm_factor<true>(ss, p, [&](float k, float c) {
         float s2 = 0.f;
-        for (int e = tx; e < p.width; e += nt) s2 = fmaf(row_sh[e] * k, row_sh[e] * k, s2);
+        for (int e = tx; e < p.width; e += nt) {       // (each thread its own elements, as above and below)
+            s2 = fmaf(row_sh[e] * k, row_sh[e] * k, s2);
+            row_sh[e] *= c;
+        }
         __syncthreads();
         return norm_reduce<false>(s2, sh_sum);
     });

@@ -220,3 +220,30 @@ def test_quant_sums_of_large_activations():
         x = torch.full((rows, k), 1e38, device=DEV).to(torch.bfloat16)
         y = lk.lckv_quant_linear(w, x, torch.empty(rows, n, device=DEV))
         assert torch.equal(y, x[:, :1].float().expand(rows, n))
+
+
+# ---- rows of the smallest and the largest numbers -----------------------------------------------------------------------------
+
+
+@pytest.mark.parametrize("out", ["bf16", "fp32", "e4m3row", "e4m3block"])
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+@pytest.mark.parametrize("width", [8, 64, 1000, 1030, 4096, 20001, 32767, 32768])
+def test_norm_of_extreme_rows(width, dtype, out):
+    """Rows near the smallest and the largest numbers of their type beside ordinary ones, with an eps of zero and one that is as
+    small as the squares; the factor of such a row lies outside fp32."""
+    g = gen(width)
+    group = 128 if out == "e4m3block" else 0
+    dt = {"bf16": torch.bfloat16, "fp32": torch.float32}.get(out, torch.float8_e4m3fn)
+    tiny = 2.0 ** -126 if dtype == torch.bfloat16 else 2.0 ** -140
+    unit = torch.tensor([1.0, tiny, 1e38, tiny * 2 ** 60, 3e19], dtype=torch.float64, device=DEV)
+    for rows in (5, 305):
+        x = torch.randn((rows, width), generator=g, device=DEV).double() * unit[torch.arange(rows, device=DEV) % 5, None]
+        x = x.clamp(-3e38, 3e38).to(dtype)
+        x[:, 0] = torch.where(x[:, 0] == 0, unit[torch.arange(rows, device=DEV) % 5].to(dtype), x[:, 0])       # no row of zeros
+        x[2] = 3e38                                        # the sum of these squares, at the first scale that suffices for most
+        w = 1 + randn(g, width, dtype=torch.float32, std=0.2)
+        for eps in (0.0, 2.0 ** -149, 1e-30):
+            y = torch.empty(rows, width, device=DEV, dtype=dt)
+            scale = torch.empty(rows, -(-width // 128) if group else 1, device=DEV) if dt == torch.float8_e4m3fn else None
+            lk.lckv_rms_norm(x, w, y, out_scale=scale, scale_group=group, eps=eps)
+            check_norm(y, scale, norm64(x, None, w, torch.tensor(eps, dtype=torch.float32).double().item())[1], group)
