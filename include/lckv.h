@@ -555,8 +555,8 @@ int lckv_rms_norm(const void* x, int64_t x_stride, int32_t x_dtype, const void* 
  * lckv_quant_pack SYNCHRONISES `stream` (set-up, like lckv_cache_alloc) and is refused while it captures;
  * lckv_quant_linear only enqueues work.  It requests packed weights before the kernel in front of it in
  * the stream has ended, so that kernel must not be the one that writes them (lckv_quant_pack's never is).
- * Errors: EINVAL (null, shape, alignment, y overlapping what is read), ENOMEM (packed too small or misaligned,
- * lckv_quant_pack only), ECUDA.
+ * Errors: EINVAL (null, shape, alignment, y overlapping what is read; a zero point above 15, in lckv_quant_pack, whose
+ * packed is then undefined), ENOMEM (packed too small or misaligned, lckv_quant_pack only), ECUDA.
  */
 size_t lckv_quant_bytes(int32_t n, int32_t k, int32_t group, int32_t has_zeros);
 int lckv_quant_pack(const void* codes, const void* scales, const void* zeros, int32_t n, int32_t k,

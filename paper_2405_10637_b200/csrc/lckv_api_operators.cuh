@@ -668,6 +668,16 @@ int lckv_quant_pack(const void* codes, const void* scales, const void* zeros, in
     int rc = LCKV_OK;
     if (capturing(st, &rc)) return LCKV_EINVAL;
     if (rc) return rc;
+    if (zeros) {
+        // a zero point above 15 has no place in the layout; the packed weight's first word serves as the flag until it is written
+        int32_t* flag = reinterpret_cast<int32_t*>(packed);
+        int32_t bad = 0;
+        if (!cuda_ok(cudaMemsetAsync(flag, 0, 4, st))) return LCKV_ECUDA;
+        lckv::quant_zeros_kernel<<<sms, 256, 0, st>>>(p.zeros, src, flag);
+        if (!cuda_ok(cudaGetLastError())) return LCKV_ECUDA;
+        if (!cuda_ok(cudaMemcpyAsync(&bad, flag, 4, cudaMemcpyDeviceToHost, st)) || !cuda_ok(cudaStreamSynchronize(st))) return LCKV_ECUDA;
+        if (bad) return LCKV_EINVAL;
+    }
     lckv::quant_pack_kernel<<<sms * 8, 256, 0, st>>>(p);
     if (!cuda_ok(cudaGetLastError())) return LCKV_ECUDA;
     // lckv_quant_linear requests weights before the kernel in front of it has ended: they are complete from here on

@@ -58,6 +58,14 @@ struct QuantPackParams {
     int32_t n, k, group;
 };
 
+// *flag = 1 if one of the n zero points lies above 15.
+__global__ void __launch_bounds__(256) quant_zeros_kernel(const uint8_t* zeros, int64_t n, int32_t* flag)
+{
+    bool bad = false;
+    for (int64_t i = (int64_t)blockIdx.x * blockDim.x + threadIdx.x; i < n; i += (int64_t)gridDim.x * blockDim.x) bad |= zeros[i] > 15;
+    if (bad) atomicExch(flag, 1);
+}
+
 // A thread block per (32 features, 128 k): one thread per 32-bit word of its codes, then one per scale.
 __global__ void __launch_bounds__(256) quant_pack_kernel(const QuantPackParams p)
 {
@@ -90,7 +98,7 @@ __global__ void __launch_bounds__(256) quant_pack_kernel(const QuantPackParams p
             const bool in = f < p.n && grp < src_groups;
             reinterpret_cast<uint16_t*>(out + kQuantCodes)[i] = in ? p.scales[(int64_t)f * src_groups + grp] : (uint16_t)0;
             // a zero point is kept as the low byte of the bf16 number 16 + z (0x4180 + 8 z)
-            if (p.zeros) out[y.zeros_off + i] = 0x80 | (in ? (p.zeros[(int64_t)f * src_groups + grp] & 15) << 3 : 0);
+            if (p.zeros) out[y.zeros_off + i] = 0x80 | (in ? p.zeros[(int64_t)f * src_groups + grp] << 3 : 0);
         }
     }
 }

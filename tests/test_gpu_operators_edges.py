@@ -5,7 +5,7 @@ import torch
 
 from paper_2405_10637_b200 import binding as lk
 
-from test_gpu_operators import DEV, E, HALF, check_linear, check_norm, gen, make_weight, make_x, norm64, randn, tables64, within
+from test_gpu_operators import DEV, E, HALF, check_linear, check_norm, gen, make_weight, make_x, norm64, randn, refused, tables64, within
 
 pytestmark = pytest.mark.gpu
 
@@ -247,3 +247,23 @@ def test_norm_of_extreme_rows(width, dtype, out):
             scale = torch.empty(rows, -(-width // 128) if group else 1, device=DEV) if dt == torch.float8_e4m3fn else None
             lk.lckv_rms_norm(x, w, y, out_scale=scale, scale_group=group, eps=eps)
             check_norm(y, scale, norm64(x, None, w, torch.tensor(eps, dtype=torch.float32).double().item())[1], group)
+
+
+# ---- zero points above 15 --------------------------------------------------------------------------------------------------------
+
+
+@pytest.mark.parametrize("n,k,group", [(1, 32, 32), (70, 256, 64), (3000, 4096, 128)])
+def test_zero_points_above_15_are_refused(n, k, group):
+    g = gen(n)
+    codes = torch.randint(0, 256, (n, k // 2), generator=g, device=DEV, dtype=torch.uint8)
+    scales = torch.ones(n, k // group, dtype=torch.bfloat16, device=DEV)
+    zeros = torch.randint(0, 16, (n, k // group), generator=g, device=DEV, dtype=torch.uint8)
+    zeros.view(-1)[0] = zeros.view(-1)[-1] = 15
+    x = randn(g, 3, k)
+    w = lk.lckv_quant_pack(codes, scales, zeros)
+    c = torch.stack([codes & 15, codes >> 4], -1).view(n, k)
+    check_linear(lk.lckv_quant_linear(w, x, torch.empty(3, n, device=DEV)), x.double(), c.double() - zeros.double().repeat_interleave(group, 1), k)
+    for at, value in [(0, 16), (-1, 16), (zeros.numel() // 2, 255)]:
+        bad = zeros.clone()
+        bad.view(-1)[at] = value
+        refused(lk.EINVAL, lk.lckv_quant_pack, codes, scales, bad)
