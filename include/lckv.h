@@ -491,8 +491,8 @@ int lckv_rope_apply(const lckv_rope_t* rope, const int32_t* positions, const voi
  *   advance_len   != 0: every len[b], b < batch, grows by n_new afterwards (all slots; needs k_new)
  * The three inputs may be views of one fused projection.  rope->rot_dim <= d_h.
  * Errors: EINVAL (null, shape, overlap, rope->positions < some len[b] + n_new, n_new > max_seq - stream_sink in
- * a sink + recent-window cache), ECAPACITY (some len[b] + n_new > T_cap, or no page left; nothing written),
- * ECUDA.  While `stream` is capturing, the call is refused with EINVAL if advance_len != 0 (the library's
+ * a sink + recent-window cache), ECAPACITY (with k_new: some len[b] + n_new > T_cap, or no page left; nothing
+ * written), ECUDA.  While `stream` is capturing, the call is refused with EINVAL if advance_len != 0 (the library's
  * lengths could not follow the replays) or if new pages are needed (make room with an eager call first).  A replay
  * uses the lengths it finds on the device; a row that has no place there is not written, of a token whose position
  * lies behind the tables nothing is written (neither its row nor its part of q_out), and lckv_cache_status then

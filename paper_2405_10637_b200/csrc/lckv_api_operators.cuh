@@ -152,7 +152,7 @@ int rope_into_cache(lckv_cache* c, int slot, const lckv_rope_t* rope, const void
         if (c->cfg.stream_sink > 0) {
             // no two tokens of one call may share a row of the ring
             if (k && n > c->cfg.max_seq - c->cfg.stream_sink) return LCKV_EINVAL;
-        } else if (longest + n > c->cfg.max_seq) {
+        } else if (k && longest + n > c->cfg.max_seq) {      // (a query alone needs a position, not a row)
             return LCKV_ECAPACITY;
         }
     }

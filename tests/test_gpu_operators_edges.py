@@ -5,7 +5,7 @@ import torch
 
 from paper_2405_10637_b200 import binding as lk
 
-from test_gpu_operators import DEV, E, HALF, check_linear, check_norm, gen, make_weight, make_x, norm64, randn, refused, tables64, within
+from test_gpu_operators import DEV, E, HALF, check_linear, check_norm, gen, make_weight, make_x, norm64, randn, refused, rotate64, tables64, within
 
 pytestmark = pytest.mark.gpu
 
@@ -267,3 +267,27 @@ def test_zero_points_above_15_are_refused(n, k, group):
         bad = zeros.clone()
         bad.view(-1)[at] = value
         refused(lk.EINVAL, lk.lckv_quant_pack, codes, scales, bad)
+
+
+# ---- a query alone behind the last row ----------------------------------------------------------------------------------------
+
+
+@pytest.mark.parametrize("layout", [dict(), dict(page_rows=64, n_pages=4)])
+@pytest.mark.parametrize("rot", [64, 24])
+def test_query_alone_needs_no_row(rot, layout):
+    """A condensed layer's query at the end of a full cache: it has a position, and no row is written for it."""
+    g = gen(rot)
+    c = lk.Cache(lk.make_config(2, 0, 4, 2, 64, 2, 128, **layout))
+    c.lckv_cache_reset([128, 126])
+    pools = [t.fill_(5.0) for t in c.slot_tensors(0)]
+    cos, sin = (t.float() for t in tables64(rot, 131))
+    rope = lk.make_rope(cos, sin)
+    q, k, v = (randn(g, 2, 3, h, 64) for h in (4, 2, 2))
+    out = c.lckv_rope_append_kv(0, rope, q, None, None)
+    pos = torch.tensor([128, 126], device=DEV)[:, None] + torch.arange(3, device=DEV)
+    want, mag = rotate64(q, cos[pos], sin[pos], rot, False)
+    within(out, want, 3 * E * mag * (1 + 2.0 ** -8) + 2.0 ** -8 * want.abs())
+    assert c.lckv_cache_status() == 0 and all(bool((t == 5.0).all()) for t in pools)
+    refused(lk.ECAPACITY, c.lckv_rope_append_kv, 0, rope, q, k, v)
+    refused(lk.EINVAL, c.lckv_rope_append_kv, 0, rope, *(randn(g, 2, 4, 4, 64), None, None))       # position 131 is not there
+    c.close()
