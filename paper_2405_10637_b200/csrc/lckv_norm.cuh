@@ -85,16 +85,16 @@ __device__ __forceinline__ Raw8 norm_load8(const void* base, int is32, int64_t e
     }
     return r;
 }
-// The weights, which every row reads: through the L1.
+// The weights, which every row reads: through the L1.  (Ordinary loads: see lckv_rope.cuh.)
 __device__ __forceinline__ Raw8 norm_weight8(const void* base, int is32, int64_t e)
 {
     Raw8 r;
     if (is32) {
         const uint4* p = reinterpret_cast<const uint4*>(static_cast<const float*>(base) + e);
-        r.a = __ldg(p);
-        r.b = __ldg(p + 1);
+        r.a = p[0];
+        r.b = p[1];
     } else {
-        r.a = __ldg(reinterpret_cast<const uint4*>(static_cast<const uint16_t*>(base) + e));
+        r.a = *reinterpret_cast<const uint4*>(static_cast<const uint16_t*>(base) + e);
     }
     return r;
 }

@@ -141,21 +141,22 @@ template <int N>
 __device__ __forceinline__ void cp_async_wait() { asm volatile("cp.async.wait_group %0;" ::"n"(N) : "memory"); }
 __device__ __forceinline__ void prefetch_l2(const void* p) { asm volatile("prefetch.global.L2 [%0];" ::"l"(p)); }
 
-// A lane's part of x for one half (64 k) of a block and one tile of 8 rows: 4 k of each k16 step of row g, raw.
+// A lane's part of x for one half (64 k) of a block and one tile of 8 rows: 4 k of each k16 step of row g, raw.  (Ordinary loads:
+// see lckv_rope.cuh.)
 template <bool F8> struct QuantX;
 template <> struct QuantX<false> {
     uint2 v[4];
     __device__ __forceinline__ void load(const uint8_t* p)
     {
 #pragma unroll
-        for (int s = 0; s < 4; ++s) v[s] = __ldg(reinterpret_cast<const uint2*>(p + s * 32));
+        for (int s = 0; s < 4; ++s) v[s] = *reinterpret_cast<const uint2*>(p + s * 32);
     }
     __device__ __forceinline__ void load_part(const uint8_t* p, bool in, bool in2)
     {
 #pragma unroll
         for (int s = 0; s < 4; ++s) {
             v[s] = make_uint2(0, 0);
-            if (s < 2 ? in : in2) v[s] = __ldg(reinterpret_cast<const uint2*>(p + s * 32));
+            if (s < 2 ? in : in2) v[s] = *reinterpret_cast<const uint2*>(p + s * 32);
         }
     }
     // k16 step S of the half
@@ -166,14 +167,14 @@ template <> struct QuantX<true> {
     __device__ __forceinline__ void load(const uint8_t* p)
     {
 #pragma unroll
-        for (int s = 0; s < 4; ++s) v[s] = __ldg(reinterpret_cast<const uint32_t*>(p + s * 16));
+        for (int s = 0; s < 4; ++s) v[s] = *reinterpret_cast<const uint32_t*>(p + s * 16);
     }
     __device__ __forceinline__ void load_part(const uint8_t* p, bool in, bool in2)
     {
 #pragma unroll
         for (int s = 0; s < 4; ++s) {
             v[s] = 0;
-            if (s < 2 ? in : in2) v[s] = __ldg(reinterpret_cast<const uint32_t*>(p + s * 16));
+            if (s < 2 ? in : in2) v[s] = *reinterpret_cast<const uint32_t*>(p + s * 16);
         }
     }
     // k16 step S of the half, in fp16
@@ -329,7 +330,7 @@ __global__ void __launch_bounds__(quant_warps(NT) * 32, quant_ctas(FT, NT)) quan
             for (int e = 0; e < 2; ++e) {
                 const int m = m0 + j * 8 + t * 2 + e;
                 px_scale[j][e] = p.x_scale + (int64_t)(m < p.m ? m : p.m - 1) * (p.x_blocks ? p.x_blocks : 1) + (p.x_blocks ? kb0 : 0);
-                xs[j][e] = p.x_blocks && kb0 < kb1 ? __ldg(px_scale[j][e]) : 1.f;
+                xs[j][e] = p.x_blocks && kb0 < kb1 ? *px_scale[j][e] : 1.f;
             }
     }
 
@@ -413,7 +414,7 @@ __global__ void __launch_bounds__(quant_warps(NT) * 32, quant_ctas(FT, NT)) quan
                     for (int hi = 0; hi < 2; ++hi) acc[i][j][hi] = ffma2(x2, blk_sum[i][j][hi], acc[i][j][hi]);
                 if (p.x_blocks && kb + 1 < kb1) {
 #pragma unroll
-                    for (int e = 0; e < 2; ++e) xs[j][e] = __ldg(++px_scale[j][e]);
+                    for (int e = 0; e < 2; ++e) xs[j][e] = *++px_scale[j][e];
                 }
             }
         }
@@ -430,7 +431,7 @@ __global__ void __launch_bounds__(quant_warps(NT) * 32, quant_ctas(FT, NT)) quan
         float xr_scale[2] = {1.f, 1.f};
         if (F8 && !p.x_blocks) {
 #pragma unroll
-            for (int e = 0; e < 2; ++e) xr_scale[e] = __ldg(px_scale[j][e]);
+            for (int e = 0; e < 2; ++e) xr_scale[e] = *px_scale[j][e];
         }
 #pragma unroll
         for (int i = 0; i < FT; ++i)

@@ -353,7 +353,7 @@ quant_tc5_kernel(const Quant5Params p, const __grid_constant__ CUtensorMap tmX)
         float xn[2];
         auto fetch_scales = [&](int k, float& to) {
             const int m = m0 + c0 + lane;
-            to = k < n_k && c0 + lane < NB && m < p.m ? __ldg(p.x_scale + (int64_t)m * p.x_blocks + k_lo + k) : 0.f;
+            to = k < n_k && c0 + lane < NB && m < p.m ? p.x_scale[(int64_t)m * p.x_blocks + k_lo + k] : 0.f;
         };
         if (F8 && p.x_blocks) {
             fetch_scales(0, xn[0]);
@@ -526,7 +526,7 @@ quant_tc5_kernel(const Quant5Params p, const __grid_constant__ CUtensorMap tmX)
             v[0] += u.x; v[1] += u.y; v[2] += u.z; v[3] += u.w;
         }
         if (F8 && !p.x_blocks) {
-            const float xs = __ldg(p.x_scale + m);
+            const float xs = p.x_scale[m];
 #pragma unroll
             for (int e = 0; e < 4; ++e) v[e] *= xs;
         }

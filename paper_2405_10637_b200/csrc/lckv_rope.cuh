@@ -16,6 +16,11 @@
 // interleaved pair lies within them, the other half of a pair in the half layout comes through the warp's corner of
 // shared memory, and the thread serves more heads, since its factors are 16 separate loads (kRopeAnySize).
 // Tensors off the 16-byte grid go pair by pair (kRopePairs).
+//
+// A launch may begin before the kernel in front of it has ended, and any operand may come from that one.  So what is read
+// after griddepcontrol.wait is read with ordinary loads: __ldg promises that the data do not change while the kernel
+// runs, and may be moved in front of the wait.  (The same holds for the norm and the products, whose packed weights alone
+// are complete before.)
 #pragma once
 #include "lckv_attn_mma.cuh"      // cvt_bf16x2
 
@@ -149,7 +154,7 @@ struct RopeUnit {
         pos = pos < 0 ? 0 : (pos < r.positions ? pos : r.positions - 1);
         const float4* pc = reinterpret_cast<const float4*>(r.cos + (int64_t)pos * r.half + u * 8);
         const float4* ps = reinterpret_cast<const float4*>(r.sin + (int64_t)pos * r.half + u * 8);
-        const float4 c0 = __ldg(pc), c1 = __ldg(pc + 1), s0 = __ldg(ps), s1 = __ldg(ps + 1);
+        const float4 c0 = pc[0], c1 = pc[1], s0 = ps[0], s1 = ps[1];
         c[0] = c0.x; c[1] = c0.y; c[2] = c0.z; c[3] = c0.w; c[4] = c1.x; c[5] = c1.y; c[6] = c1.z; c[7] = c1.w;
         s[0] = s0.x; s[1] = s0.y; s[2] = s0.z; s[3] = s0.w; s[4] = s1.x; s[5] = s1.y; s[6] = s1.z; s[7] = s1.w;
 #pragma unroll
@@ -204,8 +209,8 @@ struct RopeAny {
             c[i] = s[i] = 0.f;
             from[i] = 0;
             if (i < n) {
-                c[i] = __ldg(pc + j);
-                s[i] = (low ? -r.sgn : r.sgn) * __ldg(ps + j);
+                c[i] = pc[j];
+                s[i] = (low ? -r.sgn : r.sgn) * ps[j];
                 from[i] = (o & 7) * 32 + first + (o >> 3);
             }
         }
@@ -245,7 +250,7 @@ __device__ __forceinline__ void rope_pair(const RopeArgs& r, int u, int pos, con
         return;
     }
     pos = pos < 0 ? 0 : (pos < r.positions ? pos : r.positions - 1);
-    const float c = __ldg(r.cos + (int64_t)pos * r.half + u), s = r.sgn * __ldg(r.sin + (int64_t)pos * r.half + u);
+    const float c = r.cos[(int64_t)pos * r.half + u], s = r.sgn * r.sin[(int64_t)pos * r.half + u];
     const float a = rope_ld(src + e0), b = rope_ld(src + e1);
     rope_st(dst + e0, fmaf(-b, s, a * c));
     rope_st(dst + e1, fmaf(a, s, b * c));
@@ -288,7 +293,7 @@ __global__ void __launch_bounds__(PATH == kRopeAnySize ? kRopeThreads : kRopeMos
     const int t = w.ok ? w.t : 0;
     const T* x = static_cast<const T*>(p.x) + (int64_t)t * p.x_tok;
     T* y = static_cast<T*>(p.y) + (int64_t)t * p.y_tok;
-    const int pos = __ldg(p.pos + t);
+    const int pos = p.pos[t];
     if constexpr (PATH == kRopeAnySize) {
         RopeAny any;
         any.fetch(p.r, w.u, pos);
@@ -349,7 +354,7 @@ __global__ void __launch_bounds__(PATH == kRopeAnySize ? kRopeThreads : kRopeMos
     if (PATH != kRopeAnySize && !w.ok) return;
     if (!w.ok) w.t = 0;
     const int b = p.n_new == 1 ? w.t : w.t / p.n_new, i = w.t - b * p.n_new;
-    const int len = __ldg(p.lens + b);
+    const int len = p.lens[b];
     if (p.prompt && i >= len) {
         if (PATH != kRopeAnySize) return;
         w.ok = false;
@@ -361,7 +366,7 @@ __global__ void __launch_bounds__(PATH == kRopeAnySize ? kRopeThreads : kRopeMos
     bool place = row >= 0 && row < p.T_cap;
     int64_t row0 = 0, head_step = p.T_cap;        // row of head 0, rows between heads
     if (p.page_table) {
-        const int id = place ? __ldg(p.page_table + (int64_t)b * p.pt_stride + (row >> p.page_shift)) : -1;
+        const int id = place ? p.page_table[(int64_t)b * p.pt_stride + (row >> p.page_shift)] : -1;
         place = place && id >= 0;
         head_step = (int64_t)1 << p.page_shift;
         row0 = (((int64_t)id * p.hkv) << p.page_shift) + (row & (head_step - 1));

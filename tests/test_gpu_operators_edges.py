@@ -291,3 +291,50 @@ def test_query_alone_needs_no_row(rot, layout):
     refused(lk.ECAPACITY, c.lckv_rope_append_kv, 0, rope, q, k, v)
     refused(lk.EINVAL, c.lckv_rope_append_kv, 0, rope, *(randn(g, 2, 4, 4, 64), None, None))       # position 131 is not there
     c.close()
+
+
+# ---- operands that the kernel in front has written ----------------------------------------------------------------------------
+
+
+def test_operands_of_the_kernel_in_front():
+    """A launch may begin before the one in front has ended: tables, positions' products, weights, scales and x that the calls
+    in front wrote into the same memory, queued without a pause, give the bits that they give with a pause after each call."""
+    g = gen(77)
+    T, H, d, width = 64, 16, 128, 2048
+    w, _ = make_weight(g, width, width, 64, True)
+    pos = torch.randint(0, 200, (T,), generator=g, device=DEV, dtype=torch.int32)
+    xs = [randn(g, T, H, d, dtype=torch.float32) for _ in range(3)]
+    scalings = [lk.make_rope_scaling(0, base) for base in (1e4, 5e5, 1e3)]
+    cache = lk.Cache(lk.make_config(2, 0, H, H, d, T, 256))
+    cache.lckv_cache_reset(list(range(T)))
+
+    def chain(pause):
+        cos, sin = (torch.empty(256, d // 2, device=DEV) for _ in range(2))
+        rope = lk.make_rope(cos, sin)
+        turned = torch.empty_like(xs[0])
+        normed, scale = torch.empty(T, width, dtype=torch.float8_e4m3fn, device=DEV), torch.empty(T, width // 128, device=DEV)
+        few = torch.empty(8, width, device=DEV)
+        y, q = torch.empty(T, width, dtype=torch.bfloat16, device=DEV), torch.empty(T, H, d, dtype=torch.bfloat16, device=DEV)
+        outs = []
+        torch.cuda.synchronize()
+        for step in range(12):
+            for call in (lambda: lk.lckv_rope_tables(cos, sin, scalings[step % 3]),
+                         lambda: lk.lckv_rope_apply(rope, pos, xs[step % 3], turned),
+                         # the norm's weight is a row that the rotation has just written
+                         lambda: lk.lckv_rms_norm(turned.view(T, width), turned.view(T, width)[step], normed, out_scale=scale, scale_group=128),
+                         lambda: lk.lckv_quant_linear(w, normed, y, x_scale=scale),
+                         lambda: lk.lckv_quant_linear(w, normed[:8], few, x_scale=scale[:8]),
+                         lambda: lk.lckv_rope_tables(cos, sin, scalings[(step + 1) % 3]),
+                         lambda: cache.lckv_rope_append_kv(0, rope, y.view(T, H, d), y.view(T, H, d), y.view(T, H, d), q)):
+                call()
+                if pause:
+                    torch.cuda.synchronize()
+            outs.append([t.clone() for t in (turned, normed.view(torch.uint8), scale, y, few, q)])
+        torch.cuda.synchronize()
+        return outs
+
+    want = chain(True)
+    for _ in range(5):
+        for got, ref in zip(chain(False), want):
+            assert all(torch.equal(a, b) for a, b in zip(got, ref))
+    cache.close()
