@@ -268,7 +268,10 @@ bool norm_row_fits(int n_vec) { return n_vec <= 512 * kNormMostVectors; }
 // where fp32 tensors make the bytes and not the instructions the bound and rows are short: 2^26 elements, ring / one row
 // per thread block, us, with 512, 2048, 4096, 8192 columns: bf16 49 / 60, 43 / 64, 43 / 70, 44 / 78; bf16 + bf16 94 / 102,
 // 95 / 105, 95 / 109, 95 / 115; bf16 + fp32 148 / 121, 146 / 124, 146 / 128, 148 / 132; fp32 99 / 80, 101 / 84, 101 / 89,
-// 88 / 106; bf16 + fp32 to e4m3 134 / 123, 136 / 128, 114 / 131, 122 / 138.  Nor with an eps of 0 (norm_factor).
+// 88 / 106; bf16 + fp32 to e4m3 134 / 123, 136 / 128, 114 / 131, 122 / 138.  Few more rows than SMs, 150, 300, 512, 1024,
+// 2048 of 4096: bf16 + bf16 2.5 / 2.8, 3.3 / 3.3, 3.6 / 3.6, 5.7 / 6.6, 9.6 / 13.9; to e4m3 by row 3.0 / 3.3, 4.2 / 4.1, 4.5 / 4.4, 7.6 / 7.5,
+// 12.8 / 15.6; bf16 + fp32 to e4m3 3.4 / 3.9, 4.7 / 5.5, 5.6 / 5.9, 9.3 / 10.4, 15.5 / 19.4; of 6656: bf16 + bf16 3.1 / 3.3, 4.2 / 5.4, 5.3 / 6.7,
+// 9.5 / 13.3, 16.4 / 26.1; to e4m3 by row 4.0 / 3.8, 5.5 / 6.2, 7.0 / 7.6, 12.9 / 15.6, 21.4 / 28.0.  Nor with an eps of 0 (norm_factor).
 cudaError_t norm_launch(const lckv::NormParams& p, int n_vec, bool edges, int sms, cudaStream_t st)
 {
     const bool fp32 = p.x32 || (p.r && p.r32);
@@ -601,10 +604,11 @@ int launch_quant_tc5(const lckv::QuantParams& q, int sms, int32_t* status, cudaS
     return cuda_ok(cudaLaunchKernelEx(&cfg, kernel, p, tm)) ? LCKV_OK : LCKV_ECUDA;
 }
 
-// Up to 16 rows: mma.sync kernel, 8 rows a tile; a warp takes 32 or 64 features, whichever shares out better (measured at
-// 1 row, k = 4096: 4096 features 5.5 / 4.6 us, 12288 7.5 / 8.4 us, 22016 12.6 / 13.5 us), 64 for two tiles of rows, where x
-// costs as much to fetch as the weights (16 rows, 22016 features: 22.3 / 16.6 us).  Beyond, the tcgen05 kernel (32 rows,
-// 4096 x 4096: 10.4 us there, 8.6 us here; at 16 rows 7.0 and 7.8 us, with 22016 features 16.6 and 29.0 us).
+// Up to 16 rows: mma.sync kernel, 8 rows a tile; a warp takes 32 or 64 features, whichever the count above says shares out
+// better (measured at 1 row, k = 4096: 4096 features 4.4 / 4.8 us, 12288 7.5 / 8.6 us, 22016 12.4 / 13.4 us; the count takes 32 in the
+// last two and 64 in the first, which was the faster one, 5.5 / 4.6, while a tile of ones corrected for zero points), 64 for two
+// tiles of rows, where x costs as much to fetch as the weights (16 rows, 22016 features: 22.3 / 16.6 us).  Beyond, the tcgen05 kernel
+// (mma.sync / tcgen05, 4096 features: 16 rows 6.8 / 7.9 us, 32 rows 10.2 / 8.6; 22016 features: 16 rows 16.3 / 29.2, 32 rows 27.0 / 30.6).
 template <bool F8, bool ZEROS, int GROUP>
 int launch_quant_rows(lckv::QuantParams& p, int sms, int32_t* status, cudaStream_t st)
 {

@@ -37,7 +37,8 @@ constexpr int kQ5MaxStages = 12;
 
 __host__ __device__ constexpr int q5_fold_warps(int NBMAX) { return NBMAX / 8; }     // 32 columns each, by 4 quadrants
 // Sets of nibble warps, and A buffers.  In e4m3, with half of the nibbles' instructions, two sets suffice, which leaves the
-// fold warps 72 registers a thread and no spills (512 rows, 4096 x 12288: 92.9 / 89.6 us with three / two).
+// fold warps 72 registers a thread (512 rows, 4096 x 12288: 92.9 / 89.6 us with three / two).  Groups of 128 need no more; groups
+// of 64 and 32 still spill a few (stack frames of 8 and 24 to 32 bytes).
 __host__ __device__ constexpr int q5_sets(int NBMAX, bool f8) { return NBMAX > 32 ? (f8 ? 2 : 3) : 4; }
 __host__ __device__ constexpr int q5_threads(int NBMAX, bool f8) { return (4 + q5_fold_warps(NBMAX) + 4 * q5_sets(NBMAX, f8)) * 32; }
 __host__ __device__ constexpr int q5_block(int group, bool zeros)      // bytes of 32 features x 128 k
