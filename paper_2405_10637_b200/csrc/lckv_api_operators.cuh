@@ -146,7 +146,6 @@ int rope_into_cache(lckv_cache* c, int slot, const lckv_rope_t* rope, const void
     if (prompt) {
         if (int rc = prefill_check(c, n, batch, false)) return rc;
         if (longest > rope->positions) return LCKV_EINVAL;
-        if (longest == 0) return LCKV_OK;
     } else {
         if (longest + n > rope->positions) return LCKV_EINVAL;
         if (c->cfg.stream_sink > 0) {

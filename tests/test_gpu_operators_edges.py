@@ -338,3 +338,33 @@ def test_operands_of_the_kernel_in_front():
         for got, ref in zip(chain(False), want):
             assert all(torch.equal(a, b) for a, b in zip(got, ref))
     cache.close()
+
+
+@pytest.mark.parametrize("layout", [dict(), dict(page_rows=64, n_pages=4)])
+def test_prompts_captured_while_they_are_empty(layout):
+    """A call captured at lengths of zero writes the prompts that a replay finds."""
+    g = gen(5)
+    c = lk.Cache(lk.make_config(2, 0, 4, 2, 64, 2, 128, **layout))
+    rope = lk.make_rope(*(t.float() for t in tables64(64, 64)))
+    q, k, v = (randn(g, 2, 9, h, 64) for h in (4, 2, 2))
+    out = torch.full((2, 9, 4, 64), 9.0, dtype=torch.bfloat16, device=DEV)
+    c.lckv_cache_reset([0, 0])
+    c.lckv_rope_prefill_write_kv(0, rope, q, k, v, out)
+    assert bool((out == 9.0).all()) and c.lckv_cache_status() == 0
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        c.lckv_rope_prefill_write_kv(0, rope, q, k, v, out)
+    c.lckv_cache_reset([9, 4])
+    graph.replay()
+    got, pools = out.clone(), [t.clone() for t in c.slot_tensors(0)]
+    want = torch.full_like(out, 9.0)
+    for t in c.slot_tensors(0):
+        t.fill_(0)
+    c.lckv_rope_prefill_write_kv(0, rope, q, k, v, want)
+    assert torch.equal(got, want) and bool((got[1, 4:] == 9.0).all()) and c.lckv_cache_status() == 0
+    table = c.lckv_cache_page_table() if c.cfg.page_rows else None
+    for b, m in ((0, 9), (1, 4)):
+        page = b if table is None else int(table[b, 0])
+        for a, w in zip(pools, c.slot_tensors(0)):
+            assert torch.equal(a[page, :, :m], w[page, :, :m])
+    c.close()
