@@ -454,8 +454,8 @@ typedef struct {
 /*
  * Fills cos and sin, [positions, rot_dim / 2] fp32 on the device, with amplitude * cos(p theta_j) and
  * amplitude * sin(p theta_j), p = 0 .. positions-1.  theta_j is fp64, angles are reduced in 64-bit
- * integers, so far positions are nearly as exact as near ones: sine and cosine are off by at most 1e-7, and the
- * amplitude is rounded to fp32 before it multiplies them.  rot_dim even, 2 .. 128.  Errors: EINVAL (also a base
+ * integers, so far positions are nearly as exact as near ones: sine and cosine of the angle are off by at most 1e-7, the
+ * angle by p times the rounding of theta_j to fp64, and the amplitude is rounded to fp32 before it multiplies them.  rot_dim even, 2 .. 128.  Errors: EINVAL (also a base
  * or a frequency outside fp64's range after scaling), ECUDA.
  */
 int lckv_rope_tables(float* cos, float* sin, int32_t positions, int32_t rot_dim,
@@ -541,7 +541,8 @@ int lckv_rms_norm(const void* x, int64_t x_stride, int32_t x_dtype, const void* 
  *     y[m, f] = sum_c x[m, c] * scales[f, c / group] * (codes[f, c] - zeros[f, c / group])
  * lckv_quant_pack lays a weight out once, lckv_quant_linear multiplies by it.
  *   codes      [n, k / 2] bytes, low nibble = even column
- *   scales     [n, k / group] bf16;  zeros [n, k / group] bytes 0 .. 15, or NULL (8 everywhere)
+ *   scales     [n, k / group] bf16 (below 2^119 for e4m3 x of more than 16 rows, where they are multiplied by 512);
+ *              zeros [n, k / group] bytes 0 .. 15, or NULL (8 everywhere)
  *   group      32, 64 or 128, dividing k
  *   packed     lckv_quant_bytes(n, k, group, zeros != NULL) bytes, 256-byte aligned (0: bad shape)
  *   x          [rows, k], x_stride elements between rows (0 => k), 16-byte aligned rows: bf16 (x_kind 0) or

@@ -309,7 +309,8 @@ def lckv_quant_pack(codes, scales, zeros=None, stream=None):
 
 def lckv_quant_linear(w, x, out=None, x_scale=None, dev_status=None, stream=None):
     """out [rows, n] (bf16 or fp32) = x [rows, k] (bf16, or float8_e4m3fn with x_scale) times the 4-bit weight w.
-    dev_status: optional CUDA int32 tensor that receives ETIMEOUT if a device-side wait gave up."""
+    dev_status: optional CUDA int32 tensor that receives ETIMEOUT if a device-side wait gave up.  The kernel in front of the
+    call must not be one that writes w.buf (lckv_quant_pack never is): the first weights are requested before it has ended."""
     if out is None:
         out = _made(torch.empty, stream, (x.shape[0], w.n), dtype=torch.bfloat16, device=x.device)
     rc = (_CALLS or calls()).quant_linear(*w.call, x, out, x_scale, dev_status,
