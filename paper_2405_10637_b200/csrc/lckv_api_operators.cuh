@@ -265,12 +265,12 @@ bool norm_row_fits(int n_vec) { return n_vec <= 512 * kNormMostVectors; }
 // Few rows (up to one per SM): one vector per thread, the shortest chain.  More: the ring, two vectors per thread
 // (a thread block of 256 threads serves a row of 4096), four where a row has more than 1024 vectors.  Not the ring
 // where fp32 tensors make the bytes and not the instructions the bound and rows are short: 2^26 elements, ring / one row
-// per thread block, us, with 512, 2048, 4096, 8192 columns: bf16 49 / 60, 43 / 64, 43 / 70, 44 / 78; bf16 + bf16 94 / 102,
-// 95 / 105, 95 / 109, 95 / 115; bf16 + fp32 148 / 121, 146 / 124, 146 / 128, 148 / 132; fp32 99 / 80, 101 / 84, 101 / 89,
-// 88 / 106; bf16 + fp32 to e4m3 134 / 123, 136 / 128, 114 / 131, 122 / 138.  Few more rows than SMs, 150, 300, 512, 1024,
+// per thread block, us, with 512, 2048, 4096, 8192 columns: bf16 50 / 61, 45 / 65, 43 / 70, 45 / 77; bf16 + bf16 95 / 103,
+// 98 / 104, 96 / 110, 96 / 116; bf16 + fp32 149 / 121, 150 / 125, 150 / 129, 150 / 133; fp32 to bf16 69 / 67, 68 / 71, 65 / 74,
+// 61 / 80; bf16 + fp32 to e4m3 144 / 120, 138 / 126, 122 / 131, 135 / 138.  Few more rows than SMs, 150, 300, 512, 1024,
 // 2048 of 4096: bf16 + bf16 2.5 / 2.8, 3.3 / 3.3, 3.6 / 3.6, 5.7 / 6.6, 9.6 / 13.9; to e4m3 by row 3.0 / 3.3, 4.2 / 4.1, 4.5 / 4.4, 7.6 / 7.5,
 // 12.8 / 15.6; bf16 + fp32 to e4m3 3.4 / 3.9, 4.7 / 5.5, 5.6 / 5.9, 9.3 / 10.4, 15.5 / 19.4; of 6656: bf16 + bf16 3.1 / 3.3, 4.2 / 5.4, 5.3 / 6.7,
-// 9.5 / 13.3, 16.4 / 26.1; to e4m3 by row 4.0 / 3.8, 5.5 / 6.2, 7.0 / 7.6, 12.9 / 15.6, 21.4 / 28.0.  Nor with an eps of 0 (norm_factor).
+// 9.5 / 13.3, 16.4 / 26.1; to e4m3 by row 4.0 / 3.8, 5.5 / 6.2, 7.0 / 7.6, 12.9 / 15.6, 21.4 / 28.0.  Nor the ring with an eps of 0 (norm_factor).
 cudaError_t norm_launch(const lckv::NormParams& p, int n_vec, bool edges, int sms, cudaStream_t st)
 {
     const bool fp32 = p.x32 || (p.r && p.r32);
