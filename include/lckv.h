@@ -85,6 +85,7 @@ typedef struct {
     int32_t n_pages;       /* pool size per slot when page_rows > 0                            */
     int32_t kernel_kind;   /* 0 = choose (tensor-core kernel for query groups of 2 ... 7 and
                               multiples of 8, else the FP32-ALU kernel); 1 = force FP32-ALU  */
+    int32_t kv_bits;       /* 0 or 16 = bf16 rows; 4 = rows held in 4 bits (see "Rows in 4 bits")    */
 } lckv_config_t;
 
 /* Facts about a built cache that a caller or a benchmark may want. */
@@ -575,6 +576,72 @@ int lckv_quant_linear(const void* packed, int32_t n, int32_t k, int32_t group, i
  * process; a captured call keeps the one that it was captured with.  Errors: EINVAL.
  */
 int lckv_quant_set_copy_limits(int32_t weights, int32_t x);
+
+/*
+ * Rows in 4 bits (kv_bits = 4).  64 neighbouring dimensions of a key or of a value form a group with a lowest
+ * value and a step, both bf16: with the group's smallest and largest element low and high,
+ *     step = bf16((high/16 - low/16) * fp32(16/15)), 0 where below 2^-120
+ *     code = rint((x/16 - low/16) * (1 / (step/16))), ties to even, 0 .. 15        (fp32 throughout)
+ * and the element stands for low + step * code.  A group with an infinity or a NaN stands for NaN.  A row of a kv
+ * head takes d_h + d_h / 8 bytes for key and value, where bf16 takes 4 d_h.  On such a cache
+ *   - lckv_append_kv and lckv_prefill_write_kv take bf16 and write rows in 4 bits; lckv_decode_attention and
+ *     lckv_layer_stack_step (_host) attend to what the rows stand for: codes enter the tensor cores exactly,
+ *     q as well (elements below 2^-25 of the head's largest one are rounded there; |q| < 2^100), everything
+ *     else is fp32, with 22 bits of a row's weight times its step;
+ *   - stream_sink and page_rows work as ever, kernel_kind is 0;
+ *   - lckv_cache_slot_ptrs, lckv_project_append_kv, the keys of lckv_rope_append_kv and
+ *     lckv_rope_prefill_write_kv (rotate with lckv_rope_apply first), lckv_prefill_attention and
+ *     lckv_prefill_iteration return EINVAL.  Prompts are encoded in a bf16 cache; lckv_evict_kv takes them over.
+ *
+ * lckv_cache_read_kv: what the rows 0 .. len[b]-1 of a slot stand for, as tokens (bf16 caches too: the rows).
+ *   k, v       [batch, n_max, H_kv, d_h], bf16 (dtype 0) or fp32 (1), 16-byte aligned; tokens behind a sequence
+ *              are left as they were.  Errors as lckv_prefill_write_kv; EINVAL also if k and v overlap.
+ */
+int lckv_cache_read_kv(lckv_cache_t* cache, int32_t slot, void* k, void* v, int32_t dtype, int32_t n_max,
+                       int32_t batch, void* stream);
+
+/*
+ * The attention weight that a cached row gathers (what an eviction goes by), after lckv_decode_attention over
+ * the same rows:
+ *     weights[b, h, j] = previous[b, h, j] + sum_{q heads i of kv head h} exp(scale * <q[b,i], K[b,h,j]> - lse[b,i])
+ * for the visible rows j (mode as in lckv_decode_attention); entries behind them are left as they were.
+ *   q          [batch, H_q, d_h] bf16, 16-byte aligned; lse [batch, H_q] as lckv_decode_attention wrote it
+ *   previous   fp32 like weights, or NULL for zeros; may be weights itself
+ *   weights    [batch, H_kv, stride] fp32, stride >= max_seq elements between heads (0 => max_seq); row j of a
+ *              cache with stream_sink is the cache's row j
+ * Sums are taken in a fixed order.  Errors: EINVAL (null, shape, alignment, overlap; pages missing while `stream`
+ * is capturing), ECAPACITY as lckv_decode_attention, ECUDA.
+ */
+int lckv_attention_weights(lckv_cache_t* cache, int32_t slot, int32_t mode, const void* q, const float* lse,
+                           const float* previous, float* weights, int64_t stride, int32_t batch, void* stream);
+
+/*
+ * Eviction: of the len[b] rows of every (sequence b, kv head) of src's slot, n_keep stay: the first n_sink, the
+ * last n_recent, and those of the others with the largest weights (of equal ones the lowest rows; a NaN counts as
+ * less than any number).  Where len[b] <= n_keep all stay.  The rows that stay keep their order and become
+ * rows 0, 1, ... of the same sequence and head in dst's slot.
+ *   dst, src   the same cache and slot (in place), or two caches with equal n_kv_heads and head_dim: bf16 to bf16,
+ *              4 bits to 4 bits (codes are copied), or bf16 to 4 bits (rows are encoded on the way; with
+ *              n_keep >= all lengths, a prompt's way into a 4-bit cache).  No stream_sink.  A paged dst takes pages
+ *              for the rows.  Rows of dst behind those that stay are left as they were
+ *   weights    [batch, H_kv, weights_stride] fp32 (0 => src's max_seq), or NULL: all equal
+ *   weights_out  [batch, H_kv, out_stride] fp32 (0 => dst's max_seq), or NULL: the weights of the rows that stay,
+ *              then zeros up to dst's max_seq.  May be weights itself at the same stride
+ *   kept       [batch, H_kv, n_keep] int32: which rows stayed, ascending, then -1
+ *   set_len    != 0: dst's len[b], b < batch, becomes min(src's len[b], n_keep) afterwards.  In place this goes for
+ *              all slots: evict from every slot first, with set_len only in the last call.  Pages behind the
+ *              new lengths go back to the pool
+ * Keys keep the rotation of their token; after an eviction len[b] counts rows and is no longer a position, so new
+ * tokens are rotated by lckv_rope_apply at their positions, not by calls that take the position from len[b].
+ * Errors: EINVAL (null, shape, overlap, n_sink + n_recent > n_keep, n_keep > dst's max_seq, caches that do not
+ * match), ECAPACITY (no page left; nothing written), ECUDA.  While `stream` is capturing the call is refused with
+ * EINVAL if set_len != 0 or if dst needs new pages.  A replay uses the lengths it finds on the device; a row that has no place is left
+ * out, and dst's lckv_cache_status then reports LCKV_ECAPACITY.
+ */
+int lckv_evict_kv(lckv_cache_t* dst, int32_t dst_slot, const lckv_cache_t* src, int32_t src_slot,
+                  const float* weights, int64_t weights_stride, float* weights_out, int64_t out_stride,
+                  int32_t* kept, int32_t n_sink, int32_t n_recent, int32_t n_keep, int32_t batch,
+                  int32_t set_len, void* stream);
 
 /* Short English name of a status code. */
 const char* lckv_status_string(int status);

@@ -22,7 +22,7 @@ class Config(C.Structure):
                 ("max_batch", C.c_int32), ("max_seq", C.c_int32), ("softmax_scale", C.c_float),
                 ("top_variant", C.c_int32), ("out_dtype", C.c_int32), ("host_staging", C.c_int32),
                 ("use_graph", C.c_int32), ("stream_sink", C.c_int32), ("page_rows", C.c_int32), ("n_pages", C.c_int32),
-                ("kernel_kind", C.c_int32)]
+                ("kernel_kind", C.c_int32), ("kv_bits", C.c_int32)]
 
 
 class Info(C.Structure):
@@ -81,6 +81,9 @@ SIGNATURES = {
     "lckv_quant_linear": (C.c_int, [_vp, _i32, _i32, _i32, _i32, _vp, _i64, _i32, _vp, _i32, _vp, _i64, _i32, _i32,
                                     _vp, _vp]),
     "lckv_quant_set_copy_limits": (C.c_int, [_i32, _i32]),
+    "lckv_cache_read_kv": (C.c_int, [_vp, _i32, _vp, _vp, _i32, _i32, _i32, _vp]),
+    "lckv_attention_weights": (C.c_int, [_vp, _i32, _i32, _vp, _vp, _vp, _vp, _i64, _i32, _vp]),
+    "lckv_evict_kv": (C.c_int, [_vp, _i32, _vp, _i32, _vp, _i64, _vp, _i64, _vp, _i32, _i32, _i32, _i32, _i32, _vp]),
     "lckv_status_string": (C.c_char_p, [C.c_int]),
     "lckv_last_cuda_error": (C.c_int, []),
 }
@@ -145,10 +148,10 @@ def lckv_plan(n_layers, n_warmup, top_variant=0):
 
 def make_config(n_layers, n_warmup, n_q_heads, n_kv_heads, head_dim, max_batch, max_seq,
                 softmax_scale=0.0, top_variant=0, out_dtype=0, host_staging=0, use_graph=0,
-                kernel_kind=0, stream_sink=0, page_rows=0, n_pages=0):
+                kernel_kind=0, stream_sink=0, page_rows=0, n_pages=0, kv_bits=0):
     return Config(C.sizeof(Config), n_layers, n_warmup, n_q_heads, n_kv_heads, head_dim,
                   max_batch, max_seq, softmax_scale, top_variant, out_dtype, host_staging,
-                  use_graph, stream_sink, page_rows, n_pages, kernel_kind)
+                  use_graph, stream_sink, page_rows, n_pages, kernel_kind, kv_bits)
 
 
 def lckv_cache_bytes(cfg):
@@ -404,7 +407,7 @@ class Cache:
 
     def slot_tensors(self, slot):
         """torch views of a slot's K and V (same memory): [B_max, H_kv, T_cap, d_h] bf16, or
-        [n_pages, H_kv, page_rows, d_h] for a paged cache."""
+        [n_pages, H_kv, page_rows, d_h] for a paged cache.  Not for rows in 4 bits (lckv_cache_read_kv)."""
         k, v = self.lckv_cache_slot_ptrs(slot)
         c = self.cfg
         shape = (c.max_batch, c.n_kv_heads, c.max_seq, c.head_dim)
@@ -495,3 +498,42 @@ class Cache:
         _chk(lib().lckv_prefill_iteration(self.h, _ptr_array(q_layers), _ptr_array(out_layers),
                                           _ptr_array(k_layers), _ptr_array(v_layers), q0.shape[1],
                                           q0.shape[0], _stream(stream)), "lckv_prefill_iteration")
+
+    # -- compact caches --------------------------------------------------------------------------
+    def lckv_cache_read_kv(self, slot, k, v, stream=None):
+        """Rows 0 .. len-1 of a slot as tokens, into k and v [batch, n_max, H_kv, d_h] (bf16 or fp32); tokens behind a
+        sequence are left as they were.  Returns k, v."""
+        h, dev = self.call
+        rc = (_CALLS or calls()).read_kv(h, dev, slot, *self.heads[1:], k, v, None if stream is None else _address(dev, stream))
+        if rc:
+            _fail(rc, "lckv_cache_read_kv", "k and v are contiguous [batch, n_max, H_kv, d_h], bf16 or fp32 alike, on the cache's device")
+        return k, v
+
+    def lckv_attention_weights(self, slot, mode, q, lse, weights=None, previous=None, stream=None):
+        """weights [batch, H_kv, n] fp32, n >= max_seq: what lckv_decode_attention of q (with its lse) gave every visible
+        row, added to `previous` (zeros if None; may be weights).  Entries behind the visible rows are left as they were (zero
+        where weights is made here).  Returns weights."""
+        h, dev = self.call
+        if weights is None:
+            weights = _made(torch.zeros, stream, (q.shape[0], self.heads[1], self.cfg.max_seq), dtype=torch.float32, device=q.device)
+        rc = (_CALLS or calls()).attention_weights(h, dev, slot, mode, *self.heads, self.cfg.max_seq, q, lse, previous, weights,
+                                                   None if stream is None else _address(dev, stream))
+        if rc:
+            _fail(rc, "lckv_attention_weights", "q is [batch, H_q, d_h] bf16, lse [batch, H_q] fp32, weights and previous [batch, H_kv, n] "
+                                                "fp32 with n >= max_seq, contiguous, on the cache's device")
+        return weights
+
+    def lckv_evict_kv(self, slot, src, src_slot, kept, weights=None, weights_out=None, n_sink=0, n_recent=0, set_len=0, stream=None):
+        """Of src's slot (this cache's own, in place, or another cache's) kept.shape[2] rows of every (sequence, kv head) stay,
+        the first n_sink, the last n_recent and the heaviest others, and become this slot's first rows.  kept [batch, H_kv, n_keep]
+        int32 receives which; weights [batch, H_kv, n >= src max_seq] fp32; weights_out [batch, H_kv, n >= max_seq] fp32 receives
+        the weights of the rows that stay (may be weights).  set_len: this cache's lengths become min(len, n_keep).
+        Returns kept."""
+        h, dev = self.call
+        rc = (_CALLS or calls()).evict_kv(h, dev, slot, *src.call, src_slot, self.heads[1], src.cfg.max_seq, self.cfg.max_seq, kept, weights,
+                                          weights_out, n_sink, n_recent, 1 if set_len else 0,
+                                          None if stream is None else _address(dev, stream))
+        if rc:
+            _fail(rc, "lckv_evict_kv", "kept is [batch, H_kv, n_keep] int32, weights and weights_out [batch, H_kv, n] fp32 with n >= the "
+                                       "max_seq of their cache, contiguous, all on the caches' device")
+        return kept

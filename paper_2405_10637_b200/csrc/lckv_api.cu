@@ -9,6 +9,7 @@
 #include <cstring>
 #include <mutex>
 #include <new>
+#include <type_traits>
 #include <vector>
 
 #include "../../include/lckv.h"
@@ -23,6 +24,8 @@
 #include "lckv_norm.cuh"
 #include "lckv_quant.cuh"
 #include "lckv_quant_tc5.cuh"
+#include "lckv_attn_packed.cuh"
+#include "lckv_evict.cuh"
 
 namespace {
 
@@ -130,9 +133,18 @@ struct lckv_cache {
 
 namespace {
 
+// The caller's configuration with the fields that a caller built before they existed does not have (their default: 0).
+int read_config(const lckv_config_t* c, lckv_config_t* out)
+{
+    if (!c || (c->struct_size != sizeof(lckv_config_t) && c->struct_size != offsetof(lckv_config_t, kv_bits))) return LCKV_EINVAL;
+    std::memset(out, 0, sizeof(*out));
+    std::memcpy(out, c, c->struct_size);
+    out->struct_size = sizeof(*out);
+    return LCKV_OK;
+}
+
 int validate_config(const lckv_config_t* c)
 {
-    if (!c || c->struct_size != sizeof(lckv_config_t)) return LCKV_EINVAL;
     if (c->n_layers < 1 || c->n_q_heads < 1 || c->n_kv_heads < 1) return LCKV_EINVAL;
     if (c->n_q_heads % c->n_kv_heads) return LCKV_EINVAL;
     if (c->head_dim != 64 && c->head_dim != 128) return LCKV_EINVAL;
@@ -140,6 +152,8 @@ int validate_config(const lckv_config_t* c)
     if (!(c->softmax_scale >= 0.f) || !std::isfinite(c->softmax_scale)) return LCKV_EINVAL;
     if (c->out_dtype != 0 && c->out_dtype != 1) return LCKV_EINVAL;
     if (c->kernel_kind != 0 && c->kernel_kind != 1) return LCKV_EINVAL;
+    if (c->kv_bits != 0 && c->kv_bits != 16 && c->kv_bits != 4) return LCKV_EINVAL;
+    if (c->kv_bits == 4 && c->kernel_kind != 0) return LCKV_EINVAL;
     if (c->stream_sink < 0 || (c->stream_sink > 0 && c->stream_sink >= c->max_seq)) return LCKV_EINVAL;
     if (c->page_rows != 0) {
         const int P = c->page_rows;
@@ -150,12 +164,15 @@ int validate_config(const lckv_config_t* c)
     // tile counts are kept in 32 bits
     const uint64_t tiles = (uint64_t)c->max_batch * (((uint64_t)c->max_seq + 15) / 16);
     if (tiles >= (1ull << 31)) return LCKV_EINVAL;
+    // ... those of all pairs as well, over 4-bit rows
+    if (c->kv_bits == 4 && (uint64_t)c->max_batch * (((uint64_t)c->max_seq + 63) / 64) * (uint64_t)c->n_q_heads >= (1ull << 32)) return LCKV_EINVAL;
     return LCKV_OK;
 }
 
-// 1 = FP32-ALU kernel, 2 = tensor-core kernel (query groups of 2 ... 7 and multiples of 8).
+// 1 = FP32-ALU kernel, 2 = tensor-core kernel (query groups of 2 ... 7 and multiples of 8), 3 = the kernel for 4-bit rows.
 int resolve_kernel_kind(const lckv_config_t& c)
 {
+    if (c.kv_bits == 4) return 3;
     const int g = c.n_q_heads / c.n_kv_heads;
     // the tensor-core kernel addresses cache rows through 32-bit TMA coordinates
     const uint64_t rows = c.page_rows ? (uint64_t)c.n_pages * c.n_kv_heads * (uint64_t)c.page_rows
@@ -166,21 +183,26 @@ int resolve_kernel_kind(const lckv_config_t& c)
     return (c.kernel_kind == 0 && fits && rows < (1ull << 31)) ? 2 : 1;
 }
 
-// Query heads per pair of the tensor-core kernel: 8, or the whole group when it is smaller.
+// Query heads per pair of the tensor-core kernels: 8, or the whole group when it is smaller; over 4-bit rows, whatever the
+// group, its largest divisor up to 8.
 int mma_heads_per_pair(const lckv_config_t& c)
 {
     const int g = c.n_q_heads / c.n_kv_heads;
-    return g < 8 ? g : 8;
+    if (c.kv_bits != 4) return g < 8 ? g : 8;
+    int n = g < 8 ? g : 8;
+    while (g % n) --n;
+    return n;
 }
 
 int workers_per_sm(const lckv_config_t& c)
 {
+    if (resolve_kernel_kind(c) == 3) return lckv::kPackedWarps;
     return resolve_kernel_kind(c) == 2 ? lckv::kMmaWarps * lckv::kMmaCtas : lckv::kAluWarps * lckv::kAluCtas;
 }
 
 int partial_record_floats(const lckv_config_t& c)
 {
-    return resolve_kernel_kind(c) == 2 ? c.head_dim * 8 + 16 : c.head_dim + 4;
+    return resolve_kernel_kind(c) >= 2 ? c.head_dim * 8 + 16 : c.head_dim + 4;
 }
 
 typedef CUresult (*EncodeTiledFn)(CUtensorMap*, CUtensorMapDataType, cuuint32_t, void*,
@@ -231,6 +253,13 @@ int make_tensor_map_pitch(CUtensorMap* tm, void* base, uint64_t rows, uint64_t c
     return make_tensor_map_typed(tm, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 64, base, rows, cols, pitch_bytes, box_rows);
 }
 
+// Rows between the (sequence, kv head)s of a slot that is not paged: 4-bit slots hold whole tiles of 64 rows.
+int64_t row_pitch(const lckv_config_t& c) { return c.kv_bits == 4 ? (int64_t)align_up((size_t)c.max_seq, lckv::kPackedRows) : c.max_seq; }
+int64_t slot_rows(const lckv_config_t& c)
+{
+    return c.page_rows ? (int64_t)c.n_pages * c.n_kv_heads * c.page_rows : (int64_t)c.max_batch * c.n_kv_heads * row_pitch(c);
+}
+
 void make_layout(const lckv_config_t& c, int n_slots, int n_workers, int n_kv_layers, Layout& y)
 {
     const size_t A = 256;
@@ -246,6 +275,8 @@ void make_layout(const lckv_config_t& c, int n_slots, int n_workers, int n_kv_la
     y.slot_bytes =
         c.page_rows ? align_up((size_t)c.n_pages * c.n_kv_heads * (size_t)c.page_rows * c.head_dim * 2, A)
                     : align_up((size_t)c.max_batch * c.n_kv_heads * (size_t)c.max_seq * c.head_dim * 2, A);
+    // a 4-bit slot is one piece of two such halves: keys' codes, values' codes, groups' parameters
+    if (c.kv_bits == 4) y.slot_bytes = align_up((size_t)slot_rows(c) * (c.head_dim / 2 + c.head_dim / 16), A);
     y.off_pt = off;
     if (c.page_rows)
         off = align_up(off + (size_t)c.max_batch * ((c.max_seq + c.page_rows - 1) / c.page_rows) * 4, A);
@@ -280,6 +311,27 @@ uint16_t* slot_v(const lckv_cache* c, int s)
 {
     return reinterpret_cast<uint16_t*>(c->base + c->lay.off_slots +
                                        (size_t)(2 * s + 1) * c->lay.slot_bytes);
+}
+
+lckv::PackedSlot packed_slot(const lckv_cache* c, int s)
+{
+    lckv::PackedSlot p;
+    const int64_t codes = slot_rows(c->cfg) * (c->cfg.head_dim / 2);
+    p.kc = c->base + c->lay.off_slots + (size_t)(2 * s) * c->lay.slot_bytes;
+    p.vc = p.kc + codes;
+    p.par = reinterpret_cast<uint32_t*>(p.vc + codes);
+    return p;
+}
+
+lckv::RowMap row_map(const lckv_cache* c)
+{
+    lckv::RowMap m;
+    m.page_table = c->cfg.page_rows ? c->d_pt : nullptr;
+    m.pitch = row_pitch(c->cfg);
+    m.H_kv = c->cfg.n_kv_heads;
+    m.pt_stride = c->pt_stride;
+    m.page_shift = c->page_shift;
+    return m;
 }
 
 // Longest sequence, for capacity checks; 0 in streaming mode (a ring never overflows).
@@ -364,6 +416,7 @@ int sync_page_table(lckv_cache* c, cudaStream_t st)
 
 int launch_plan(lckv_cache* c, int batch, cudaStream_t st)
 {
+    if (c->kernel_kind == 3) return LCKV_OK;     // the kernel over 4-bit rows works its shares out by itself
     lckv::plan_kernel<<<1, 1024, 0, st>>>(c->d_lens, batch, c->rows_per_tile, c->h_pairs,
                                           c->active_workers, c->d_pre, c->lay.pre_stride, c->d_start,
                                           c->cfg.max_seq);
@@ -387,6 +440,22 @@ cudaError_t launch_pdl(void (*kernel)(KArgs...), int grid, int block, size_t sme
     cfg.attrs = attr;
     cfg.numAttrs = 1;
     return cudaLaunchKernelEx(&cfg, kernel, args...);
+}
+
+// The kernel over 4-bit rows for a configuration: columns for a pair's query heads, and what the outputs' type asks for.
+template <int D, bool PAGED>
+void (*packed_variant_of(int heads, bool exact))(lckv::PackedParams)
+{
+    if (heads <= 2) return exact ? lckv::attn_packed_kernel<D, PAGED, 2, true> : lckv::attn_packed_kernel<D, PAGED, 2, false>;
+    if (heads <= 4) return exact ? lckv::attn_packed_kernel<D, PAGED, 4, true> : lckv::attn_packed_kernel<D, PAGED, 4, false>;
+    return exact ? lckv::attn_packed_kernel<D, PAGED, 8, true> : lckv::attn_packed_kernel<D, PAGED, 8, false>;
+}
+void (*packed_variant(const lckv_config_t& c))(lckv::PackedParams)
+{
+    const int heads = mma_heads_per_pair(c);
+    const bool exact = c.out_dtype == 1;
+    if (c.head_dim == 128) return c.page_rows ? packed_variant_of<128, true>(heads, exact) : packed_variant_of<128, false>(heads, exact);
+    return c.page_rows ? packed_variant_of<64, true>(heads, exact) : packed_variant_of<64, false>(heads, exact);
 }
 
 // early: the previous kernel in the stream is an attention launch of the same step and this one
@@ -425,7 +494,19 @@ int launch_attention(lckv_cache* c, int slot, int mode, const void* q, void* out
     p.page_shift = c->page_shift;
     const bool paged = c->cfg.page_rows != 0;
     cudaError_t e;
-    if (c->kernel_kind == 2) {
+    if (c->kernel_kind == 3) {
+        lckv::PackedParams pp;
+        pp.m.a = p;
+        pp.m.a.H_q = c->h_pairs;
+        pp.m.n_q_heads = c->cfg.n_q_heads;
+        pp.m.heads_per_pair = mma_heads_per_pair(c->cfg);
+        pp.m.groups_per_kv = c->cfg.n_q_heads / c->cfg.n_kv_heads / pp.m.heads_per_pair;
+        pp.s = packed_slot(c, slot);
+        pp.pitch = row_pitch(c->cfg);
+        const bool wide = c->cfg.head_dim == 128;
+        e = launch_pdl(packed_variant(c->cfg), c->grid, lckv::kPackedWarps * 32,
+                       wide ? lckv::packed_smem_bytes<128>() : lckv::packed_smem_bytes<64>(), st, pp);
+    } else if (c->kernel_kind == 2) {
         lckv::MmaParams mp;
         mp.a = p;
         mp.a.H_q = c->h_pairs;  // pairs per sequence = groups of up to 8 query heads
@@ -453,9 +534,31 @@ int launch_attention(lckv_cache* c, int slot, int mode, const void* q, void* out
     return cuda_ok(e) ? LCKV_OK : LCKV_ECUDA;
 }
 
+// Rows written in 4 bits: the new token of every sequence, or prompts of up to n tokens.
+int launch_packed_write(lckv_cache* c, int slot, const void* k, const void* v, int n, bool prompt, int batch, cudaStream_t st)
+{
+    lckv::PackedWriteParams p;
+    p.s = packed_slot(c, slot);
+    p.map = row_map(c);
+    p.k = static_cast<const uint16_t*>(k);
+    p.v = static_cast<const uint16_t*>(v);
+    p.lens = c->d_lens;
+    p.T_cap = c->cfg.max_seq;
+    p.batch = batch;
+    p.n = n;
+    p.n_sink = c->cfg.stream_sink;
+    p.prompt = prompt ? 1 : 0;
+    const int64_t threads = (int64_t)batch * n * c->cfg.n_kv_heads * (c->cfg.head_dim / 4);
+    if (threads / 256 >= INT32_MAX) return LCKV_EINVAL;
+    const cudaError_t e = launch_pdl(c->cfg.head_dim == 128 ? lckv::packed_write_kernel<128> : lckv::packed_write_kernel<64>,
+                                     (int)((threads + 255) / 256), 256, 0, st, p);
+    return cuda_ok(e) ? LCKV_OK : LCKV_ECUDA;
+}
+
 int launch_append(lckv_cache* c, int slot, const void* k_new, const void* v_new, int batch,
                   cudaStream_t st)
 {
+    if (c->cfg.kv_bits == 4) return launch_packed_write(c, slot, k_new, v_new, 1, false, batch, st);
     const int64_t n = (int64_t)batch * c->cfg.n_kv_heads * (c->cfg.head_dim / 8);
     const int threads = 256;
     const int blocks = (int)((n + threads - 1) / threads);
@@ -485,7 +588,8 @@ float step_keep_frac(const lckv_cache* c, int batch)
     int64_t rows = 0;
     for (int b = 0; b < batch; ++b)
         rows += c->h_lens[b] < c->cfg.max_seq ? c->h_lens[b] : c->cfg.max_seq;
-    const double bytes = (double)rows * 4.0 * c->cfg.n_kv_heads * c->cfg.head_dim;
+    const double row_bytes = c->cfg.kv_bits == 4 ? c->cfg.head_dim + c->cfg.head_dim / 8 : 4.0 * c->cfg.head_dim;
+    const double bytes = (double)rows * c->cfg.n_kv_heads * row_bytes;
     if (bytes <= 0 || c->l2_keep_bytes <= 0) return 0.f;
     const double f = std::fmin(1.0, c->l2_keep_bytes / bytes);
     return (float)(std::floor(f * 16.0) / 16.0);
@@ -625,6 +729,7 @@ int prefill_check(const lckv_cache* c, int n_max, int batch, bool attention)
 int launch_prefill_write(lckv_cache* c, int slot, const void* k, const void* v, int n_max,
                          int batch, cudaStream_t st)
 {
+    if (c->cfg.kv_bits == 4) return launch_packed_write(c, slot, k, v, n_max, true, batch, st);
     const int64_t n = (int64_t)batch * n_max * c->cfg.n_kv_heads * (c->cfg.head_dim / 8);
     const int threads = 256;
     lckv::prefill_write_kv_kernel<<<(unsigned)((n + threads - 1) / threads), threads, 0, st>>>(
@@ -738,9 +843,11 @@ int lckv_plan(int32_t n_layers, int32_t n_warmup, int32_t top_variant, int32_t* 
     return LCKV_OK;
 }
 
-size_t lckv_cache_bytes(const lckv_config_t* cfg)
+size_t lckv_cache_bytes(const lckv_config_t* given)
 {
-    if (validate_config(cfg)) return 0;
+    lckv_config_t full;
+    if (read_config(given, &full) || validate_config(&full)) return 0;
+    const lckv_config_t* cfg = &full;
     int sm = 0;
     if (device_sm_count(&sm)) return 0;
     Plan pl;
@@ -752,9 +859,12 @@ size_t lckv_cache_bytes(const lckv_config_t* cfg)
     return y.total_bytes;
 }
 
-int lckv_cache_alloc(lckv_cache_t** out, const lckv_config_t* cfg, void* dev_buf, size_t dev_bytes)
+int lckv_cache_alloc(lckv_cache_t** out, const lckv_config_t* given, void* dev_buf, size_t dev_bytes)
 {
     if (!out || !dev_buf) return LCKV_EINVAL;
+    lckv_config_t full;
+    if (int rc = read_config(given, &full)) return rc;
+    const lckv_config_t* cfg = &full;
     if (int rc = validate_config(cfg)) return rc;
     if (reinterpret_cast<uintptr_t>(dev_buf) % 256) return LCKV_ENOMEM;
     int sm = 0;
@@ -766,12 +876,12 @@ int lckv_cache_alloc(lckv_cache_t** out, const lckv_config_t* cfg, void* dev_buf
     c->n_kv_layers = 0;
     for (int l = 0; l < cfg->n_layers; ++l) c->n_kv_layers += c->plan.write_slot[l] >= 0;
     c->sm_count = sm;
-    c->grid = sm * (resolve_kernel_kind(*cfg) == 2 ? lckv::kMmaCtas : lckv::kAluCtas);
+    c->grid = resolve_kernel_kind(*cfg) == 3 ? sm : sm * (resolve_kernel_kind(*cfg) == 2 ? lckv::kMmaCtas : lckv::kAluCtas);
     c->n_workers = sm * workers_per_sm(*cfg);
     c->active_workers = c->n_workers;
     c->kernel_kind = resolve_kernel_kind(*cfg);
-    c->rows_per_tile = (c->kernel_kind == 2 ? lckv::kMmaSlotBytes : lckv::kAluSlotBytes) / (cfg->head_dim * 2);
-    c->h_pairs = c->kernel_kind == 2 ? cfg->n_q_heads / mma_heads_per_pair(*cfg) : cfg->n_q_heads;
+    c->rows_per_tile = c->kernel_kind == 3 ? lckv::kPackedRows : (c->kernel_kind == 2 ? lckv::kMmaSlotBytes : lckv::kAluSlotBytes) / (cfg->head_dim * 2);
+    c->h_pairs = c->kernel_kind >= 2 ? cfg->n_q_heads / mma_heads_per_pair(*cfg) : cfg->n_q_heads;
     make_layout(*cfg, c->plan.n_slots, c->n_workers, c->n_kv_layers, c->lay);
     if (dev_bytes < c->lay.total_bytes) { delete c; return LCKV_ENOMEM; }
     const float scale = cfg->softmax_scale > 0.f ? cfg->softmax_scale
@@ -827,7 +937,7 @@ int lckv_cache_alloc(lckv_cache_t** out, const lckv_config_t* cfg, void* dev_buf
             if (rc) { delete c; return rc; }
         }
     }
-    {
+    if (cfg->kv_bits != 4) {
         // prompt-encoding kernel: 64-row boxes over every slot (coordinates are 32-bit)
         const uint64_t rows = cfg->page_rows
                                   ? (uint64_t)cfg->n_pages * cfg->n_kv_heads * (uint64_t)cfg->page_rows
@@ -881,6 +991,10 @@ int lckv_cache_alloc(lckv_cache_t** out, const lckv_config_t* cfg, void* dev_buf
               cuda_ok(cudaFuncSetAttribute(lckv::attn_alu_kernel<64>,
                                            cudaFuncAttributeMaxDynamicSharedMemorySize,
                                            lckv::kAluSmemBytes)) &&
+              (cfg->kv_bits != 4 ||
+               cuda_ok(cudaFuncSetAttribute(packed_variant(*cfg), cudaFuncAttributeMaxDynamicSharedMemorySize,
+                                            cfg->head_dim == 128 ? lckv::packed_smem_bytes<128>()
+                                                                 : lckv::packed_smem_bytes<64>()))) &&
               cuda_ok(cudaMemset(c->base, 0, c->lay.workspace_bytes)) &&
               cuda_ok(cudaDeviceSynchronize());
     if (!ok) { delete c; return LCKV_ECUDA; }
@@ -906,7 +1020,7 @@ int lckv_cache_info(const lckv_cache_t* c, lckv_info_t* info)
     info->n_workers = c->n_workers;
     info->rows_per_tile = c->rows_per_tile;
     info->kernel_kind = c->kernel_kind;
-    int launches = 2 + c->cfg.n_layers + c->n_kv_layers;  // plan + advance + attention + appends
+    int launches = (c->kernel_kind == 3 ? 1 : 2) + c->cfg.n_layers + c->n_kv_layers;  // plan + advance + attention + appends
     info->launches_per_step = launches;
     info->sm_count = c->sm_count;
     info->slot_bytes = c->lay.slot_bytes;
@@ -977,6 +1091,7 @@ int lckv_cache_set_worker_limit(lckv_cache_t* c, int32_t workers)
 int lckv_cache_slot_ptrs(const lckv_cache_t* c, int32_t slot, void** k, void** v)
 {
     if (!c || !k || !v || slot < 0 || slot >= c->plan.n_slots) return LCKV_EINVAL;
+    if (c->cfg.kv_bits == 4) return LCKV_EINVAL;   // no such tensors: lckv_cache_read_kv gives the rows' values
     *k = slot_k(c, slot);
     *v = slot_v(c, slot);
     return LCKV_OK;
@@ -1037,6 +1152,7 @@ int lckv_project_append_kv(lckv_cache_t* c, int32_t slot, const void* x, int32_t
                            int32_t advance_len, void* stream)
 {
     if (!c || !x || !w_k || !w_v || batch < 1 || batch > c->cfg.max_batch) return LCKV_EINVAL;
+    if (c->cfg.kv_bits == 4) return LCKV_EINVAL;
     if (slot < 0 || slot >= c->plan.n_slots) return LCKV_EINVAL;
     const int D = c->cfg.head_dim, F = c->cfg.n_kv_heads * D;
     if (d_model < 64 || d_model % 64 || F % lckv::kProjBM) return LCKV_EINVAL;
@@ -1481,3 +1597,4 @@ extern "C" int lckv_decode_attention_static(const void* k, const void* v, const 
 }
 
 #include "lckv_api_operators.cuh"
+#include "lckv_api_packed.cuh"

@@ -120,6 +120,7 @@ int rope_into_cache(lckv_cache* c, int slot, const lckv_rope_t* rope, const void
 {
     if (!c || batch < 1 || batch > c->cfg.max_batch || n < 1) return LCKV_EINVAL;
     if (slot < 0 || slot >= c->plan.n_slots) return LCKV_EINVAL;
+    if (k && c->cfg.kv_bits == 4) return LCKV_EINVAL;       // (rotate, then lckv_append_kv)
     if ((q == nullptr) != (q_out == nullptr) || (k == nullptr) != (v == nullptr) || (!q && !k)) return LCKV_EINVAL;
     if (advance_len && !k) return LCKV_EINVAL;
     const int d = c->cfg.head_dim, hq = q ? c->cfg.n_q_heads : 0, hkv = k ? c->cfg.n_kv_heads : 0;

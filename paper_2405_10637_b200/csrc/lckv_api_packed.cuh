@@ -1,0 +1,229 @@
+// C entry points of compact caches: reading rows back, gathered attention weights, eviction.  Included at the end of
+// lckv_api.cu (they share its cache object and helpers).
+#pragma once
+
+namespace {
+
+// Does sequence b < batch own pages for its first rows[b] rows, on the device too?
+bool pages_cover(const lckv_cache* c, const std::vector<int>& rows)
+{
+    if (!c->cfg.page_rows) return true;
+    if (c->pt_dirty) return false;
+    for (size_t b = 0; b < rows.size(); ++b)
+        if (((int64_t)c->n_pages_of[b] << c->page_shift) < rows[b]) return false;
+    return true;
+}
+
+// Pages for the first rows[b] rows of every sequence; on exhaustion nothing changes.
+int cover_pages(lckv_cache* c, const std::vector<int>& rows)
+{
+    if (!c->cfg.page_rows) return LCKV_OK;
+    size_t need = 0;
+    for (size_t b = 0; b < rows.size(); ++b)
+        need += (size_t)std::max(0, ((rows[b] + c->cfg.page_rows - 1) >> c->page_shift) - c->n_pages_of[b]);
+    if (need > c->free_pages.size()) return LCKV_ECAPACITY;
+    for (size_t b = 0; b < rows.size(); ++b)
+        while (((int64_t)c->n_pages_of[b] << c->page_shift) < rows[b]) {
+            c->h_pt[b * c->pt_stride + c->n_pages_of[b]++] = c->free_pages.back();
+            c->free_pages.pop_back();
+            c->pt_dirty = true;
+        }
+    return LCKV_OK;
+}
+
+// Pages behind the first rows[b] rows go back to the pool.
+void release_pages(lckv_cache* c, const std::vector<int>& rows)
+{
+    if (!c->cfg.page_rows) return;
+    for (size_t b = 0; b < rows.size(); ++b)
+        while (c->n_pages_of[b] > 0 && ((int64_t)(c->n_pages_of[b] - 1) << c->page_shift) >= rows[b]) {
+            int32_t& e = c->h_pt[b * c->pt_stride + --c->n_pages_of[b]];
+            c->free_pages.push_back(e);
+            e = -1;
+            c->pt_dirty = true;
+        }
+}
+
+template <bool PACKED>
+cudaError_t launch_move(const lckv::MoveParams& p, int d, int64_t items, bool in_place, int64_t heads, cudaStream_t st)
+{
+    if (in_place)
+        return launch_pdl_dims(d == 128 ? lckv::evict_in_place_kernel<128, PACKED> : lckv::evict_in_place_kernel<64, PACKED>, dim3((unsigned)heads),
+                               dim3(1024), 0, st, p);
+    const int64_t units = d == 128 ? lckv::RowUnits<128, PACKED>::kUnits : lckv::RowUnits<64, PACKED>::kUnits;
+    return launch_pdl_dims(d == 128 ? lckv::evict_move_kernel<128, PACKED> : lckv::evict_move_kernel<64, PACKED>,
+                           dim3((unsigned)((items * units + 255) / 256)), dim3(256), 0, st, p, items);
+}
+
+}  // namespace
+
+extern "C" {
+
+int lckv_cache_read_kv(lckv_cache_t* c, int32_t slot, void* k, void* v, int32_t dtype, int32_t n_max, int32_t batch, void* stream)
+{
+    if (!c || !k || !v || slot < 0 || slot >= c->plan.n_slots || (dtype != 0 && dtype != 1)) return LCKV_EINVAL;
+    if (!aligned(k, 16) || !aligned(v, 16)) return LCKV_EINVAL;
+    if (int rc = prefill_check(c, n_max, batch, false)) return rc;
+    const int d = c->cfg.head_dim;
+    const int64_t threads = (int64_t)batch * n_max * c->cfg.n_kv_heads * (d / 4), bytes = threads * 4 * (dtype ? 4 : 2);
+    if (ranges_meet(k, bytes, v, bytes) || ranges_meet(k, bytes, c->base, (int64_t)c->lay.total_bytes) ||
+        ranges_meet(v, bytes, c->base, (int64_t)c->lay.total_bytes) || threads / 256 >= INT32_MAX)
+        return LCKV_EINVAL;
+    cudaStream_t st = static_cast<cudaStream_t>(stream);
+    if (int rc = sync_page_table(c, st)) return rc;
+    lckv::RowReadParams p;
+    p.s = packed_slot(c, slot);
+    p.K = c->cfg.kv_bits == 4 ? nullptr : slot_k(c, slot);
+    p.V = slot_v(c, slot);
+    p.map = row_map(c);
+    p.lens = c->d_lens;
+    p.k = k;
+    p.v = v;
+    p.T_cap = c->cfg.max_seq;
+    p.batch = batch;
+    p.n = n_max;
+    p.f32 = dtype;
+    const cudaError_t e = launch_pdl_dims(d == 128 ? lckv::row_read_kernel<128> : lckv::row_read_kernel<64>, dim3((unsigned)((threads + 255) / 256)),
+                                          dim3(256), 0, st, p);
+    return cuda_ok(e) ? LCKV_OK : LCKV_ECUDA;
+}
+
+int lckv_attention_weights(lckv_cache_t* c, int32_t slot, int32_t mode, const void* q, const float* lse, const float* previous, float* weights,
+                           int64_t stride, int32_t batch, void* stream)
+{
+    if (!c || !q || !lse || !weights || batch < 1 || batch > c->cfg.max_batch) return LCKV_EINVAL;
+    if (slot < 0 || slot >= c->plan.n_slots) return LCKV_EINVAL;
+    if (mode != LCKV_MODE_CONDENSED && mode != LCKV_MODE_STANDARD) return LCKV_EINVAL;
+    if (stride == 0) stride = c->cfg.max_seq;
+    if (stride < c->cfg.max_seq || !aligned(q, 16) || !aligned(lse, 4) || !aligned(previous, 4) || !aligned(weights, 4)) return LCKV_EINVAL;
+    const int64_t rows = (int64_t)batch * c->cfg.n_kv_heads, heads = (int64_t)batch * c->cfg.n_q_heads;
+    if (rows > INT32_MAX) return LCKV_EINVAL;
+    const int64_t bytes = ((rows - 1) * stride + c->cfg.max_seq) * 4;
+    if ((previous && previous != weights && ranges_meet(weights, bytes, previous, bytes)) || ranges_meet(weights, bytes, q, heads * c->cfg.head_dim * 2) ||
+        ranges_meet(weights, bytes, lse, heads * 4) || ranges_meet(weights, bytes, c->base, (int64_t)c->lay.total_bytes))
+        return LCKV_EINVAL;
+    if (max_len(c, batch) + mode > c->cfg.max_seq) return LCKV_ECAPACITY;
+    cudaStream_t st = static_cast<cudaStream_t>(stream);
+    int rc = LCKV_OK;
+    const bool capture = capturing(st, &rc);
+    if (rc) return rc;
+    if (capture && !pages_ready(c, batch, mode)) return LCKV_EINVAL;
+    if (int rc2 = ensure_pages(c, batch, mode)) return rc2;
+    if (int rc2 = sync_page_table(c, st)) return rc2;
+    lckv::WeightParams p;
+    p.s = packed_slot(c, slot);
+    p.K = slot_k(c, slot);
+    p.map = row_map(c);
+    p.lens = c->d_lens;
+    p.q = static_cast<const uint16_t*>(q);
+    p.lse = lse;
+    p.prev = previous;
+    p.weights = weights;
+    p.T_cap = c->cfg.max_seq;
+    p.stride = stride;
+    p.H_q = c->cfg.n_q_heads;
+    p.mode = mode;
+    p.scale_log2 = c->scale_log2;
+    // thread blocks for the longest sequence that the host knows; they go on behind it if a replay finds longer ones
+    int64_t longest = 1;
+    for (int b = 0; b < batch; ++b) longest = std::max<int64_t>(longest, std::min(c->h_lens[b], c->cfg.max_seq - mode) + mode);
+    const int64_t chunk = 64 * lckv::kWeightWarps;
+    const dim3 grid((unsigned)rows, (unsigned)std::min<int64_t>(65535, (longest + chunk - 1) / chunk));
+    const bool packed = c->cfg.kv_bits == 4;
+    const auto kernel = c->cfg.head_dim == 128 ? (packed ? lckv::attention_weights_kernel<128, true> : lckv::attention_weights_kernel<128, false>)
+                                               : (packed ? lckv::attention_weights_kernel<64, true> : lckv::attention_weights_kernel<64, false>);
+    return cuda_ok(launch_pdl_dims(kernel, grid, dim3(32 * lckv::kWeightWarps), 0, st, p)) ? LCKV_OK : LCKV_ECUDA;
+}
+
+int lckv_evict_kv(lckv_cache_t* dst, int32_t dst_slot, const lckv_cache_t* src, int32_t src_slot, const float* weights, int64_t weights_stride,
+                  float* weights_out, int64_t out_stride, int32_t* kept, int32_t n_sink, int32_t n_recent, int32_t n_keep, int32_t batch,
+                  int32_t set_len, void* stream)
+{
+    if (!dst || !src || !kept || batch < 1 || batch > dst->cfg.max_batch || batch > src->cfg.max_batch) return LCKV_EINVAL;
+    if (dst_slot < 0 || dst_slot >= dst->plan.n_slots || src_slot < 0 || src_slot >= src->plan.n_slots) return LCKV_EINVAL;
+    const bool in_place = dst == src;
+    if (in_place && dst_slot != src_slot) return LCKV_EINVAL;
+    const int d = src->cfg.head_dim, hkv = src->cfg.n_kv_heads;
+    if (dst->cfg.head_dim != d || dst->cfg.n_kv_heads != hkv || dst->cfg.stream_sink > 0 || src->cfg.stream_sink > 0) return LCKV_EINVAL;
+    if (src->cfg.kv_bits == 4 && dst->cfg.kv_bits != 4) return LCKV_EINVAL;
+    if (n_keep < 1 || n_keep > dst->cfg.max_seq || n_sink < 0 || n_recent < 0 || (int64_t)n_sink + n_recent > n_keep) return LCKV_EINVAL;
+    if (weights_stride == 0) weights_stride = src->cfg.max_seq;
+    if (out_stride == 0) out_stride = dst->cfg.max_seq;
+    if (weights_stride < src->cfg.max_seq || out_stride < dst->cfg.max_seq) return LCKV_EINVAL;
+    if (!aligned(weights, 4) || !aligned(weights_out, 4) || !aligned(kept, 4)) return LCKV_EINVAL;
+    const int64_t rows = (int64_t)batch * hkv, items = rows * n_keep;
+    if (rows > INT32_MAX || items * (d / 4) / 256 >= INT32_MAX) return LCKV_EINVAL;
+    const int64_t w_bytes = ((rows - 1) * weights_stride + src->cfg.max_seq) * 4, o_bytes = ((rows - 1) * out_stride + dst->cfg.max_seq) * 4;
+    const bool same = weights_out && weights_out == weights && out_stride == weights_stride;
+    if (weights && weights_out && !same && ranges_meet(weights, w_bytes, weights_out, o_bytes)) return LCKV_EINVAL;
+    if ((weights && ranges_meet(kept, items * 4, weights, w_bytes)) || (weights_out && ranges_meet(kept, items * 4, weights_out, o_bytes))) return LCKV_EINVAL;
+    for (const lckv_cache* c : {(const lckv_cache*)dst, src}) {
+        const int64_t total = (int64_t)c->lay.total_bytes;
+        if (ranges_meet(kept, items * 4, c->base, total) || (weights_out && ranges_meet(weights_out, o_bytes, c->base, total))) return LCKV_EINVAL;
+    }
+    std::vector<int> count(batch);
+    for (int b = 0; b < batch; ++b) count[b] = std::min(src->h_lens[b], n_keep);
+    cudaStream_t st = static_cast<cudaStream_t>(stream);
+    int rc = LCKV_OK;
+    const bool capture = capturing(st, &rc);
+    if (rc) return rc;
+    if (src->pt_dirty && !in_place) return LCKV_EINVAL;     // (no call has brought the source's pages to the device yet)
+    if (capture && (set_len || !pages_cover(dst, count))) return LCKV_EINVAL;
+    if (int rc2 = cover_pages(dst, count)) return rc2;
+    if (int rc2 = sync_page_table(dst, st)) return rc2;
+
+    lckv::SelectParams s;
+    s.weights = weights;
+    s.weights_out = weights_out;
+    s.kept = kept;
+    s.lens = src->d_lens;
+    s.lens_out = set_len && !in_place ? dst->d_lens : nullptr;
+    s.stride = weights_stride;
+    s.out_stride = out_stride;
+    s.T_cap = src->cfg.max_seq;
+    s.H_kv = hkv;
+    s.n_sink = n_sink;
+    s.n_recent = n_recent;
+    s.n_keep = n_keep;
+    s.out_rows = dst->cfg.max_seq;
+    s.keys = std::min(src->cfg.max_seq, lckv::kSelectMostKeys);
+    const size_t smem = (size_t)s.keys * 4;
+    if (smem > 40 * 1024 &&
+        !cuda_ok(cudaFuncSetAttribute(lckv::evict_select_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, lckv::kSelectMostKeys * 4)))
+        return LCKV_ECUDA;
+    if (!cuda_ok(launch_pdl_dims(lckv::evict_select_kernel, dim3((unsigned)rows), dim3(lckv::kSelectThreads), smem, st, s))) return LCKV_ECUDA;
+
+    lckv::MoveParams p;
+    p.from = packed_slot(src, src_slot);
+    p.to = packed_slot(dst, dst_slot);
+    p.K = slot_k(src, src_slot);
+    p.V = slot_v(src, src_slot);
+    p.K_to = slot_k(dst, dst_slot);
+    p.V_to = slot_v(dst, dst_slot);
+    p.map = row_map(src);
+    p.map_to = row_map(dst);
+    p.kept = kept;
+    p.lens = src->d_lens;
+    p.lens_out = set_len && in_place ? dst->d_lens : nullptr;
+    p.status = dst->d_status;
+    p.T_cap = src->cfg.max_seq;
+    p.batch = batch;
+    p.n_keep = n_keep;
+    cudaError_t e;
+    if (src->cfg.kv_bits == 4) {
+        e = launch_move<true>(p, d, items, in_place, rows, st);
+    } else if (dst->cfg.kv_bits == 4) {
+        const dim3 grid((unsigned)((items * (d / 4) + 255) / 256));
+        e = launch_pdl_dims(d == 128 ? lckv::evict_pack_kernel<128> : lckv::evict_pack_kernel<64>, grid, dim3(256), 0, st, p, items);
+    } else {
+        e = launch_move<false>(p, d, items, in_place, rows, st);
+    }
+    if (!cuda_ok(e)) return LCKV_ECUDA;
+    if (set_len) {
+        for (int b = 0; b < batch; ++b) dst->h_lens[b] = count[b];
+        release_pages(dst, count);
+    }
+    return LCKV_OK;
+}
+
+}  // extern "C"

@@ -232,8 +232,70 @@ PyObject* rope_cache(Args& a)
     });
 }
 
+// cache, its device, slot, H_kv, d, k, v, stream
+PyObject* read_kv(Args& a)
+{
+    auto* cache = static_cast<lckv_cache_t*>(a.address());
+    const int64_t dev = a.integer();
+    const int32_t slot = a.integer32();
+    const int64_t hkv = a.integer(), d = a.integer();
+    const at::Tensor *k = a.tensor(), *v = a.tensor();
+    if (!a.ok || !cache || !k || !v || k->dim() != 4 || k->sizes() != v->sizes() || k->size(2) != hkv || k->size(3) != d) return code(kBadTensor);
+    const int kind = float_kind(k);
+    if (kind < 0 || !dense(k, k->scalar_type(), dev) || !dense(v, k->scalar_type(), dev) || k->size(0) > INT32_MAX || k->size(1) > INT32_MAX) return code(kBadTensor);
+    return run(a, dev, [&](void* st) { return lckv_cache_read_kv(cache, slot, mut(k), mut(v), kind, (int32_t)k->size(1), (int32_t)k->size(0), st); });
+}
+
+// fp32 [batch, heads, n] with n >= rows
+bool weights_like(const at::Tensor* t, int64_t dev, int64_t batch, int64_t heads, int64_t rows)
+{
+    return dense(t, at::kFloat, dev) && t->dim() == 3 && t->size(0) == batch && t->size(1) == heads && t->size(2) >= rows;
+}
+
+// cache, its device, slot, mode, H_q, H_kv, d, max_seq, q, lse, previous, weights, stream
+PyObject* attention_weights(Args& a)
+{
+    auto* cache = static_cast<lckv_cache_t*>(a.address());
+    const int64_t dev = a.integer();
+    const int32_t slot = a.integer32(), mode = a.integer32();
+    const int64_t hq = a.integer(), hkv = a.integer(), d = a.integer(), rows = a.integer();
+    const at::Tensor *q = a.tensor(), *lse = a.tensor(), *prev = a.tensor(), *w = a.tensor();
+    if (!a.ok || !cache || !q || !lse || !w || !dense(q, at::kBFloat16, dev) || q->dim() != 3 || q->size(1) != hq || q->size(2) != d) return code(kBadTensor);
+    const int64_t batch = q->size(0);
+    if (!dense(lse, at::kFloat, dev) || lse->dim() != 2 || lse->size(0) != batch || lse->size(1) != hq || batch > INT32_MAX) return code(kBadTensor);
+    if (!weights_like(w, dev, batch, hkv, rows) || (prev && (!weights_like(prev, dev, batch, hkv, rows) || prev->size(2) != w->size(2)))) return code(kBadTensor);
+    return run(a, dev, [&](void* st) {
+        return lckv_attention_weights(cache, slot, mode, ptr(q), static_cast<const float*>(ptr(lse)), static_cast<const float*>(ptr(prev)),
+                                      static_cast<float*>(mut(w)), w->size(2), (int32_t)batch, st);
+    });
+}
+
+// cache, its device, slot, source cache, its device, its slot, H_kv, the source's max_seq, the cache's, kept, weights, weights_out, n_sink,
+// n_recent, set_len, stream
+PyObject* evict_kv(Args& a)
+{
+    auto* cache = static_cast<lckv_cache_t*>(a.address());
+    const int64_t dev = a.integer();
+    const int32_t slot = a.integer32();
+    const auto* src = static_cast<const lckv_cache_t*>(a.address());
+    const int64_t src_dev = a.integer();
+    const int32_t src_slot = a.integer32();
+    const int64_t hkv = a.integer(), src_rows = a.integer(), rows = a.integer();
+    const at::Tensor *kept = a.tensor(), *w = a.tensor(), *out = a.tensor();
+    const int32_t sink = a.integer32(), recent = a.integer32(), set_len = a.integer32();
+    if (!a.ok || !cache || !src || src_dev != dev || !kept || !dense(kept, at::kInt, dev) || kept->dim() != 3 || kept->size(1) != hkv) return code(kBadTensor);
+    const int64_t batch = kept->size(0), keep = kept->size(2);
+    if (batch > INT32_MAX || keep > INT32_MAX) return code(kBadTensor);
+    if ((w && !weights_like(w, dev, batch, hkv, src_rows)) || (out && !weights_like(out, dev, batch, hkv, rows))) return code(kBadTensor);
+    return run(a, dev, [&](void* st) {
+        return lckv_evict_kv(cache, slot, src, src_slot, static_cast<const float*>(ptr(w)), w ? w->size(2) : 0, static_cast<float*>(mut(out)),
+                             out ? out->size(2) : 0, static_cast<int32_t*>(mut(kept)), sink, recent, (int32_t)keep, (int32_t)batch, set_len, st);
+    });
+}
+
 #define LCKV_CALL(name) {#name, reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)(void)>(entry<name>)), METH_FASTCALL, nullptr}
 PyMethodDef methods[] = {LCKV_CALL(rope_tables), LCKV_CALL(rope_apply), LCKV_CALL(rms_norm), LCKV_CALL(quant_linear), LCKV_CALL(rope_cache),
+                         LCKV_CALL(read_kv), LCKV_CALL(attention_weights), LCKV_CALL(evict_kv),
                          {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_lckv_calls", "Per-layer calls of liblckv.so on torch tensors.", -1, methods, nullptr, nullptr, nullptr, nullptr};
 
