@@ -534,6 +534,18 @@ int launch_attention(lckv_cache* c, int slot, int mode, const void* q, void* out
     return cuda_ok(e) ? LCKV_OK : LCKV_ECUDA;
 }
 
+template <typename... KArgs, typename... Args>
+cudaError_t launch_pdl_dims(void (*kernel)(KArgs...), dim3 grid, dim3 block, size_t smem, cudaStream_t st, Args... args);
+
+// Thread blocks over the (kRowTokens tokens, kv head) items of `tokens` tokens of each of `seqs` sequences.
+bool row_grid(const lckv_cache* c, int64_t tokens, int seqs, dim3* grid)
+{
+    const int64_t items = (tokens + lckv::kRowTokens - 1) / lckv::kRowTokens * c->cfg.n_kv_heads;
+    const int64_t per = c->cfg.head_dim == 128 ? lckv::rows_per_block<128>() : lckv::rows_per_block<64>();
+    *grid = dim3((unsigned)((items + per - 1) / per), (unsigned)std::min(seqs, 65535));
+    return items <= INT32_MAX - per && tokens <= INT32_MAX - lckv::kRowTokens;      // (the kernels count both in 32 bits)
+}
+
 // Rows written in 4 bits: the new token of every sequence, or prompts of up to n tokens.
 int launch_packed_write(lckv_cache* c, int slot, const void* k, const void* v, int n, bool prompt, int batch, cudaStream_t st)
 {
@@ -548,10 +560,10 @@ int launch_packed_write(lckv_cache* c, int slot, const void* k, const void* v, i
     p.n = n;
     p.n_sink = c->cfg.stream_sink;
     p.prompt = prompt ? 1 : 0;
-    const int64_t threads = (int64_t)batch * n * c->cfg.n_kv_heads * (c->cfg.head_dim / 4);
-    if (threads / 256 >= INT32_MAX) return LCKV_EINVAL;
-    const cudaError_t e = launch_pdl(c->cfg.head_dim == 128 ? lckv::packed_write_kernel<128> : lckv::packed_write_kernel<64>,
-                                     (int)((threads + 255) / 256), 256, 0, st, p);
+    dim3 grid;
+    if (!row_grid(c, prompt ? n : batch, prompt ? batch : 1, &grid)) return LCKV_EINVAL;
+    const cudaError_t e = launch_pdl_dims(c->cfg.head_dim == 128 ? lckv::packed_write_kernel<128> : lckv::packed_write_kernel<64>, grid,
+                                          dim3(lckv::kRowThreads), 0, st, p);
     return cuda_ok(e) ? LCKV_OK : LCKV_ECUDA;
 }
 

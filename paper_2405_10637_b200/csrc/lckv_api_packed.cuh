@@ -44,15 +44,35 @@ void release_pages(lckv_cache* c, const std::vector<int>& rows)
         }
 }
 
-template <bool PACKED>
-cudaError_t launch_move(const lckv::MoveParams& p, int d, int64_t items, bool in_place, int64_t heads, cudaStream_t st)
+// Thread blocks for `units` pieces of every (sequence, kv head), `per` a block.
+dim3 move_grid(int64_t heads, int64_t units, int64_t per) { return dim3((unsigned)heads, (unsigned)std::min<int64_t>(65535, (units + per - 1) / per)); }
+
+template <int D, bool PACKED>
+cudaError_t launch_move(const lckv::MoveParams& p, bool in_place, int64_t heads, cudaStream_t st)
 {
-    if (in_place)
-        return launch_pdl_dims(d == 128 ? lckv::evict_in_place_kernel<128, PACKED> : lckv::evict_in_place_kernel<64, PACKED>, dim3((unsigned)heads),
-                               dim3(1024), 0, st, p);
-    const int64_t units = d == 128 ? lckv::RowUnits<128, PACKED>::kUnits : lckv::RowUnits<64, PACKED>::kUnits;
-    return launch_pdl_dims(d == 128 ? lckv::evict_move_kernel<128, PACKED> : lckv::evict_move_kernel<64, PACKED>,
-                           dim3((unsigned)((items * units + 255) / 256)), dim3(256), 0, st, p, items);
+    if (in_place) return launch_pdl_dims(lckv::evict_in_place_kernel<D, PACKED>, dim3((unsigned)heads), dim3(1024), 0, st, p);
+    const dim3 grid = move_grid(heads, (int64_t)p.n_keep * lckv::RowUnits<D, PACKED>::kUnits, lckv::kRowThreads * lckv::kMoveUnits);
+    return launch_pdl_dims(lckv::evict_move_kernel<D, PACKED>, grid, dim3(lckv::kRowThreads), 0, st, p);
+}
+
+// The smallest thread block that holds the rows.
+cudaError_t launch_select(const lckv::SelectParams& s, int64_t most, int64_t heads, cudaStream_t st)
+{
+    const dim3 grid((unsigned)heads);
+    if (most <= 1024) return launch_pdl_dims(lckv::evict_select_kernel<128, 8>, grid, dim3(128), 0, st, s);
+    if (most <= 4096) return launch_pdl_dims(lckv::evict_select_kernel<256, 16>, grid, dim3(256), 0, st, s);
+    if (most <= 8192) return launch_pdl_dims(lckv::evict_select_kernel<512, 16>, grid, dim3(512), 0, st, s);
+    if (most <= 32768) return launch_pdl_dims(lckv::evict_select_kernel<1024, 32>, grid, dim3(1024), 0, st, s);
+    return launch_pdl_dims(lckv::evict_select_kernel<1024, 0>, grid, dim3(1024), 0, st, s);
+}
+
+template <int D, bool PACKED>
+cudaError_t launch_weights(const lckv::WeightParams& p, int group, dim3 grid, cudaStream_t st)
+{
+    const auto kernel = group <= 2   ? lckv::attention_weights_kernel<D, PACKED, 2>
+                        : group <= 4 ? lckv::attention_weights_kernel<D, PACKED, 4>
+                                     : lckv::attention_weights_kernel<D, PACKED, 8>;
+    return launch_pdl_dims(kernel, grid, dim3(32 * lckv::kWeightWarps), 0, st, p);
 }
 
 }  // namespace
@@ -65,15 +85,16 @@ int lckv_cache_read_kv(lckv_cache_t* c, int32_t slot, void* k, void* v, int32_t 
     if (!aligned(k, 16) || !aligned(v, 16)) return LCKV_EINVAL;
     if (int rc = prefill_check(c, n_max, batch, false)) return rc;
     const int d = c->cfg.head_dim;
-    const int64_t threads = (int64_t)batch * n_max * c->cfg.n_kv_heads * (d / 4), bytes = threads * 4 * (dtype ? 4 : 2);
+    const int64_t bytes = (int64_t)batch * n_max * c->cfg.n_kv_heads * d * (dtype ? 4 : 2);
+    dim3 grid;
     if (ranges_meet(k, bytes, v, bytes) || ranges_meet(k, bytes, c->base, (int64_t)c->lay.total_bytes) ||
-        ranges_meet(v, bytes, c->base, (int64_t)c->lay.total_bytes) || threads / 256 >= INT32_MAX)
+        ranges_meet(v, bytes, c->base, (int64_t)c->lay.total_bytes) || !row_grid(c, n_max, batch, &grid))
         return LCKV_EINVAL;
     cudaStream_t st = static_cast<cudaStream_t>(stream);
     if (int rc = sync_page_table(c, st)) return rc;
     lckv::RowReadParams p;
     p.s = packed_slot(c, slot);
-    p.K = c->cfg.kv_bits == 4 ? nullptr : slot_k(c, slot);
+    p.K = slot_k(c, slot);
     p.V = slot_v(c, slot);
     p.map = row_map(c);
     p.lens = c->d_lens;
@@ -82,9 +103,12 @@ int lckv_cache_read_kv(lckv_cache_t* c, int32_t slot, void* k, void* v, int32_t 
     p.T_cap = c->cfg.max_seq;
     p.batch = batch;
     p.n = n_max;
-    p.f32 = dtype;
-    const cudaError_t e = launch_pdl_dims(d == 128 ? lckv::row_read_kernel<128> : lckv::row_read_kernel<64>, dim3((unsigned)((threads + 255) / 256)),
-                                          dim3(256), 0, st, p);
+    const bool packed = c->cfg.kv_bits == 4;
+    const auto kernel = d == 128 ? (packed ? (dtype ? lckv::row_read_kernel<128, true, true> : lckv::row_read_kernel<128, true, false>)
+                                           : (dtype ? lckv::row_read_kernel<128, false, true> : lckv::row_read_kernel<128, false, false>))
+                                 : (packed ? (dtype ? lckv::row_read_kernel<64, true, true> : lckv::row_read_kernel<64, true, false>)
+                                           : (dtype ? lckv::row_read_kernel<64, false, true> : lckv::row_read_kernel<64, false, false>));
+    const cudaError_t e = launch_pdl_dims(kernel, grid, dim3(lckv::kRowThreads), 0, st, p);
     return cuda_ok(e) ? LCKV_OK : LCKV_ECUDA;
 }
 
@@ -124,15 +148,22 @@ int lckv_attention_weights(lckv_cache_t* c, int32_t slot, int32_t mode, const vo
     p.H_q = c->cfg.n_q_heads;
     p.mode = mode;
     p.scale_log2 = c->scale_log2;
-    // thread blocks for the longest sequence that the host knows; they go on behind it if a replay finds longer ones
     int64_t longest = 1;
     for (int b = 0; b < batch; ++b) longest = std::max<int64_t>(longest, std::min(c->h_lens[b], c->cfg.max_seq - mode) + mode);
-    const int64_t chunk = 64 * lckv::kWeightWarps;
-    const dim3 grid((unsigned)rows, (unsigned)std::min<int64_t>(65535, (longest + chunk - 1) / chunk));
+    // tiles of 64 rows per warp: as many as leave 16 warps an SM (q is prepared once per run), up to eight
+    const int64_t tiles = (longest + 63) / 64;
+    p.run = (int)std::max<int64_t>(1, std::min<int64_t>(8, tiles * rows / (16 * (int64_t)c->sm_count)));
+    p.runs = (int)((tiles + p.run - 1) / p.run);
+    p.heads = (int)rows;
+    // (a warp whose sequence turns out longer in a replay goes on behind the last run)
+    const int64_t blocks = ((int64_t)p.runs * rows + lckv::kWeightWarps - 1) / lckv::kWeightWarps;
+    if (blocks > INT32_MAX) return LCKV_EINVAL;
+    const dim3 grid((unsigned)blocks);
     const bool packed = c->cfg.kv_bits == 4;
-    const auto kernel = c->cfg.head_dim == 128 ? (packed ? lckv::attention_weights_kernel<128, true> : lckv::attention_weights_kernel<128, false>)
-                                               : (packed ? lckv::attention_weights_kernel<64, true> : lckv::attention_weights_kernel<64, false>);
-    return cuda_ok(launch_pdl_dims(kernel, grid, dim3(32 * lckv::kWeightWarps), 0, st, p)) ? LCKV_OK : LCKV_ECUDA;
+    const int group = c->cfg.n_q_heads / c->cfg.n_kv_heads;
+    const cudaError_t e = c->cfg.head_dim == 128 ? (packed ? launch_weights<128, true>(p, group, grid, st) : launch_weights<128, false>(p, group, grid, st))
+                                                 : (packed ? launch_weights<64, true>(p, group, grid, st) : launch_weights<64, false>(p, group, grid, st));
+    return cuda_ok(e) ? LCKV_OK : LCKV_ECUDA;
 }
 
 int lckv_evict_kv(lckv_cache_t* dst, int32_t dst_slot, const lckv_cache_t* src, int32_t src_slot, const float* weights, int64_t weights_stride,
@@ -152,7 +183,7 @@ int lckv_evict_kv(lckv_cache_t* dst, int32_t dst_slot, const lckv_cache_t* src, 
     if (weights_stride < src->cfg.max_seq || out_stride < dst->cfg.max_seq) return LCKV_EINVAL;
     if (!aligned(weights, 4) || !aligned(weights_out, 4) || !aligned(kept, 4)) return LCKV_EINVAL;
     const int64_t rows = (int64_t)batch * hkv, items = rows * n_keep;
-    if (rows > INT32_MAX || items * (d / 4) / 256 >= INT32_MAX) return LCKV_EINVAL;
+    if (rows > INT32_MAX || (int64_t)n_keep * (d / 4) > INT32_MAX) return LCKV_EINVAL;    // (units of a head are counted in 32 bits)
     const int64_t w_bytes = ((rows - 1) * weights_stride + src->cfg.max_seq) * 4, o_bytes = ((rows - 1) * out_stride + dst->cfg.max_seq) * 4;
     const bool same = weights_out && weights_out == weights && out_stride == weights_stride;
     if (weights && weights_out && !same && ranges_meet(weights, w_bytes, weights_out, o_bytes)) return LCKV_EINVAL;
@@ -186,12 +217,11 @@ int lckv_evict_kv(lckv_cache_t* dst, int32_t dst_slot, const lckv_cache_t* src, 
     s.n_recent = n_recent;
     s.n_keep = n_keep;
     s.out_rows = dst->cfg.max_seq;
-    s.keys = std::min(src->cfg.max_seq, lckv::kSelectMostKeys);
-    const size_t smem = (size_t)s.keys * 4;
-    if (smem > 40 * 1024 &&
-        !cuda_ok(cudaFuncSetAttribute(lckv::evict_select_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, lckv::kSelectMostKeys * 4)))
-        return LCKV_ECUDA;
-    if (!cuda_ok(launch_pdl_dims(lckv::evict_select_kernel, dim3((unsigned)rows), dim3(lckv::kSelectThreads), smem, st, s))) return LCKV_ECUDA;
+    // A replay may find any length up to the capacity; an eager call's are known.
+    int64_t most = 1;
+    for (int b = 0; b < batch; ++b) most = std::max<int64_t>(most, src->h_lens[b]);
+    if (capture) most = src->cfg.max_seq;
+    if (!cuda_ok(launch_select(s, most, rows, st))) return LCKV_ECUDA;
 
     lckv::MoveParams p;
     p.from = packed_slot(src, src_slot);
@@ -211,12 +241,12 @@ int lckv_evict_kv(lckv_cache_t* dst, int32_t dst_slot, const lckv_cache_t* src, 
     p.n_keep = n_keep;
     cudaError_t e;
     if (src->cfg.kv_bits == 4) {
-        e = launch_move<true>(p, d, items, in_place, rows, st);
+        e = d == 128 ? launch_move<128, true>(p, in_place, rows, st) : launch_move<64, true>(p, in_place, rows, st);
     } else if (dst->cfg.kv_bits == 4) {
-        const dim3 grid((unsigned)((items * (d / 4) + 255) / 256));
-        e = launch_pdl_dims(d == 128 ? lckv::evict_pack_kernel<128> : lckv::evict_pack_kernel<64>, grid, dim3(256), 0, st, p, items);
+        e = d == 128 ? launch_pdl_dims(lckv::evict_pack_kernel<128>, move_grid(rows, n_keep, lckv::rows_per_block<128>() * lckv::kRowTokens), dim3(lckv::kRowThreads), 0, st, p)
+                     : launch_pdl_dims(lckv::evict_pack_kernel<64>, move_grid(rows, n_keep, lckv::rows_per_block<64>() * lckv::kRowTokens), dim3(lckv::kRowThreads), 0, st, p);
     } else {
-        e = launch_move<false>(p, d, items, in_place, rows, st);
+        e = d == 128 ? launch_move<128, false>(p, in_place, rows, st) : launch_move<64, false>(p, in_place, rows, st);
     }
     if (!cuda_ok(e)) return LCKV_ECUDA;
     if (set_len) {

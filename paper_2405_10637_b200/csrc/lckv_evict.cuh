@@ -17,119 +17,155 @@ struct WeightParams {
     float* weights;
     int64_t T_cap, stride;
     int32_t H_q, mode;
+    int32_t run;              // consecutive tiles of 64 rows per warp
+    int32_t runs, heads;      // such runs per (sequence, kv head), and those
     float scale_log2;
 };
 
-// weights[b, h, j] = prev[b, h, j] + sum over the query heads of kv head h of exp(s_j - lse), for the visible rows j.
-// One thread block per (sequence, kv head) and 256 rows, a warp per 64.  The keys go straight from memory into MMA
-// fragments: the four lanes of a row take 16 bytes each, which fixes the order of the dimensions, and q follows it.
+// A row's part of an MMA fragment: the four lanes of a row take 16 bytes (4 bits, D = 64: 8) at a time.
 template <int D, bool PACKED>
+struct KeyFragment {
+    static constexpr int J = D / 32;
+    typename std::conditional<PACKED, uint32_t, uint4>::type w[J];
+    __device__ __forceinline__ void load(const WeightParams& p, int64_t row, int c4)
+    {
+        if constexpr (!PACKED) {
+            const uint4* x = reinterpret_cast<const uint4*>(p.K + row * D) + c4;
+#pragma unroll
+            for (int j = 0; j < J; ++j) w[j] = x[4 * j];
+        } else if constexpr (D == 128) {
+            const uint4 x = *reinterpret_cast<const uint4*>(p.s.kc + row * 64 + c4 * 16);
+            w[0] = x.x; w[1] = x.y; w[2] = x.z; w[3] = x.w;
+        } else {
+            const uint2 x = *reinterpret_cast<const uint2*>(p.s.kc + row * 32 + c4 * 8);
+            w[0] = x.x; w[1] = x.y;
+        }
+    }
+};
+
+// weights[b, h, j] = prev[b, h, j] + sum over the query heads of kv head h of exp(s_j - lse), for the visible rows j.
+//
+// A warp takes `run` tiles of 64 rows of one (sequence, kv head).  Keys go straight from memory into MMA fragments, all of a
+// tile (bf16, D = 128: of half a tile) under way before the first is used; the order in which a row's four lanes take its
+// dimensions is the order in which q enters.  QP columns hold query heads (up to eight at a time), and their NC = 8 / QP
+// copies share the exponentials as in lckv_attn_packed.cuh: copy k has every NC-th block of 16 rows.  Of the QP / 2 lanes
+// that end up with a row's sum each writes another block's.
+template <int D, bool PACKED, int QP>
 __global__ void __launch_bounds__(kWeightWarps * 32) attention_weights_kernel(const WeightParams p)
 {
-    constexpr int J = D / 32, G = D / 64;
+    constexpr int J = D / 32, G = D / 64, NC = 8 / QP, NB = 4 / NC;
+    constexpr int LOAD = !PACKED && D == 128 && NC <= 2 ? 2 : 4;     // blocks whose keys are loaded at once
     pdl_wait_then_release();
     const uint32_t FULL = 0xffffffffu;
-    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, g4 = lane >> 2, c4 = lane & 3;
-    const int b = blockIdx.x / p.map.H_kv, h = blockIdx.x % p.map.H_kv;
+    const int lane = threadIdx.x & 31, g4 = lane >> 2, c4 = lane & 3;
+    const int copy = 2 * c4 / QP, q0 = 2 * c4 % QP, mine = q0 / 2;
+    const int64_t unit = (int64_t)blockIdx.x * kWeightWarps + (threadIdx.x >> 5);
+    if (unit >= (int64_t)p.heads * p.runs) return;
+    const int bh = (int)(unit / p.runs), b = bh / p.map.H_kv, h = bh - b * p.map.H_kv;
     const int nv = visible_rows(p.lens[b], p.mode, p.T_cap);
     const int group = p.H_q / p.map.H_kv;
     const int64_t head0 = (int64_t)b * p.H_q + (int64_t)h * group;
-    const int64_t w0 = ((int64_t)b * p.map.H_kv + h) * p.stride;
-    for (int64_t r64 = ((int64_t)blockIdx.y * kWeightWarps + warp) * 64; r64 < nv; r64 += (int64_t)gridDim.y * kWeightWarps * 64) {
-        const int base = (int)r64, rows = min(64, nv - base);
-        const int64_t at = p.map.at(b, h, base);
-        float sum[4][2];
-#pragma unroll
-        for (int rb = 0; rb < 4; ++rb) sum[rb][0] = sum[rb][1] = 0.f;
-        for (int first = 0; first < group; first += 8) {     // eight query heads at a time
+    const int64_t w0 = (int64_t)bh * p.stride;
+    const int64_t step = (int64_t)p.run * 64;
+    for (int64_t r0 = (unit - (int64_t)bh * p.runs) * step; r0 < nv; r0 += p.runs * step) {
+        const int end = (int)min((int64_t)nv, r0 + step);
+        for (int first = 0; first < group; first += QP) {    // QP query heads at a time; the sums of those before are read back
             uint4 raw[J];
-            const bool real = first + g4 < group;
-            const uint4* q4 = reinterpret_cast<const uint4*>(p.q + (head0 + first + (real ? g4 : 0)) * D) + c4;
+            const uint4* q4 = reinterpret_cast<const uint4*>(p.q + (head0 + min(first + g4 % QP, group - 1)) * D) + c4;
 #pragma unroll
             for (int j = 0; j < J; ++j) raw[j] = q4[4 * j];
-            const bool real0 = first + 2 * c4 < group, real1 = first + 2 * c4 + 1 < group;
-            const float l0 = real0 ? p.lse[head0 + first + 2 * c4] * 1.4426950408889634f : 0.f;
-            const float l1 = real1 ? p.lse[head0 + first + 2 * c4 + 1] * 1.4426950408889634f : 0.f;
+            const bool real0 = first + q0 < group, real1 = first + q0 + 1 < group;
+            const float l0 = real0 ? p.lse[head0 + first + q0] * 1.4426950408889634f : 0.f;
+            const float l1 = real1 ? p.lse[head0 + first + q0 + 1] * 1.4426950408889634f : 0.f;
             PackedQuery<D> q;
             if constexpr (PACKED) packed_query<D>(raw, p.scale_log2, lane, q);
+            const float* from = first ? p.weights : p.prev;
+            for (int base = (int)r0; base < end; base += 64) {
+                const int rows = min(64, end - base);
+                const int64_t page = p.map.at(b, h, base), at = page < 0 ? 0 : page;
+                KeyFragment<D, PACKED> ka[LOAD], kb[LOAD];
+                uint32_t pa[NB][G], pb[NB][G];
+                // (rows behind the last one are not read: the last one's keys do in their place)
+                const auto fetch = [&](int rb) {
+                    if (rb * 16 >= rows) return;
+                    ka[rb % LOAD].load(p, at + min(rb * 16 + g4, rows - 1), c4);
+                    kb[rb % LOAD].load(p, at + min(rb * 16 + g4 + 8, rows - 1), c4);
+                };
 #pragma unroll
-            for (int rb = 0; rb < 4; ++rb) {
-                if (rb * 16 >= rows) continue;
-                const int r0 = rb * 16 + g4, r1 = r0 + 8;
-                // (rows behind the last one are not read: any row's keys do in their place)
-                const int64_t a0 = at < 0 ? 0 : at + min(r0, rows - 1), a1 = at < 0 ? 0 : at + min(r1, rows - 1);
-                float s[4];
+                for (int rb = 0; rb < LOAD; ++rb) fetch(rb);
                 if constexpr (PACKED) {
-                    uint32_t ka[J], kb[J];
-                    if constexpr (D == 128) {
-                        const uint4 x = *reinterpret_cast<const uint4*>(p.s.kc + a0 * 64 + c4 * 16), y = *reinterpret_cast<const uint4*>(p.s.kc + a1 * 64 + c4 * 16);
-                        ka[0] = x.x; ka[1] = x.y; ka[2] = x.z; ka[3] = x.w;
-                        kb[0] = y.x; kb[1] = y.y; kb[2] = y.z; kb[3] = y.w;
-                    } else {
-                        const uint2 x = *reinterpret_cast<const uint2*>(p.s.kc + a0 * 32 + c4 * 8), y = *reinterpret_cast<const uint2*>(p.s.kc + a1 * 32 + c4 * 8);
-                        ka[0] = x.x; ka[1] = x.y;
-                        kb[0] = y.x; kb[1] = y.y;
-                    }
-                    uint32_t pa[G], pb[G];
 #pragma unroll
-                    for (int g = 0; g < G; ++g) {
-                        pa[g] = p.s.par[a0 * (2 * G) + g];
-                        pb[g] = p.s.par[a1 * (2 * G) + g];
-                    }
-                    float acc[G][4];
+                    for (int i = 0; i < NB; ++i)
 #pragma unroll
-                    for (int g = 0; g < G; ++g)
-#pragma unroll
-                        for (int i = 0; i < 4; ++i) acc[g][i] = 0.f;
-#pragma unroll
-                    for (int j = 0; j < J; ++j) {
-                        uint32_t xa[4], xb[4];
-                        nibble_pairs(ka[j], xa);
-                        nibble_pairs(kb[j], xb);
-                        mma_f16_16816(acc[j / 2], xa[0], xb[0], xa[1], xb[1], q.b[2 * j][0], q.b[2 * j][1]);
-                        mma_f16_16816(acc[j / 2], xa[2], xb[2], xa[3], xb[3], q.b[2 * j + 1][0], q.b[2 * j + 1][1]);
-                    }
-#pragma unroll
-                    for (int i = 0; i < 4; ++i) {
-                        const uint32_t* pr = i < 2 ? pa : pb;
-                        float t = bf16lo(pr[0]) * acc[0][i], u = bf16hi(pr[0]) * q.sum[i & 1][0];
-                        if constexpr (G == 2) {
-                            t = fmaf(bf16lo(pr[1]), acc[1][i], t);
-                            u = fmaf(bf16hi(pr[1]), q.sum[i & 1][1], u);
+                        for (int g = 0; g < G; ++g) {
+                            pa[i][g] = p.s.par[(at + min((i * NC + copy) * 16 + g4, rows - 1)) * (2 * G) + g];
+                            pb[i][g] = p.s.par[(at + min((i * NC + copy) * 16 + g4 + 8, rows - 1)) * (2 * G) + g];
                         }
-                        s[i] = fmaf(t, q.f[i & 1], u);
-                    }
-                } else {
-                    float acc[4] = {0.f, 0.f, 0.f, 0.f};
-                    const uint4* x = reinterpret_cast<const uint4*>(p.K + a0 * D) + c4;
-                    const uint4* y = reinterpret_cast<const uint4*>(p.K + a1 * D) + c4;
-                    uint4 ka[J], kb[J];
-#pragma unroll
-                    for (int j = 0; j < J; ++j) { ka[j] = x[4 * j]; kb[j] = y[4 * j]; }
-#pragma unroll
-                    for (int j = 0; j < J; ++j) {
-                        mma_bf16_16816(acc, ka[j].x, kb[j].x, ka[j].y, kb[j].y, raw[j].x, raw[j].y);
-                        mma_bf16_16816(acc, ka[j].z, kb[j].z, ka[j].w, kb[j].w, raw[j].z, raw[j].w);
-                    }
-#pragma unroll
-                    for (int i = 0; i < 4; ++i) s[i] = acc[i] * p.scale_log2;
                 }
-                sum[rb][0] += (real0 ? ex2(s[0] - l0) : 0.f) + (real1 ? ex2(s[1] - l1) : 0.f);
-                sum[rb][1] += (real0 ? ex2(s[2] - l0) : 0.f) + (real1 ? ex2(s[3] - l1) : 0.f);
-            }
-        }
+                const int ma = (mine * NC + copy) * 16 + g4, mb = ma + 8;        // rows that this lane writes
+                const int64_t o = w0 + base + ma;
+                const float before_a = from && ma < rows ? from[o] : 0.f, before_b = from && mb < rows ? from[o + 8] : 0.f;
+                float ta = 0.f, tb = 0.f;
 #pragma unroll
-        for (int rb = 0; rb < 4; ++rb) {
+                for (int i = 0; i < NB; ++i) {
+                    float own[PACKED ? G : 1][4];
 #pragma unroll
-            for (int i = 0; i < 2; ++i) {
-                float t = sum[rb][i];
-                t += __shfl_xor_sync(FULL, t, 1);
-                t += __shfl_xor_sync(FULL, t, 2);
-                const int r = rb * 16 + 8 * i + g4;
-                if (c4 == i && r < rows) {
-                    const int64_t o = w0 + base + r;
-                    p.weights[o] = p.prev ? p.prev[o] + t : t;
+                    for (int k = 0; k < NC; ++k) {
+                        const int rb = i * NC + k;
+                        float acc[PACKED ? G : 1][4];
+#pragma unroll
+                        for (int g = 0; g < (PACKED ? G : 1); ++g)
+#pragma unroll
+                            for (int e = 0; e < 4; ++e) acc[g][e] = 0.f;
+                        if (rb * 16 < rows) {
+                            const auto& x = ka[rb % LOAD].w;
+                            const auto& y = kb[rb % LOAD].w;
+#pragma unroll
+                            for (int j = 0; j < J; ++j) {
+                                if constexpr (PACKED) {
+                                    uint32_t xa[4], xb[4];
+                                    nibble_pairs(x[j], xa);
+                                    nibble_pairs(y[j], xb);
+                                    mma_f16_16816(acc[j / 2], xa[0], xb[0], xa[1], xb[1], q.b[2 * j][0], q.b[2 * j][1]);
+                                    mma_f16_16816(acc[j / 2], xa[2], xb[2], xa[3], xb[3], q.b[2 * j + 1][0], q.b[2 * j + 1][1]);
+                                } else {
+                                    mma_bf16_16816(acc[0], x[j].x, y[j].x, x[j].y, y[j].y, raw[j].x, raw[j].y);
+                                    mma_bf16_16816(acc[0], x[j].z, y[j].z, x[j].w, y[j].w, raw[j].z, raw[j].w);
+                                }
+                            }
+                        }
+                        if (LOAD < 4 && rb + LOAD < 4) fetch(rb + LOAD);
+#pragma unroll
+                        for (int g = 0; g < (PACKED ? G : 1); ++g)
+#pragma unroll
+                            for (int e = 0; e < 4; ++e) own[g][e] = k == 0 || copy == k ? acc[g][e] : own[g][e];
+                    }
+                    float s[4];
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) {
+                        if constexpr (PACKED) {
+                            const uint32_t* pr = e < 2 ? pa[i] : pb[i];
+                            float t = bf16lo(pr[0]) * own[0][e], u = bf16hi(pr[0]) * q.sum[e & 1][0];
+                            if constexpr (G == 2) {
+                                t = fmaf(bf16lo(pr[1]), own[1][e], t);
+                                u = fmaf(bf16hi(pr[1]), q.sum[e & 1][1], u);
+                            }
+                            s[e] = fmaf(t, q.f[e & 1], u);
+                        } else {
+                            s[e] = own[0][e] * p.scale_log2;
+                        }
+                    }
+                    float a = (real0 ? ex2(s[0] - l0) : 0.f) + (real1 ? ex2(s[1] - l1) : 0.f);
+                    float c = (real0 ? ex2(s[2] - l0) : 0.f) + (real1 ? ex2(s[3] - l1) : 0.f);
+#pragma unroll
+                    for (int off = 1; off < QP / 2; off <<= 1) {
+                        a += __shfl_xor_sync(FULL, a, off);
+                        c += __shfl_xor_sync(FULL, c, off);
+                    }
+                    if (i == mine) { ta = a; tb = c; }
                 }
+                if (ma < rows) p.weights[o] = before_a + ta;
+                if (mb < rows) p.weights[o + 8] = before_b + tb;
             }
         }
     }
@@ -137,15 +173,16 @@ __global__ void __launch_bounds__(kWeightWarps * 32) attention_weights_kernel(co
 
 // ---- eviction -----------------------------------------------------------------------------------------------------------
 
-constexpr int kSelectThreads = 1024;
-constexpr int kSelectMostKeys = 48 * 1024;   // keys that a thread block keeps in shared memory
-
-// Order of weights as whole numbers: larger weight, larger key; -0 as 0; a NaN below all.
+// Order of weights as whole numbers: larger weight, larger key; -0 as 0; a NaN below all.  And the weight of a key.
 __device__ __forceinline__ uint32_t weight_key(float w)
 {
     const uint32_t u = __float_as_uint(w + 0.f);
     if ((u & 0x7fffffffu) > 0x7f800000u) return 0u;
     return (u & 0x80000000u) ? ~u : u | 0x80000000u;
+}
+__device__ __forceinline__ float key_weight(uint32_t k)
+{
+    return __uint_as_float(k == 0u ? 0x7fffffffu : (k & 0x80000000u) ? k & 0x7fffffffu : ~k);
 }
 
 struct SelectParams {
@@ -155,96 +192,141 @@ struct SelectParams {
     const int32_t* lens;
     int32_t* lens_out;        // lengths to set (another cache's), or null
     int64_t stride, out_stride, T_cap;
-    int32_t H_kv, n_sink, n_recent, n_keep, out_rows, keys;
+    int32_t H_kv, n_sink, n_recent, n_keep, out_rows;
 };
 
-// One thread block per (sequence, kv head).  The smallest key that stays is found bit by bit: with t the bits found so
-// far, count the keys >= t | bit.  That is at most 32 counts, fewer when a count meets the target (as with distinct
-// weights it soon does).  Then every warp lists its own stretch of rows behind what the warps in front of it keep, so rows
-// stay in order and equal weights go by the lowest row.
-__global__ void __launch_bounds__(kSelectThreads) evict_select_kernel(const SelectParams p)
+// One thread block per (sequence, kv head); a warp holds the keys of 32 KPT consecutive rows, KPT a thread, in registers
+// (KPT = 0, for more rows than the block can hold: keys from memory each time).  The smallest key that stays is found two bits at a time: with t the
+// bits found so far, count the keys >= t + 1, 2 and 3 units of those bits.  That is at most 16 rounds, fewer when a count
+// meets the target (as with distinct weights it soon does).  Then every warp lists its own stretch of rows behind what
+// the warps in front of it keep, so rows stay in order and equal weights go by the lowest row.
+//
+// What bounds it is the chain of rounds, each a block-wide sum, not the 4 bytes per row: thread blocks are as small as the rows
+// allow, so that several on an SM cover for each other.
+template <int WARPS>
+struct SelectShared { int counts[2][3][WARPS], stay[WARPS], middle[WARPS], equal[WARPS]; };
+
+template <int THREADS, int KPT>
+__device__ __forceinline__ void evict_select(const SelectParams& p, SelectShared<THREADS / 32>& sh, int n)
 {
-    extern __shared__ uint32_t keys[];
-    __shared__ int counts[2][32], above[32], equal[32];
-    pdl_wait_then_release();
+    constexpr int WARPS = THREADS / 32;
+    const uint32_t FULL = 0xffffffffu;
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
     const int b = blockIdx.x / p.H_kv;
-    const int len = p.lens[b];
-    const int n = (int)min((int64_t)max(len, 0), p.T_cap);
     const float* w = p.weights ? p.weights + (int64_t)blockIdx.x * p.stride : nullptr;
+    float* out = p.weights_out ? p.weights_out + (int64_t)blockIdx.x * p.out_stride : nullptr;
     int32_t* kept = p.kept + (int64_t)blockIdx.x * p.n_keep;
     const int count = min(n, p.n_keep);
     if (p.lens_out && blockIdx.x % p.H_kv == 0 && tid == 0) p.lens_out[b] = count;
-    if (n <= p.n_keep) {
-        for (int i = tid; i < p.n_keep; i += kSelectThreads) kept[i] = i < n ? i : -1;
-    } else {
-        const int first = p.n_sink, m = n - p.n_recent - first;      // rows that compete
-        const int target = p.n_keep - p.n_sink - p.n_recent;         // and how many of them stay (< m)
-        const bool held = m <= p.keys;
-        const auto key = [&](int i) { return held ? keys[i] : w ? weight_key(w[first + i]) : 0x80000000u; };
-        if (held) {
-            for (int i = tid; i < m; i += kSelectThreads) keys[i] = w ? weight_key(w[first + i]) : 0x80000000u;
-            __syncthreads();
+    // rows lo .. hi - 1 are this warp's; row lo + 32 i + lane is the thread's i-th
+    const int each = KPT ? 32 * KPT : ((n + WARPS - 1) / WARPS + 31) / 32 * 32;
+    const int lo = min(n, warp * each), hi = min(n, lo + each);
+    const int turns = KPT ? KPT : each / 32;
+    uint32_t held[KPT ? KPT : 1] = {};
+    const auto weight = [&](int row) { return w ? w[row] : 0.f; };
+    const auto key = [&](int i) {
+        if constexpr (KPT != 0) return held[i];
+        const int row = lo + 32 * i + lane;
+        return row < hi ? weight_key(weight(row)) : 0u;
+    };
+    if constexpr (KPT != 0) {
+#pragma unroll
+        for (int i = 0; i < KPT; ++i) {
+            const int row = lo + 32 * i + lane;
+            held[i] = row < hi ? weight_key(weight(row)) : 0u;
         }
-        uint32_t t = 0;
-        int turn = 0;
-        const auto count_from = [&](uint32_t from) {
-            int c = 0;
-            for (int i = tid; i < m; i += kSelectThreads) c += key(i) >= from;
-            c = __reduce_add_sync(0xffffffffu, c);
-            if (lane == 0) counts[turn][warp] = c;
-            __syncthreads();
-            c = __reduce_add_sync(0xffffffffu, counts[turn][lane]);
-            turn ^= 1;
-            return c;
-        };
-        bool met = target == 0;
+    }
+    const int first = n > p.n_keep ? p.n_sink : 0, behind = n > p.n_keep ? n - p.n_recent : 0;   // rows that compete
+    const auto competes = [&](int i) { const int row = lo + 32 * i + lane; return row >= first && row < behind; };
+    uint32_t t = 0;
+    int target = 0;
+    bool met = true;
+    if (n > p.n_keep) {
+        target = p.n_keep - p.n_sink - p.n_recent;                   // how many of them stay (fewer than compete)
+        met = target == 0;
         if (met) t = 0xffffffffu;                                    // (no weight has this key: nothing stays)
-        for (int bit = 31; bit >= 0 && !met; --bit) {
-            const int c = count_from(t | (1u << bit));
-            if (c >= target) t |= 1u << bit;
-            met = c == target;
+        int turn = 0;
+        for (int shift = 30; shift >= 0 && !met; shift -= 2) {
+            int c[3] = {0, 0, 0};
+#pragma unroll
+            for (int i = 0; i < (KPT ? KPT : turns); ++i) {
+                const uint32_t k = competes(i) ? key(i) : 0u;
+#pragma unroll
+                for (int x = 0; x < 3; ++x) c[x] += k >= t + ((uint32_t)(x + 1) << shift);
+            }
+#pragma unroll
+            for (int x = 0; x < 3; ++x) {
+                c[x] = __reduce_add_sync(FULL, c[x]);
+                if (lane == 0) sh.counts[turn][x][warp] = c[x];
+            }
+            __syncthreads();
+#pragma unroll
+            for (int x = 0; x < 3; ++x) c[x] = __reduce_add_sync(FULL, lane < WARPS ? sh.counts[turn][x][lane] : 0);
+            turn ^= 1;
+            const int digit = c[2] >= target ? 3 : c[1] >= target ? 2 : c[0] >= target ? 1 : 0;
+            t += (uint32_t)digit << shift;
+            met = digit > 0 && c[digit > 0 ? digit - 1 : 0] == target;
         }
-        // met: all keys >= t stay; else all keys > t, and of those equal to t the first `ties`
-        const int each = ((m + 31) / 32 + 31) / 32 * 32;             // rows per warp
-        const int lo = min(m, warp * each), hi = min(m, lo + each);
-        int n_above = 0, n_equal = 0;
-        for (int i = lo + lane; i - lane < hi; i += 32) {
-            const uint32_t k = i < hi ? key(i) : 0u;
-            n_above += __popc(__ballot_sync(0xffffffffu, i < hi && (met ? k >= t : k > t)));
-            n_equal += __popc(__ballot_sync(0xffffffffu, i < hi && !met && k == t));
-        }
-        if (lane == 0) { above[warp] = n_above; equal[warp] = n_equal; }
-        __syncthreads();
-        const int all_above = __reduce_add_sync(0xffffffffu, above[lane]);
-        n_above = __reduce_add_sync(0xffffffffu, lane < warp ? above[lane] : 0);
-        n_equal = __reduce_add_sync(0xffffffffu, lane < warp ? equal[lane] : 0);
-        const int ties = target - all_above;
-        const uint32_t below = (1u << lane) - 1u;
-        for (int i = lo + lane; i - lane < hi; i += 32) {
-            const uint32_t k = i < hi ? key(i) : 0u;
-            const bool a = i < hi && (met ? k >= t : k > t), e = i < hi && !met && k == t;
-            const uint32_t ab = __ballot_sync(0xffffffffu, a), eb = __ballot_sync(0xffffffffu, e);
-            const int e_rank = n_equal + __popc(eb & below);
-            const int at = first + n_above + __popc(ab & below) + min(e_rank, ties);
-            if (a || (e && e_rank < ties)) kept[at] = first + i;
-            n_above += __popc(ab);
-            n_equal += __popc(eb);
-        }
-        for (int i = tid; i < p.n_sink; i += kSelectThreads) kept[i] = i;
-        for (int i = tid; i < p.n_recent; i += kSelectThreads) kept[p.n_keep - p.n_recent + i] = n - p.n_recent + i;
     }
-    if (!p.weights_out) return;
-    // Rows only move down, so with weights in place a tile is read before it is written, and tiles go upwards.
-    __syncthreads();
-    float* out = p.weights_out + (int64_t)blockIdx.x * p.out_stride;
-    for (int i0 = 0; i0 < p.out_rows; i0 += kSelectThreads) {
-        const int i = i0 + tid;
-        float x = 0.f;
-        if (i < count && w) x = w[kept[i]];
-        __syncthreads();
-        if (i < p.out_rows) out[i] = x;
+    // met: all keys >= t stay; else all keys > t, and of those equal to t the first `ties`.  Rows that do not compete: the first
+    // and the last (all, where n <= n_keep).
+    const auto stays = [&](int i) {
+        const int row = lo + 32 * i + lane;
+        return row < hi && (!competes(i) || (met ? key(i) >= t : key(i) > t));
+    };
+    const auto ties_with = [&](int i) { return !met && competes(i) && lo + 32 * i + lane < hi && key(i) == t; };
+    int n_stay = 0, n_equal = 0, n_out = 0;
+#pragma unroll
+    for (int i = 0; i < (KPT ? KPT : turns); ++i) {
+        n_stay += __popc(__ballot_sync(FULL, stays(i)));
+        n_equal += __popc(__ballot_sync(FULL, ties_with(i)));
+        n_out += __popc(__ballot_sync(FULL, stays(i) && !competes(i)));
     }
+    if (lane == 0) { sh.stay[warp] = n_stay; sh.equal[warp] = n_equal; sh.middle[warp] = n_stay - n_out; }
+    __syncthreads();                                                 // (behind it the weights in memory are read no more, if KPT)
+    const int all_above = __reduce_add_sync(FULL, lane < WARPS ? sh.middle[lane] : 0);
+    n_stay = __reduce_add_sync(FULL, lane < warp ? sh.stay[lane] : 0);
+    n_equal = __reduce_add_sync(FULL, lane < warp ? sh.equal[lane] : 0);
+    const int ties = target - all_above;
+    const uint32_t below = (1u << lane) - 1u;
+#pragma unroll
+    for (int i = 0; i < (KPT ? KPT : turns); ++i) {
+        const bool a = stays(i), e = ties_with(i);
+        const uint32_t ab = __ballot_sync(FULL, a), eb = __ballot_sync(FULL, e);
+        const int e_rank = n_equal + __popc(eb & below);
+        const int at = n_stay + __popc(ab & below) + min(e_rank, max(ties, 0));
+        if (a || (e && e_rank < ties)) {
+            kept[at] = lo + 32 * i + lane;
+            if (KPT != 0 && out) out[at] = key_weight(key(i));
+        }
+        n_stay += __popc(ab);
+        n_equal += __popc(eb);
+    }
+    for (int i = count + tid; i < p.n_keep; i += THREADS) kept[i] = -1;
+    if (!out) return;
+    if constexpr (KPT != 0) {
+        for (int i = count + tid; i < p.out_rows; i += THREADS) out[i] = 0.f;
+    } else {
+        // Rows only move down, so with weights in place a tile is read before it is written, and tiles go upwards.
+        __syncthreads();
+        for (int i0 = 0; i0 < p.out_rows; i0 += THREADS) {
+            const int i = i0 + tid;
+            const float x = i < count ? weight(kept[i]) : 0.f;
+            __syncthreads();
+            if (i < p.out_rows) out[i] = x;
+        }
+    }
+}
+
+template <int THREADS, int KPT>
+__global__ void __launch_bounds__(THREADS) evict_select_kernel(const SelectParams p)
+{
+    __shared__ SelectShared<THREADS / 32> sh;
+    pdl_wait_then_release();
+    const int n = (int)min((int64_t)max(p.lens[blockIdx.x / p.H_kv], 0), p.T_cap);
+    // (the launcher goes by the lengths that the host knows, which a replayed advance leaves behind)
+    if (KPT != 0 && n <= THREADS * KPT) evict_select<THREADS, KPT>(p, sh, n);
+    else evict_select<THREADS, 0>(p, sh, n);
 }
 
 struct MoveParams {
@@ -262,16 +344,14 @@ struct MoveParams {
 
 constexpr int kStatusNoRow = 2;   // a row had no place (LCKV_ECAPACITY)
 
-// Physical rows of item (b, h, i): from and to; negative where there is nothing to do.
+// Physical rows of row i of the result of (sequence, kv head) number bh: from and to; negative where there is nothing to do.
 struct MoveRow { int64_t from, to; };
-__device__ __forceinline__ MoveRow move_row(const MoveParams& p, int64_t item)
+__device__ __forceinline__ MoveRow move_row(const MoveParams& p, int bh, int i)
 {
     MoveRow r = {-1, -1};
-    const int row = p.kept[item];
+    const int row = i < p.n_keep ? p.kept[(int64_t)bh * p.n_keep + i] : -1;
     if (row < 0) return r;
-    const int i = (int)(item % p.n_keep);
-    const int64_t bh = item / p.n_keep;
-    const int h = (int)(bh % p.map.H_kv), b = (int)(bh / p.map.H_kv);
+    const int b = bh / p.map.H_kv, h = bh - b * p.map.H_kv;
     r.from = p.map.at(b, h, row);
     r.to = p.map_to.at(b, h, i);
     if (r.from < 0 || r.to < 0) {
@@ -299,41 +379,59 @@ struct RowUnits {
     }
 };
 
-// From one slot to another of the same kind.
+// From one slot to another of the same kind: blockIdx.x is the (sequence, kv head), blockIdx.y a stretch of its rows' units.
+constexpr int kMoveUnits = 4;             // a thread's
 template <int D, bool PACKED>
-__global__ void __launch_bounds__(256) evict_move_kernel(const MoveParams p, int64_t items)
+__global__ void __launch_bounds__(kRowThreads) evict_move_kernel(const MoveParams p)
 {
     using U = RowUnits<D, PACKED>;
     pdl_wait_then_release();
-    const int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x;
-    const int64_t item = i / U::kUnits;
-    if (item >= items) return;
-    const int u = (int)(i % U::kUnits);
-    const MoveRow r = move_row(p, item);
-    if (r.from < 0) return;
-    const auto v = *U::at(p.from, p.K, p.V, r.from, u);
-    *const_cast<typename U::Unit*>(U::at(p.to, p.K_to, p.V_to, r.to, u)) = v;
+    for (int64_t k0 = (int64_t)blockIdx.y * kRowThreads * kMoveUnits; k0 < (int64_t)p.n_keep * U::kUnits; k0 += (int64_t)gridDim.y * kRowThreads * kMoveUnits) {
+        typename U::Unit v[kMoveUnits];
+        MoveRow r[kMoveUnits];
+        int u[kMoveUnits];
+#pragma unroll
+        for (int x = 0; x < kMoveUnits; ++x) {
+            const uint32_t k = (uint32_t)k0 + x * kRowThreads + threadIdx.x;
+            u[x] = (int)(k % U::kUnits);
+            r[x] = move_row(p, (int)blockIdx.x, (int)(k / U::kUnits));
+        }
+#pragma unroll
+        for (int x = 0; x < kMoveUnits; ++x)
+            if (r[x].from >= 0) v[x] = *U::at(p.from, p.K, p.V, r[x].from, u[x]);
+#pragma unroll
+        for (int x = 0; x < kMoveUnits; ++x)
+            if (r[x].from >= 0) *const_cast<typename U::Unit*>(U::at(p.to, p.K_to, p.V_to, r[x].to, u[x])) = v[x];
+    }
 }
 
-// From bf16 rows to 4-bit rows; lanes as in packed_write_kernel.
+// From bf16 rows to 4-bit rows; lanes as in packed_write_kernel, blocks as above.
 template <int D>
-__global__ void __launch_bounds__(256) evict_pack_kernel(const MoveParams p, int64_t items)
+__global__ void __launch_bounds__(kRowThreads) evict_pack_kernel(const MoveParams p)
 {
-    constexpr int LANES = D / 4;
     pdl_wait_then_release();
-    const int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x;
-    const int64_t item = i / LANES;
-    const int l = (int)(i % LANES), is_v = l >= D / 8, w = l % (D / 8);
-    MoveRow r = {-1, -1};
-    if (item < items) r = move_row(p, item);
-    uint4 x = make_uint4(0, 0, 0, 0);
-    if (r.from >= 0) x = *reinterpret_cast<const uint4*>((is_v ? p.V : p.K) + r.from * D + w * 8);
-    uint32_t word, par;
-    packed_encode(x, word, par);
-    if (r.from < 0) return;
-    uint32_t* codes = reinterpret_cast<uint32_t*>(is_v ? p.to.vc : p.to.kc) + r.to * (D / 8);
-    codes[is_v ? packed_v_word<D>(w) : packed_k_word<D>(w)] = word;
-    if ((w & 7) == 0) p.to.par[r.to * (D / 32) + is_v * (D / 64) + (w >> 3)] = par;
+    const PackedLane<D> lane((int)threadIdx.x % PackedLane<D>::kLanes);
+    constexpr int ROWS = rows_per_block<D>();
+    for (int64_t i0 = (int64_t)blockIdx.y * ROWS * kRowTokens; i0 < p.n_keep; i0 += (int64_t)gridDim.y * ROWS * kRowTokens) {
+        MoveRow r[kRowTokens];
+        uint4 x[kRowTokens], y[kRowTokens];
+#pragma unroll
+        for (int u = 0; u < kRowTokens; ++u) r[u] = move_row(p, (int)blockIdx.x, (int)i0 + u * ROWS + (int)threadIdx.x / PackedLane<D>::kLanes);
+#pragma unroll
+        for (int u = 0; u < kRowTokens; ++u) {
+            x[u] = y[u] = make_uint4(0, 0, 0, 0);
+            if (r[u].from < 0) continue;
+            const uint16_t* src = (lane.is_v ? p.V : p.K) + r[u].from * D;
+            x[u] = *reinterpret_cast<const uint4*>(src + lane.word(0) * 8);
+            y[u] = *reinterpret_cast<const uint4*>(src + lane.word(1) * 8);
+        }
+#pragma unroll
+        for (int u = 0; u < kRowTokens; ++u) {
+            uint32_t w0, w1, par;
+            packed_encode(x[u], y[u], w0, w1, par);
+            if (r[u].from >= 0) lane.store(p.to, r[u].to, w0, w1, par);
+        }
+    }
 }
 
 // Within one slot: a thread block per (sequence, head) moves tiles upwards; a tile is read whole before it is written, and
@@ -345,7 +443,6 @@ __global__ void __launch_bounds__(1024) evict_in_place_kernel(const MoveParams p
     constexpr int X = 4;                                   // units per thread and tile
     constexpr int ROWS = X * 1024 / U::kUnits;
     pdl_wait_then_release();
-    const int64_t item0 = (int64_t)blockIdx.x * p.n_keep;
     for (int i0 = 0; i0 < p.n_keep; i0 += ROWS) {
         typename U::Unit v[X];
         int64_t to[X];
@@ -354,7 +451,7 @@ __global__ void __launch_bounds__(1024) evict_in_place_kernel(const MoveParams p
             const int k = x * 1024 + threadIdx.x, i = i0 + k / U::kUnits;
             to[x] = -1;
             if (k < ROWS * U::kUnits && i < p.n_keep) {
-                const MoveRow r = move_row(p, item0 + i);
+                const MoveRow r = move_row(p, (int)blockIdx.x, i);
                 if (r.from >= 0 && r.from != r.to) {
                     to[x] = r.to;
                     v[x] = *U::at(p.from, p.K, p.V, r.from, k % U::kUnits);

@@ -15,7 +15,7 @@
 // Row pitch of a (sequence, head) is the capacity rounded up to 64 rows, so that every tile starts on 16 bytes and none
 // leaves the slot; pages hold a multiple of 64 rows anyway.
 #pragma once
-#include "lckv_small_kernels.cuh"
+#include "lckv_attn_mma.cuh"
 
 namespace lckv {
 
@@ -62,18 +62,67 @@ __device__ __forceinline__ int packed_k_word(int w) { return (w & 3) * (D / 32) 
 template <int D>
 __device__ __forceinline__ int packed_v_word(int w) { return D == 128 ? 2 * (w & 7) + (w >> 3) : w; }
 
-// Eight lanes (a multiple of eight and the seven behind it) hold a group, eight elements each: their codes and the group's
-// parameters (the same in all eight).
-__device__ __forceinline__ void packed_encode(uint4 x, uint32_t& word, uint32_t& par)
+// Where a lane stands in a row: D/16 lanes for the key, then as many for the value; four lanes share a group, and lane c of a
+// group has its words c and c + 4 (16 elements), which lie side by side among a key's codes.
+template <int D>
+struct PackedLane {
+    static constexpr int kLanes = D / 8;          // of a row
+    int is_v, c, g;
+    __device__ __forceinline__ explicit PackedLane(int l) : is_v(l >= D / 16), c(l & 3), g(D == 128 ? (l >> 2) & 1 : 0) {}
+    __device__ __forceinline__ int word(int i) const { return 8 * g + c + 4 * i; }
+    __device__ __forceinline__ void store(const PackedSlot& s, int64_t row, uint32_t w0, uint32_t w1, uint32_t par) const
+    {
+        uint32_t* codes = reinterpret_cast<uint32_t*>(is_v ? s.vc : s.kc) + row * (D / 8);
+        if (is_v) {
+            codes[packed_v_word<D>(word(0))] = w0;
+            codes[packed_v_word<D>(word(1))] = w1;
+        } else {
+            *reinterpret_cast<uint2*>(codes + packed_k_word<D>(word(0))) = make_uint2(w0, w1);
+        }
+        if (c == 0) s.par[row * (D / 32) + is_v * (D / 64) + g] = par;
+    }
+    __device__ __forceinline__ void load(const PackedSlot& s, int64_t row, uint32_t& w0, uint32_t& w1, uint32_t& par) const
+    {
+        const uint32_t* codes = reinterpret_cast<const uint32_t*>(is_v ? s.vc : s.kc) + row * (D / 8);
+        if (is_v) {
+            w0 = codes[packed_v_word<D>(word(0))];
+            w1 = codes[packed_v_word<D>(word(1))];
+        } else {
+            const uint2 w = *reinterpret_cast<const uint2*>(codes + packed_k_word<D>(word(0)));
+            w0 = w.x;
+            w1 = w.y;
+        }
+        par = s.par[row * (D / 32) + is_v * (D / 64) + g];
+    }
+};
+
+// Eight elements as a word of codes.  Adding 1.5 * 2^23 rounds to a whole number, ties to even, and leaves it in the low bits;
+// the sum of those numbers' bit patterns times 16^i is the word plus a constant.  (A quotient is below 15.5 without a limit: the
+// step is off by 2^-8 at most.)
+__device__ __forceinline__ uint32_t packed_codes(uint4 x, float low16, float inv)
 {
-    uint32_t mx = max2_nan(max2_nan(x.x, x.y), max2_nan(x.z, x.w));
-    uint32_t mn = min2_nan(min2_nan(x.x, x.y), min2_nan(x.z, x.w));
-    mx = max2_nan(mx, (mx >> 16) | (mx << 16));
-    mn = min2_nan(mn, (mn >> 16) | (mn << 16));
+    const uint32_t w[4] = {x.x, x.y, x.z, x.w};
+    uint32_t word = 0u - 0x4b400000u * 0x11111111u;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+        const float v = (i & 1) ? bf16hi(w[i >> 1]) : bf16lo(w[i >> 1]);
+        word += __float_as_uint(__fadd_rn(__fmul_rn(__fmaf_rn(v, 0.0625f, -low16), inv), 12582912.f)) * (1u << (4 * i));
+    }
+    return word;
+}
+
+// Four lanes (a multiple of four and the three behind it) hold a group, 16 elements each: their codes and the group's
+// parameters (the same in all four).
+__device__ __forceinline__ void packed_encode(uint4 x, uint4 y, uint32_t& w0, uint32_t& w1, uint32_t& par)
+{
+    uint32_t mx = max2_nan(max2_nan(max2_nan(x.x, x.y), max2_nan(x.z, x.w)), max2_nan(max2_nan(y.x, y.y), max2_nan(y.z, y.w)));
+    uint32_t mn = min2_nan(min2_nan(min2_nan(x.x, x.y), min2_nan(x.z, x.w)), min2_nan(min2_nan(y.x, y.y), min2_nan(y.z, y.w)));
+    mx = max2_nan(mx, __byte_perm(mx, 0, 0x1032));
+    mn = min2_nan(mn, __byte_perm(mn, 0, 0x1032));
     // largest in the low half, smallest in the high half: one exchange serves both
 #pragma unroll
-    for (int off = 1; off <= 4; off <<= 1) {
-        const uint32_t o = __shfl_xor_sync(0xffffffffu, (mx & 0xffffu) | (mn & 0xffff0000u), off);
+    for (int off = 1; off <= 2; off <<= 1) {
+        const uint32_t o = __shfl_xor_sync(0xffffffffu, __byte_perm(mx, mn, 0x7610), off);
         mx = max2_nan(mx, o);
         mn = min2_nan(mn, o);
     }
@@ -84,23 +133,16 @@ __device__ __forceinline__ void packed_encode(uint4 x, uint32_t& word, uint32_t&
     if (step < kPackedMinStep) { step = 0.f; step_bits = 0; }
     const bool finite = fabsf(high) < INFINITY && fabsf(low) < INFINITY;    // (false for a NaN)
     const float inv = step > 0.f && finite ? __frcp_rn(step * 0.0625f) : 0.f;
-    const uint32_t w[4] = {x.x, x.y, x.z, x.w};
-    word = 0;
-#pragma unroll
-    for (int i = 0; i < 8; ++i) {
-        const float v = (i & 1) ? bf16hi(w[i >> 1]) : bf16lo(w[i >> 1]);
-        const float t = fminf(__fmul_rn(__fmaf_rn(v, 0.0625f, -low16), inv), 15.f);
-        // adding 1.5 * 2^23 rounds to a whole number, ties to even, and leaves it in the low bits
-        word |= (__float_as_uint(__fadd_rn(t, 12582912.f)) & 15u) << (4 * i);
-    }
+    w0 = packed_codes(x, low16, inv);
+    w1 = packed_codes(y, low16, inv);
     par = step_bits | (mn & 0xffff0000u);
-    if (!finite) { word = 0; par = 0x7fc00000u; }
+    if (!finite) { w0 = w1 = 0; par = 0x7fc00000u; }
 }
 
-// Element i of a word: low + step * code.
+// What element i of a word stands for.
 __device__ __forceinline__ float packed_value(uint32_t word, int i, float step, float low)
 {
-    return __fmaf_rn(step, (float)((word >> (4 * i)) & 15u), low);
+    return __fmaf_rn(step, __uint_as_float(((word >> (4 * i)) & 15u) | 0x4b000000u) - 8388608.f, low);
 }
 
 struct PackedWriteParams {
@@ -114,97 +156,125 @@ struct PackedWriteParams {
     int32_t prompt;           // 1: token i < len goes to row i; 0: one token, to row len (ring position with n_sink)
 };
 
-// A token's key and value of one head take D/8 lanes each, side by side: one warp holds one such row of D = 128 or two of
-// D = 64, and a row's parameters leave in one store of neighbouring words.
+// Thread blocks over rows: 256 threads, and kRowTokens rows a thread whose loads are all under way before the first is used (a
+// block of one row a thread spent its time waiting for the length, then for the row: prompts of 8 x 4096 tokens of 32
+// heads of 128 took 164 us to write and 132 us to read, now 133 and 107).
+constexpr int kRowThreads = 256;
+constexpr int kRowTokens = 4;
 template <int D>
-__global__ void __launch_bounds__(256) packed_write_kernel(const PackedWriteParams p)
+__host__ __device__ constexpr int rows_per_block() { return kRowThreads / PackedLane<D>::kLanes; }
+
+// Prompts: blockIdx.y (and on in steps of the grid) is the sequence, blockIdx.x a stretch of its (four tokens, head) items.  New
+// tokens: one stretch of all (four sequences, head) items.
+template <int D>
+__global__ void __launch_bounds__(kRowThreads) packed_write_kernel(const PackedWriteParams p)
 {
-    constexpr int LANES = D / 4;                 // lanes of a row: D/8 for the key, D/8 for the value
     pdl_wait_then_release();
-    const int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x;
-    const int64_t item = i / LANES;
-    const int l = (int)(i % LANES);
-    const int64_t n_items = (int64_t)p.batch * p.n * p.map.H_kv;
-    const bool there = item < n_items;
-    const int64_t it = there ? item : n_items - 1;
-    const int h = (int)(it % p.map.H_kv);
-    const int64_t tok = it / p.map.H_kv;
-    const int b = (int)(tok / p.n);
-    const int is_v = l >= D / 8, w = l % (D / 8);
-    int64_t row;
-    bool ok = there;
-    if (p.prompt) {
-        row = tok % p.n;
-        ok = ok && row < p.lens[b] && row < p.T_cap;
-    } else {
-        row = p.lens[b];
-        if (p.n_sink > 0 && row >= p.T_cap) row = p.n_sink + (row - p.n_sink) % (p.T_cap - p.n_sink);
-        ok = ok && row >= 0 && row < p.T_cap;
+    const PackedLane<D> lane((int)threadIdx.x % PackedLane<D>::kLanes);
+    const uint32_t H = (uint32_t)p.map.H_kv;
+    const uint32_t item = blockIdx.x * rows_per_block<D>() + threadIdx.x / PackedLane<D>::kLanes;
+    const uint32_t h = item % H, tok = item / H * kRowTokens;
+    const int seqs = p.prompt ? p.batch : 1;
+    for (int seq = blockIdx.y; seq < seqs; seq += gridDim.y) {
+        const int n = p.prompt ? (int)min((int64_t)min(p.n, p.lens[seq]), p.T_cap) : p.batch;
+        if ((int64_t)(blockIdx.x * rows_per_block<D>() / H) * kRowTokens >= n) continue;      // (the whole block)
+        uint4 x[kRowTokens], y[kRowTokens];
+        int64_t at[kRowTokens];
+#pragma unroll
+        for (int u = 0; u < kRowTokens; ++u) {
+            const int t = (int)tok + u;
+            int64_t row = -1;
+            if (t < n) {
+                row = t;
+                if (!p.prompt) {
+                    row = p.lens[t];
+                    if (p.n_sink > 0 && row >= p.T_cap) row = p.n_sink + (row - p.n_sink) % (p.T_cap - p.n_sink);
+                    if (row >= p.T_cap) row = -1;
+                }
+            }
+            at[u] = row >= 0 ? p.map.at(p.prompt ? seq : t, (int)h, (int)row) : -1;
+            x[u] = y[u] = make_uint4(0, 0, 0, 0);
+            if (t < n) {
+                const uint16_t* src = (lane.is_v ? p.v : p.k) + (((int64_t)seq * p.n + t) * H + h) * D;
+                x[u] = *reinterpret_cast<const uint4*>(src + lane.word(0) * 8);
+                y[u] = *reinterpret_cast<const uint4*>(src + lane.word(1) * 8);
+            }
+        }
+#pragma unroll
+        for (int u = 0; u < kRowTokens; ++u) {
+            uint32_t w0, w1, par;
+            packed_encode(x[u], y[u], w0, w1, par);        // (all lanes: it exchanges between them)
+            if (at[u] >= 0) lane.store(p.s, at[u], w0, w1, par);
+        }
     }
-    const int64_t at = ok ? p.map.at(b, h, (int)row) : -1;
-    ok = at >= 0;
-    uint4 x = make_uint4(0, 0, 0, 0);
-    if (ok) x = *reinterpret_cast<const uint4*>((is_v ? p.v : p.k) + it * D + w * 8);
-    uint32_t word, par;
-    packed_encode(x, word, par);                 // (all lanes: it exchanges between them)
-    if (!ok) return;
-    uint32_t* codes = reinterpret_cast<uint32_t*>(is_v ? p.s.vc : p.s.kc) + at * (D / 8);
-    codes[is_v ? packed_v_word<D>(w) : packed_k_word<D>(w)] = word;
-    if ((w & 7) == 0) p.s.par[at * (D / 32) + is_v * (D / 64) + (w >> 3)] = par;
 }
 
 struct RowReadParams {
     PackedSlot s;             // 4-bit rows, or
-    const uint16_t* K;        // bf16 rows (null: 4-bit)
+    const uint16_t* K;        // bf16 rows
     const uint16_t* V;
     RowMap map;
     const int32_t* lens;
     void* k;                  // [batch, n, H_kv, D] bf16 or fp32
     void* v;
     int64_t T_cap;
-    int32_t batch, n, f32;
+    int32_t batch, n;
 };
 
-// Rows 0 .. len-1 of a slot as tokens; the same lanes per row as packed_write_kernel.
-template <int D>
-__global__ void __launch_bounds__(256) row_read_kernel(const RowReadParams p)
+// Rows 0 .. len-1 of a slot as tokens; lanes and blocks as in packed_write_kernel.
+template <int D, bool PACKED, bool F32>
+__global__ void __launch_bounds__(kRowThreads) row_read_kernel(const RowReadParams p)
 {
-    constexpr int LANES = D / 4;
     pdl_wait_then_release();
-    const int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x;
-    const int64_t item = i / LANES;
-    if (item >= (int64_t)p.batch * p.n * p.map.H_kv) return;
-    const int l = (int)(i % LANES), is_v = l >= D / 8, w = l % (D / 8);
-    const int h = (int)(item % p.map.H_kv);
-    const int64_t tok = item / p.map.H_kv;
-    const int b = (int)(tok / p.n), row = (int)(tok % p.n);
-    if (row >= p.lens[b] || row >= p.T_cap) return;
-    const int64_t at = p.map.at(b, h, row);
-    if (at < 0) return;
-    const int64_t dst = item * D + w * 8;
-    float y[8];
-    if (p.K) {
-        const uint4 x = *reinterpret_cast<const uint4*>((is_v ? p.V : p.K) + at * D + w * 8);
-        if (!p.f32) {
-            *reinterpret_cast<uint4*>(static_cast<uint16_t*>(is_v ? p.v : p.k) + dst) = x;
-            return;
+    const PackedLane<D> lane((int)threadIdx.x % PackedLane<D>::kLanes);
+    const uint32_t H = (uint32_t)p.map.H_kv;
+    const uint32_t item = blockIdx.x * rows_per_block<D>() + threadIdx.x / PackedLane<D>::kLanes;
+    const uint32_t h = item % H, tok = item / H * kRowTokens;
+    for (int b = blockIdx.y; b < p.batch; b += gridDim.y) {
+        const int64_t n = min((int64_t)min(p.n, p.lens[b]), p.T_cap);
+        if ((int64_t)tok >= n) continue;
+        uint32_t w[kRowTokens][2], par[kRowTokens];
+        uint4 x[kRowTokens][2];
+        int64_t at[kRowTokens];
+#pragma unroll
+        for (int u = 0; u < kRowTokens; ++u) {
+            at[u] = (int64_t)tok + u < n ? p.map.at(b, (int)h, (int)tok + u) : -1;
+            if (at[u] < 0) continue;
+            if constexpr (PACKED) lane.load(p.s, at[u], w[u][0], w[u][1], par[u]);
+            else
+#pragma unroll
+                for (int i = 0; i < 2; ++i) x[u][i] = *reinterpret_cast<const uint4*>((lane.is_v ? p.V : p.K) + at[u] * D + lane.word(i) * 8);
         }
-        const uint32_t u[4] = {x.x, x.y, x.z, x.w};
 #pragma unroll
-        for (int e = 0; e < 8; ++e) y[e] = (e & 1) ? bf16hi(u[e >> 1]) : bf16lo(u[e >> 1]);
-    } else {
-        const uint32_t word = reinterpret_cast<const uint32_t*>(is_v ? p.s.vc : p.s.kc)[at * (D / 8) + (is_v ? packed_v_word<D>(w) : packed_k_word<D>(w))];
-        const uint32_t par = p.s.par[at * (D / 32) + is_v * (D / 64) + (w >> 3)];
+        for (int u = 0; u < kRowTokens; ++u) {
+            if (at[u] < 0) continue;
 #pragma unroll
-        for (int e = 0; e < 8; ++e) y[e] = packed_value(word, e, bf16lo(par), bf16hi(par));
-    }
-    if (p.f32) {
-        float4* o = reinterpret_cast<float4*>(static_cast<float*>(is_v ? p.v : p.k) + dst);
-        o[0] = make_float4(y[0], y[1], y[2], y[3]);
-        o[1] = make_float4(y[4], y[5], y[6], y[7]);
-    } else {
-        *reinterpret_cast<uint4*>(static_cast<uint16_t*>(is_v ? p.v : p.k) + dst) =
-            make_uint4(pack_bf16x2(y[0], y[1]), pack_bf16x2(y[2], y[3]), pack_bf16x2(y[4], y[5]), pack_bf16x2(y[6], y[7]));
+            for (int i = 0; i < 2; ++i) {
+                const int64_t dst = (((int64_t)b * p.n + tok + u) * H + h) * D + lane.word(i) * 8;
+                if constexpr (!PACKED && !F32) {
+                    *reinterpret_cast<uint4*>(static_cast<uint16_t*>(lane.is_v ? p.v : p.k) + dst) = x[u][i];
+                } else {
+                    float y[8];
+#pragma unroll
+                    for (int e = 0; e < 8; ++e) {
+                        if constexpr (PACKED) {
+                            y[e] = packed_value(w[u][i], e, bf16lo(par[u]), bf16hi(par[u]));
+                        } else {
+                            const uint32_t pair = (&x[u][i].x)[e >> 1];
+                            y[e] = (e & 1) ? bf16hi(pair) : bf16lo(pair);
+                        }
+                    }
+                    if constexpr (F32) {
+                        float4* o = reinterpret_cast<float4*>(static_cast<float*>(lane.is_v ? p.v : p.k) + dst);
+                        o[0] = make_float4(y[0], y[1], y[2], y[3]);
+                        o[1] = make_float4(y[4], y[5], y[6], y[7]);
+                    } else {
+                        *reinterpret_cast<uint4*>(static_cast<uint16_t*>(lane.is_v ? p.v : p.k) + dst) =
+                            make_uint4(cvt_bf16x2(y[0], y[1]), cvt_bf16x2(y[2], y[3]), cvt_bf16x2(y[4], y[5]), cvt_bf16x2(y[6], y[7]));
+                    }
+                }
+            }
+        }
     }
 }
 
