@@ -421,8 +421,9 @@ class Cache:
 
     def lckv_append_kv(self, slot, k_new, v_new, batch=None, advance_len=0, stream=None):
         batch = k_new.shape[0] if batch is None else batch
-        _chk(lib().lckv_append_kv(self.h, slot, _ptr(k_new), _ptr(v_new), batch, advance_len,
-                                  _stream(stream)), "lckv_append_kv")
+        rc = (_CALLS or calls()).append_kv(self.call[0] or 0, slot, k_new, v_new, batch, advance_len, None if stream is None else stream.cuda_stream)
+        if rc:
+            _fail(rc, "lckv_append_kv", "k_new and v_new are CUDA tensors")
 
     def lckv_project_append_kv(self, slot, x, w_k, w_v, rope_cos=None, rope_sin=None, batch=None,
                                advance_len=0, stream=None):
@@ -461,8 +462,9 @@ class Cache:
         batch = q.shape[0] if batch is None else batch
         if out is None:
             out = torch.empty(q.shape, dtype=self.out_torch_dtype, device=q.device)
-        _chk(lib().lckv_decode_attention(self.h, slot, mode, _ptr(q), _ptr(out), _ptr(lse), batch,
-                                         _stream(stream)), "lckv_decode_attention")
+        rc = (_CALLS or calls()).decode_attention(self.call[0] or 0, slot, mode, q, out, lse, batch, None if stream is None else stream.cuda_stream)
+        if rc:
+            _fail(rc, "lckv_decode_attention", "q, out and lse are CUDA tensors")
         return out
 
     def lckv_layer_stack_step(self, q_layers, out_layers, k_new_layers, v_new_layers, batch=None,
@@ -483,8 +485,9 @@ class Cache:
 
     # -- prompt encoding (token-major tensors [B, n_max, H, d_h]) -------------------------------
     def lckv_prefill_write_kv(self, slot, k, v, stream=None):
-        _chk(lib().lckv_prefill_write_kv(self.h, slot, _ptr(k), _ptr(v), k.shape[1], k.shape[0],
-                                         _stream(stream)), "lckv_prefill_write_kv")
+        rc = (_CALLS or calls()).prefill_write_kv(self.call[0] or 0, slot, k, v, k.shape[1], k.shape[0], None if stream is None else stream.cuda_stream)
+        if rc:
+            _fail(rc, "lckv_prefill_write_kv", "k and v are CUDA tensors")
 
     def lckv_prefill_attention(self, slot, mode, q, out=None, stream=None):
         if out is None:

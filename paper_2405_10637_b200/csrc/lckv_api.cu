@@ -275,7 +275,7 @@ void make_layout(const lckv_config_t& c, int n_slots, int n_workers, int n_kv_la
     y.slot_bytes =
         c.page_rows ? align_up((size_t)c.n_pages * c.n_kv_heads * (size_t)c.page_rows * c.head_dim * 2, A)
                     : align_up((size_t)c.max_batch * c.n_kv_heads * (size_t)c.max_seq * c.head_dim * 2, A);
-    // a 4-bit slot is one piece of two such halves: keys' codes, values' codes, groups' parameters
+    // a 4-bit slot is one piece of two such halves: tiles of 64 rows
     if (c.kv_bits == 4) y.slot_bytes = align_up((size_t)slot_rows(c) * (c.head_dim / 2 + c.head_dim / 16), A);
     y.off_pt = off;
     if (c.page_rows)
@@ -313,15 +313,7 @@ uint16_t* slot_v(const lckv_cache* c, int s)
                                        (size_t)(2 * s + 1) * c->lay.slot_bytes);
 }
 
-lckv::PackedSlot packed_slot(const lckv_cache* c, int s)
-{
-    lckv::PackedSlot p;
-    const int64_t codes = slot_rows(c->cfg) * (c->cfg.head_dim / 2);
-    p.kc = c->base + c->lay.off_slots + (size_t)(2 * s) * c->lay.slot_bytes;
-    p.vc = p.kc + codes;
-    p.par = reinterpret_cast<uint32_t*>(p.vc + codes);
-    return p;
-}
+lckv::PackedSlot packed_slot(const lckv_cache* c, int s) { return lckv::PackedSlot{c->base + c->lay.off_slots + (size_t)(2 * s) * c->lay.slot_bytes}; }
 
 lckv::RowMap row_map(const lckv_cache* c)
 {

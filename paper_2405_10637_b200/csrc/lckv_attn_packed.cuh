@@ -25,7 +25,7 @@
 // low + 8 step in place of low.  A bf16 output's own rounding (2^-9) is 20 times what that would gain.
 //
 // Work decomposition, merge of split pairs and tickets are those of lckv_attn_mma.cuh.  A worker (warp) has a ring of
-// whole tiles: 64 rows of keys, values and parameters arrive as three bulk copies on one barrier.
+// whole tiles: 64 rows of keys, values and parameters arrive as one bulk copy (the last rows of a sequence as three).
 #pragma once
 #include "lckv_attn_mma.cuh"
 #include "lckv_packed.cuh"
@@ -40,9 +40,6 @@ namespace lckv {
 #endif
 constexpr int kPackedWarps = LCKV_PACKED_WARPS;   // workers per CTA, one CTA per SM
 constexpr int kPackedSlots = LCKV_PACKED_SLOTS;   // tiles in a worker's ring
-constexpr int kPackedRows = 64;                   // rows of a tile
-template <int D>
-__host__ __device__ constexpr int packed_tile_bytes() { return kPackedRows * (D + D / 8); }
 template <int D>
 __host__ __device__ constexpr int packed_smem_bytes() { return kPackedWarps * kPackedSlots * (packed_tile_bytes<D>() + 8) + 128; }
 
@@ -226,7 +223,16 @@ __device__ __forceinline__ uint32_t packed_range(const AttnParams& p, uint32_t w
 {
     const uint32_t FULL = 0xffffffffu, H = (uint32_t)p.H_q;
     int lo = 0, n = p.B, per = (n + 31) / 32;
-    uint32_t mine = packed_lane_tiles(p, min(n, lane * per), min(n, (lane + 1) * per)), all;
+    int32_t nv = 0;                                  // of the lane's sequence, where it has one
+    const auto tiles_of_lane = [&]() {
+        const int b0 = lo + min(n, lane * per), b1 = lo + min(n, (lane + 1) * per);
+        if (per == 1) {
+            nv = b0 < b1 ? packed_visible(p, b0) : 0;
+            return packed_tiles(nv);
+        }
+        return packed_lane_tiles(p, b0, b1);
+    };
+    uint32_t mine = tiles_of_lane(), all;
     uint32_t before = warp_sum_before(mine, lane, all);
     share.each = all * H / (uint32_t)p.n_workers;
     share.more = all * H - share.each * (uint32_t)p.n_workers;
@@ -239,14 +245,13 @@ __device__ __forceinline__ uint32_t packed_range(const AttnParams& p, uint32_t w
         const int l = __ffs(there) - 1;
         base += __shfl_sync(FULL, before, l);
         lo += l * per;
+        if (per == 1) { c.nv = __shfl_sync(FULL, nv, l); break; }
         n = min(per, n - l * per);
-        if (n == 1) break;
         per = (n + 31) / 32;
-        mine = packed_lane_tiles(p, lo + min(n, lane * per), lo + min(n, (lane + 1) * per));
+        mine = tiles_of_lane();
         before = warp_sum_before(mine, lane, all);
     }
     c.b = lo;
-    c.nv = packed_visible(p, lo);
     c.nt = packed_tiles(c.nv);
     const uint32_t rel = first - base * H, h = rel / c.nt;
     c.t = rel - h * c.nt;
@@ -300,6 +305,10 @@ __global__ void __launch_bounds__(kPackedWarps * 32, 1) attn_packed_kernel(const
     const uint32_t n_tiles = packed_range(p, (uint32_t)w, per_kv, lane, share, cc);
     PackedCursor ci = cc;
 
+    const int head = min(g4 % QP, HP - 1);       // of the column g4; columns without a head repeat the last one's query
+    auto query_of = [&](const PackedCursor& c) {
+        return p.q + ((size_t)c.b * n_q_heads + (size_t)(c.kvh * per_kv + c.sub) * HP + head) * D + 8 * c4;
+    };
     const uint64_t l2pol = make_l2_policy(p.l2_keep);
     uint32_t issued = 0, islot = 0;
     PageWalker walker;
@@ -308,23 +317,42 @@ __global__ void __launch_bounds__(kPackedWarps * 32, 1) attn_packed_kernel(const
         if constexpr (PAGED) row = max((int64_t)0, walker.row(p, ci.b, ci.kvh, (int)ci.t * R));   // (a row without a page: any row)
         else row = ((int64_t)ci.b * p.H_kv + ci.kvh) * pp.pitch + (int64_t)ci.t * R;
         if (lane == 0) {
-            // (an even number of rows: a row's parameters are 8 bytes where D = 64; the slot holds whole tiles)
-            const uint32_t rows = ((uint32_t)min(R, ci.nv - (int)ci.t * R) + 1u) & ~1u;
             const uint32_t bar = bars + 8 * islot, dst = ring + islot * TILE;
-            mbar_expect_tx(bar, rows * (D + D / 8));
-            bulk_g2s_hint(dst, pp.s.kc + row * (D / 2), rows * (D / 2), bar, l2pol);
-            bulk_g2s_hint(dst + 2 * CODES, pp.s.par + row * (2 * G), rows * (8 * G), bar, l2pol);
-            bulk_g2s_hint(dst + CODES, pp.s.vc + row * (D / 2), rows * (D / 2), bar, l2pol);
+            const uint8_t* src = pp.s.tile<D>(row);
+            const int left = ci.nv - (int)ci.t * R;
+            if (left >= R) {
+                mbar_expect_tx(bar, TILE);
+                bulk_g2s_hint(dst, src, TILE, bar, l2pol);
+            } else {
+                // (an even number of rows: a row's parameters are 8 bytes where D = 64)
+                const uint32_t rows = ((uint32_t)left + 1u) & ~1u;
+                mbar_expect_tx(bar, rows * (D + D / 8));
+                bulk_g2s_hint(dst, src, rows * (D / 2), bar, l2pol);
+                bulk_g2s_hint(dst + 2 * CODES, src + 2 * CODES, rows * (8 * G), bar, l2pol);
+                bulk_g2s_hint(dst + CODES, src + CODES, rows * (D / 2), bar, l2pol);
+            }
         }
         packed_next(ci, p, per_kv);
         ++issued;
         islot = (islot + 1 == NS) ? 0 : islot + 1;
     };
+    // The first pair's queries are asked for in front of the tiles, behind which they would wait in line (20 us with 12 workers'
+    // tiles in front of them: 4800 cycles), unless only the tiles may be read yet.
+    uint4 q_raw[J];
+    auto load_q = [&]() {                        // the query heads of pair cc, NC times
+        const uint4* src = reinterpret_cast<const uint4*>(query_of(cc));
+#pragma unroll
+        for (int j = 0; j < J; ++j) q_raw[j] = src[4 * j];
+    };
+    if (!p.early_kv && n_tiles) load_q();
     {
         const uint32_t pro = n_tiles < (uint32_t)NS ? n_tiles : (uint32_t)NS;
         while (issued < pro) issue();
     }
-    if (p.early_kv) pdl_wait_then_release();
+    if (p.early_kv) {
+        pdl_wait_then_release();
+        if (n_tiles) load_q();
+    }
 
     // Sequences that see nothing: zero rows (zero dummy key and value), lse 0.
     for (int b = w < p.n_workers ? w : p.B; b < p.B; b += p.n_workers) {
@@ -343,18 +371,7 @@ __global__ void __launch_bounds__(kPackedWarps * 32, 1) attn_packed_kernel(const
     bool ok = true;
 
     PackedQuery<D> q;
-    const int head = min(g4 % QP, HP - 1);       // of the column g4; columns without a head repeat the last one's query
-    auto query_of = [&](const PackedCursor& c) {
-        return p.q + ((size_t)c.b * n_q_heads + (size_t)(c.kvh * per_kv + c.sub) * HP + head) * D + 8 * c4;
-    };
-    auto load_q = [&]() {                        // the query heads of pair cc, NC times
-        const uint4* src = reinterpret_cast<const uint4*>(query_of(cc));
-        uint4 raw[J];
-#pragma unroll
-        for (int j = 0; j < J; ++j) raw[j] = src[4 * j];
-        packed_query<D>(raw, p.scale_log2, lane, q);
-    };
-    load_q();
+    packed_query<D>(q_raw, p.scale_log2, lane, q);
 
     // running state of this lane's two columns
     float m_run[2], l_run[2];
@@ -452,26 +469,34 @@ __global__ void __launch_bounds__(kPackedWarps * 32, 1) attn_packed_kernel(const
             for (int e = 0; e < 4; ++e) r[i][e] = 0.f;
         if (!holds) return;
         constexpr int AHEAD = MTL <= 2 ? 8 : MTL == 4 ? 4 : 2;     // records in flight
-#pragma unroll AHEAD
-        for (int i = 0; i < n; ++i) {
-            const float* rec = rec0 + (size_t)i * rstride + (i == 0 ? (size_t)first_slot * REC : 0);
-            const float2 mm = __ldcg(reinterpret_cast<const float2*>(rec + MTL * 128 + q0));
-            const float2 ll = __ldcg(reinterpret_cast<const float2*>(rec + MTL * 128 + 8 + q0));
-            float4 x[MTL];
+        for (int i0 = 0; i0 < n; i0 += AHEAD) {
+            float2 mm[AHEAD], ll[AHEAD];
+            float4 x[AHEAD][MTL];
 #pragma unroll
-            for (int k = 0; k < MTL; ++k) x[k] = __ldcg(reinterpret_cast<const float4*>(rec) + k * 32 + lane);
-            const float M0 = fmaxf(m_fin[0], mm.x), M1 = fmaxf(m_fin[1], mm.y);
-            const float a0 = ex2(m_fin[0] - M0), a1 = ex2(m_fin[1] - M1);      // ex2(-inf) = 0 for the first record
-            const float w0 = ex2(mm.x - M0), w1 = ex2(mm.y - M1);
-            m_fin[0] = M0; m_fin[1] = M1;
-            l_tot[0] = fmaf(l_tot[0], a0, ll.x * w0);
-            l_tot[1] = fmaf(l_tot[1], a1, ll.y * w1);
+            for (int a = 0; a < AHEAD; ++a) {
+                const int i = min(i0 + a, n - 1);
+                const float* rec = rec0 + (size_t)i * rstride + (i == 0 ? (size_t)first_slot * REC : 0);
+                mm[a] = __ldcg(reinterpret_cast<const float2*>(rec + MTL * 128 + q0));
+                ll[a] = __ldcg(reinterpret_cast<const float2*>(rec + MTL * 128 + 8 + q0));
 #pragma unroll
-            for (int k = 0; k < MTL; ++k) {
-                r[k][0] = fmaf(r[k][0], a0, x[k].x * w0);
-                r[k][1] = fmaf(r[k][1], a1, x[k].y * w1);
-                r[k][2] = fmaf(r[k][2], a0, x[k].z * w0);
-                r[k][3] = fmaf(r[k][3], a1, x[k].w * w1);
+                for (int k = 0; k < MTL; ++k) x[a][k] = __ldcg(reinterpret_cast<const float4*>(rec) + k * 32 + lane);
+            }
+#pragma unroll
+            for (int a = 0; a < AHEAD; ++a) {
+                if (i0 + a >= n) break;
+                const float M0 = fmaxf(m_fin[0], mm[a].x), M1 = fmaxf(m_fin[1], mm[a].y);
+                const float a0 = ex2(m_fin[0] - M0), a1 = ex2(m_fin[1] - M1);      // ex2(-inf) = 0 for the first record
+                const float w0 = ex2(mm[a].x - M0), w1 = ex2(mm[a].y - M1);
+                m_fin[0] = M0; m_fin[1] = M1;
+                l_tot[0] = fmaf(l_tot[0], a0, ll[a].x * w0);
+                l_tot[1] = fmaf(l_tot[1], a1, ll[a].y * w1);
+#pragma unroll
+                for (int k = 0; k < MTL; ++k) {
+                    r[k][0] = fmaf(r[k][0], a0, x[a][k].x * w0);
+                    r[k][1] = fmaf(r[k][1], a1, x[a][k].y * w1);
+                    r[k][2] = fmaf(r[k][2], a0, x[a][k].z * w0);
+                    r[k][3] = fmaf(r[k][3], a1, x[a][k].w * w1);
+                }
             }
         }
     };
@@ -766,6 +791,7 @@ __global__ void __launch_bounds__(kPackedWarps * 32, 1) attn_packed_kernel(const
             packed_next(cc, p, per_kv);
             if (pair_end) {
                 load_q();
+                packed_query<D>(q_raw, p.scale_log2, lane, q);
                 seg_t0 = 0;
                 first_seg = false;
                 if (n_tiles - (tile + 1) < cc.nt) cur = split_of(first_tile + tile + 1, cc.nt);   // the range ends inside this pair
@@ -788,7 +814,7 @@ __global__ void __launch_bounds__(kPackedWarps * 32, 1) attn_packed_kernel(const
 #pragma unroll 1
             for (bool whole = !two_level;;) {
                 if (ticket != n - 1) break;              // someone else arrives later and merges
-                __threadfence();
+                __syncwarp();                            // lane 0's acquire is in front of all lanes' reads of the records
                 merge_records(n, (uint32_t)first, step, slot);
                 if (lane == 0) *at = 0;                  // ready for the next launch
                 if (whole) { write_rows(pd.b, pd.h); break; }

@@ -232,6 +232,53 @@ PyObject* rope_cache(Args& a)
     });
 }
 
+// The calls below hand pointers on as they are: what they take of their tensors is the caller's to keep, as in the header.  The stream
+// is the one given, or the current one of the current device.
+template <typename F>
+PyObject* pass(Args& args, F call)
+{
+    PyObject* given = args.take();
+    if (!args.ok) return code(kBadTensor);
+    void* stream = nullptr;
+    if (given == Py_None) {
+        stream = c10::cuda::getCurrentCUDAStream().stream();
+    } else {
+        stream = PyLong_AsVoidPtr(given);
+        if (!stream && PyErr_Occurred()) return nullptr;
+    }
+    return code(call(stream));
+}
+
+// cache, slot, mode, q, out, lse, batch, stream
+PyObject* decode_attention(Args& a)
+{
+    auto* cache = static_cast<lckv_cache_t*>(a.address());
+    const int32_t slot = a.integer32(), mode = a.integer32();
+    const at::Tensor *q = a.tensor(), *out = a.tensor(), *lse = a.tensor();
+    const int32_t batch = a.integer32();
+    return pass(a, [&](void* st) { return lckv_decode_attention(cache, slot, mode, ptr(q), mut(out), static_cast<float*>(mut(lse)), batch, st); });
+}
+
+// cache, slot, k, v, batch, advance, stream
+PyObject* append_kv(Args& a)
+{
+    auto* cache = static_cast<lckv_cache_t*>(a.address());
+    const int32_t slot = a.integer32();
+    const at::Tensor *k = a.tensor(), *v = a.tensor();
+    const int32_t batch = a.integer32(), advance = a.integer32();
+    return pass(a, [&](void* st) { return lckv_append_kv(cache, slot, ptr(k), ptr(v), batch, advance, st); });
+}
+
+// cache, slot, k, v, n_max, batch, stream
+PyObject* prefill_write_kv(Args& a)
+{
+    auto* cache = static_cast<lckv_cache_t*>(a.address());
+    const int32_t slot = a.integer32();
+    const at::Tensor *k = a.tensor(), *v = a.tensor();
+    const int32_t n = a.integer32(), batch = a.integer32();
+    return pass(a, [&](void* st) { return lckv_prefill_write_kv(cache, slot, ptr(k), ptr(v), n, batch, st); });
+}
+
 // cache, its device, slot, H_kv, d, k, v, stream
 PyObject* read_kv(Args& a)
 {
@@ -295,7 +342,7 @@ PyObject* evict_kv(Args& a)
 
 #define LCKV_CALL(name) {#name, reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)(void)>(entry<name>)), METH_FASTCALL, nullptr}
 PyMethodDef methods[] = {LCKV_CALL(rope_tables), LCKV_CALL(rope_apply), LCKV_CALL(rms_norm), LCKV_CALL(quant_linear), LCKV_CALL(rope_cache),
-                         LCKV_CALL(read_kv), LCKV_CALL(attention_weights), LCKV_CALL(evict_kv),
+                         LCKV_CALL(decode_attention), LCKV_CALL(append_kv), LCKV_CALL(prefill_write_kv), LCKV_CALL(read_kv), LCKV_CALL(attention_weights), LCKV_CALL(evict_kv),
                          {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_lckv_calls", "Per-layer calls of liblckv.so on torch tensors.", -1, methods, nullptr, nullptr, nullptr, nullptr};
 

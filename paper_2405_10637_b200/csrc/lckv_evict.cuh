@@ -34,10 +34,10 @@ struct KeyFragment {
 #pragma unroll
             for (int j = 0; j < J; ++j) w[j] = x[4 * j];
         } else if constexpr (D == 128) {
-            const uint4 x = *reinterpret_cast<const uint4*>(p.s.kc + row * 64 + c4 * 16);
+            const uint4 x = *reinterpret_cast<const uint4*>(p.s.keys<D>(row) + c4 * 16);
             w[0] = x.x; w[1] = x.y; w[2] = x.z; w[3] = x.w;
         } else {
-            const uint2 x = *reinterpret_cast<const uint2*>(p.s.kc + row * 32 + c4 * 8);
+            const uint2 x = *reinterpret_cast<const uint2*>(p.s.keys<D>(row) + c4 * 8);
             w[0] = x.x; w[1] = x.y;
         }
     }
@@ -98,8 +98,8 @@ __global__ void __launch_bounds__(kWeightWarps * 32) attention_weights_kernel(co
                     for (int i = 0; i < NB; ++i)
 #pragma unroll
                         for (int g = 0; g < G; ++g) {
-                            pa[i][g] = p.s.par[(at + min((i * NC + copy) * 16 + g4, rows - 1)) * (2 * G) + g];
-                            pb[i][g] = p.s.par[(at + min((i * NC + copy) * 16 + g4 + 8, rows - 1)) * (2 * G) + g];
+                            pa[i][g] = p.s.par<D>(at + min((i * NC + copy) * 16 + g4, rows - 1))[g];
+                            pb[i][g] = p.s.par<D>(at + min((i * NC + copy) * 16 + g4 + 8, rows - 1))[g];
                         }
                 }
                 const int ma = (mine * NC + copy) * 16 + g4, mb = ma + 8;        // rows that this lane writes
@@ -370,9 +370,8 @@ struct RowUnits {
     static __device__ __forceinline__ const Unit* at(const PackedSlot& s, const uint16_t* K, const uint16_t* V, int64_t row, int u)
     {
         if constexpr (PACKED) {
-            if (u < 4) return reinterpret_cast<const Unit*>(s.kc + row * (D / 2)) + u;
-            if (u < 8) return reinterpret_cast<const Unit*>(s.vc + row * (D / 2)) + (u - 4);
-            return reinterpret_cast<const Unit*>(s.par + row * (D / 32));
+            if (u < 8) return reinterpret_cast<const Unit*>(s.keys<D>(row) + (u < 4 ? 0 : kPackedRows * (D / 2))) + (u & 3);
+            return reinterpret_cast<const Unit*>(s.par<D>(row));
         } else {
             return reinterpret_cast<const Unit*>((u < D / 8 ? K : V) + row * D) + (u < D / 8 ? u : u - D / 8);
         }

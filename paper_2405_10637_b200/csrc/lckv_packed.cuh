@@ -6,14 +6,13 @@
 // (fp32; the sixteenths keep a group that spans bf16's whole range from overflowing).  A group with an infinity or a NaN
 // stands for NaN: low is NaN, step 0 (steps are always finite and not negative).
 //
-// Three arrays per slot, indexed by the physical row:
-//   kc, vc [rows][D/2] bytes   codes.  A 32-bit word holds eight neighbouring dimensions, dimension 8 w + i in bits 4 i.
-//                              A key's words lie in the order in which the four lanes that share a row of an MMA tile
-//                              take them (word 4 j + c at c * D/32 + j); a value's so that the words of the two groups
-//                              alternate (D = 128: word w at 2 (w mod 8) + w / 8).
-//   par    [rows][2 D/64]      per group step (low half) and low (high half), bf16: the key's groups, then the value's.
-// Row pitch of a (sequence, head) is the capacity rounded up to 64 rows, so that every tile starts on 16 bytes and none
-// leaves the slot; pages hold a multiple of 64 rows anyway.
+// A slot is a sequence of tiles of 64 physical rows, 72 D bytes each, which one bulk copy brings:
+//     keys   [64][D/2] bytes      codes.  A 32-bit word holds eight neighbouring dimensions, dimension 8 w + i in bits 4 i.
+//                                 A key's words lie in the order in which the four lanes that share a row of an MMA tile
+//                                 take them: word 4 j + c at c * D/32 + j.
+//     values [64][D/2] bytes      ..., so that the words of the two groups alternate: word w at 2 (w mod 8) + w / 8 (D = 128)
+//     parameters [64][2 D/64]     per group step (low half) and low (high half), bf16: the key's groups, then the value's
+// Row pitch of a (sequence, head) is the capacity rounded up to 64 rows; pages hold a multiple of 64 rows anyway.
 #pragma once
 #include "lckv_attn_mma.cuh"
 
@@ -22,10 +21,20 @@ namespace lckv {
 constexpr float kPackedRatio = 1.0666667222976685f;   // fp32(16 / 15)
 constexpr float kPackedMinStep = 7.523163845262640e-37f;   // 2^-120
 
+constexpr int kPackedRows = 64;                   // rows of a tile
+template <int D>
+__host__ __device__ constexpr int packed_tile_bytes() { return kPackedRows * (D + D / 8); }
+
 struct PackedSlot {
-    uint8_t* kc;
-    uint8_t* vc;
-    uint32_t* par;
+    uint8_t* base;
+    template <int D>
+    __device__ __forceinline__ uint8_t* tile(int64_t row) const { return base + (row >> 6) * packed_tile_bytes<D>(); }
+    template <int D>
+    __device__ __forceinline__ uint8_t* keys(int64_t row) const { return tile<D>(row) + (row & 63) * (D / 2); }
+    template <int D>
+    __device__ __forceinline__ uint8_t* values(int64_t row) const { return keys<D>(row) + kPackedRows * (D / 2); }
+    template <int D>
+    __device__ __forceinline__ uint32_t* par(int64_t row) const { return reinterpret_cast<uint32_t*>(tile<D>(row) + kPackedRows * D + (row & 63) * (D / 8)); }
 };
 
 // Physical row of row r of (sequence, kv head): slots of `pitch` rows per (sequence, head), or pages.
@@ -72,18 +81,18 @@ struct PackedLane {
     __device__ __forceinline__ int word(int i) const { return 8 * g + c + 4 * i; }
     __device__ __forceinline__ void store(const PackedSlot& s, int64_t row, uint32_t w0, uint32_t w1, uint32_t par) const
     {
-        uint32_t* codes = reinterpret_cast<uint32_t*>(is_v ? s.vc : s.kc) + row * (D / 8);
+        uint32_t* codes = reinterpret_cast<uint32_t*>(is_v ? s.values<D>(row) : s.keys<D>(row));
         if (is_v) {
             codes[packed_v_word<D>(word(0))] = w0;
             codes[packed_v_word<D>(word(1))] = w1;
         } else {
             *reinterpret_cast<uint2*>(codes + packed_k_word<D>(word(0))) = make_uint2(w0, w1);
         }
-        if (c == 0) s.par[row * (D / 32) + is_v * (D / 64) + g] = par;
+        if (c == 0) s.par<D>(row)[is_v * (D / 64) + g] = par;
     }
     __device__ __forceinline__ void load(const PackedSlot& s, int64_t row, uint32_t& w0, uint32_t& w1, uint32_t& par) const
     {
-        const uint32_t* codes = reinterpret_cast<const uint32_t*>(is_v ? s.vc : s.kc) + row * (D / 8);
+        const uint32_t* codes = reinterpret_cast<const uint32_t*>(is_v ? s.values<D>(row) : s.keys<D>(row));
         if (is_v) {
             w0 = codes[packed_v_word<D>(word(0))];
             w1 = codes[packed_v_word<D>(word(1))];
@@ -92,7 +101,7 @@ struct PackedLane {
             w0 = w.x;
             w1 = w.y;
         }
-        par = s.par[row * (D / 32) + is_v * (D / 64) + g];
+        par = s.par<D>(row)[is_v * (D / 64) + g];
     }
 };
 
