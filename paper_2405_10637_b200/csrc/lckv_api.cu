@@ -196,7 +196,7 @@ int mma_heads_per_pair(const lckv_config_t& c)
 
 int workers_per_sm(const lckv_config_t& c)
 {
-    if (resolve_kernel_kind(c) == 3) return lckv::kPackedWarps;
+    if (resolve_kernel_kind(c) == 3) return lckv::packed_warps(c.head_dim);
     return resolve_kernel_kind(c) == 2 ? lckv::kMmaWarps * lckv::kMmaCtas : lckv::kAluWarps * lckv::kAluCtas;
 }
 
@@ -495,8 +495,13 @@ int launch_attention(lckv_cache* c, int slot, int mode, const void* q, void* out
         pp.m.groups_per_kv = c->cfg.n_q_heads / c->cfg.n_kv_heads / pp.m.heads_per_pair;
         pp.s = packed_slot(c, slot);
         pp.pitch = row_pitch(c->cfg);
+        const int warps = lckv::packed_warps(c->cfg.head_dim);
+        pp.n_blocks = std::min(c->grid, (c->active_workers + warps - 1) / warps);
+        pp.n_warps = (c->active_workers + pp.n_blocks - 1) / pp.n_blocks;
+        pp.pairs_per_block = (int32_t)(((int64_t)batch * c->h_pairs + pp.n_blocks - 1) / pp.n_blocks);
+        pp.warps_inverse = (uint32_t)(((1ull << 32) + pp.n_warps - 1) / pp.n_warps);
         const bool wide = c->cfg.head_dim == 128;
-        e = launch_pdl(packed_variant(c->cfg), c->grid, lckv::kPackedWarps * 32,
+        e = launch_pdl(packed_variant(c->cfg), c->grid, warps * 32,
                        wide ? lckv::packed_smem_bytes<128>() : lckv::packed_smem_bytes<64>(), st, pp);
     } else if (c->kernel_kind == 2) {
         lckv::MmaParams mp;

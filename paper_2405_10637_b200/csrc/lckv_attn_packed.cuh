@@ -24,24 +24,32 @@
 // the rest (a second MMA), and codes enter as c - 8, which is exact too (one more instruction for two codes), with
 // low + 8 step in place of low.  A bf16 output's own rounding (2^-9) is 20 times what that would gain.
 //
-// Work decomposition, merge of split pairs and tickets are those of lckv_attn_mma.cuh.  A worker (warp) has a ring of
-// whole tiles: 64 rows of keys, values and parameters arrive as one bulk copy (the last rows of a sequence as three).
+// Work: a launch is one long sequence of tiles of 64 rows, (sequence, pair, tile), cut into one range per thread block and
+// those into one per worker (warp).  A pair that several warps of a block share is joined behind a block barrier; only what
+// crosses blocks, at most the first and the last pair of each, takes records, tickets and merging as in lckv_attn_mma.cuh, which
+// costs 3 us.  Where whole pairs fill the blocks about as evenly (all rule and no exception with equal lengths),
+// blocks are cut between pairs and nothing crosses.  A worker has a ring of whole tiles: keys, values and parameters of
+// 64 rows arrive as one bulk copy (the last rows of a sequence as three).
 #pragma once
 #include "lckv_attn_mma.cuh"
 #include "lckv_packed.cuh"
 
 namespace lckv {
 
-#ifndef LCKV_PACKED_WARPS
-#define LCKV_PACKED_WARPS 12
+#ifndef LCKV_PACKED_WARPS_128
+#define LCKV_PACKED_WARPS_128 12
+#endif
+#ifndef LCKV_PACKED_WARPS_64
+#define LCKV_PACKED_WARPS_64 16
 #endif
 #ifndef LCKV_PACKED_SLOTS
 #define LCKV_PACKED_SLOTS 2
 #endif
-constexpr int kPackedWarps = LCKV_PACKED_WARPS;   // workers per CTA, one CTA per SM
 constexpr int kPackedSlots = LCKV_PACKED_SLOTS;   // tiles in a worker's ring
+// Workers per thread block, one block per SM.
+__host__ __device__ constexpr int packed_warps(int d) { return d == 128 ? LCKV_PACKED_WARPS_128 : LCKV_PACKED_WARPS_64; }
 template <int D>
-__host__ __device__ constexpr int packed_smem_bytes() { return kPackedWarps * kPackedSlots * (packed_tile_bytes<D>() + 8) + 128; }
+__host__ __device__ constexpr int packed_smem_bytes() { return packed_warps(D) * kPackedSlots * (packed_tile_bytes<D>() + 8) + 128; }
 
 __device__ __forceinline__ void mma_f16_16816(float (&c)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1)
 {
@@ -159,6 +167,9 @@ struct PackedParams {
     MmaParams m;         // a.K, a.V, a.pre and a.start unused; a.H_q = pairs per sequence
     PackedSlot s;
     int64_t pitch;       // rows of a (sequence, kv head)
+    int32_t n_blocks, n_warps;   // thread blocks and warps of each that work
+    int32_t pairs_per_block;     // ceil(all pairs / n_blocks)
+    uint32_t warps_inverse;      // ceil(2^32 / n_warps)
 };
 
 // Position in a launch's tile sequence, in (b, pair, tile) order; pair h = kvh * (pairs per kv head) + sub.
@@ -188,83 +199,144 @@ __device__ __forceinline__ void packed_next(PackedCursor& c, const AttnParams& p
     } while (c.nt == 0);
 }
 
-// The launch's tiles are cut into one range per worker; the first `more` ranges are one tile longer.  A warp works out the
-// total and where its range begins by itself: the lanes add up the tiles of B / 32 sequences each, and the lane in whose
-// part the range begins is looked into with all lanes again, until a lane has one sequence.
+// n things cut into parts of `each`, the first `more` with one more.
 struct PackedShare {
-    uint32_t each, more;          // tiles of a range; ranges with one more
+    uint32_t each, more;
+    __device__ __forceinline__ PackedShare(uint32_t n, uint32_t parts) : each(n / parts), more(n - n / parts * parts) {}
     __device__ __forceinline__ uint32_t begin(uint32_t w) const { return w * each + min(w, more); }
-    __device__ __forceinline__ uint32_t worker(uint32_t tile) const
+    __device__ __forceinline__ uint32_t part(uint32_t i) const
     {
         const uint32_t longer = more * (each + 1);
-        return tile < longer ? tile / (each + 1) : more + (tile - longer) / each;
+        return i < longer ? i / (each + 1) : more + (i - longer) / each;
     }
 };
-__device__ __forceinline__ uint32_t packed_lane_tiles(const AttnParams& p, int b0, int b1)
+// The tiles in front of every sequence, per pair of a sequence: before[i] of those in front of sequence i * per (per = 1 up to
+// kPackedTable sequences; with more, a stretch of `per` sequences is walked through where it is needed).
+constexpr int kPackedTable = 1024;
+struct PackedTable {
+    uint32_t before[kPackedTable + 1];
+    int32_t rows[kPackedTable];   // visible rows (per = 1)
+    uint32_t sums[32], longest[32];
+};
+
+// The block's threads fill the table; returns the longest sequence's tiles.
+template <int THREADS>
+__device__ __forceinline__ uint32_t packed_table(const AttnParams& p, int per, PackedTable& t)
 {
-    uint32_t n = 0;
-#pragma unroll 4
-    for (int b = b0; b < b1; ++b) n += packed_tiles(packed_visible(p, b));
-    return n;
-}
-__device__ __forceinline__ uint32_t warp_sum_before(uint32_t v, int lane, uint32_t& all)
-{
-    uint32_t incl = v;
+    const uint32_t FULL = 0xffffffffu;
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+    constexpr int EACH = (kPackedTable + THREADS - 1) / THREADS;     // entries of a thread, side by side
+    const int n = (p.B + per - 1) / per;
+    uint32_t mine[EACH], sum = 0, longest = 0;
+#pragma unroll
+    for (int e = 0; e < EACH; ++e) {
+        const int i = (int)threadIdx.x * EACH + e;
+        mine[e] = 0;
+        if (i < n) {
+            for (int b = i * per; b < min(p.B, (i + 1) * per); ++b) {
+                const int32_t nv = packed_visible(p, b);
+                const uint32_t nt = packed_tiles(nv);
+                if (per == 1) t.rows[i] = nv;
+                mine[e] += nt;
+                longest = max(longest, nt);
+            }
+        }
+        sum += mine[e];
+    }
+    uint32_t incl = sum;
 #pragma unroll
     for (int off = 1; off < 32; off <<= 1) {
-        const uint32_t x = __shfl_up_sync(0xffffffffu, incl, off);
+        const uint32_t x = __shfl_up_sync(FULL, incl, off);
         if (lane >= off) incl += x;
     }
-    all = __shfl_sync(0xffffffffu, incl, 31);
-    return incl - v;
-}
-// Fills share and, if worker w has tiles, their number and the cursor of the first.
-__device__ __forceinline__ uint32_t packed_range(const AttnParams& p, uint32_t w, int per_kv, int lane, PackedShare& share, PackedCursor& c)
-{
-    const uint32_t FULL = 0xffffffffu, H = (uint32_t)p.H_q;
-    int lo = 0, n = p.B, per = (n + 31) / 32;
-    int32_t nv = 0;                                  // of the lane's sequence, where it has one
-    const auto tiles_of_lane = [&]() {
-        const int b0 = lo + min(n, lane * per), b1 = lo + min(n, (lane + 1) * per);
-        if (per == 1) {
-            nv = b0 < b1 ? packed_visible(p, b0) : 0;
-            return packed_tiles(nv);
-        }
-        return packed_lane_tiles(p, b0, b1);
-    };
-    uint32_t mine = tiles_of_lane(), all;
-    uint32_t before = warp_sum_before(mine, lane, all);
-    share.each = all * H / (uint32_t)p.n_workers;
-    share.more = all * H - share.each * (uint32_t)p.n_workers;
-    const uint32_t first = share.begin(w), count = share.each + (w < share.more ? 1u : 0u);
-    if (w >= (uint32_t)p.n_workers || count == 0) return 0;
-    const uint32_t x = first / H;                    // tile of the sequences' concatenation in which the range begins
-    uint32_t base = 0;
-    for (;;) {
-        const uint32_t there = __ballot_sync(FULL, base + before <= x && x < base + before + mine);
-        const int l = __ffs(there) - 1;
-        base += __shfl_sync(FULL, before, l);
-        lo += l * per;
-        if (per == 1) { c.nv = __shfl_sync(FULL, nv, l); break; }
-        n = min(per, n - l * per);
-        per = (n + 31) / 32;
-        mine = tiles_of_lane();
-        before = warp_sum_before(mine, lane, all);
+    longest = __reduce_max_sync(FULL, longest);
+    if (lane == 31) { t.sums[warp] = incl; t.longest[warp] = longest; }
+    __syncthreads();
+    uint32_t at = incl - sum + __reduce_add_sync(FULL, lane < warp ? t.sums[lane] : 0u);
+    longest = __reduce_max_sync(FULL, lane < THREADS / 32 ? t.longest[lane] : 0u);
+#pragma unroll
+    for (int e = 0; e < EACH; ++e) {
+        const int i = (int)threadIdx.x * EACH + e;
+        if (i <= n) t.before[i] = at;
+        at += mine[e];
     }
-    c.b = lo;
-    c.nt = packed_tiles(c.nv);
-    const uint32_t rel = first - base * H, h = rel / c.nt;
-    c.t = rel - h * c.nt;
-    c.kvh = (int)h / per_kv;
-    c.sub = (int)h - c.kvh * per_kv;
-    return count;
+    if (threadIdx.x == THREADS - 1 && n == THREADS * EACH) t.before[n] = at;
+    __syncthreads();
+    return longest;
 }
 
-// A ticket posted for one of the (at most two) pairs that a worker shares with others.
-struct PackedPending { int32_t n, first_odd, b, h, c_first; };
+// What a warp does: from the table, by itself.
+struct PackedRange {
+    uint32_t all;                 // tiles of the launch
+    uint32_t begin, end;          // the thread block's
+    uint32_t first, count;        // the warp's
+    bool whole;                   // blocks are cut between pairs
+};
+__device__ __forceinline__ PackedRange packed_range(const PackedParams& pp, const PackedTable& t, int per, uint32_t longest, uint32_t block, uint32_t warp,
+                                                    int lane, PackedCursor& c)
+{
+    const AttnParams& p = pp.m.a;
+    const uint32_t FULL = 0xffffffffu, H = (uint32_t)p.H_q;
+    const int n = (p.B + per - 1) / per;
+    PackedRange r;
+    r.all = t.before[n] * H;
+    // Blocks cut between pairs, if that leaves a warp at most about one tile more than an even cut: a tile is 1 us, records and
+    // tickets 3.
+    const uint32_t pairs = (uint32_t)p.B * H, blocks = (uint32_t)pp.n_blocks, warps = (uint32_t)pp.n_warps, per_block = (uint32_t)pp.pairs_per_block;
+    r.whole = (uint64_t)per_block * longest * blocks <= (uint64_t)r.all + blocks * warps;
+    if (r.whole) {
+        const auto tiles_before = [&](uint32_t pair) {
+            const int b = (int)(pair / H);
+            if (b >= p.B) return r.all;
+            const int i = b / per;
+            uint32_t x = t.before[i];
+            for (int k = i * per; k < b; ++k) x += packed_tiles(packed_visible(p, k));
+            const uint32_t nt = per == 1 ? t.before[i + 1] - x : packed_tiles(packed_visible(p, b));
+            return x * H + (pair - (uint32_t)b * H) * nt;
+        };
+        r.begin = tiles_before(min(pairs, block * per_block));
+        r.end = tiles_before(min(pairs, (block + 1) * per_block));
+    } else {
+        const PackedShare share(r.all, blocks);
+        r.begin = block < blocks ? share.begin(block) : 0u;
+        r.end = block < blocks ? share.begin(block + 1) : 0u;
+    }
+    const uint32_t n_block = r.end - r.begin, each = warps == 1 ? n_block : __umulhi(n_block, pp.warps_inverse), more = n_block - each * warps;
+    r.first = r.begin + warp * each + min(warp, more);
+    r.count = warp < warps ? each + (warp < more ? 1u : 0u) : 0u;
+    if (r.count == 0) return r;
+    // the last entry whose tiles begin at or in front of x: 32 entries apart, then one by one
+    const uint32_t x = r.first / H;
+    int i = 32 * (31 - __clz(__ballot_sync(FULL, 32 * lane < n && t.before[min(32 * lane, n)] <= x)));
+    i += 31 - __clz(__ballot_sync(FULL, i + lane < n && t.before[min(i + lane, n)] <= x));
+    uint32_t base = t.before[i];
+    c.b = i;
+    if (per == 1) {
+        c.nv = t.rows[i];
+    } else {
+        c.b = i * per;
+        for (;;) {
+            c.nv = packed_visible(p, c.b);
+            const uint32_t nt = packed_tiles(c.nv);
+            if (x < base + nt) break;
+            base += nt;
+            ++c.b;
+        }
+    }
+    c.nt = packed_tiles(c.nv);
+    const uint32_t rel = r.first - base * H, h = rel / c.nt;
+    c.t = rel - h * c.nt;
+    c.kvh = (int)h / pp.m.groups_per_kv;
+    c.sub = (int)h - c.kvh * pp.m.groups_per_kv;
+    return r;
+}
+
+// Part of a pair that a warp leaves to be joined: the pair's first tile, its tiles (0: none), sequence, number, and whether the
+// part is in the warp's ring (else in its first record: its ring was still in use).
+struct PackedPart { uint32_t begin, nt; int32_t b, h, in_ring; };
 
 template <int D, bool PAGED, int QP, bool EXACT>
-__global__ void __launch_bounds__(kPackedWarps * 32, 1) attn_packed_kernel(const PackedParams pp)
+__global__ void __launch_bounds__(packed_warps(D) * 32, 1) attn_packed_kernel(const PackedParams pp)
 {
     constexpr int R = kPackedRows;
     constexpr int RB = R / 16;                   // 16-row blocks of a tile
@@ -274,6 +346,7 @@ __global__ void __launch_bounds__(kPackedWarps * 32, 1) attn_packed_kernel(const
     constexpr int NC = 8 / QP;                   // copies of the pair's heads in a tile's columns
     constexpr int NB = RB / NC;                  // blocks whose scores a lane works on
     constexpr int NS = kPackedSlots;
+    constexpr int WARPS = packed_warps(D);
     constexpr int TILE = packed_tile_bytes<D>();
     constexpr int CODES = R * (D / 2);           // bytes of a tile's keys; its values follow, then the parameters
     constexpr int MTL = MT / NC;                 // m-tiles of a finished pair that a lane holds
@@ -282,27 +355,34 @@ __global__ void __launch_bounds__(kPackedWarps * 32, 1) attn_packed_kernel(const
     const int HP = pp.m.heads_per_pair, per_kv = pp.m.groups_per_kv, n_q_heads = pp.m.n_q_heads;
 
     extern __shared__ uint8_t smem_raw[];
-    __shared__ PackedPending pending[kPackedWarps][2];
+    __shared__ PackedPart parts[WARPS][2];
+    __shared__ PackedTable table;
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-    const int w = warp * gridDim.x + blockIdx.x;     // (ranges that are one longer spread over the SMs)
+    const int w = blockIdx.x * WARPS + warp;
     const uint32_t FULL = 0xffffffffu;
     const int g4 = lane >> 2, c4 = lane & 3;
     const int copy = 2 * c4 / QP;                // the copy that this lane's columns belong to
 
     const uint32_t smem0 = (smem_u32(smem_raw) + 127u) & ~127u;
     const uint32_t ring = smem0 + warp * (NS * TILE);
-    const uint32_t bars = smem0 + kPackedWarps * NS * TILE + warp * (NS * 8);
+    uint8_t* const ring0 = smem_raw + (smem0 - smem_u32(smem_raw));
+    uint8_t* const ring_bytes = ring0 + warp * (NS * TILE);
+    static_assert(REC * 4 <= NS * TILE, "a record fits a ring");
+    const uint32_t bars = smem0 + WARPS * NS * TILE + warp * (NS * 8);
     if (lane == 0) {
         for (int s = 0; s < NS; ++s) mbar_init(bars + 8 * s, 1);
         fence_mbar_init();
+        parts[warp][0].nt = parts[warp][1].nt = 0;
     }
     __syncwarp();
 
     if (!p.early_kv) pdl_wait_then_release();
 
-    PackedShare share;
     PackedCursor cc = {0, 0, 0, 0u, 0u, 0};
-    const uint32_t n_tiles = packed_range(p, (uint32_t)w, per_kv, lane, share, cc);
+    const int per = (p.B + kPackedTable - 1) / kPackedTable;
+    const uint32_t longest = packed_table<WARPS * 32>(p, per, table);
+    const PackedRange range = packed_range(pp, table, per, longest, blockIdx.x, (uint32_t)warp, lane, cc);
+    const uint32_t n_tiles = range.count;
     PackedCursor ci = cc;
 
     const int head = min(g4 % QP, HP - 1);       // of the column g4; columns without a head repeat the last one's query
@@ -355,7 +435,7 @@ __global__ void __launch_bounds__(kPackedWarps * 32, 1) attn_packed_kernel(const
     }
 
     // Sequences that see nothing: zero rows (zero dummy key and value), lse 0.
-    for (int b = w < p.n_workers ? w : p.B; b < p.B; b += p.n_workers) {
+    for (int b = w; b < p.B; b += gridDim.x * WARPS) {
         if (packed_visible(p, b) == 0) {
             const int n16 = n_q_heads * D * (EXACT ? 4 : 2) / 16;
             uint4* o16 = reinterpret_cast<uint4*>(static_cast<uint8_t*>(p.out) + (size_t)b * n16 * 16);
@@ -365,13 +445,11 @@ __global__ void __launch_bounds__(kPackedWarps * 32, 1) attn_packed_kernel(const
         }
     }
 
-    if (n_tiles == 0) return;
-
     uint32_t cslot = 0, cphase = 0;
     bool ok = true;
 
     PackedQuery<D> q;
-    packed_query<D>(q_raw, p.scale_log2, lane, q);
+    if (n_tiles) packed_query<D>(q_raw, p.scale_log2, lane, q);
 
     // running state of this lane's two columns
     float m_run[2], l_run[2];
@@ -392,113 +470,63 @@ __global__ void __launch_bounds__(kPackedWarps * 32, 1) attn_packed_kernel(const
     clear();
     uint32_t seg_t0 = cc.t;
 
-    // Which workers share a pair (of nt tiles from tile `begin` on): worked out when the worker enters a pair that its range
-    // cuts, at most its first and its last.
-    struct Split { int32_t c_first, n_parts, first_odd; };
-    auto split_of = [&](uint32_t begin, uint32_t nt) {
-        Split sp;
-        sp.c_first = (int32_t)share.worker(begin);
-        sp.n_parts = (int32_t)share.worker(begin + nt - 1) - sp.c_first + 1;
-        sp.first_odd = begin != share.begin((uint32_t)sp.c_first) ? 1 : 0;   // which record of c_first belongs to this pair
-        return sp;
-    };
-    Split cur = {0, 1, 0};
-    const uint32_t first_tile = share.begin((uint32_t)w);
-    if (cc.t != 0 || n_tiles < cc.nt) cur = split_of(first_tile - cc.t, cc.nt);
     bool first_seg = true;
-    int32_t ticket0 = 0, ticket1 = 0;
-    bool armed0 = false, armed1 = false;
     // A finished part of a pair: the lanes of a row's copies share its dimensions.  r[i] are the values of m-tile copy * MTL + i,
     // [0], [1] of dimension 64 g + 8 g4 + 2 k for the lane's two columns, [2], [3] of the one behind it, with 4 g + k the m-tile.
     float r[MTL][4], l_tot[2], m_fin[2];
     const int q0 = 2 * c4 % QP;                  // the lane's columns: query heads q0 and q0 + 1 of the pair
     const bool holds = q0 < HP, both = q0 + 1 < HP;
 
-    // r / l_tot and lse -> the output rows of pair (b, h)
-    auto write_rows = [&](int b, int h) {
+    // m-tile copy * MTL + i of r / l_tot -> the output rows of pair (b, h), N of them whose dimensions are neighbours; with the first, lse
+    auto write_tiles = [&](auto n_tag, const float (*v)[4], int i, int b, int h) {
+        constexpr int N = decltype(n_tag)::value;
         const size_t row0 = (size_t)b * n_q_heads + (size_t)h * HP + q0;
+        const int mt = copy * MTL + i;
 #pragma unroll
         for (int j = 0; j < 2; ++j) {
             if (j == 0 ? !holds : !both) break;
             const float inv = 1.0f / l_tot[j];
-            constexpr int RUN = MTL < 4 ? MTL : 4;           // m-tiles whose dimensions are neighbours
+            const size_t at = (row0 + j) * D + 64 * (mt / 4) + 8 * g4 + 2 * (mt % 4);
+            [[maybe_unused]] uint32_t y[N];
 #pragma unroll
-            for (int i0 = 0; i0 < MTL; i0 += RUN) {
-                const int mt = copy * MTL + i0;
-                const size_t at = (row0 + j) * D + 64 * (mt / 4) + 8 * g4 + 2 * (mt % 4);
-                float v[2 * RUN];
-#pragma unroll
-                for (int i = 0; i < RUN; ++i) { v[2 * i] = r[i0 + i][j] * inv; v[2 * i + 1] = r[i0 + i][2 + j] * inv; }
-                if constexpr (EXACT) {
-                    float* dst = static_cast<float*>(p.out) + at;
-#pragma unroll
-                    for (int i = 0; i < RUN; ++i) *reinterpret_cast<float2*>(dst + 2 * i) = make_float2(v[2 * i], v[2 * i + 1]);
-                } else {
-                    uint16_t* dst = static_cast<uint16_t*>(p.out) + at;
-                    if constexpr (RUN == 4)
-                        *reinterpret_cast<uint4*>(dst) = make_uint4(cvt_bf16x2(v[0], v[1]), cvt_bf16x2(v[2], v[3]), cvt_bf16x2(v[4], v[5]), cvt_bf16x2(v[6], v[7]));
-                    else if constexpr (RUN == 2)
-                        *reinterpret_cast<uint2*>(dst) = make_uint2(cvt_bf16x2(v[0], v[1]), cvt_bf16x2(v[2], v[3]));
-                    else
-                        *reinterpret_cast<uint32_t*>(dst) = cvt_bf16x2(v[0], v[1]);
-                }
+            for (int e = 0; e < N; ++e) {
+                if constexpr (EXACT) *reinterpret_cast<float2*>(static_cast<float*>(p.out) + at + 2 * e) = make_float2(v[e][j] * inv, v[e][2 + j] * inv);
+                else y[e] = cvt_bf16x2(v[e][j] * inv, v[e][2 + j] * inv);
             }
-            if (p.lse && g4 == 0 && copy == 0) p.lse[row0 + j] = (m_fin[j] + lg2(l_tot[j])) * 0.6931471805599453f;
+            if constexpr (!EXACT) {
+                uint16_t* dst = static_cast<uint16_t*>(p.out) + at;
+                if constexpr (N == 4) *reinterpret_cast<uint4*>(dst) = make_uint4(y[0], y[1], y[2], y[3]);
+                else if constexpr (N == 2) *reinterpret_cast<uint2*>(dst) = make_uint2(y[0], y[1]);
+                else *reinterpret_cast<uint32_t*>(dst) = y[0];
+            }
+            if (i == 0 && p.lse && g4 == 0 && copy == 0) p.lse[row0 + j] = (m_fin[j] + lg2(l_tot[j])) * 0.6931471805599453f;
         }
     };
-    // (r, m_fin, l_tot) -> a partial record
-    auto store_record = [&](float* rec) {
-        if (!holds) return;
-#pragma unroll
-        for (int i = 0; i < MTL; ++i) reinterpret_cast<float4*>(rec)[i * 32 + lane] = make_float4(r[i][0], r[i][1], r[i][2], r[i][3]);
-        if (g4 == 0 && copy == 0) {
+    // m-tile i of a record, and its maxima and sums
+    auto store_tile = [&](float* rec, int i, const float (&v)[4]) {
+        reinterpret_cast<float4*>(rec)[i * 32 + lane] = make_float4(v[0], v[1], v[2], v[3]);
+        if (i == 0 && g4 == 0 && copy == 0) {
             *reinterpret_cast<float2*>(rec + MTL * 128 + q0) = make_float2(m_fin[0], m_fin[1]);
             *reinterpret_cast<float2*>(rec + MTL * 128 + 8 + q0) = make_float2(l_tot[0], l_tot[1]);
         }
     };
-    // Merge of n records in a fixed order, in one pass with running maxima: record i is the one of worker first_w + i * step
-    // (its second record if i == 0 and first_slot is set).
-    auto merge_records = [&](int n, uint32_t first_w, int step, int first_slot) {
-        const float* rec0 = p.partials + (size_t)(2 * first_w) * REC;
-        const size_t rstride = (size_t)(2 * step) * REC;
+    // One more record's m-tile, with a running maximum
+    auto begin_join = [&](float (&v)[4]) {
         m_fin[0] = m_fin[1] = -INFINITY;
         l_tot[0] = l_tot[1] = 0.f;
-#pragma unroll
-        for (int i = 0; i < MTL; ++i)
-#pragma unroll
-            for (int e = 0; e < 4; ++e) r[i][e] = 0.f;
-        if (!holds) return;
-        constexpr int AHEAD = MTL <= 2 ? 8 : MTL == 4 ? 4 : 2;     // records in flight
-        for (int i0 = 0; i0 < n; i0 += AHEAD) {
-            float2 mm[AHEAD], ll[AHEAD];
-            float4 x[AHEAD][MTL];
-#pragma unroll
-            for (int a = 0; a < AHEAD; ++a) {
-                const int i = min(i0 + a, n - 1);
-                const float* rec = rec0 + (size_t)i * rstride + (i == 0 ? (size_t)first_slot * REC : 0);
-                mm[a] = __ldcg(reinterpret_cast<const float2*>(rec + MTL * 128 + q0));
-                ll[a] = __ldcg(reinterpret_cast<const float2*>(rec + MTL * 128 + 8 + q0));
-#pragma unroll
-                for (int k = 0; k < MTL; ++k) x[a][k] = __ldcg(reinterpret_cast<const float4*>(rec) + k * 32 + lane);
-            }
-#pragma unroll
-            for (int a = 0; a < AHEAD; ++a) {
-                if (i0 + a >= n) break;
-                const float M0 = fmaxf(m_fin[0], mm[a].x), M1 = fmaxf(m_fin[1], mm[a].y);
-                const float a0 = ex2(m_fin[0] - M0), a1 = ex2(m_fin[1] - M1);      // ex2(-inf) = 0 for the first record
-                const float w0 = ex2(mm[a].x - M0), w1 = ex2(mm[a].y - M1);
-                m_fin[0] = M0; m_fin[1] = M1;
-                l_tot[0] = fmaf(l_tot[0], a0, ll[a].x * w0);
-                l_tot[1] = fmaf(l_tot[1], a1, ll[a].y * w1);
-#pragma unroll
-                for (int k = 0; k < MTL; ++k) {
-                    r[k][0] = fmaf(r[k][0], a0, x[a][k].x * w0);
-                    r[k][1] = fmaf(r[k][1], a1, x[a][k].y * w1);
-                    r[k][2] = fmaf(r[k][2], a0, x[a][k].z * w0);
-                    r[k][3] = fmaf(r[k][3], a1, x[a][k].w * w1);
-                }
-            }
-        }
+        v[0] = v[1] = v[2] = v[3] = 0.f;
+    };
+    auto join = [&](float (&v)[4], float2 m, float2 l, float4 x) {
+        const float M0 = fmaxf(m_fin[0], m.x), M1 = fmaxf(m_fin[1], m.y);
+        const float a0 = ex2(m_fin[0] - M0), a1 = ex2(m_fin[1] - M1);      // ex2(-inf) = 0 for the first record
+        const float w0 = ex2(m.x - M0), w1 = ex2(m.y - M1);
+        m_fin[0] = M0; m_fin[1] = M1;
+        l_tot[0] = fmaf(l_tot[0], a0, l.x * w0);
+        l_tot[1] = fmaf(l_tot[1], a1, l.y * w1);
+        v[0] = fmaf(v[0], a0, x.x * w0);
+        v[1] = fmaf(v[1], a1, x.y * w1);
+        v[2] = fmaf(v[2], a0, x.z * w0);
+        v[3] = fmaf(v[3], a1, x.w * w1);
     };
 
     for (uint32_t tile = 0; tile < n_tiles; ++tile) {
@@ -759,31 +787,16 @@ __global__ void __launch_bounds__(kPackedWarps * 32, 1) attn_packed_kernel(const
                     r[i][e] = fmaf(r[i][e] * (EXACT ? 0x1p-14f : e < 2 ? 0x1p10f : 0x1p6f), pow_e, low);
                 }
 
-            const bool complete = pair_end && seg_t0 == 0;
-            if (complete) {
-                write_rows(cc.b, h);
-            } else {
-                const int c_first = cur.c_first;
-                const int first_odd = cur.first_odd, n_parts = cur.n_parts;
-                store_record(p.partials + (size_t)(2 * w + (first_seg ? 0 : 1)) * REC);
-                // Few parts: the contributor that arrives last merges them all.  Many (few pairs, long sequences): chunks of
-                // kMmaChunk consecutive workers first, then the chunks' records; a fixed order either way.  The ticket is
-                // posted here and looked at after the last tile; each goes into a variable of its own that nothing reads
-                // before.
-                int32_t* ticket_at = p.counters + c_first;
-                if (n_parts > kMmaTreeMin) {
-                    const int ck = (w - c_first) / kMmaChunk * kMmaChunk;
-                    ticket_at = p.counters2 + 2 * (c_first + ck) + (ck == 0 ? first_odd : 0);
-                }
-                if (lane == 0) pending[warp][first_seg ? 0 : 1] = {n_parts, first_odd, cc.b, h, c_first};
-                __syncwarp();       // the record's stores (all lanes) are ordered before lane 0's release
-                if (first_seg) {
-                    if (lane == 0) ticket0 = atom_add_acq_rel_gpu(ticket_at, 1);
-                    armed0 = true;
-                } else {
-                    if (lane == 0) ticket1 = atom_add_acq_rel_gpu(ticket_at, 1);
-                    armed1 = true;
-                }
+            if (pair_end && seg_t0 == 0) {
+                constexpr int N = MTL < 4 ? MTL : 4;
+#pragma unroll
+                for (int i = 0; i < MTL; i += N) write_tiles(std::integral_constant<int, N>(), r + i, i, cc.b, h);
+            } else {                             // left to be joined
+                const int k = first_seg ? 0 : 1;
+                float* rec = last ? reinterpret_cast<float*>(ring_bytes) : p.partials + (size_t)(2 * w) * REC;
+#pragma unroll
+                for (int i = 0; i < MTL; ++i) store_tile(rec, i, r[i]);
+                if (lane == 0) parts[warp][k] = {range.first + tile - cc.t, cc.nt, cc.b, h, last ? 1 : 0};
             }
             clear();
         }
@@ -794,46 +807,142 @@ __global__ void __launch_bounds__(kPackedWarps * 32, 1) attn_packed_kernel(const
                 packed_query<D>(q_raw, p.scale_log2, lane, q);
                 seg_t0 = 0;
                 first_seg = false;
-                if (n_tiles - (tile + 1) < cc.nt) cur = split_of(first_tile + tile + 1, cc.nt);   // the range ends inside this pair
             }
         }
     }
 
-    if (ok) {
-        __syncwarp();
-#pragma unroll 1
-        for (int i = 0; i < 2; ++i) {
-            if (!(i == 0 ? armed0 : armed1)) continue;
-            const PackedPending pd = pending[warp][i];
-            int ticket = __shfl_sync(FULL, i == 0 ? ticket0 : ticket1, 0);
-            // a chunk of many parts, or all parts of few
-            const bool two_level = pd.n > kMmaTreeMin;
-            const int ck = two_level ? (w - pd.c_first) / kMmaChunk * kMmaChunk : 0;
-            int n = two_level ? min(kMmaChunk, pd.n - ck) : pd.n, first = pd.c_first + ck, step = 1, slot = ck == 0 ? pd.first_odd : 0;
-            int32_t* at = two_level ? p.counters2 + 2 * first + slot : p.counters + first;
-#pragma unroll 1
-            for (bool whole = !two_level;;) {
-                if (ticket != n - 1) break;              // someone else arrives later and merges
-                __syncwarp();                            // lane 0's acquire is in front of all lanes' reads of the records
-                merge_records(n, (uint32_t)first, step, slot);
-                if (lane == 0) *at = 0;                  // ready for the next launch
-                if (whole) { write_rows(pd.b, pd.h); break; }
-                // the chunk's result becomes the record of the chunk's first worker
-                store_record(p.partials + (size_t)(2 * first + slot) * REC);
-                __syncwarp();
-                at = p.counters + pd.c_first;
-                if (lane == 0) ticket = atom_add_acq_rel_gpu(at, 1);
-                ticket = __shfl_sync(FULL, ticket, 0);
-                n = (pd.n + kMmaChunk - 1) / kMmaChunk; first = pd.c_first; step = kMmaChunk; slot = pd.first_odd;
-                whole = true;
-            }
-        }
-    } else {
+    if (!ok) {
         if (lane == 0) atomicExch(p.status, kStatusTimeout);
         for (int s = 0; s < NS; ++s) {
             mbar_wait_bounded(bars + 8 * s, 0, 1u << 10);
             mbar_wait_bounded(bars + 8 * s, 1, 1u << 10);
         }
+    }
+
+    // ---- pairs that several warps share -------------------------------------------------------------
+    // Lane 2 w + k looks at part k of warp w.  Parts of one pair follow one another; (pair, m-tile) items go to the block's warps.
+    __syncthreads();
+    PackedPart pt = {0, 0, 0, 0, 0};
+    if (lane < 2 * WARPS) pt = parts[lane >> 1][lane & 1];
+    const uint32_t there = __ballot_sync(FULL, pt.nt != 0);
+    if (there == 0) return;
+    const uint32_t in_ring = __ballot_sync(FULL, pt.in_ring != 0);
+    const uint32_t below = there & ((1u << lane) - 1u);
+    const uint32_t before = __shfl_sync(FULL, pt.begin, below ? 31 - __clz(below) : 0);
+    const uint32_t heads = __ballot_sync(FULL, pt.nt != 0 && (below == 0 || before != pt.begin));    // first parts of their pairs
+    const bool crosses = pt.begin < range.begin || pt.begin + pt.nt > range.end;
+    const uint32_t crossing = __ballot_sync(FULL, crosses) & heads;
+    const int n_items = __popc(heads) * MTL;
+    // what crosses the block's borders becomes one of its two records: 0 for the pair that began before, 1 for one that goes on
+    const auto block_record = [&](int block, int k) { return p.partials + (size_t)(2 * (block * WARPS + k) + 1) * REC; };
+#pragma unroll 1
+    for (int item = warp; item < n_items; item += WARPS) {
+        const int i = item % MTL;
+        uint32_t left = heads;
+        for (int skip = item / MTL; skip > 0; --skip) left &= left - 1;
+        const int head_lane = __ffs(left) - 1;
+        left &= left - 1;
+        uint32_t members = there & ~((1u << head_lane) - 1u) & (left ? (left & -left) - 1u : 0xffffffffu);
+        float v[4];
+        begin_join(v);
+        while (members) {                        // four parts on their way at a time
+            float2 m[4], l[4];
+            float4 x[4];
+            bool is[4];
+#pragma unroll
+            for (int a = 0; a < 4; ++a) {
+                is[a] = members != 0;
+                const int e = is[a] ? __ffs(members) - 1 : head_lane;
+                members &= members - 1;          // (0 stays 0)
+                const float* rec = in_ring >> e & 1 ? reinterpret_cast<const float*>(ring0 + (e >> 1) * (NS * TILE))
+                                                    : p.partials + (size_t)(2 * (blockIdx.x * WARPS + (e >> 1))) * REC;
+                m[a] = *reinterpret_cast<const float2*>(rec + MTL * 128 + q0);
+                l[a] = *reinterpret_cast<const float2*>(rec + MTL * 128 + 8 + q0);
+                x[a] = reinterpret_cast<const float4*>(rec)[i * 32 + lane];
+            }
+#pragma unroll
+            for (int a = 0; a < 4; ++a)
+                if (is[a]) join(v, m[a], l[a], x[a]);
+        }
+        const int b = __shfl_sync(FULL, pt.b, head_lane), h = __shfl_sync(FULL, pt.h, head_lane);
+        if (crossing >> head_lane & 1) store_tile(block_record((int)blockIdx.x, __shfl_sync(FULL, pt.begin, head_lane) < range.begin ? 0 : 1), i, v);
+        else write_tiles(std::integral_constant<int, 1>(), &v, i, b, h);
+    }
+    if (crossing == 0) return;
+
+    // ---- pairs that several thread blocks share -----------------------------------------------------
+    // Few blocks: the one that arrives last merges all.  Many (few pairs, long sequences): chunks of kMmaChunk blocks first, then
+    // the chunks' records; a fixed order either way.  Warp k takes the ticket of the k-th of the (at most two) pairs, all warps merge.
+    __shared__ struct { int32_t b, h, c_first, first, count, step, kind, merge, all; } join_of[2];
+    const int n_cross = __popc(crossing);
+    int32_t* at = nullptr;
+    int n_parts = 0;
+    bool waits = warp < n_cross;
+    if (waits) {
+        const int head_lane = __ffs(warp == 0 ? crossing : crossing & (crossing - 1)) - 1;
+        const uint32_t begin = __shfl_sync(FULL, pt.begin, head_lane), nt = __shfl_sync(FULL, pt.nt, head_lane);
+        const PackedShare share(range.all, (uint32_t)pp.n_blocks);
+        const int c_first = (int)share.part(begin);
+        n_parts = (int)share.part(begin + nt - 1) - c_first + 1;
+        const bool two_level = n_parts > kMmaTreeMin;
+        const int ck = two_level ? ((int)blockIdx.x - c_first) / kMmaChunk * kMmaChunk : 0;
+        at = two_level ? p.counters2 + 2 * (c_first + ck) + (ck == 0 ? 1 : 0) : p.counters + c_first;
+        if (lane == head_lane)
+            join_of[warp] = {pt.b, pt.h, c_first, c_first + ck, two_level ? min(kMmaChunk, n_parts - ck) : n_parts, 1, 0, 0, two_level ? 0 : 1};
+    }
+    __syncthreads();                             // (the records' stores are in front of it)
+    for (int round = 0; round < 2; ++round) {
+        if (waits) {
+            if (lane == 0) join_of[warp].merge = atom_add_acq_rel_gpu(at, 1) == join_of[warp].count - 1 ? 1 : 0;
+            __syncwarp();
+            waits = join_of[warp].merge != 0;    // else someone else arrives later and merges
+        }
+        if (!__syncthreads_or(waits)) return;
+        for (int item = warp; item < n_cross * MTL; item += WARPS) {
+            const int i = item % MTL;
+            const auto jo = join_of[item / MTL];
+            if (!jo.merge) continue;
+            // a block's records 0 and 1 are above; 2 and 3 are of a chunk that begins with it; the odd ones are of a pair that began in it
+            const auto record = [&](int block) { return block_record(block, jo.kind + (block == jo.c_first ? 1 : 0)); };
+            float v[4];
+            begin_join(v);
+#pragma unroll 1
+            for (int r0 = 0; r0 < jo.count; r0 += 8) {       // eight records on their way at a time
+                float2 m[8], l[8];
+                float4 x[8];
+#pragma unroll
+                for (int a = 0; a < 8; ++a) {
+                    const float* rec = record(jo.first + min(r0 + a, jo.count - 1) * jo.step);
+                    m[a] = __ldcg(reinterpret_cast<const float2*>(rec + MTL * 128 + q0));
+                    l[a] = __ldcg(reinterpret_cast<const float2*>(rec + MTL * 128 + 8 + q0));
+                    x[a] = __ldcg(reinterpret_cast<const float4*>(rec) + i * 32 + lane);
+                }
+#pragma unroll
+                for (int a = 0; a < 8; ++a)
+                    if (r0 + a < jo.count) join(v, m[a], l[a], x[a]);
+            }
+            if (jo.all) write_tiles(std::integral_constant<int, 1>(), &v, i, jo.b, jo.h);
+            else store_tile(block_record(jo.first, 2 + (jo.first == jo.c_first ? 1 : 0)), i, v);
+        }
+        __syncthreads();
+        if (waits) {
+            if (lane == 0) *at = 0;              // ready for the next launch
+            waits = join_of[warp].all == 0;
+            __syncwarp();
+            if (waits) {                         // from the chunk to the pair
+                at = p.counters + join_of[warp].c_first;
+                if (lane == 0) {
+                    auto& jo = join_of[warp];
+                    jo.first = jo.c_first;
+                    jo.count = (n_parts + kMmaChunk - 1) / kMmaChunk;
+                    jo.step = kMmaChunk;
+                    jo.kind = 2;
+                    jo.all = 1;
+                }
+                __syncwarp();
+            }
+        }
+        if (!waits && warp < n_cross && lane == 0) join_of[warp].merge = 0;
     }
 }
 

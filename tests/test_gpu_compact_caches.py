@@ -744,3 +744,25 @@ def test_a_cache_beyond_32_bits_of_rows_and_bytes():
     assert torch.equal(ko[-1], value64(k[-1]).float().bfloat16()) and not ko[:-1].any()
     w = c.lckv_attention_weights(0, CONDENSED, q, lse)
     assert (w[-1].sum(-1) - 1).abs().max() < LSE[4] and not w[:-1].any()
+
+
+@pytest.mark.parametrize("B", [31, 32, 33, 385, 1023, 1024, 1025, 2500])
+@pytest.mark.parametrize("d,Hq", [(64, 1), (128, 2)])
+def test_attention_of_many_sequences(B, d, Hq):
+    """Batches around the sizes at which the kernel's table of sequences changes its form; many of them empty."""
+    g = gen(20)
+    lens = torch.randint(0, 150, (B,), generator=torch.Generator().manual_seed(B)).tolist()
+    for i in range(0, B, 3):
+        lens[i] = 0
+    lens[-1] = 0
+    k, v, q = rows_bf16(g, B, 150, 1, d), rows_bf16(g, B, 150, 1, d), randn(g, B, Hq, d)
+    c = make(4, B, Hq, 1, d, 150, lens, out32=1)
+    c.lckv_prefill_write_kv(0, k, v)
+    for limit in (0, 37):
+        c.lckv_cache_set_worker_limit(limit)
+        lse = torch.full((B, Hq), 9.0, device=DEV)
+        out = c.lckv_decode_attention(0, CONDENSED, q, lse=lse)
+        assert not out[::3].any() and not lse[::3].any() and not out[-1].any()
+        some = [b for b in range(B) if lens[b]][::max(1, B // 40)]
+        check_attention(out[some], lse[some], q[some], k[some], v[some], [lens[b] for b in some])
+        assert torch.isfinite(out).all() and (out[[b for b in range(B) if lens[b]]].abs().amax((1, 2)) > 0).all()
