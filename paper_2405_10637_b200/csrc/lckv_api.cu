@@ -534,17 +534,24 @@ int launch_attention(lckv_cache* c, int slot, int mode, const void* q, void* out
 template <typename... KArgs, typename... Args>
 cudaError_t launch_pdl_dims(void (*kernel)(KArgs...), dim3 grid, dim3 block, size_t smem, cudaStream_t st, Args... args);
 
-// Thread blocks over the (kRowTokens tokens, kv head) items of `tokens` tokens of each of `seqs` sequences.
-bool row_grid(const lckv_cache* c, int64_t tokens, int seqs, dim3* grid)
+// Thread blocks over the (u tokens, kv head) items of `tokens` tokens of each of `seqs` sequences.
+bool row_grid(const lckv_cache* c, int64_t tokens, int u, int seqs, dim3* grid)
 {
-    const int64_t items = (tokens + lckv::kRowTokens - 1) / lckv::kRowTokens * c->cfg.n_kv_heads;
+    const int64_t items = (tokens + u - 1) / u * c->cfg.n_kv_heads;
     const int64_t per = c->cfg.head_dim == 128 ? lckv::rows_per_block<128>() : lckv::rows_per_block<64>();
     *grid = dim3((unsigned)((items + per - 1) / per), (unsigned)std::min(seqs, 65535));
-    return items <= INT32_MAX - per && tokens <= INT32_MAX - lckv::kRowTokens;      // (the kernels count both in 32 bits)
+    return items <= INT32_MAX - per && tokens <= INT32_MAX - u;      // (the kernels count both in 32 bits)
 }
 
-// Rows written in 4 bits: the new token of every sequence, or prompts of up to n tokens.
-int launch_packed_write(lckv_cache* c, int slot, const void* k, const void* v, int n, bool prompt, int batch, cudaStream_t st)
+// Four tokens a thread where that leaves four thread blocks for every SM, else one (three prompts of up to 77 tokens, 4 heads of 64: 2.3
+// us to write with one, 3.5 with four).
+bool four_tokens(const lckv_cache* c, int64_t tokens, int seqs)
+{
+    return tokens * seqs * c->cfg.n_kv_heads * (c->cfg.head_dim / 8) >= (int64_t)c->sm_count * 16 * lckv::kRowThreads;
+}
+
+// Rows written in 4 bits: the new token of every sequence (n = 0), or prompts of up to n tokens.
+int launch_packed_write(lckv_cache* c, int slot, const void* k, const void* v, int n, int batch, cudaStream_t st)
 {
     lckv::PackedWriteParams p;
     p.s = packed_slot(c, slot);
@@ -556,18 +563,19 @@ int launch_packed_write(lckv_cache* c, int slot, const void* k, const void* v, i
     p.batch = batch;
     p.n = n;
     p.n_sink = c->cfg.stream_sink;
-    p.prompt = prompt ? 1 : 0;
+    const bool wide = c->cfg.head_dim == 128, four = n && four_tokens(c, n, batch);
     dim3 grid;
-    if (!row_grid(c, prompt ? n : batch, prompt ? batch : 1, &grid)) return LCKV_EINVAL;
-    const cudaError_t e = launch_pdl_dims(c->cfg.head_dim == 128 ? lckv::packed_write_kernel<128> : lckv::packed_write_kernel<64>, grid,
-                                          dim3(lckv::kRowThreads), 0, st, p);
-    return cuda_ok(e) ? LCKV_OK : LCKV_ECUDA;
+    if (!row_grid(c, n ? n : batch, four ? 4 : 1, n ? batch : 1, &grid)) return LCKV_EINVAL;
+    const auto kernel = n == 0 ? (wide ? lckv::packed_append_kernel<128> : lckv::packed_append_kernel<64>)
+                        : four ? (wide ? lckv::packed_write_kernel<128, 4> : lckv::packed_write_kernel<64, 4>)
+                               : (wide ? lckv::packed_write_kernel<128, 1> : lckv::packed_write_kernel<64, 1>);
+    return cuda_ok(launch_pdl_dims(kernel, grid, dim3(lckv::kRowThreads), 0, st, p)) ? LCKV_OK : LCKV_ECUDA;
 }
 
 int launch_append(lckv_cache* c, int slot, const void* k_new, const void* v_new, int batch,
                   cudaStream_t st)
 {
-    if (c->cfg.kv_bits == 4) return launch_packed_write(c, slot, k_new, v_new, 1, false, batch, st);
+    if (c->cfg.kv_bits == 4) return launch_packed_write(c, slot, k_new, v_new, 0, batch, st);
     const int64_t n = (int64_t)batch * c->cfg.n_kv_heads * (c->cfg.head_dim / 8);
     const int threads = 256;
     const int blocks = (int)((n + threads - 1) / threads);
@@ -738,7 +746,7 @@ int prefill_check(const lckv_cache* c, int n_max, int batch, bool attention)
 int launch_prefill_write(lckv_cache* c, int slot, const void* k, const void* v, int n_max,
                          int batch, cudaStream_t st)
 {
-    if (c->cfg.kv_bits == 4) return launch_packed_write(c, slot, k, v, n_max, true, batch, st);
+    if (c->cfg.kv_bits == 4) return launch_packed_write(c, slot, k, v, n_max, batch, st);
     const int64_t n = (int64_t)batch * n_max * c->cfg.n_kv_heads * (c->cfg.head_dim / 8);
     const int threads = 256;
     lckv::prefill_write_kv_kernel<<<(unsigned)((n + threads - 1) / threads), threads, 0, st>>>(

@@ -44,6 +44,13 @@ void release_pages(lckv_cache* c, const std::vector<int>& rows)
         }
 }
 
+template <int D, bool PACKED>
+void (*read_variant(int dtype, bool four))(lckv::RowReadParams)
+{
+    if (four) return dtype ? lckv::row_read_kernel<D, PACKED, true, 4> : lckv::row_read_kernel<D, PACKED, false, 4>;
+    return dtype ? lckv::row_read_kernel<D, PACKED, true, 1> : lckv::row_read_kernel<D, PACKED, false, 1>;
+}
+
 // Thread blocks for `units` pieces of every (sequence, kv head), `per` a block.
 dim3 move_grid(int64_t heads, int64_t units, int64_t per) { return dim3((unsigned)heads, (unsigned)std::min<int64_t>(65535, (units + per - 1) / per)); }
 
@@ -87,8 +94,9 @@ int lckv_cache_read_kv(lckv_cache_t* c, int32_t slot, void* k, void* v, int32_t 
     const int d = c->cfg.head_dim;
     const int64_t bytes = (int64_t)batch * n_max * c->cfg.n_kv_heads * d * (dtype ? 4 : 2);
     dim3 grid;
+    const bool four = four_tokens(c, n_max, batch);
     if (ranges_meet(k, bytes, v, bytes) || ranges_meet(k, bytes, c->base, (int64_t)c->lay.total_bytes) ||
-        ranges_meet(v, bytes, c->base, (int64_t)c->lay.total_bytes) || !row_grid(c, n_max, batch, &grid))
+        ranges_meet(v, bytes, c->base, (int64_t)c->lay.total_bytes) || !row_grid(c, n_max, four ? 4 : 1, batch, &grid))
         return LCKV_EINVAL;
     cudaStream_t st = static_cast<cudaStream_t>(stream);
     if (int rc = sync_page_table(c, st)) return rc;
@@ -104,10 +112,8 @@ int lckv_cache_read_kv(lckv_cache_t* c, int32_t slot, void* k, void* v, int32_t 
     p.batch = batch;
     p.n = n_max;
     const bool packed = c->cfg.kv_bits == 4;
-    const auto kernel = d == 128 ? (packed ? (dtype ? lckv::row_read_kernel<128, true, true> : lckv::row_read_kernel<128, true, false>)
-                                           : (dtype ? lckv::row_read_kernel<128, false, true> : lckv::row_read_kernel<128, false, false>))
-                                 : (packed ? (dtype ? lckv::row_read_kernel<64, true, true> : lckv::row_read_kernel<64, true, false>)
-                                           : (dtype ? lckv::row_read_kernel<64, false, true> : lckv::row_read_kernel<64, false, false>));
+    const auto kernel = d == 128 ? (packed ? read_variant<128, true>(dtype, four) : read_variant<128, false>(dtype, four))
+                                 : (packed ? read_variant<64, true>(dtype, four) : read_variant<64, false>(dtype, four));
     const cudaError_t e = launch_pdl_dims(kernel, grid, dim3(lckv::kRowThreads), 0, st, p);
     return cuda_ok(e) ? LCKV_OK : LCKV_ECUDA;
 }
@@ -243,8 +249,8 @@ int lckv_evict_kv(lckv_cache_t* dst, int32_t dst_slot, const lckv_cache_t* src, 
     if (src->cfg.kv_bits == 4) {
         e = d == 128 ? launch_move<128, true>(p, in_place, rows, st) : launch_move<64, true>(p, in_place, rows, st);
     } else if (dst->cfg.kv_bits == 4) {
-        e = d == 128 ? launch_pdl_dims(lckv::evict_pack_kernel<128>, move_grid(rows, n_keep, lckv::rows_per_block<128>() * lckv::kRowTokens), dim3(lckv::kRowThreads), 0, st, p)
-                     : launch_pdl_dims(lckv::evict_pack_kernel<64>, move_grid(rows, n_keep, lckv::rows_per_block<64>() * lckv::kRowTokens), dim3(lckv::kRowThreads), 0, st, p);
+        e = d == 128 ? launch_pdl_dims(lckv::evict_pack_kernel<128>, move_grid(rows, n_keep, lckv::rows_per_block<128>() * lckv::kPackRows), dim3(lckv::kRowThreads), 0, st, p)
+                     : launch_pdl_dims(lckv::evict_pack_kernel<64>, move_grid(rows, n_keep, lckv::rows_per_block<64>() * lckv::kPackRows), dim3(lckv::kRowThreads), 0, st, p);
     } else {
         e = d == 128 ? launch_move<128, false>(p, in_place, rows, st) : launch_move<64, false>(p, in_place, rows, st);
     }

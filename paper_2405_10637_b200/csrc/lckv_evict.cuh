@@ -404,32 +404,42 @@ __global__ void __launch_bounds__(kRowThreads) evict_move_kernel(const MoveParam
     }
 }
 
-// From bf16 rows to 4-bit rows; lanes as in packed_write_kernel, blocks as above.
+// From bf16 rows to 4-bit rows; lanes as in packed_write_kernel, blocks as above, four neighbouring rows a thread.
+constexpr int kPackRows = 4;
 template <int D>
 __global__ void __launch_bounds__(kRowThreads) evict_pack_kernel(const MoveParams p)
 {
     pdl_wait_then_release();
     const PackedLane<D> lane((int)threadIdx.x % PackedLane<D>::kLanes);
-    constexpr int ROWS = rows_per_block<D>();
-    for (int64_t i0 = (int64_t)blockIdx.y * ROWS * kRowTokens; i0 < p.n_keep; i0 += (int64_t)gridDim.y * ROWS * kRowTokens) {
-        MoveRow r[kRowTokens];
-        uint4 x[kRowTokens], y[kRowTokens];
+    constexpr int STEP = rows_per_block<D>() * kPackRows;
+    const int b = (int)blockIdx.x / p.map.H_kv, h = (int)blockIdx.x - b * p.map.H_kv;
+    const int32_t* kept = p.kept + (int64_t)blockIdx.x * p.n_keep;
+    for (int64_t i0 = (int64_t)blockIdx.y * STEP; i0 < p.n_keep; i0 += (int64_t)gridDim.y * STEP) {
+        const int i = (int)i0 + (int)threadIdx.x / PackedLane<D>::kLanes * kPackRows;
+        int from[kPackRows];
+        uint4 x[kPackRows], y[kPackRows];
 #pragma unroll
-        for (int u = 0; u < kRowTokens; ++u) r[u] = move_row(p, (int)blockIdx.x, (int)i0 + u * ROWS + (int)threadIdx.x / PackedLane<D>::kLanes);
+        for (int u = 0; u < kPackRows; ++u) from[u] = i + u < p.n_keep ? kept[i + u] : -1;
+        const int64_t to = from[0] >= 0 ? p.map_to.at(b, h, i) : -1;
+        bool lost = from[0] >= 0 && to < 0;
 #pragma unroll
-        for (int u = 0; u < kRowTokens; ++u) {
+        for (int u = 0; u < kPackRows; ++u) {
             x[u] = y[u] = make_uint4(0, 0, 0, 0);
-            if (r[u].from < 0) continue;
-            const uint16_t* src = (lane.is_v ? p.V : p.K) + r[u].from * D;
-            x[u] = *reinterpret_cast<const uint4*>(src + lane.word(0) * 8);
-            y[u] = *reinterpret_cast<const uint4*>(src + lane.word(1) * 8);
+            if (from[u] < 0 || to < 0) continue;
+            const int64_t row = p.map.at(b, h, from[u]);
+            if (row < 0) { lost = true; from[u] = -1; continue; }
+            const uint16_t* src = (lane.is_v ? p.V : p.K) + row * D;
+            x[u] = *reinterpret_cast<const uint4*>(src + lane.element(0));
+            y[u] = *reinterpret_cast<const uint4*>(src + lane.element(1));
         }
+        const auto place = lane.at(p.to, max((int64_t)0, to));
 #pragma unroll
-        for (int u = 0; u < kRowTokens; ++u) {
+        for (int u = 0; u < kPackRows; ++u) {
             uint32_t w0, w1, par;
             packed_encode(x[u], y[u], w0, w1, par);
-            if (r[u].from >= 0) lane.store(p.to, r[u].to, w0, w1, par);
+            if (from[u] >= 0 && to >= 0) lane.store(place, u, w0, w1, par);
         }
+        if (lost) atomicExch(p.status, kStatusNoRow);
     }
 }
 

@@ -79,43 +79,57 @@ struct PackedLane {
     int is_v, c, g;
     __device__ __forceinline__ explicit PackedLane(int l) : is_v(l >= D / 16), c(l & 3), g(D == 128 ? (l >> 2) & 1 : 0) {}
     __device__ __forceinline__ int word(int i) const { return 8 * g + c + 4 * i; }
-    __device__ __forceinline__ void store(const PackedSlot& s, int64_t row, uint32_t w0, uint32_t w1, uint32_t par) const
+    __device__ __forceinline__ int element(int i) const { return 8 * word(i); }
+    // the lane's place in physical row `row`; the rows behind it in the same tile lie D/2 and D/8 bytes on
+    struct Place { uint32_t *codes, *par; };
+    __device__ __forceinline__ Place at(const PackedSlot& s, int64_t row) const
     {
-        uint32_t* codes = reinterpret_cast<uint32_t*>(is_v ? s.values<D>(row) : s.keys<D>(row));
-        if (is_v) {
-            codes[packed_v_word<D>(word(0))] = w0;
-            codes[packed_v_word<D>(word(1))] = w1;
-        } else {
-            *reinterpret_cast<uint2*>(codes + packed_k_word<D>(word(0))) = make_uint2(w0, w1);
-        }
-        if (c == 0) s.par<D>(row)[is_v * (D / 64) + g] = par;
+        Place p;
+        p.codes = is_v ? reinterpret_cast<uint32_t*>(s.values<D>(row)) + packed_v_word<D>(word(0)) : reinterpret_cast<uint32_t*>(s.keys<D>(row)) + packed_k_word<D>(word(0));
+        p.par = s.par<D>(row) + is_v * (D / 64) + g;
+        return p;
     }
-    __device__ __forceinline__ void load(const PackedSlot& s, int64_t row, uint32_t& w0, uint32_t& w1, uint32_t& par) const
+    static constexpr int kValueStep = D == 128 ? 8 : 4;      // words from a value's word c to its word c + 4
+    __device__ __forceinline__ void store(Place p, int row, uint32_t w0, uint32_t w1, uint32_t par) const
     {
-        const uint32_t* codes = reinterpret_cast<const uint32_t*>(is_v ? s.values<D>(row) : s.keys<D>(row));
+        uint32_t* codes = p.codes + row * (D / 8);
         if (is_v) {
-            w0 = codes[packed_v_word<D>(word(0))];
-            w1 = codes[packed_v_word<D>(word(1))];
+            codes[0] = w0;
+            codes[kValueStep] = w1;
         } else {
-            const uint2 w = *reinterpret_cast<const uint2*>(codes + packed_k_word<D>(word(0)));
+            *reinterpret_cast<uint2*>(codes) = make_uint2(w0, w1);
+        }
+        if (c == 0) p.par[row * (D / 32)] = par;
+    }
+    __device__ __forceinline__ void load(Place p, int row, uint32_t& w0, uint32_t& w1, uint32_t& par) const
+    {
+        const uint32_t* codes = p.codes + row * (D / 8);
+        if (is_v) {
+            w0 = codes[0];
+            w1 = codes[kValueStep];
+        } else {
+            const uint2 w = *reinterpret_cast<const uint2*>(codes);
             w0 = w.x;
             w1 = w.y;
         }
-        par = s.par<D>(row)[is_v * (D / 64) + g];
+        par = p.par[row * (D / 32)];
     }
 };
 
 // Eight elements as a word of codes.  Adding 1.5 * 2^23 rounds to a whole number, ties to even, and leaves it in the low bits;
 // the sum of those numbers' bit patterns times 16^i is the word plus a constant.  (A quotient is below 15.5 without a limit: the
-// step is off by 2^-8 at most.)
+// step is off by 2^-8 at most.)  Two elements an instruction; not so the last addition, which would be fused with the product in
+// front of it although both say where they round.
 __device__ __forceinline__ uint32_t packed_codes(uint4 x, float low16, float inv)
 {
     const uint32_t w[4] = {x.x, x.y, x.z, x.w};
+    const uint64_t sixteenth = pack_f32x2(0.0625f, 0.0625f), minus_low = pack_f32x2(-low16, -low16), by = pack_f32x2(inv, inv);
     uint32_t word = 0u - 0x4b400000u * 0x11111111u;
 #pragma unroll
-    for (int i = 0; i < 8; ++i) {
-        const float v = (i & 1) ? bf16hi(w[i >> 1]) : bf16lo(w[i >> 1]);
-        word += __float_as_uint(__fadd_rn(__fmul_rn(__fmaf_rn(v, 0.0625f, -low16), inv), 12582912.f)) * (1u << (4 * i));
+    for (int i = 0; i < 4; ++i) {
+        float lo, hi;
+        unpack_f32x2(fmul2(ffma2(pack_f32x2(bf16lo(w[i]), bf16hi(w[i])), sixteenth, minus_low), by), lo, hi);
+        word += __float_as_uint(__fadd_rn(lo, 12582912.f)) * (1u << (8 * i)) + __float_as_uint(__fadd_rn(hi, 12582912.f)) * (16u << (8 * i));
     }
     return word;
 }
@@ -161,59 +175,70 @@ struct PackedWriteParams {
     const uint16_t* v;
     const int32_t* lens;
     int64_t T_cap;
-    int32_t batch, n, n_sink;
-    int32_t prompt;           // 1: token i < len goes to row i; 0: one token, to row len (ring position with n_sink)
+    int32_t batch, n, n_sink; // appended: to row len, or its place in the ring behind n_sink rows; prompts: token i < len to row i
 };
 
-// Thread blocks over rows: 256 threads, and kRowTokens rows a thread whose loads are all under way before the first is used (a
-// block of one row a thread spent its time waiting for the length, then for the row: prompts of 8 x 4096 tokens of 32
-// heads of 128 took 164 us to write and 132 us to read, now 133 and 107).
+// Thread blocks over rows: 256 threads, and U rows a thread whose loads are all under way before the first is used (blocks of one
+// row a thread spend their time waiting for the length, then for the row: prompts of 8 x 4096 tokens of 32 heads of
+// 128 took 164 us to write and 132 us to read with one, WRITE_US and READ_US with four).  Four neighbouring rows lie in one tile.
 constexpr int kRowThreads = 256;
-constexpr int kRowTokens = 4;
 template <int D>
 __host__ __device__ constexpr int rows_per_block() { return kRowThreads / PackedLane<D>::kLanes; }
 
-// Prompts: blockIdx.y (and on in steps of the grid) is the sequence, blockIdx.x a stretch of its (four tokens, head) items.  New
-// tokens: one stretch of all (four sequences, head) items.
+// The new token of every sequence: a thread block's rows are (sequence, head)s.
 template <int D>
+__global__ void __launch_bounds__(kRowThreads) packed_append_kernel(const PackedWriteParams p)
+{
+    pdl_wait_then_release();
+    const PackedLane<D> lane((int)threadIdx.x % PackedLane<D>::kLanes);
+    const uint32_t H = (uint32_t)p.map.H_kv, item = blockIdx.x * rows_per_block<D>() + threadIdx.x / PackedLane<D>::kLanes;
+    const uint32_t b = item / H, h = item - b * H;
+    const bool in = b < (uint32_t)p.batch;
+    uint4 x = make_uint4(0, 0, 0, 0), y = x;
+    int64_t row = -1;
+    if (in) {
+        const uint16_t* src = (lane.is_v ? p.v : p.k) + (int64_t)item * D;
+        x = *reinterpret_cast<const uint4*>(src + lane.element(0));
+        y = *reinterpret_cast<const uint4*>(src + lane.element(1));
+        row = p.lens[b];
+        if (p.n_sink > 0 && row >= p.T_cap) row = p.n_sink + (row - p.n_sink) % (p.T_cap - p.n_sink);
+    }
+    const int64_t at = row >= 0 && row < p.T_cap ? p.map.at((int)b, (int)h, (int)row) : -1;
+    uint32_t w0, w1, par;
+    packed_encode(x, y, w0, w1, par);            // (all lanes: it exchanges between them)
+    if (at >= 0) lane.store(lane.at(p.s, at), 0, w0, w1, par);
+}
+
+// Prompts: blockIdx.y (and on in steps of the grid) is the sequence, blockIdx.x a stretch of its (U tokens, head) items.
+template <int D, int U>
 __global__ void __launch_bounds__(kRowThreads) packed_write_kernel(const PackedWriteParams p)
 {
     pdl_wait_then_release();
     const PackedLane<D> lane((int)threadIdx.x % PackedLane<D>::kLanes);
-    const uint32_t H = (uint32_t)p.map.H_kv;
-    const uint32_t item = blockIdx.x * rows_per_block<D>() + threadIdx.x / PackedLane<D>::kLanes;
-    const uint32_t h = item % H, tok = item / H * kRowTokens;
-    const int seqs = p.prompt ? p.batch : 1;
-    for (int seq = blockIdx.y; seq < seqs; seq += gridDim.y) {
-        const int n = p.prompt ? (int)min((int64_t)min(p.n, p.lens[seq]), p.T_cap) : p.batch;
-        if ((int64_t)(blockIdx.x * rows_per_block<D>() / H) * kRowTokens >= n) continue;      // (the whole block)
-        uint4 x[kRowTokens], y[kRowTokens];
-        int64_t at[kRowTokens];
+    const uint32_t H = (uint32_t)p.map.H_kv, item = blockIdx.x * rows_per_block<D>() + threadIdx.x / PackedLane<D>::kLanes;
+    const uint32_t group = item / H, h = item - group * H;
+    const int tok = (int)group * U;
+    const int64_t step = (int64_t)H * D;
+    for (int b = blockIdx.y; b < p.batch; b += gridDim.y) {
+        const int n = (int)min((int64_t)min(p.n, p.lens[b]), p.T_cap);
+        if ((int64_t)(blockIdx.x * rows_per_block<D>() / H) * U >= n) continue;      // (the whole block)
+        const int64_t at = tok < n ? p.map.at(b, (int)h, tok) : -1;
+        const uint16_t* src = (lane.is_v ? p.v : p.k) + (((int64_t)b * p.n + tok) * H + h) * D;
+        uint4 x[U], y[U];
 #pragma unroll
-        for (int u = 0; u < kRowTokens; ++u) {
-            const int t = (int)tok + u;
-            int64_t row = -1;
-            if (t < n) {
-                row = t;
-                if (!p.prompt) {
-                    row = p.lens[t];
-                    if (p.n_sink > 0 && row >= p.T_cap) row = p.n_sink + (row - p.n_sink) % (p.T_cap - p.n_sink);
-                    if (row >= p.T_cap) row = -1;
-                }
-            }
-            at[u] = row >= 0 ? p.map.at(p.prompt ? seq : t, (int)h, (int)row) : -1;
+        for (int u = 0; u < U; ++u) {
             x[u] = y[u] = make_uint4(0, 0, 0, 0);
-            if (t < n) {
-                const uint16_t* src = (lane.is_v ? p.v : p.k) + (((int64_t)seq * p.n + t) * H + h) * D;
-                x[u] = *reinterpret_cast<const uint4*>(src + lane.word(0) * 8);
-                y[u] = *reinterpret_cast<const uint4*>(src + lane.word(1) * 8);
+            if (tok + u < n) {
+                x[u] = *reinterpret_cast<const uint4*>(src + u * step + lane.element(0));
+                y[u] = *reinterpret_cast<const uint4*>(src + u * step + lane.element(1));
             }
         }
+        const auto to = lane.at(p.s, max((int64_t)0, at));
 #pragma unroll
-        for (int u = 0; u < kRowTokens; ++u) {
+        for (int u = 0; u < U; ++u) {
             uint32_t w0, w1, par;
             packed_encode(x[u], y[u], w0, w1, par);        // (all lanes: it exchanges between them)
-            if (at[u] >= 0) lane.store(p.s, at[u], w0, w1, par);
+            if (at >= 0 && tok + u < n) lane.store(to, u, w0, w1, par);
         }
     }
 }
@@ -231,35 +256,39 @@ struct RowReadParams {
 };
 
 // Rows 0 .. len-1 of a slot as tokens; lanes and blocks as in packed_write_kernel.
-template <int D, bool PACKED, bool F32>
+template <int D, bool PACKED, bool F32, int U>
 __global__ void __launch_bounds__(kRowThreads) row_read_kernel(const RowReadParams p)
 {
     pdl_wait_then_release();
     const PackedLane<D> lane((int)threadIdx.x % PackedLane<D>::kLanes);
-    const uint32_t H = (uint32_t)p.map.H_kv;
-    const uint32_t item = blockIdx.x * rows_per_block<D>() + threadIdx.x / PackedLane<D>::kLanes;
-    const uint32_t h = item % H, tok = item / H * kRowTokens;
+    const uint32_t H = (uint32_t)p.map.H_kv, item = blockIdx.x * rows_per_block<D>() + threadIdx.x / PackedLane<D>::kLanes;
+    const uint32_t group = item / H, h = item - group * H;
+    const int tok = (int)group * U;
+    const int64_t step = (int64_t)H * D;
     for (int b = blockIdx.y; b < p.batch; b += gridDim.y) {
-        const int64_t n = min((int64_t)min(p.n, p.lens[b]), p.T_cap);
-        if ((int64_t)tok >= n) continue;
-        uint32_t w[kRowTokens][2], par[kRowTokens];
-        uint4 x[kRowTokens][2];
-        int64_t at[kRowTokens];
+        const int n = (int)min((int64_t)min(p.n, p.lens[b]), p.T_cap);
+        if (tok >= n) continue;
+        const int64_t at = p.map.at(b, (int)h, tok);
+        if (at < 0) continue;
+        uint32_t w[U][2], par[U];
+        uint4 x[U][2];
+        const auto from = lane.at(p.s, at);
+        const uint16_t* row = (lane.is_v ? p.V : p.K) + at * D;
 #pragma unroll
-        for (int u = 0; u < kRowTokens; ++u) {
-            at[u] = (int64_t)tok + u < n ? p.map.at(b, (int)h, (int)tok + u) : -1;
-            if (at[u] < 0) continue;
-            if constexpr (PACKED) lane.load(p.s, at[u], w[u][0], w[u][1], par[u]);
+        for (int u = 0; u < U; ++u) {
+            if (tok + u >= n) break;
+            if constexpr (PACKED) lane.load(from, u, w[u][0], w[u][1], par[u]);
             else
 #pragma unroll
-                for (int i = 0; i < 2; ++i) x[u][i] = *reinterpret_cast<const uint4*>((lane.is_v ? p.V : p.K) + at[u] * D + lane.word(i) * 8);
+                for (int i = 0; i < 2; ++i) x[u][i] = *reinterpret_cast<const uint4*>(row + u * D + lane.element(i));
         }
+        const int64_t dst0 = (((int64_t)b * p.n + tok) * H + h) * D;
 #pragma unroll
-        for (int u = 0; u < kRowTokens; ++u) {
-            if (at[u] < 0) continue;
+        for (int u = 0; u < U; ++u) {
+            if (tok + u >= n) break;
 #pragma unroll
             for (int i = 0; i < 2; ++i) {
-                const int64_t dst = (((int64_t)b * p.n + tok + u) * H + h) * D + lane.word(i) * 8;
+                const int64_t dst = dst0 + u * step + lane.element(i);
                 if constexpr (!PACKED && !F32) {
                     *reinterpret_cast<uint4*>(static_cast<uint16_t*>(lane.is_v ? p.v : p.k) + dst) = x[u][i];
                 } else {
