@@ -450,6 +450,15 @@ void (*packed_variant(const lckv_config_t& c))(lckv::PackedParams)
     return c.page_rows ? packed_variant_of<64, true>(heads, exact) : packed_variant_of<64, false>(heads, exact);
 }
 
+// How the pairs of pp (its batch and heads are set) are shared out: `workers` warps of `grid` thread blocks of `warps`.
+void packed_shares(lckv::PackedParams& pp, int grid, int workers, int warps)
+{
+    pp.n_blocks = std::min(grid, (workers + warps - 1) / warps);
+    pp.n_warps = (workers + pp.n_blocks - 1) / pp.n_blocks;
+    pp.pairs_per_block = (int32_t)(((int64_t)pp.m.a.B * pp.m.a.H_q + pp.n_blocks - 1) / pp.n_blocks);
+    pp.warps_inverse = (uint32_t)(((1ull << 32) + pp.n_warps - 1) / pp.n_warps);
+}
+
 // early: the previous kernel in the stream is an attention launch of the same step and this one
 // reads only rows that were final before it (condensed mode), so its first copies need not wait.
 int launch_attention(lckv_cache* c, int slot, int mode, const void* q, void* out, float* lse,
@@ -496,10 +505,7 @@ int launch_attention(lckv_cache* c, int slot, int mode, const void* q, void* out
         pp.s = packed_slot(c, slot);
         pp.pitch = row_pitch(c->cfg);
         const int warps = lckv::packed_warps(c->cfg.head_dim);
-        pp.n_blocks = std::min(c->grid, (c->active_workers + warps - 1) / warps);
-        pp.n_warps = (c->active_workers + pp.n_blocks - 1) / pp.n_blocks;
-        pp.pairs_per_block = (int32_t)(((int64_t)batch * c->h_pairs + pp.n_blocks - 1) / pp.n_blocks);
-        pp.warps_inverse = (uint32_t)(((1ull << 32) + pp.n_warps - 1) / pp.n_warps);
+        packed_shares(pp, c->grid, c->active_workers, warps);
         const bool wide = c->cfg.head_dim == 128;
         e = launch_pdl(packed_variant(c->cfg), c->grid, warps * 32,
                        wide ? lckv::packed_smem_bytes<128>() : lckv::packed_smem_bytes<64>(), st, pp);

@@ -58,7 +58,8 @@ template <int D, bool PACKED>
 cudaError_t launch_move(const lckv::MoveParams& p, bool in_place, int64_t heads, cudaStream_t st)
 {
     if (in_place) return launch_pdl_dims(lckv::evict_in_place_kernel<D, PACKED>, dim3((unsigned)heads), dim3(1024), 0, st, p);
-    const dim3 grid = move_grid(heads, (int64_t)p.n_keep * lckv::RowUnits<D, PACKED>::kUnits, lckv::kRowThreads * lckv::kMoveUnits);
+    const int64_t units = (int64_t)((p.n_keep + lckv::kMoveRows - 1) / lckv::kMoveRows) * lckv::RowUnits<D, PACKED>::kUnits;
+    const dim3 grid = move_grid(heads, units, lckv::kRowThreads);
     return launch_pdl_dims(lckv::evict_move_kernel<D, PACKED>, grid, dim3(lckv::kRowThreads), 0, st, p);
 }
 
@@ -73,13 +74,19 @@ cudaError_t launch_select(const lckv::SelectParams& s, int64_t most, int64_t hea
     return launch_pdl_dims(lckv::evict_select_kernel<1024, 0>, grid, dim3(1024), 0, st, s);
 }
 
-template <int D, bool PACKED>
-cudaError_t launch_weights(const lckv::WeightParams& p, int group, dim3 grid, cudaStream_t st)
+template <int D>
+cudaError_t launch_weights(const lckv::WeightParams& p, const lckv::PackedParams* pp, int group, int64_t blocks, cudaStream_t st)
 {
-    const auto kernel = group <= 2   ? lckv::attention_weights_kernel<D, PACKED, 2>
-                        : group <= 4 ? lckv::attention_weights_kernel<D, PACKED, 4>
-                                     : lckv::attention_weights_kernel<D, PACKED, 8>;
-    return launch_pdl_dims(kernel, grid, dim3(32 * lckv::kWeightWarps), 0, st, p);
+    if (!pp) {
+        const auto kernel = group <= 2 ? lckv::attention_weights_kernel<D, 2> : group <= 4 ? lckv::attention_weights_kernel<D, 4> : lckv::attention_weights_kernel<D, 8>;
+        return launch_pdl_dims(kernel, dim3((unsigned)blocks), dim3(32 * lckv::kWeightWarps), 0, st, p);
+    }
+    const auto kernel = group <= 2   ? lckv::attention_weights_packed_kernel<D, 2>
+                        : group <= 4 ? lckv::attention_weights_packed_kernel<D, 4>
+                                     : lckv::attention_weights_packed_kernel<D, 8>;
+    const cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, lckv::weight_smem_bytes<D>());
+    if (e != cudaSuccess) return e;
+    return launch_pdl_dims(kernel, dim3((unsigned)blocks), dim3(32 * lckv::kWeightBlockWarps), lckv::weight_smem_bytes<D>(), st, p, *pp);
 }
 
 }  // namespace
@@ -154,21 +161,33 @@ int lckv_attention_weights(lckv_cache_t* c, int32_t slot, int32_t mode, const vo
     p.H_q = c->cfg.n_q_heads;
     p.mode = mode;
     p.scale_log2 = c->scale_log2;
+    p.status = c->d_status;
+    p.wait_limit = c->wait_limit;
+    const bool wide = c->cfg.head_dim == 128;
+    const int group = c->cfg.n_q_heads / c->cfg.n_kv_heads;
+    if (c->cfg.kv_bits == 4) {
+        lckv::PackedParams pp = {};
+        pp.m.a.lens = c->d_lens;
+        pp.m.a.T_cap = c->cfg.max_seq;
+        pp.m.a.B = batch;
+        pp.m.a.H_q = pp.m.a.H_kv = c->cfg.n_kv_heads;
+        pp.m.a.mode = mode;
+        pp.m.groups_per_kv = 1;
+        packed_shares(pp, c->sm_count, c->sm_count * lckv::kWeightBlockWarps, lckv::kWeightBlockWarps);
+        const cudaError_t e = wide ? launch_weights<128>(p, &pp, group, c->sm_count, st) : launch_weights<64>(p, &pp, group, c->sm_count, st);
+        return cuda_ok(e) ? LCKV_OK : LCKV_ECUDA;
+    }
+    // Warps for the longest sequence that the host knows (one whose sequence turns out longer in a replay goes on behind the last run), of two
+    // tiles of 64 rows where there are enough.
     int64_t longest = 1;
     for (int b = 0; b < batch; ++b) longest = std::max<int64_t>(longest, std::min(c->h_lens[b], c->cfg.max_seq - mode) + mode);
-    // tiles of 64 rows per warp: as many as leave 16 warps an SM (q is prepared once per run), up to eight
     const int64_t tiles = (longest + 63) / 64;
-    p.run = (int)std::max<int64_t>(1, std::min<int64_t>(8, tiles * rows / (16 * (int64_t)c->sm_count)));
+    p.run = tiles * rows >= 64 * (int64_t)c->sm_count ? 2 : 1;
     p.runs = (int)((tiles + p.run - 1) / p.run);
     p.heads = (int)rows;
-    // (a warp whose sequence turns out longer in a replay goes on behind the last run)
     const int64_t blocks = ((int64_t)p.runs * rows + lckv::kWeightWarps - 1) / lckv::kWeightWarps;
     if (blocks > INT32_MAX) return LCKV_EINVAL;
-    const dim3 grid((unsigned)blocks);
-    const bool packed = c->cfg.kv_bits == 4;
-    const int group = c->cfg.n_q_heads / c->cfg.n_kv_heads;
-    const cudaError_t e = c->cfg.head_dim == 128 ? (packed ? launch_weights<128, true>(p, group, grid, st) : launch_weights<128, false>(p, group, grid, st))
-                                                 : (packed ? launch_weights<64, true>(p, group, grid, st) : launch_weights<64, false>(p, group, grid, st));
+    const cudaError_t e = wide ? launch_weights<128>(p, nullptr, group, blocks, st) : launch_weights<64>(p, nullptr, group, blocks, st);
     return cuda_ok(e) ? LCKV_OK : LCKV_ECUDA;
 }
 

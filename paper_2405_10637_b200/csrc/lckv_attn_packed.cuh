@@ -219,7 +219,8 @@ struct PackedTable {
     uint32_t sums[32], longest[32];
 };
 
-// The block's threads fill the table; returns the longest sequence's tiles.
+// The block's threads fill the table; returns the longest sequence's tiles.  Up to 32 sequences every warp fills it by itself (all
+// write the same), without waiting for the others.
 template <int THREADS>
 __device__ __forceinline__ uint32_t packed_table(const AttnParams& p, int per, PackedTable& t)
 {
@@ -227,6 +228,21 @@ __device__ __forceinline__ uint32_t packed_table(const AttnParams& p, int per, P
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
     constexpr int EACH = (kPackedTable + THREADS - 1) / THREADS;     // entries of a thread, side by side
     const int n = (p.B + per - 1) / per;
+    if (p.B <= 32) {
+        const int32_t nv = lane < p.B ? packed_visible(p, lane) : 0;
+        const uint32_t nt = packed_tiles(nv);
+        uint32_t incl = nt;
+#pragma unroll
+        for (int off = 1; off < 32; off <<= 1) {
+            const uint32_t x = __shfl_up_sync(FULL, incl, off);
+            if (lane >= off) incl += x;
+        }
+        t.rows[lane] = nv;
+        t.before[lane] = incl - nt;
+        if (lane == 31) t.before[32] = incl;
+        __syncwarp();
+        return __reduce_max_sync(FULL, nt);
+    }
     uint32_t mine[EACH], sum = 0, longest = 0;
 #pragma unroll
     for (int e = 0; e < EACH; ++e) {

