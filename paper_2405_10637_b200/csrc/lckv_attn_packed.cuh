@@ -19,10 +19,11 @@
 // scaling, exponentials and weights only of every NC-th block of 16 rows.  The transposed weights then stand in the columns
 // of their own copy, the columns of the others are zeroed per block, and the copies' outputs are added up at the end of a pair.
 //
-// EXACT (fp32 outputs).  Where thousands of rows cancel, two things would show: the rounding of W to 11 bits, and the
-// tensor cores' truncation of sums of codes that are all positive.  So W is split into a rounded part and the rounding of
-// the rest (a second MMA), and codes enter as c - 8, which is exact too (one more instruction for two codes), with
-// low + 8 step in place of low.  A bf16 output's own rounding (2^-9) is 20 times what that would gain.
+// EXACT (fp32 outputs).  Codes are all positive and lows all negative, more or less, so what is summed is far larger than the sums:
+// scores come out with an error of 5e-6 and, where thousands of rows cancel, the tensor cores' truncation shows.  So codes enter as
+// c - 8, which is exact too (one more instruction for two codes), with low + 8 step in place of low, and W is split into a
+// rounded part and the rounding of the rest (a second MMA), 22 bits.  A bf16 output's own rounding (2^-9) is hundreds of times
+// what that would gain.
 //
 // Work: a launch is one long sequence of tiles of 64 rows, (sequence, pair, tile), cut into one range per thread block and
 // those into one per worker (warp).  A pair that several warps of a block share is joined behind a block barrier; only what
@@ -84,8 +85,8 @@ __device__ __forceinline__ uint32_t lds32(uint32_t addr)
     return v;
 }
 
-// A query head as the B operand of the score MMAs.
-template <int D>
+// A query head as the B operand of the score MMAs.  EXACT: for codes c - 8.
+template <int D, bool EXACT>
 struct PackedQuery {
     uint32_t b[D / 16][2];
     float f[2];              // per column of this lane: softmax scale * log2(e) / the scaling of q and codes
@@ -93,8 +94,8 @@ struct PackedQuery {
 };
 
 // raw[j]: dimensions 32 j + 8 c4 .. + 7 of the query of column g4.
-template <int D>
-__device__ __forceinline__ void packed_query(const uint4 (&raw)[D / 32], float scale_log2, int lane, PackedQuery<D>& out)
+template <int D, bool EXACT>
+__device__ __forceinline__ void packed_query(const uint4 (&raw)[D / 32], float scale_log2, int lane, PackedQuery<D, EXACT>& out)
 {
     const uint32_t FULL = 0xffffffffu;
     const int c4 = lane & 3;
@@ -118,11 +119,11 @@ __device__ __forceinline__ void packed_query(const uint4 (&raw)[D / 32], float s
     }
     // largest element to [2^14, 2^15)
     const int up = max(-100, min(100, 14 + 127 - (int)(__float_as_uint(mx) >> 23)));
-    const float by = __uint_as_float((uint32_t)(up + 127) << 23), by16 = by * 0.0625f;
-    const float f = scale_log2 * __uint_as_float((uint32_t)(24 - up + 127) << 23);
+    const float by = __uint_as_float((uint32_t)(up + 127) << 23), by16 = EXACT ? by : by * 0.0625f;
+    const float f = scale_log2 * __uint_as_float((uint32_t)((EXACT ? 0 : 24) - up + 127) << 23);
 #pragma unroll
     for (int j = 0; j < D / 32; ++j) {
-        // nibble i and nibble i + 4 of a word share a register; odd i count 16 times as much
+        // nibble i and nibble i + 4 of a word share a register; odd i count 16 times as much (not EXACT)
         const uint32_t w[4] = {raw[j].x, raw[j].y, raw[j].z, raw[j].w};
         out.b[2 * j][0] = cvt_f16x2(bf16lo(w[0]) * by, bf16lo(w[2]) * by);
         out.b[2 * j][1] = cvt_f16x2(bf16hi(w[0]) * by16, bf16hi(w[2]) * by16);
@@ -138,6 +139,10 @@ __device__ __forceinline__ void packed_query(const uint4 (&raw)[D / 32], float s
         for (int g = 0; g < D / 64; ++g) out.sum[i][g] = __shfl_sync(FULL, sum[g], src) * scale_log2;
     }
 }
+
+// What a group's codes count from: 0, or EXACT 8.
+template <bool EXACT>
+__device__ __forceinline__ float packed_low(uint32_t par) { return EXACT ? fmaf(8.f, bf16lo(par), bf16hi(par)) : bf16hi(par); }
 
 // The four fp16 pairs of a word: nibbles (0, 4), (1, 5) x 16, (2, 6), (3, 7) x 16.
 __device__ __forceinline__ void nibble_pairs(uint32_t w, uint32_t (&x)[4])
@@ -157,6 +162,13 @@ __device__ __forceinline__ void nibble_pairs_signed(uint32_t w, uint32_t (&x)[4]
     asm("fma.rn.f16x2 %0, %1, %2, %3;" : "=r"(x[1]) : "r"((w & 0x00f000f0u) | 0x64006400u), "r"(0x2c002c00u), "r"(0xd480d480u));
     asm("sub.rn.f16x2 %0, %1, %2;" : "=r"(x[2]) : "r"((y & 0x000f000fu) | 0x64006400u), "r"(0x64086408u));
     asm("fma.rn.f16x2 %0, %1, %2, %3;" : "=r"(x[3]) : "r"((y & 0x00f000f0u) | 0x64006400u), "r"(0x2c002c00u), "r"(0xd480d480u));
+}
+
+template <bool EXACT>
+__device__ __forceinline__ void nibbles(uint32_t w, uint32_t (&x)[4])
+{
+    if constexpr (EXACT) nibble_pairs_signed(w, x);
+    else nibble_pairs(w, x);
 }
 
 // Token of row i (0 .. 7) of an MMA tile: pairs are swapped where bit 1 is set, so that the four tokens that a value load of a
@@ -464,8 +476,8 @@ __global__ void __launch_bounds__(packed_warps(D) * 32, 1) attn_packed_kernel(co
     uint32_t cslot = 0, cphase = 0;
     bool ok = true;
 
-    PackedQuery<D> q;
-    if (n_tiles) packed_query<D>(q_raw, p.scale_log2, lane, q);
+    PackedQuery<D, EXACT> q;
+    if (n_tiles) packed_query<D, EXACT>(q_raw, p.scale_log2, lane, q);
 
     // running state of this lane's two columns
     float m_run[2], l_run[2];
@@ -590,8 +602,8 @@ __global__ void __launch_bounds__(packed_warps(D) * 32, 1) attn_packed_kernel(co
 #pragma unroll
                     for (int j = 0; j < J; ++j) {
                         uint32_t xa[4], xb[4];
-                        nibble_pairs(ka[j], xa);
-                        nibble_pairs(kb[j], xb);
+                        nibbles<EXACT>(ka[j], xa);
+                        nibbles<EXACT>(kb[j], xb);
                         mma_f16_16816(acc[j / 2], xa[0], xb[0], xa[1], xb[1], q.b[2 * j][0], q.b[2 * j][1]);
                         mma_f16_16816(acc[j / 2], xa[2], xb[2], xa[3], xb[3], q.b[2 * j + 1][0], q.b[2 * j + 1][1]);
                     }
@@ -622,10 +634,10 @@ __global__ void __launch_bounds__(packed_warps(D) * 32, 1) attn_packed_kernel(co
 #pragma unroll
             for (int e = 0; e < 4; ++e) {
                 const uint32_t* pr = e < 2 ? pa : pb;
-                float t = bf16lo(pr[0]) * own[0][e], u = bf16hi(pr[0]) * q.sum[e & 1][0];
+                float t = bf16lo(pr[0]) * own[0][e], u = packed_low<EXACT>(pr[0]) * q.sum[e & 1][0];
                 if constexpr (G == 2) {
                     t = fmaf(bf16lo(pr[1]), own[1][e], t);
-                    u = fmaf(bf16hi(pr[1]), q.sum[e & 1][1], u);
+                    u = fmaf(packed_low<EXACT>(pr[1]), q.sum[e & 1][1], u);
                 }
                 s[i][e] = fmaf(t, q.f[e & 1], u);
             }
@@ -683,7 +695,7 @@ __global__ void __launch_bounds__(packed_warps(D) * 32, 1) attn_packed_kernel(co
 #pragma unroll
             for (int g = 0; g < G; ++g) {
                 const uint32_t pa = vp[i][0][g], pb = vp[i][1][g];
-                const float la = EXACT ? fmaf(8.f, bf16lo(pa), bf16hi(pa)) : bf16hi(pa), lb = EXACT ? fmaf(8.f, bf16lo(pb), bf16hi(pb)) : bf16hi(pb);
+                const float la = packed_low<EXACT>(pa), lb = packed_low<EXACT>(pb);
                 low_sum[g][0] = fmaf(p0, la, fmaf(p2, lb, low_sum[g][0]));
                 low_sum[g][1] = fmaf(p1, la, fmaf(p3, lb, low_sum[g][1]));
                 const float sa = bf16lo(pa) * unit, sb = bf16lo(pb) * unit;
@@ -723,25 +735,28 @@ __global__ void __launch_bounds__(packed_warps(D) * 32, 1) attn_packed_kernel(co
 #pragma unroll
             for (int g = 0; g < G; ++g) {
                 const uint32_t b0 = mine ? bw[rb / NC][g][0] : 0u, b1 = mine ? bw[rb / NC][g][1] : 0u;
+                const uint32_t r0 = EXACT && mine ? br[rb / NC][g][0] : 0u, r1 = EXACT && mine ? br[rb / NC][g][1] : 0u;
 #pragma unroll
                 for (int half = 0; half < 2; ++half) {
                     // nibbles 4 half .. 4 half + 3 of two tokens side by side
                     const uint32_t sel = half ? 0x7632u : 0x5410u;
                     uint32_t xa[4], xb[4];
                     const uint32_t lo = __byte_perm(va[0][g], va[1][g], sel), hi = __byte_perm(va[2][g], va[3][g], sel);
-                    if constexpr (EXACT) {
-                        nibble_pairs_signed(lo, xa);
-                        nibble_pairs_signed(hi, xb);
-                    } else {
-                        nibble_pairs(lo, xa);
-                        nibble_pairs(hi, xb);
-                    }
+                    nibbles<EXACT>(lo, xa);
+                    nibbles<EXACT>(hi, xb);
 #pragma unroll
                     for (int i = 0; i < 2; ++i) {
                         float (&acc)[4] = o[4 * g + 2 * half + i];
-                        mma_f16_16816(acc, xa[2 * i], xa[2 * i + 1], xb[2 * i], xb[2 * i + 1], b0, b1);
-                        if constexpr (EXACT)
-                            mma_f16_16816(acc, xa[2 * i], xa[2 * i + 1], xb[2 * i], xb[2 * i + 1], mine ? br[rb / NC][g][0] : 0u, mine ? br[rb / NC][g][1] : 0u);
+                        if constexpr (EXACT) {
+                            // (the tensor cores truncate: a sum of 40 MMAs' results came out 40 * 2^-24 too small)
+                            float t[4] = {0.f, 0.f, 0.f, 0.f};
+                            mma_f16_16816(t, xa[2 * i], xa[2 * i + 1], xb[2 * i], xb[2 * i + 1], r0, r1);
+                            mma_f16_16816(t, xa[2 * i], xa[2 * i + 1], xb[2 * i], xb[2 * i + 1], b0, b1);
+#pragma unroll
+                            for (int e = 0; e < 4; ++e) acc[e] += t[e];
+                        } else {
+                            mma_f16_16816(acc, xa[2 * i], xa[2 * i + 1], xb[2 * i], xb[2 * i + 1], b0, b1);
+                        }
                     }
                 }
             }
@@ -820,7 +835,7 @@ __global__ void __launch_bounds__(packed_warps(D) * 32, 1) attn_packed_kernel(co
             packed_next(cc, p, per_kv);
             if (pair_end) {
                 load_q();
-                packed_query<D>(q_raw, p.scale_log2, lane, q);
+                packed_query<D, EXACT>(q_raw, p.scale_log2, lane, q);
                 seg_t0 = 0;
                 first_seg = false;
             }

@@ -184,7 +184,7 @@ __global__ void __launch_bounds__(kWeightBlockWarps * 32, 1) attention_weights_p
         before_a[s] = before_b[s] = 0.f;
         if (issued < n_tiles) issue(before_a[s], before_b[s]);
     }
-    PackedQuery<D> q;
+    PackedQuery<D, false> q;
     const auto load_q = [&](int first) {         // query heads first .. of pair cc
         const int64_t head0 = (int64_t)cc.b * p.H_q + (int64_t)cc.kvh * group;
         uint4 raw[J];
@@ -192,7 +192,7 @@ __global__ void __launch_bounds__(kWeightBlockWarps * 32, 1) attention_weights_p
 #pragma unroll
         for (int j = 0; j < J; ++j) raw[j] = q4[4 * j];
         l.heads(p.lse + head0, first, group);
-        packed_query<D>(raw, p.scale_log2, lane, q);
+        packed_query<D, false>(raw, p.scale_log2, lane, q);
     };
     load_q(0);
     for (uint32_t tile = 0; tile < n_tiles; ++tile) {
