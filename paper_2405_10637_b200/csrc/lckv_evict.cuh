@@ -128,8 +128,9 @@ __global__ void __launch_bounds__(kWeightWarps * 32, D == 64 ? 4 : 1) attention_
 
 // 4-bit keys: the decode attention's division of the work (one thread block per SM, one range of tiles per warp, whatever the
 // lengths; a (sequence, kv head) is a pair) and its rings, here of two tiles' keys and parameters, two bulk copies a tile.  Nothing is to
-// be joined.  32 x 32 heads of 128 with 256 to 4096 rows (190 MB): 37 us, 5.1 TB/s; with 12 warps and three tiles a ring 41;
-// with a fixed number of tiles per warp 50 to 60; with tiles in registers and the next one's loads under way 62 to 68.
+// be joined.  Codes enter as c - 8 (EXACT there; weights are fp32, and came out 9e-7 off without).  32 x 32 heads of 128 with 256 to
+// 4096 rows (190 MB): 43 us, 4.4 TB/s (with codes as they are 37; then with 12 warps and three tiles a ring 41, with a fixed number of
+// tiles per warp 50 to 60, with tiles in registers and the next one's loads under way 62 to 68).
 constexpr int kWeightSlots = 2, kWeightBlockWarps = 16;
 template <int D>
 __host__ __device__ constexpr int weight_tile_bytes() { return kPackedRows * (D / 2 + D / 8); }
@@ -184,7 +185,7 @@ __global__ void __launch_bounds__(kWeightBlockWarps * 32, 1) attention_weights_p
         before_a[s] = before_b[s] = 0.f;
         if (issued < n_tiles) issue(before_a[s], before_b[s]);
     }
-    PackedQuery<D, false> q;
+    PackedQuery<D, true> q;
     const auto load_q = [&](int first) {         // query heads first .. of pair cc
         const int64_t head0 = (int64_t)cc.b * p.H_q + (int64_t)cc.kvh * group;
         uint4 raw[J];
@@ -192,7 +193,7 @@ __global__ void __launch_bounds__(kWeightBlockWarps * 32, 1) attention_weights_p
 #pragma unroll
         for (int j = 0; j < J; ++j) raw[j] = q4[4 * j];
         l.heads(p.lse + head0, first, group);
-        packed_query<D, false>(raw, p.scale_log2, lane, q);
+        packed_query<D, true>(raw, p.scale_log2, lane, q);
     };
     load_q(0);
     for (uint32_t tile = 0; tile < n_tiles; ++tile) {
@@ -235,8 +236,8 @@ __global__ void __launch_bounds__(kWeightBlockWarps * 32, 1) attention_weights_p
 #pragma unroll
                         for (int j = 0; j < J; ++j) {
                             uint32_t xa[4], xb[4];
-                            nibble_pairs(ka[j], xa);
-                            nibble_pairs(kb[j], xb);
+                            nibble_pairs_signed(ka[j], xa);
+                            nibble_pairs_signed(kb[j], xb);
                             mma_f16_16816(acc[j / 2], xa[0], xb[0], xa[1], xb[1], q.b[2 * j][0], q.b[2 * j][1]);
                             mma_f16_16816(acc[j / 2], xa[2], xb[2], xa[3], xb[3], q.b[2 * j + 1][0], q.b[2 * j + 1][1]);
                         }
@@ -261,10 +262,10 @@ __global__ void __launch_bounds__(kWeightBlockWarps * 32, 1) attention_weights_p
 #pragma unroll
                 for (int e = 0; e < 4; ++e) {
                     const uint32_t* pr = e < 2 ? pa : pb;
-                    float x = bf16lo(pr[0]) * own[0][e], u = bf16hi(pr[0]) * q.sum[e & 1][0];
+                    float x = bf16lo(pr[0]) * own[0][e], u = packed_low<true>(pr[0]) * q.sum[e & 1][0];
                     if constexpr (G == 2) {
                         x = fmaf(bf16lo(pr[1]), own[1][e], x);
-                        u = fmaf(bf16hi(pr[1]), q.sum[e & 1][1], u);
+                        u = fmaf(packed_low<true>(pr[1]), q.sum[e & 1][1], u);
                     }
                     s[e] = fmaf(x, q.f[e & 1], u);
                 }
