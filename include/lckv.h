@@ -94,10 +94,11 @@ typedef struct {
     int32_t n_workers;        /* independent workers (warps) per attention launch            */
     int32_t rows_per_tile;    /* cache rows moved by one bulk copy                           */
     int32_t kernel_kind;      /* 1 = FP32-ALU kernel (one q head per pair),
-                                 2 = tensor-core kernel (one kv head's query group per pair) */
+                                 2 = tensor-core kernel (one kv head's query group per pair),
+                                 3 = the kernel over 4-bit rows                            */
     int32_t launches_per_step;/* kernels lckv_layer_stack_step enqueues                      */
     int32_t sm_count;
-    uint64_t slot_bytes;      /* bytes of one K (or V) tensor of one slot                    */
+    uint64_t slot_bytes;      /* bytes of one K (or V) tensor of one slot (4 bits: half a slot) */
     uint64_t workspace_bytes; /* lengths + plan tables + split-K partials + counters         */
 } lckv_info_t;
 
@@ -587,8 +588,8 @@ int lckv_quant_set_copy_limits(int32_t weights, int32_t x);
  *   - lckv_append_kv and lckv_prefill_write_kv take bf16 and write rows in 4 bits; lckv_decode_attention and
  *     lckv_layer_stack_step (_host) attend to what the rows stand for: codes enter the tensor cores exactly,
  *     q as well (elements below 2^-25 of the head's largest one are rounded there; |q| < 2^100), everything
- *     else is fp32, with 22 bits of a row's weight times its step;
- *   - stream_sink and page_rows work as ever, kernel_kind is 0;
+ *     else is fp32, with 11 bits of a row's weight times its step (22 where out_dtype is fp32);
+ *   - stream_sink and page_rows work as ever, kernel_kind is 0; tensors off the 16-byte grid are refused (EINVAL);
  *   - lckv_cache_slot_ptrs, lckv_project_append_kv, the keys of lckv_rope_append_kv and
  *     lckv_rope_prefill_write_kv (rotate with lckv_rope_apply first), lckv_prefill_attention and
  *     lckv_prefill_iteration return EINVAL.  Prompts are encoded in a bf16 cache; lckv_evict_kv takes them over.

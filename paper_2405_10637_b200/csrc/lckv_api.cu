@@ -406,6 +406,12 @@ int sync_page_table(lckv_cache* c, cudaStream_t st)
     return LCKV_OK;
 }
 
+// The kernels over 4-bit rows move 16 bytes at a time: their tensors are looked at before anything is enqueued.
+bool on_grid(const lckv_cache* c, const void* a, const void* b)
+{
+    return c->cfg.kv_bits != 4 || ((((uintptr_t)a | (uintptr_t)b) & 15) == 0);
+}
+
 int launch_plan(lckv_cache* c, int batch, cudaStream_t st)
 {
     if (c->kernel_kind == 3) return LCKV_OK;     // the kernel over 4-bit rows works its shares out by itself
@@ -1132,7 +1138,7 @@ int lckv_append_kv(lckv_cache_t* c, int32_t slot, const void* k_new, const void*
                    int32_t batch, int32_t advance_len, void* stream)
 {
     if (!c || !k_new || !v_new || batch < 1 || batch > c->cfg.max_batch) return LCKV_EINVAL;
-    if (slot < 0 || slot >= c->plan.n_slots) return LCKV_EINVAL;
+    if (slot < 0 || slot >= c->plan.n_slots || !on_grid(c, k_new, v_new)) return LCKV_EINVAL;
     if (max_len(c, batch) + 1 > c->cfg.max_seq) return LCKV_ECAPACITY;
     cudaStream_t st = static_cast<cudaStream_t>(stream);
     if (int rc = ensure_pages(c, batch, 1)) return rc;
@@ -1262,7 +1268,7 @@ int lckv_decode_attention(lckv_cache_t* c, int32_t slot, int32_t mode, const voi
                           float* lse, int32_t batch, void* stream)
 {
     if (!c || !q || !out || batch < 1 || batch > c->cfg.max_batch) return LCKV_EINVAL;
-    if (slot < 0 || slot >= c->plan.n_slots) return LCKV_EINVAL;
+    if (slot < 0 || slot >= c->plan.n_slots || !on_grid(c, q, out)) return LCKV_EINVAL;
     if (mode != LCKV_MODE_CONDENSED && mode != LCKV_MODE_STANDARD) return LCKV_EINVAL;
     if (max_len(c, batch) + mode > c->cfg.max_seq) return LCKV_ECAPACITY;
     cudaStream_t st = static_cast<cudaStream_t>(stream);
@@ -1280,8 +1286,8 @@ int lckv_layer_stack_step(lckv_cache_t* c, const void* const* q_layers, void* co
     if (batch < 1 || batch > c->cfg.max_batch) return LCKV_EINVAL;
     const int L = c->cfg.n_layers;
     for (int l = 0; l < L; ++l) {
-        if (!q_layers[l] || !out_layers[l]) return LCKV_EINVAL;
-        if (c->plan.write_slot[l] >= 0 && (!k_new_layers[l] || !v_new_layers[l])) return LCKV_EINVAL;
+        if (!q_layers[l] || !out_layers[l] || !on_grid(c, q_layers[l], out_layers[l])) return LCKV_EINVAL;
+        if (c->plan.write_slot[l] >= 0 && (!k_new_layers[l] || !v_new_layers[l] || !on_grid(c, k_new_layers[l], v_new_layers[l]))) return LCKV_EINVAL;
     }
     if (max_len(c, batch) + 1 > c->cfg.max_seq) return LCKV_ECAPACITY;
     return run_step(c, q_layers, out_layers, k_new_layers, v_new_layers, batch,
@@ -1383,7 +1389,7 @@ int lckv_layer_stack_step_host(lckv_cache_t* c, const void* const* q_host, void*
 int lckv_prefill_write_kv(lckv_cache_t* c, int32_t slot, const void* k, const void* v,
                           int32_t n_max, int32_t batch, void* stream)
 {
-    if (!c || !k || !v || slot < 0 || slot >= c->plan.n_slots) return LCKV_EINVAL;
+    if (!c || !k || !v || slot < 0 || slot >= c->plan.n_slots || !on_grid(c, k, v)) return LCKV_EINVAL;
     if (int rc = prefill_check(c, n_max, batch, false)) return rc;
     if (int rc = sync_page_table(c, static_cast<cudaStream_t>(stream))) return rc;
     return launch_prefill_write(c, slot, k, v, n_max, batch, static_cast<cudaStream_t>(stream));

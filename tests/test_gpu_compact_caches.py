@@ -766,3 +766,87 @@ def test_attention_of_many_sequences(B, d, Hq):
         some = [b for b in range(B) if lens[b]][::max(1, B // 40)]
         check_attention(out[some], lse[some], q[some], k[some], v[some], [lens[b] for b in some])
         assert torch.isfinite(out).all() and (out[[b for b in range(B) if lens[b]]].abs().amax((1, 2)) > 0).all()
+
+
+def test_tensors_off_the_grid_are_refused():
+    c = make(4, 2, 4, 2, 64, 100, [50, 99], poison=False)
+    flat = torch.zeros(100000, dtype=torch.bfloat16, device=DEV)
+    good = [flat[8 * i:8 * i + n] for i, n in ((0, 512), (1000, 512))]
+
+    def off(shape):
+        n = math.prod(shape)
+        return flat[1:1 + n].view(shape)
+
+    q, kn = good[0].view(2, 4, 64), good[1][:256].view(2, 2, 64)
+    refused(lk.EINVAL, c.lckv_decode_attention, 0, CONDENSED, off((2, 4, 64)))
+    refused(lk.EINVAL, c.lckv_decode_attention, 0, CONDENSED, q, out=off((2, 4, 64)))
+    refused(lk.EINVAL, c.lckv_append_kv, 0, off((2, 2, 64)), kn)
+    refused(lk.EINVAL, c.lckv_prefill_write_kv, 0, off((2, 99, 2, 64)), off((2, 99, 2, 64)))
+    refused(lk.EINVAL, c.lckv_layer_stack_step, [off((2, 4, 64))], [q], [kn], [kn])
+    refused(lk.EINVAL, c.lckv_attention_weights, 0, CONDENSED, off((2, 4, 64)), torch.zeros(2, 4, device=DEV))
+    assert c.lckv_cache_lengths() == [50, 99]
+
+
+@pytest.mark.parametrize("sink", [0, 2])
+def test_steps_from_host_buffers(sink):
+    """The same outputs as the step on device buffers, and the same rows."""
+    g = gen(21)
+    L, w, B, Hq, Hkv, d, cap = 4, 2, 3, 4, 2, 64, 40
+    plan = lk.lckv_plan(L, w)
+    lens = [20, 0, 33] if not sink else [60, 0, 39]
+    a, b = (make(4, B, Hq, Hkv, d, cap, lens, L=L, w=w, host_staging=1, sink=sink, poison=False) for _ in range(2))
+    for c in (a, b):
+        c.buf[c.info.workspace_bytes:] = 0
+    for _ in range(3):
+        q = [randn(g, B, Hq, d) for _ in range(L)]
+        kn, vn = ([rows_bf16(g, B, Hkv, d) if plan["write_slot"][l] >= 0 else None for l in range(L)] for _ in range(2))
+        out = [torch.empty_like(x) for x in q]
+        a.lckv_layer_stack_step(q, out, kn, vn)
+        host = lambda ts: [None if t is None else t.cpu().pin_memory() for t in ts]
+        out_h = [torch.empty(B, Hq, d, dtype=torch.bfloat16).pin_memory() for _ in range(L)]
+        qh, kh, vh = host(q), host(kn), host(vn)
+        b.lckv_layer_stack_step_host(qh, out_h, kh, vh)
+        torch.cuda.synchronize()
+        for x, y in zip(out, out_h):
+            assert torch.equal(x.cpu(), y) and torch.isfinite(y).all()
+    assert a.lckv_cache_lengths() == b.lckv_cache_lengths() == [n + 3 for n in lens]
+
+
+def test_weights_timeout_is_reported():
+    c = make(4, 2, 4, 4, 128, 64, [64, 40], poison=False)
+    c.buf[c.info.workspace_bytes:] = 0
+    q, lse = randn(gen(22), 2, 4, 128), torch.zeros(2, 4, device=DEV)
+    c.lckv_cache_set_wait_limit(0)
+    c.lckv_attention_weights(0, CONDENSED, q, lse)
+    assert c.lckv_cache_status() == lk.ETIMEOUT
+    c.lckv_cache_set_wait_limit(1 << 18)
+    c.lckv_cache_reset([64, 40])
+    w = c.lckv_attention_weights(0, CONDENSED, q, lse)
+    assert c.lckv_cache_status() == 0 and (w[0] == 1).all() and (w[1, :, :40] == 1).all() and not w[1, :, 40:].any()
+
+
+def test_evict_after_lengths_that_only_the_device_knows():
+    """A captured advance moves the device's lengths alone; a later eviction goes by them, whatever the host thinks."""
+    g = gen(23)
+    n, keep = 1500, 300
+    c = make(16, 1, 1, 1, 64, 2000, [900])
+    k, v = rows_bf16(g, 1, n, 1, 64), rows_bf16(g, 1, n, 1, 64)
+    kn, vn = k[:, 0].contiguous(), v[:, 0].contiguous()
+    st = torch.cuda.Stream()
+    graph = torch.cuda.CUDAGraph()
+    c.lckv_prefill_write_kv(0, k[:, :900].contiguous(), v[:, :900].contiguous())
+    torch.cuda.synchronize()
+    q, o = randn(g, 1, 1, 64), torch.empty(1, 1, 64, dtype=torch.bfloat16, device=DEV)
+    with torch.cuda.graph(graph, stream=st):
+        c.lckv_layer_stack_step([q], [o], [kn], [vn])
+    for i in range(900, n):
+        kn.copy_(k[:, i]); vn.copy_(v[:, i])
+        torch.cuda.synchronize()
+        graph.replay()
+    torch.cuda.synchronize()
+    assert c.lckv_cache_lengths() == [n]
+    w = torch.rand((1, 1, 2000), generator=g, device=DEV)
+    kept = torch.empty((1, 1, keep), dtype=torch.int32, device=DEV)
+    dst = make(4, 1, 1, 1, 64, keep, [0])
+    dst.lckv_evict_kv(0, c, 0, kept, weights=w, n_sink=2, n_recent=50, set_len=1)
+    assert kept[0, 0].tolist() == kept_plain(w[0, 0].cpu().numpy(), n, 2, 50, keep).tolist()
