@@ -4,40 +4,47 @@
 
 namespace {
 
-// Does sequence b < batch own pages for its first rows[b] rows, on the device too?
-bool pages_cover(const lckv_cache* c, const std::vector<int>& rows)
+// Rows that an eviction leaves sequence b with.
+struct RowsKept {
+    const lckv_cache* src;
+    int n_keep;
+    int operator()(int b) const { return std::min(src->h_lens[b], n_keep); }
+};
+
+// Does every sequence b < batch own pages for its first rows(b) rows, on the device too?
+bool pages_cover(const lckv_cache* c, const RowsKept& rows, int batch)
 {
     if (!c->cfg.page_rows) return true;
     if (c->pt_dirty) return false;
-    for (size_t b = 0; b < rows.size(); ++b)
-        if (((int64_t)c->n_pages_of[b] << c->page_shift) < rows[b]) return false;
+    for (int b = 0; b < batch; ++b)
+        if (((int64_t)c->n_pages_of[b] << c->page_shift) < rows(b)) return false;
     return true;
 }
 
-// Pages for the first rows[b] rows of every sequence; on exhaustion nothing changes.
-int cover_pages(lckv_cache* c, const std::vector<int>& rows)
+// Pages for the first rows(b) rows of every sequence; on exhaustion nothing changes.
+int cover_pages(lckv_cache* c, const RowsKept& rows, int batch)
 {
     if (!c->cfg.page_rows) return LCKV_OK;
     size_t need = 0;
-    for (size_t b = 0; b < rows.size(); ++b)
-        need += (size_t)std::max(0, ((rows[b] + c->cfg.page_rows - 1) >> c->page_shift) - c->n_pages_of[b]);
+    for (int b = 0; b < batch; ++b)
+        need += (size_t)std::max(0, ((rows(b) + c->cfg.page_rows - 1) >> c->page_shift) - c->n_pages_of[b]);
     if (need > c->free_pages.size()) return LCKV_ECAPACITY;
-    for (size_t b = 0; b < rows.size(); ++b)
-        while (((int64_t)c->n_pages_of[b] << c->page_shift) < rows[b]) {
-            c->h_pt[b * c->pt_stride + c->n_pages_of[b]++] = c->free_pages.back();
+    for (int b = 0; b < batch; ++b)
+        while (((int64_t)c->n_pages_of[b] << c->page_shift) < rows(b)) {
+            c->h_pt[(size_t)b * c->pt_stride + c->n_pages_of[b]++] = c->free_pages.back();
             c->free_pages.pop_back();
             c->pt_dirty = true;
         }
     return LCKV_OK;
 }
 
-// Pages behind the first rows[b] rows go back to the pool.
-void release_pages(lckv_cache* c, const std::vector<int>& rows)
+// Pages behind the first rows(b) rows go back to the pool (which held them all once, so it does not grow).
+void release_pages(lckv_cache* c, const RowsKept& rows, int batch)
 {
     if (!c->cfg.page_rows) return;
-    for (size_t b = 0; b < rows.size(); ++b)
-        while (c->n_pages_of[b] > 0 && ((int64_t)(c->n_pages_of[b] - 1) << c->page_shift) >= rows[b]) {
-            int32_t& e = c->h_pt[b * c->pt_stride + --c->n_pages_of[b]];
+    for (int b = 0; b < batch; ++b)
+        while (c->n_pages_of[b] > 0 && ((int64_t)(c->n_pages_of[b] - 1) << c->page_shift) >= rows(b)) {
+            int32_t& e = c->h_pt[(size_t)b * c->pt_stride + --c->n_pages_of[b]];
             c->free_pages.push_back(e);
             e = -1;
             c->pt_dirty = true;
@@ -217,15 +224,14 @@ int lckv_evict_kv(lckv_cache_t* dst, int32_t dst_slot, const lckv_cache_t* src, 
         const int64_t total = (int64_t)c->lay.total_bytes;
         if (ranges_meet(kept, items * 4, c->base, total) || (weights_out && ranges_meet(weights_out, o_bytes, c->base, total))) return LCKV_EINVAL;
     }
-    std::vector<int> count(batch);
-    for (int b = 0; b < batch; ++b) count[b] = std::min(src->h_lens[b], n_keep);
+    const RowsKept rows_kept = {src, n_keep};
     cudaStream_t st = static_cast<cudaStream_t>(stream);
     int rc = LCKV_OK;
     const bool capture = capturing(st, &rc);
     if (rc) return rc;
     if (src->pt_dirty && !in_place) return LCKV_EINVAL;     // (no call has brought the source's pages to the device yet)
-    if (capture && (set_len || !pages_cover(dst, count))) return LCKV_EINVAL;
-    if (int rc2 = cover_pages(dst, count)) return rc2;
+    if (capture && (set_len || !pages_cover(dst, rows_kept, batch))) return LCKV_EINVAL;
+    if (int rc2 = cover_pages(dst, rows_kept, batch)) return rc2;
     if (int rc2 = sync_page_table(dst, st)) return rc2;
 
     lckv::SelectParams s;
@@ -275,8 +281,8 @@ int lckv_evict_kv(lckv_cache_t* dst, int32_t dst_slot, const lckv_cache_t* src, 
     }
     if (!cuda_ok(e)) return LCKV_ECUDA;
     if (set_len) {
-        for (int b = 0; b < batch; ++b) dst->h_lens[b] = count[b];
-        release_pages(dst, count);
+        for (int b = 0; b < batch; ++b) dst->h_lens[b] = rows_kept(b);
+        release_pages(dst, rows_kept, batch);
     }
     return LCKV_OK;
 }
