@@ -444,8 +444,8 @@ __global__ void __launch_bounds__(packed_warps(D) * 32, 1) attn_packed_kernel(co
         ++issued;
         islot = (islot + 1 == NS) ? 0 : islot + 1;
     };
-    // The first pair's queries are asked for in front of the tiles, behind which they would wait in line (20 us with 12 workers'
-    // tiles in front of them: 4800 cycles), unless only the tiles may be read yet.
+    // The first pair's queries are asked for in front of the tiles (behind those of 12 workers they arrived after 4800 cycles),
+    // unless only the tiles may be read yet.
     uint4 q_raw[J];
     auto load_q = [&]() {                        // the query heads of pair cc, NC times
         const uint4* src = reinterpret_cast<const uint4*>(query_of(cc));
@@ -567,7 +567,8 @@ __global__ void __launch_bounds__(packed_warps(D) * 32, 1) attn_packed_kernel(co
 #pragma unroll
             for (int j = 0; j < J; ++j) asm volatile("prefetch.global.L1 [%0];" ::"l"(next + 32 * j));
         }
-        if (!mbar_wait_bounded(bars + 8 * cslot, cphase, p.wait_limit)) { ok = false; break; }
+        // (the whole warp gives up or none: what follows exchanges between its lanes, and a block barrier ends the kernel)
+        if (!__all_sync(FULL, mbar_wait_bounded(bars + 8 * cslot, cphase, p.wait_limit))) { ok = false; break; }
         const uint32_t kc = ring + cslot * TILE, vc = kc + CODES, par = kc + 2 * CODES;
         const bool partial = rows < R;
 

@@ -129,8 +129,8 @@ __global__ void __launch_bounds__(kWeightWarps * 32, D == 64 ? 4 : 1) attention_
 // 4-bit keys: the decode attention's division of the work (one thread block per SM, one range of tiles per warp, whatever the
 // lengths; a (sequence, kv head) is a pair) and its rings, here of two tiles' keys and parameters, two bulk copies a tile.  Nothing is to
 // be joined.  Codes enter as c - 8 (EXACT there; weights are fp32, and came out 9e-7 off without).  32 x 32 heads of 128 with 256 to
-// 4096 rows (190 MB): 43 us, 4.4 TB/s (with codes as they are 37; then with 12 warps and three tiles a ring 41, with a fixed number of
-// tiles per warp 50 to 60, with tiles in registers and the next one's loads under way 62 to 68).
+// 4096 rows (190 MB): 49 us, 3.9 TB/s, instructions; with codes as they are 37, 5.1 TB/s (then with 12 warps and three tiles a ring 41, with a
+// fixed number of tiles per warp 48 to 60, with tiles in registers and the next one's loads under way 60 to 68).
 constexpr int kWeightSlots = 2, kWeightBlockWarps = 16;
 template <int D>
 __host__ __device__ constexpr int weight_tile_bytes() { return kPackedRows * (D / 2 + D / 8); }
@@ -199,7 +199,7 @@ __global__ void __launch_bounds__(kWeightBlockWarps * 32, 1) attention_weights_p
     for (uint32_t tile = 0; tile < n_tiles; ++tile) {
         const int rows = min(64, cc.nv - (int)cc.t * 64);
         const uint32_t slot = tile % NS, kc = ring + slot * TILE, par = kc + CODES;
-        if (!mbar_wait_bounded(bars + 8 * slot, tile / NS & 1, p.wait_limit)) {
+        if (!__all_sync(0xffffffffu, mbar_wait_bounded(bars + 8 * slot, tile / NS & 1, p.wait_limit))) {      // (all lanes or none)
             if (lane == 0) atomicExch(p.status, kStatusTimeout);
             for (int s = 0; s < NS; ++s) {
                 mbar_wait_bounded(bars + 8 * s, 0, 1u << 10);
