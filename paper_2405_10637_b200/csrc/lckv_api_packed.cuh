@@ -268,7 +268,6 @@ int lckv_evict_kv(lckv_cache_t* dst, int32_t dst_slot, const lckv_cache_t* src, 
     p.lens_out = set_len && in_place ? dst->d_lens : nullptr;
     p.status = dst->d_status;
     p.T_cap = src->cfg.max_seq;
-    p.batch = batch;
     p.n_keep = n_keep;
     cudaError_t e;
     if (src->cfg.kv_bits == 4) {

@@ -477,7 +477,7 @@ struct MoveParams {
     int32_t* lens_out;        // set by the block of head 0 (in place), or null
     int32_t* status;          // of the cache written to
     int64_t T_cap;
-    int32_t batch, n_keep;
+    int32_t n_keep;
 };
 
 constexpr int kStatusNoRow = 2;   // a row had no place (LCKV_ECAPACITY)
