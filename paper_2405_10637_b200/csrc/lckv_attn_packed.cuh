@@ -20,10 +20,16 @@
 // of their own copy, the columns of the others are zeroed per block, and the copies' outputs are added up at the end of a pair.
 //
 // EXACT (fp32 outputs).  Codes are all positive and lows all negative, more or less, so what is summed is far larger than the sums:
-// scores come out with an error of 5e-6 and, where thousands of rows cancel, the tensor cores' truncation shows.  So codes enter as
-// c - 8, which is exact too (one more instruction for two codes), with low + 8 step in place of low, and W is split into a
-// rounded part and the rounding of the rest (a second MMA), 22 bits.  A bf16 output's own rounding (2^-9) is hundreds of times
-// what that would gain.
+// scores come out with an error of up to 5e-6 and, where thousands of rows cancel, the tensor cores' truncation shows.  So codes enter as
+// c - 8, which is exact too (one more instruction for two codes), with low + 8 step in place of low, W is split into a
+// rounded part and the rounding of the rest (a second MMA), 22 bits, and blocks of 16 rows are added in fp32.
+//
+// bf16 outputs take codes as they are and one W of 11 bits, whose roundings are independent: with the output's own (2^-8 of it at most) the
+// rms error over 200 to 32768 rows is 1.52e-3 to 1.82e-3 of the output, where rounding alone makes 1.49e-3 to 1.76e-3.  W in two parts
+// would make that 1.49e-3 to 1.76e-3 and 32 x 32 heads of 256 to 4096 rows 66 -> 74 us, 48 x 52 of 4096 245 -> 289, 128 x 4 of 64 19.7 -> 21.1.
+// What must not stay is the truncation: it has one sign, so it grows with the rows that a warp sums while what is left of the sums shrinks
+// (32768 rows in one warp, eight heads: 3.7e-2 of the output).  So a tile's four blocks are summed by the tensor cores and tiles in fp32
+// (48 x 52 heads 238 -> 245 us, the others 0 to 2 %).
 //
 // Work: a launch is one long sequence of tiles of 64 rows, (sequence, pair, tile), cut into one range per thread block and
 // those into one per worker (warp).  A pair that several warps of a block share is joined behind a block barrier; only what
@@ -669,14 +675,18 @@ __global__ void __launch_bounds__(packed_warps(D) * 32, 1) attn_packed_kernel(co
             alpha[j] = ex2(m_run[j] - m_new);
             m_run[j] = m_new;
         }
+        // (columns of o are those of the transposed weights: this lane's two, whatever the copy)
+        float b0 = 1.f, b1 = 1.f;
         if (__any_sync(FULL, alpha[0] != 1.f || alpha[1] != 1.f || e_new != e_run)) {
             const float de = e_new - e_run > 120 ? 0.f : __uint_as_float((uint32_t)(e_run - e_new + 127) << 23);
-            // (columns of o are those of the transposed weights: this lane's two, whatever the copy)
-            const float b0 = alpha[0] * de, b1 = alpha[1] * de;
+            b0 = alpha[0] * de;
+            b1 = alpha[1] * de;
+            if constexpr (EXACT) {
 #pragma unroll
-            for (int mt = 0; mt < MT; ++mt) {
-                o[mt][0] *= b0; o[mt][1] *= b1;
-                o[mt][2] *= b0; o[mt][3] *= b1;
+                for (int mt = 0; mt < MT; ++mt) {
+                    o[mt][0] *= b0; o[mt][1] *= b1;
+                    o[mt][2] *= b0; o[mt][3] *= b1;
+                }
             }
 #pragma unroll
             for (int g = 0; g < G; ++g) { low_sum[g][0] *= alpha[0]; low_sum[g][1] *= alpha[1]; }
@@ -716,6 +726,13 @@ __global__ void __launch_bounds__(packed_warps(D) * 32, 1) attn_packed_kernel(co
         }
 
         // ---- O^T += C_V^T . W^T -------------------------------------------------------------------
+        [[maybe_unused]] float sum[EXACT ? 1 : MT][4];       // of this tile (EXACT adds blocks)
+        if constexpr (!EXACT) {
+#pragma unroll
+            for (int mt = 0; mt < MT; ++mt)
+#pragma unroll
+                for (int i = 0; i < 4; ++i) sum[mt][i] = 0.f;
+        }
 #pragma unroll
         for (int rb = 0; rb < RB; ++rb) {
             if (rb * 16 >= rows) continue;
@@ -748,19 +765,27 @@ __global__ void __launch_bounds__(packed_warps(D) * 32, 1) attn_packed_kernel(co
                     nibbles<EXACT>(hi, xb);
 #pragma unroll
                     for (int i = 0; i < 2; ++i) {
-                        float (&acc)[4] = o[4 * g + 2 * half + i];
+                        const int mt = 4 * g + 2 * half + i;
                         if constexpr (EXACT) {
                             // (the tensor cores truncate: a sum of 40 MMAs' results came out 40 * 2^-24 too small)
                             float t[4] = {0.f, 0.f, 0.f, 0.f};
                             mma_f16_16816(t, xa[2 * i], xa[2 * i + 1], xb[2 * i], xb[2 * i + 1], r0, r1);
                             mma_f16_16816(t, xa[2 * i], xa[2 * i + 1], xb[2 * i], xb[2 * i + 1], b0, b1);
 #pragma unroll
-                            for (int e = 0; e < 4; ++e) acc[e] += t[e];
+                            for (int e = 0; e < 4; ++e) o[mt][e] += t[e];
                         } else {
-                            mma_f16_16816(acc, xa[2 * i], xa[2 * i + 1], xb[2 * i], xb[2 * i + 1], b0, b1);
+                            mma_f16_16816(sum[mt], xa[2 * i], xa[2 * i + 1], xb[2 * i], xb[2 * i + 1], b0, b1);
                         }
                     }
                 }
+            }
+        }
+        if constexpr (!EXACT) {
+#pragma unroll
+            for (int mt = 0; mt < MT; ++mt) {
+                const uint64_t by = pack_f32x2(b0, b1);
+                unpack_f32x2(ffma2(pack_f32x2(o[mt][0], o[mt][1]), by, pack_f32x2(sum[mt][0], sum[mt][1])), o[mt][0], o[mt][1]);
+                unpack_f32x2(ffma2(pack_f32x2(o[mt][2], o[mt][3]), by, pack_f32x2(sum[mt][2], sum[mt][3])), o[mt][2], o[mt][3]);
             }
         }
         __syncwarp();
