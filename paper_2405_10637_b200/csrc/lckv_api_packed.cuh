@@ -282,6 +282,7 @@ int lckv_evict_kv(lckv_cache_t* dst, int32_t dst_slot, const lckv_cache_t* src, 
     if (set_len) {
         for (int b = 0; b < batch; ++b) dst->h_lens[b] = rows_kept(b);
         release_pages(dst, rows_kept, batch);
+        return sync_page_table(dst, st);    // (not capturing; behind the moves, which go by the table as it was)
     }
     return LCKV_OK;
 }
