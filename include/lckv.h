@@ -596,7 +596,8 @@ int lckv_quant_set_copy_limits(int32_t weights, int32_t x);
  *
  * lckv_cache_read_kv: what the rows 0 .. len[b]-1 of a slot stand for, as tokens (bf16 caches too: the rows).
  *   k, v       [batch, n_max, H_kv, d_h], bf16 (dtype 0) or fp32 (1), 16-byte aligned; tokens behind a sequence
- *              are left as they were.  Errors as lckv_prefill_write_kv; EINVAL also if k and v overlap.
+ *              are left as they were.  Errors as lckv_prefill_write_kv; EINVAL also if k and v overlap, or while
+ *              `stream` is capturing before any call has brought a paged cache's table to the device.
  */
 int lckv_cache_read_kv(lckv_cache_t* cache, int32_t slot, void* k, void* v, int32_t dtype, int32_t n_max,
                        int32_t batch, void* stream);

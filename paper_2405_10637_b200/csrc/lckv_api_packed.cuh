@@ -113,7 +113,11 @@ int lckv_cache_read_kv(lckv_cache_t* c, int32_t slot, void* k, void* v, int32_t 
         ranges_meet(v, bytes, c->base, (int64_t)c->lay.total_bytes) || !row_grid(c, n_max, four ? 4 : 1, batch, &grid))
         return LCKV_EINVAL;
     cudaStream_t st = static_cast<cudaStream_t>(stream);
-    if (int rc = sync_page_table(c, st)) return rc;
+    int rc = LCKV_OK;
+    const bool capture = capturing(st, &rc);
+    if (rc) return rc;
+    if (capture && !pages_ready(c, 0, 0)) return LCKV_EINVAL;      // (the rows' pages are there; is the table?)
+    if (int rc2 = sync_page_table(c, st)) return rc2;
     lckv::RowReadParams p;
     p.s = packed_slot(c, slot);
     p.K = slot_k(c, slot);

@@ -2,7 +2,8 @@
 import pytest
 import torch
 
-from test_gpu_compact_caches import CONDENSED, DEV, check_attention, gen, kept_plain, make, randn, rows_bf16, value64
+from paper_2405_10637_b200 import binding as lk
+from test_gpu_compact_caches import CONDENSED, DEV, check_attention, gen, kept_plain, make, randn, refused, rows_bf16, value64
 
 pytestmark = pytest.mark.gpu
 
@@ -95,3 +96,30 @@ def test_captures_right_after_pages_were_given_back(bits):
     for t in (*read, w):
         t.zero_()
     check()
+
+
+def test_reading_is_captured_only_with_the_table_on_the_device():
+    """A cache whose table no call has brought to the device yet: the upload does not belong into the caller's graph."""
+    c = lk.Cache(lk.make_config(1, 0, 4, 2, 64, 2, 100, page_rows=64, n_pages=4, kv_bits=4))
+    out = [torch.full((2, 100, 2, 64), 3.0, device=DEV) for _ in range(2)]
+    other = torch.zeros(4, device=DEV)
+    torch.cuda.synchronize()
+    st = torch.cuda.Stream()
+    with torch.cuda.graph(torch.cuda.CUDAGraph(), stream=st):
+        refused(lk.EINVAL, c.lckv_cache_read_kv, 0, *out)
+        other.add_(1.0)                                      # (so that the graph is not empty)
+    assert (out[0] == 3.0).all()
+    c.lckv_cache_read_kv(0, *out)                            # eager: uploads; no rows yet
+    graph = torch.cuda.CUDAGraph()
+    torch.cuda.synchronize()
+    with torch.cuda.graph(graph, stream=st):
+        c.lckv_cache_read_kv(0, *out)
+    c.lckv_cache_reset([70, 1])
+    k = rows_bf16(gen(43), 2, 100, 2, 64)
+    c.lckv_prefill_write_kv(0, k, -k)
+    torch.cuda.synchronize()
+    graph.replay()
+    torch.cuda.synchronize()
+    for got, x in zip(out, (k, -k)):
+        for b, n in enumerate((70, 1)):
+            assert torch.equal(got[b, :n], value64(x)[b, :n].float()) and (got[b, n:] == 3.0).all()
