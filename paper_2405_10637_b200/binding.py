@@ -345,7 +345,7 @@ class Cache:
                  "lckv_cache_alloc")
         self.h = h
         self.call = (h.value, self.buf.get_device())       # what the native calls take
-        self.views = {}                                    # slot -> its K and V as tensors
+        self.views = {}                                    # slot -> its K and V as tensors, which no caller gets
         self.heads = (cfg.n_q_heads, cfg.n_kv_heads, cfg.head_dim)
         info = Info()
         _chk(lib().lckv_cache_info(self.h, C.byref(info)), "lckv_cache_info")
@@ -411,7 +411,8 @@ class Cache:
         """torch views of a slot's K and V (same memory): [B_max, H_kv, T_cap, d_h] bf16, or
         [n_pages, H_kv, page_rows, d_h] for a paged cache.  Not for rows in 4 bits (lckv_cache_read_kv)."""
         if slot in self.views:
-            return self.views[slot]
+            kt, vt = self.views[slot]
+            return kt.detach(), vt.detach()      # the caller's own objects over the same memory
         k, v = self.lckv_cache_slot_ptrs(slot)
         c = self.cfg
         shape = (c.max_batch, c.n_kv_heads, c.max_seq, c.head_dim)
@@ -422,7 +423,7 @@ class Cache:
         kt = self.buf[k - base:k - base + n].view(torch.bfloat16).view(shape)
         vt = self.buf[v - base:v - base + n].view(torch.bfloat16).view(shape)
         self.views[slot] = kt, vt
-        return kt, vt
+        return kt.detach(), vt.detach()
 
     def lckv_append_kv(self, slot, k_new, v_new, batch=None, advance_len=0, stream=None):
         batch = k_new.shape[0] if batch is None else batch
