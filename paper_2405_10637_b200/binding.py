@@ -427,9 +427,11 @@ class Cache:
 
     def lckv_append_kv(self, slot, k_new, v_new, batch=None, advance_len=0, stream=None):
         batch = k_new.shape[0] if batch is None else batch
-        rc = (_CALLS or calls()).append_kv(self.call[0] or 0, slot, k_new, v_new, batch, advance_len, None if stream is None else stream.cuda_stream)
+        h, dev = self.call
+        rc = (_CALLS or calls()).append_kv(h, dev, slot, *self.heads[1:], k_new, v_new, batch, advance_len,
+                                           None if stream is None else _address(dev, stream))
         if rc:
-            _fail(rc, "lckv_append_kv", "k_new and v_new are CUDA tensors")
+            _fail(rc, "lckv_append_kv", "k_new and v_new are contiguous bf16 [batch, H_kv, d_h] on the cache's device")
 
     def lckv_project_append_kv(self, slot, x, w_k, w_v, rope_cos=None, rope_sin=None, batch=None,
                                advance_len=0, stream=None):
@@ -468,9 +470,12 @@ class Cache:
         batch = q.shape[0] if batch is None else batch
         if out is None:
             out = torch.empty(q.shape, dtype=self.out_torch_dtype, device=q.device)
-        rc = (_CALLS or calls()).decode_attention(self.call[0] or 0, slot, mode, q, out, lse, batch, None if stream is None else stream.cuda_stream)
+        h, dev = self.call
+        rc = (_CALLS or calls()).decode_attention(h, dev, slot, mode, self.heads[0], self.heads[2], self.cfg.out_dtype, q, out, lse, batch,
+                                                  None if stream is None else _address(dev, stream))
         if rc:
-            _fail(rc, "lckv_decode_attention", "q, out and lse are CUDA tensors")
+            _fail(rc, "lckv_decode_attention", "q is bf16 and out of the cache's output type, both [batch, H_q, d_h], lse [batch, H_q] fp32, "
+                                               "contiguous, on the cache's device")
         return out
 
     def lckv_layer_stack_step(self, q_layers, out_layers, k_new_layers, v_new_layers, batch=None,
@@ -491,9 +496,11 @@ class Cache:
 
     # -- prompt encoding (token-major tensors [B, n_max, H, d_h]) -------------------------------
     def lckv_prefill_write_kv(self, slot, k, v, stream=None):
-        rc = (_CALLS or calls()).prefill_write_kv(self.call[0] or 0, slot, k, v, k.shape[1], k.shape[0], None if stream is None else stream.cuda_stream)
+        h, dev = self.call
+        rc = (_CALLS or calls()).prefill_write_kv(h, dev, slot, *self.heads[1:], k, v, k.shape[1], k.shape[0],
+                                                  None if stream is None else _address(dev, stream))
         if rc:
-            _fail(rc, "lckv_prefill_write_kv", "k and v are CUDA tensors")
+            _fail(rc, "lckv_prefill_write_kv", "k and v are contiguous bf16 [batch, n_max, H_kv, d_h] on the cache's device")
 
     def lckv_prefill_attention(self, slot, mode, q, out=None, stream=None):
         if out is None:

@@ -232,51 +232,56 @@ PyObject* rope_cache(Args& a)
     });
 }
 
-// The calls below hand pointers on as they are: what they take of their tensors is the caller's to keep, as in the header.  The stream
-// is the one given, or the current one of the current device.
-template <typename F>
-PyObject* pass(Args& args, F call)
+// Is t dense, on the device, with at least n elements of the type: fp32, or bf16 (as such or as raw 16-bit patterns)?  Not more is
+// asked of its shape.
+bool holds(const at::Tensor* t, int64_t dev, int64_t n, bool f32 = false)
 {
-    PyObject* given = args.take();
-    if (!args.ok) return code(kBadTensor);
-    void* stream = nullptr;
-    if (given == Py_None) {
-        stream = c10::cuda::getCurrentCUDAStream().stream();
-    } else {
-        stream = PyLong_AsVoidPtr(given);
-        if (!stream && PyErr_Occurred()) return nullptr;
-    }
-    return code(call(stream));
+    if (!t) return false;
+    const auto type = t->scalar_type();
+    const bool fits = f32 ? type == at::kFloat : type == at::kBFloat16 || type == at::kShort || type == at::kUInt16;
+    return fits && t->is_contiguous() && on(t, dev) && n >= 0 && t->numel() >= n;
 }
 
-// cache, slot, mode, q, out, lse, batch, stream
+// cache, its device, slot, mode, H_q, d, fp32 outputs?, q, out, lse, batch, stream
 PyObject* decode_attention(Args& a)
 {
     auto* cache = static_cast<lckv_cache_t*>(a.address());
+    const int64_t dev = a.integer();
     const int32_t slot = a.integer32(), mode = a.integer32();
+    const int64_t hq = a.integer(), d = a.integer(), f32 = a.integer();
     const at::Tensor *q = a.tensor(), *out = a.tensor(), *lse = a.tensor();
     const int32_t batch = a.integer32();
-    return pass(a, [&](void* st) { return lckv_decode_attention(cache, slot, mode, ptr(q), mut(out), static_cast<float*>(mut(lse)), batch, st); });
+    if (!a.ok || !cache || !holds(q, dev, batch * hq * d) || !holds(out, dev, batch * hq * d, f32 != 0) || (lse && !holds(lse, dev, batch * hq, true)))
+        return code(kBadTensor);
+    return run(a, dev, [&](void* st) { return lckv_decode_attention(cache, slot, mode, ptr(q), mut(out), static_cast<float*>(mut(lse)), batch, st); });
 }
 
-// cache, slot, k, v, batch, advance, stream
+// cache, its device, slot, H_kv, d, k, v, batch, advance, stream
 PyObject* append_kv(Args& a)
 {
     auto* cache = static_cast<lckv_cache_t*>(a.address());
+    const int64_t dev = a.integer();
     const int32_t slot = a.integer32();
+    const int64_t hkv = a.integer(), d = a.integer();
     const at::Tensor *k = a.tensor(), *v = a.tensor();
     const int32_t batch = a.integer32(), advance = a.integer32();
-    return pass(a, [&](void* st) { return lckv_append_kv(cache, slot, ptr(k), ptr(v), batch, advance, st); });
+    if (!a.ok || !cache || !holds(k, dev, batch * hkv * d) || !holds(v, dev, batch * hkv * d)) return code(kBadTensor);
+    return run(a, dev, [&](void* st) { return lckv_append_kv(cache, slot, ptr(k), ptr(v), batch, advance, st); });
 }
 
-// cache, slot, k, v, n_max, batch, stream
+// cache, its device, slot, H_kv, d, k, v, n_max, batch, stream
 PyObject* prefill_write_kv(Args& a)
 {
     auto* cache = static_cast<lckv_cache_t*>(a.address());
+    const int64_t dev = a.integer();
     const int32_t slot = a.integer32();
+    const int64_t hkv = a.integer(), d = a.integer();
     const at::Tensor *k = a.tensor(), *v = a.tensor();
     const int32_t n = a.integer32(), batch = a.integer32();
-    return pass(a, [&](void* st) { return lckv_prefill_write_kv(cache, slot, ptr(k), ptr(v), n, batch, st); });
+    if (!a.ok || !cache || n < 0 || batch < 0 || hkv < 1 || d < 1 || (int64_t)n * batch > INT64_MAX / (hkv * d)) return code(kBadTensor);
+    const int64_t elements = (int64_t)n * batch * hkv * d;
+    if (!holds(k, dev, elements) || !holds(v, dev, elements)) return code(kBadTensor);
+    return run(a, dev, [&](void* st) { return lckv_prefill_write_kv(cache, slot, ptr(k), ptr(v), n, batch, st); });
 }
 
 // cache, its device, slot, H_kv, d, k, v, stream
