@@ -70,13 +70,16 @@ cudaError_t launch_move(const lckv::MoveParams& p, bool in_place, int64_t heads,
     return launch_pdl_dims(lckv::evict_move_kernel<D, PACKED>, grid, dim3(lckv::kRowThreads), 0, st, p);
 }
 
-// The smallest thread block that holds the rows.
+// The smallest thread block that holds the rows in registers.  148 heads, us, and with the next larger block: 1024 rows 6.1, 14.5; 4096 rows 14.7,
+// 21.0; 8192 rows 25.5, 26.7; 16384 rows 29.9, 53.8 (the same order for 1 to 1184 heads).  A block that holds them, and one that reads
+// the weights again in every round: 1500 rows 11.6, 14.4; 8192 rows 25.5, 44; 16384 rows 29.9, 78; 32768 rows 58, 152.
 cudaError_t launch_select(const lckv::SelectParams& s, int64_t most, int64_t heads, cudaStream_t st)
 {
     const dim3 grid((unsigned)heads);
     if (most <= 1024) return launch_pdl_dims(lckv::evict_select_kernel<128, 8>, grid, dim3(128), 0, st, s);
     if (most <= 4096) return launch_pdl_dims(lckv::evict_select_kernel<256, 16>, grid, dim3(256), 0, st, s);
     if (most <= 8192) return launch_pdl_dims(lckv::evict_select_kernel<512, 16>, grid, dim3(512), 0, st, s);
+    if (most <= 16384) return launch_pdl_dims(lckv::evict_select_kernel<1024, 16>, grid, dim3(1024), 0, st, s);
     if (most <= 32768) return launch_pdl_dims(lckv::evict_select_kernel<1024, 32>, grid, dim3(1024), 0, st, s);
     return launch_pdl_dims(lckv::evict_select_kernel<1024, 0>, grid, dim3(1024), 0, st, s);
 }
@@ -189,7 +192,9 @@ int lckv_attention_weights(lckv_cache_t* c, int32_t slot, int32_t mode, const vo
         return cuda_ok(e) ? LCKV_OK : LCKV_ECUDA;
     }
     // Warps for the longest sequence that the host knows (one whose sequence turns out longer in a replay goes on behind the last run), of two
-    // tiles of 64 rows where there are enough.
+    // tiles of 64 rows where an SM has 64 or more: the second tile's keys are asked for while the first's are used, and the query is loaded once (64
+    // tiles an SM of 16 kv heads of 128 32.5 us, with one a warp 34.1; 221 tiles 91.3, 98.5, with four 98.2).  With few, fewer warps are what
+    // counts (7 tiles an SM 5.6 us, with one 4.2); from 24 to 60 both take the same within 5 %.
     int64_t longest = 1;
     for (int b = 0; b < batch; ++b) longest = std::max<int64_t>(longest, std::min(c->h_lens[b], c->cfg.max_seq - mode) + mode);
     const int64_t tiles = (longest + 63) / 64;

@@ -60,7 +60,10 @@ struct WeightLane {
 };
 
 // bf16 keys go straight from memory into MMA fragments, all of a tile under way before the first is used; a row's four lanes take
-// 16 bytes each at a time, and q enters in the order which that gives.
+// 16 bytes each at a time, and q enters in the order which that gives.  Thread blocks per SM, which registers limit: four over 64 dimensions (128
+// registers; the two narrow forms spill 4 and 28 bytes: 128 x 4 kv heads x 1024 rows 15.0 us, with three and no spill 16.9, with five 19.4); over
+// 128 dimensions a tile is 128 registers by itself, and two blocks fit without being asked for (32 x 32 heads x 2048 rows 91.5 us; with three, which spill
+// 108 bytes, 94.1 and small calls 4.3 -> 6.1, with four 133).
 template <int D, int QP>
 __global__ void __launch_bounds__(kWeightWarps * 32, D == 64 ? 4 : 1) attention_weights_kernel(const WeightParams p)
 {
@@ -315,7 +318,9 @@ struct SelectParams {
 };
 
 // One thread block per (sequence, kv head); a warp holds the keys of 32 KPT consecutive rows, KPT a thread, in registers
-// (KPT = 0, for more rows than the block can hold: keys from memory each time).  The smallest key that stays is found two bits at a time: with t the
+// (KPT = 0, for more rows than the block can hold: keys from memory each time.  KPT = 32 does not fit the 64 registers that 1024 threads leave;
+// ptxas spills 540 bytes a thread, and it is still 1.5 to 2.6 times as fast as reading the weights in every round).  The smallest key
+// that stays is found two bits at a time: with t the
 // bits found so far, count the keys >= t + 1, 2 and 3 units of those bits.  That is at most 16 rounds, fewer when a count
 // meets the target (as with distinct weights it soon does).  Then every warp lists its own stretch of rows behind what
 // the warps in front of it keep, so rows stay in order and equal weights go by the lowest row.

@@ -20,7 +20,7 @@ def weights_of(kind, g, shape):
     return w
 
 
-@pytest.mark.parametrize("n", [1023, 1024, 1025, 2500, 4096, 4097, 6001, 8192, 8193, 20000, 32767, 32768, 32769])
+@pytest.mark.parametrize("n", [1023, 1024, 1025, 2500, 4096, 4097, 6001, 8192, 8193, 16384, 16385, 20000, 32767, 32768, 32769])
 @pytest.mark.parametrize("kind", ["distinct", "ties", "infinite"])
 def test_selection_of_any_number_of_rows(n, kind):
     """Both sides of every size at which the thread block changes, weights of the rows that stay in place of all."""
