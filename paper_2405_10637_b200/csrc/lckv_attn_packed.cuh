@@ -336,7 +336,10 @@ __device__ __forceinline__ PackedRange packed_range(const PackedParams& pp, cons
         r.begin = block < blocks ? share.begin(block) : 0u;
         r.end = block < blocks ? share.begin(block + 1) : 0u;
     }
-    const uint32_t n_block = r.end - r.begin, each = warps == 1 ? n_block : __umulhi(n_block, pp.warps_inverse), more = n_block - each * warps;
+    // n / warps by the inverse, which is too large by less than 16 in 2^32: from 2^28 tiles on the quotient may be one too many
+    const uint32_t n_block = r.end - r.begin;
+    uint32_t each = warps == 1 ? n_block : __umulhi(n_block, pp.warps_inverse), more = n_block - each * warps;
+    if ((int32_t)more < 0) { --each; more += warps; }
     r.first = r.begin + warp * each + min(warp, more);
     r.count = warp < warps ? each + (warp < more ? 1u : 0u) : 0u;
     if (r.count == 0) return r;
