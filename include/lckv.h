@@ -587,8 +587,13 @@ int lckv_quant_set_copy_limits(int32_t weights, int32_t x);
  * head takes d_h + d_h / 8 bytes for key and value, where bf16 takes 4 d_h.  On such a cache
  *   - lckv_append_kv and lckv_prefill_write_kv take bf16 and write rows in 4 bits; lckv_decode_attention and
  *     lckv_layer_stack_step (_host) attend to what the rows stand for: codes enter the tensor cores exactly,
- *     q as well (elements below 2^-25 of the head's largest one are rounded there; |q| < 2^100), everything
- *     else is fp32, with 11 bits of a row's weight times its step (22 where out_dtype is fp32);
+ *     q as well (elements below 2^-25 of the head's largest one are rounded there; |q| < 2^100), sums are fp32.
+ *     With bf16 outputs a row's weight times its step has 11 bits, which adds up to 7 % to the rms error that
+ *     rounding the output makes, and lse is off by up to 2^-21 of the largest row's scale * sum (|q| step code +
+ *     |q low|) (1e-5 where that is 700).  With fp32 outputs it has 22 bits, and scores are summed about the codes'
+ *     middle: 2^-19 for scores of up to 16 (base 2).  lckv_attention_weights does the latter, given lse;
+ *   - query heads of a kv head share its rows up to eight at a time, in the largest divisor of H_q / H_kv up to 8: where
+ *     that is 1 (11, 13, 17 ... heads), rows are read once per query head;
  *   - stream_sink and page_rows work as ever, kernel_kind is 0; tensors off the 16-byte grid are refused (EINVAL);
  *   - lckv_cache_slot_ptrs, lckv_project_append_kv, the keys of lckv_rope_append_kv and
  *     lckv_rope_prefill_write_kv (rotate with lckv_rope_apply first), lckv_prefill_attention and
@@ -636,7 +641,7 @@ int lckv_attention_weights(lckv_cache_t* cache, int32_t slot, int32_t mode, cons
  * Keys keep the rotation of their token; after an eviction len[b] counts rows and is no longer a position, so new
  * tokens are rotated by lckv_rope_apply at their positions, not by calls that take the position from len[b].
  * Errors: EINVAL (null, shape, overlap, n_sink + n_recent > n_keep, n_keep > dst's max_seq, caches that do not
- * match), ECAPACITY (no page left; nothing written), ECUDA.  While `stream` is capturing the call is refused with
+ * match, a paged src whose table no call has brought to the device yet), ECAPACITY (no page left; nothing written), ECUDA.  While `stream` is capturing the call is refused with
  * EINVAL if set_len != 0 or if dst needs new pages.  A replay uses the lengths it finds on the device; a row that has no place is left
  * out, and dst's lckv_cache_status then reports LCKV_ECAPACITY.
  */
