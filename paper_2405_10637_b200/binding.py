@@ -467,12 +467,12 @@ class Cache:
         return self._rope_call("lckv_rope_prefill_write_kv", slot, rope, q, k, v, q_out, -1, stream)
 
     def lckv_decode_attention(self, slot, mode, q, out=None, lse=None, batch=None, stream=None):
+        h, dev = self.call
+        at = None if stream is None else _address(dev, stream)
         batch = q.shape[0] if batch is None else batch
         if out is None:
-            out = torch.empty(q.shape, dtype=self.out_torch_dtype, device=q.device)
-        h, dev = self.call
-        rc = (_CALLS or calls()).decode_attention(h, dev, slot, mode, self.heads[0], self.heads[2], self.cfg.out_dtype, q, out, lse, batch,
-                                                  None if stream is None else _address(dev, stream))
+            out = _made(torch.empty, stream, q.shape, dtype=self.out_torch_dtype, device=q.device)
+        rc = (_CALLS or calls()).decode_attention(h, dev, slot, mode, self.heads[0], self.heads[2], self.cfg.out_dtype, q, out, lse, batch, at)
         if rc:
             _fail(rc, "lckv_decode_attention", "q is bf16 and out of the cache's output type, both [batch, H_q, d_h], lse [batch, H_q] fp32, "
                                                "contiguous, on the cache's device")
@@ -504,7 +504,7 @@ class Cache:
 
     def lckv_prefill_attention(self, slot, mode, q, out=None, stream=None):
         if out is None:
-            out = torch.zeros(q.shape, dtype=self.out_torch_dtype, device=q.device)
+            out = _made(torch.zeros, stream, q.shape, dtype=self.out_torch_dtype, device=q.device)
         _chk(lib().lckv_prefill_attention(self.h, slot, mode, _ptr(q), _ptr(out), q.shape[1],
                                           q.shape[0], _stream(stream)), "lckv_prefill_attention")
         return out

@@ -89,3 +89,19 @@ def test_calls_use_the_caches_device_and_a_stream_of_it():
     c.close()
     refused(lk.EINVAL, c.lckv_decode_attention, 0, CONDENSED, q, out=out)
     refused(lk.EINVAL, c.lckv_append_kv, 0, q, q)
+
+
+def test_outputs_made_by_a_call_belong_to_its_stream():
+    """An output that a call makes on a given stream is made, and for prompts zeroed, there: not behind what the current stream still does."""
+    n = 200
+    g = gen(54)
+    c = make(16, 1, 2, 2, 64, n, [n])
+    k, q, pq = rows_bf16(g, 1, n, 2, 64), randn(g, 1, 2, 64), randn(g, 1, n, 2, 64)
+    c.lckv_prefill_write_kv(0, k, k)
+    want, want_p = c.lckv_decode_attention(0, CONDENSED, q), c.lckv_prefill_attention(0, CONDENSED, pq)
+    torch.cuda.synchronize()
+    st = torch.cuda.Stream()
+    torch.cuda._sleep(20_000_000)                            # some 10 ms of the current stream
+    got, got_p = c.lckv_decode_attention(0, CONDENSED, q, stream=st), c.lckv_prefill_attention(0, CONDENSED, pq, stream=st)
+    torch.cuda.synchronize()
+    assert torch.equal(got, want) and torch.equal(got_p, want_p)
